@@ -419,6 +419,82 @@ hs_status hs_dit_forward(hs_context* ctx, const hs_dit_cfg* cfg, const hs_dit_we
                          const void* x_in, void* x_out, const float* cond, const int32_t* seq_offsets,
                          int32_t n_seqs, int32_t cu_budget, void* stream, void* workspace, size_t ws_bytes);
 
+/* ------------------------------------------------------------------------
+ * From the residual stream to an answer: the final RMSNorm and 8-bit rows, the
+ * vocabulary head (or any other projection) as an 8-bit integer product, and
+ * log probabilities of its logits.  The stack calls above end at the residual
+ * stream; hs_quantize_rows -> hs_linear_i8 -> hs_logprobs take it from there.
+ *
+ * Common to the three calls:
+ *   - Matrices are device pointers with a row stride (ld, elements) at least
+ *     the row's length; rows may start anywhere their elements are aligned.
+ *     Rows whose start and stride are multiples of 16 bytes are the fast case.
+ *   - cu_budget and stream: stream NULL selects the context's SHARED stream of
+ *     that budget; another stream must carry exactly cu_budget CUs and belong
+ *     to the context's device (a DOWN stream serves the downstream stage).
+ *   - The calls allocate nothing, stage nothing on the host and never
+ *     synchronise, so they can be captured into a graph on the caller's
+ *     stream.  The caller's current device is left as it was.
+ *   - No rows: HS_OK, nothing is enqueued.  Outputs that overlap an input or
+ *     each other, strides below the row length and misaligned pointers are
+ *     HS_ERR_INVALID_ARG. */
+enum { HS_TYPE_F32 = 0, HS_TYPE_BF16 = 1, HS_TYPE_F16 = 2 };
+
+/* Rows to 8-bit integers with one scale each:
+ *   y = x                                    (gain NULL)
+ *   y = x / sqrt(mean(x^2) + eps) * gain     (RMSNorm, gain bf16 [d], eps > 0)
+ *   scale[r] = max |y| / 127,  q = round(127 y / max |y|), ties to even
+ *   x      [rows, d] of x_type;  q int8 [rows, d], in [-127, 127];
+ *   scale  fp32 [rows], so y is about q * scale.
+ * The integers are those of exact arithmetic: the norm's factor cancels in
+ * them, and every border is decided on exact products.  A row of zeros has
+ * scale 0; a row with a NaN or an infinity (in x, or in x * gain) has q 0 and
+ * scale NaN, so its products are NaN.  Weight channels are rows as well:
+ * an [out, in] bf16 matrix becomes hs_linear_i8's w and w_scale with gain NULL.
+ * eps is not read when gain is NULL. */
+hs_status hs_quantize_rows(hs_context* ctx, const void* x, int32_t x_type, int64_t ldx, const void* gain, float eps,
+                           int32_t rows, int32_t d, void* q, int64_t ldq, float* scale, int32_t cu_budget,
+                           void* stream);
+
+/* out[i, j] = a_scale[i] * w_scale[j] * sum_k a[i, k] w[j, k] + bias[j]
+ *   a    int8 [m, k] with a_scale fp32 [m] (tokens);
+ *   w    int8 [n, k] with w_scale fp32 [n] (channels; [out, in] like all weights);
+ *   bias bf16 [n] or NULL;  out [m, n] of out_type.
+ * The sum is exact (k <= 131071, else HS_ERR_UNSUPPORTED); then
+ * fp32(sum) * fp32(a_scale * w_scale) + bias, each step rounded to fp32, and one
+ * rounding to out_type (beyond its range: infinity).  The result does not depend
+ * on the budget or on the other rows of the call. */
+hs_status hs_linear_i8(hs_context* ctx, const void* a, int64_t lda, const float* a_scale, const void* w, int64_t ldw,
+                       const float* w_scale, const void* bias, void* out, int32_t out_type, int64_t ldo, int32_t m,
+                       int32_t n, int32_t k, int32_t cu_budget, void* stream);
+
+/* Workspace bytes of hs_logprobs for up to max_rows rows (any budget; 0 when it
+ * needs none). */
+hs_status hs_logprobs_workspace_size(int32_t max_rows, int32_t vocab, int32_t top_k, size_t* bytes);
+
+/* Log probabilities of rows of logits, log p[t] = z[t] - log sum_j e^z[j]:
+ *   logits          [rows, vocab] of `type`; -inf marks a masked token (p = 0).
+ *   tokens          int32 [rows, n_tokens] device (n_tokens 0: none);
+ *   token_logprobs  fp32 [rows, n_tokens]: their log probabilities.  Token -1 is
+ *                   no token and gives 0; any other outside [0, vocab) gives NaN.
+ *   entropy         fp32 [rows] or NULL: -sum p log p (nats).
+ *   top_k           0 .. 64 alternatives a row: top_tokens int32 [rows, top_k] by
+ *                   logit, equal ones (-0 equals +0) by the lower token, with
+ *                   top_logprobs fp32 [rows, top_k].  A row with fewer unmasked
+ *                   tokens lists -1 with -inf after them.
+ * Statistics are fp32 over one read of the logits; probabilities close to 1 keep
+ * their distance from it (log1p).  A row whose tokens are all masked has
+ * entropy 0, -inf for every token and no alternatives; a row with a NaN or +inf
+ * has no distribution: NaN for every output, alternatives -1 (padding tokens -1
+ * still give 0).
+ * workspace: hs_logprobs_workspace_size() bytes for this shape or a larger
+ * max_rows, 16-byte aligned; may be reused as soon as the stream has passed the
+ * call, and two calls that may overlap need one each. */
+hs_status hs_logprobs(hs_context* ctx, const void* logits, int32_t type, int64_t ld, int32_t rows, int32_t vocab,
+                      const int32_t* tokens, int32_t n_tokens, float* token_logprobs, float* entropy, int32_t top_k,
+                      float* top_logprobs, int32_t* top_tokens, int32_t cu_budget, void* stream, void* workspace,
+                      size_t ws_bytes);
+
 /* Topology probe: launches n_groups work-groups on `stream` (NULL = the
  * context's full-budget stream); each writes, into out_ids (device, uint32
  * [n_groups * 4]): XCC id, shader engine, CU id, and the low 32 bits of the
@@ -455,7 +531,10 @@ enum {
   HS_KERNEL_LN_MOD = 9,       /* DiT: modulated LayerNorm */
   HS_KERNEL_MLP_UP = 10,      /* DiT: first MLP projection + bias + GELU */
   HS_KERNEL_MLP_DOWN = 11,    /* DiT: second MLP projection + bias + gated residual */
-  HS_KERNEL_KINDS = 12
+  HS_KERNEL_QUANTIZE = 12,    /* hs_quantize_rows */
+  HS_KERNEL_LINEAR_I8 = 13,   /* hs_linear_i8 */
+  HS_KERNEL_LOGPROBS = 14,    /* hs_logprobs */
+  HS_KERNEL_KINDS = 15
 };
 
 hs_status hs_timing_enable(hs_context* ctx, int32_t enable);

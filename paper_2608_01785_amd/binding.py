@@ -29,11 +29,15 @@ SYMBOLS = (
     "hs_probe_hw_ids", "hs_timing_enable", "hs_timing_read", "hs_timing_read_clock", "hs_convert_weights_f16",
     "hs_controller_create", "hs_controller_step", "hs_controller_destroy", "hs_pressure_sample",
     "hs_temporal_create", "hs_temporal_step", "hs_temporal_destroy",
+    "hs_quantize_rows", "hs_linear_i8", "hs_logprobs_workspace_size", "hs_logprobs",
 )
 HS_WEIGHTS_BF16, HS_WEIGHTS_F16 = 0, 1
+HS_TYPE_F32, HS_TYPE_BF16, HS_TYPE_F16 = 0, 1, 2
+_TYPES = {"torch.float32": HS_TYPE_F32, "torch.bfloat16": HS_TYPE_BF16, "torch.float16": HS_TYPE_F16}
 
 KERNEL_KINDS = {"rmsnorm": 0, "qkv": 1, "attention": 2, "decode_attn": 3, "o_proj": 4, "gate_up": 5,
-                "down": 6, "rope_table": 7, "modulation": 8, "ln_mod": 9, "mlp_up": 10, "mlp_down": 11}
+                "down": 6, "rope_table": 7, "modulation": 8, "ln_mod": 9, "mlp_up": 10, "mlp_down": 11,
+                "quantize": 12, "linear_i8": 13, "logprobs": 14}
 
 
 class LayerCfg(ctypes.Structure):
@@ -129,6 +133,7 @@ def lib() -> ctypes.CDLL:
             raise ImportError(f"{_LIB_PATH} is missing: build it with python -m paper_2608_01785_amd.build")
         L = ctypes.CDLL(_LIB_PATH)
         vp, i32, u32p, i32p = ctypes.c_void_p, ctypes.c_int32, ctypes.POINTER(ctypes.c_uint32), ctypes.POINTER(ctypes.c_int32)
+        i64, f32 = ctypes.c_int64, ctypes.c_float
         L.hs_status_string.restype = ctypes.c_char_p
         L.hs_status_string.argtypes = [ctypes.c_int]
         L.hs_last_error.restype = ctypes.c_char_p
@@ -178,6 +183,10 @@ def lib() -> ctypes.CDLL:
             "hs_temporal_step": [vp, ctypes.c_double, ctypes.POINTER(RequestView), i32,
                                  ctypes.POINTER(ctypes.c_uint8), ctypes.POINTER(TemporalStepInfo)],
             "hs_temporal_destroy": [vp],
+            "hs_quantize_rows": [vp, vp, i32, i64, vp, f32, i32, i32, vp, i64, vp, i32, vp],
+            "hs_linear_i8": [vp, vp, i64, vp, vp, i64, vp, vp, vp, i32, i64, i32, i32, i32, i32, vp],
+            "hs_logprobs_workspace_size": [i32, i32, i32, ctypes.POINTER(ctypes.c_size_t)],
+            "hs_logprobs": [vp, vp, i32, i64, i32, i32, vp, i32, vp, vp, i32, vp, vp, i32, vp, vp, ctypes.c_size_t],
         }
         for name, args in sigs.items():
             fn = getattr(L, name)
@@ -560,6 +569,96 @@ def hs_dit_forward(ctx: Context, cfg, weights, x_in, x_out, cond, seq_offsets, c
     _check(lib().hs_dit_forward(ctx.handle, ctypes.byref(DitCfg.of(cfg)), warr, len(weights), _ptr(x_in),
                                 _ptr(x_out), _ptr(cond), off, len(off) - 1, cu_budget, _ptr(stream),
                                 _ptr(workspace), ws_bytes))
+
+
+# The calls below take torch tensors and read types, sizes and strides off them, so a
+# tensor that does not fit is a ValueError here, before the library sees a pointer.
+
+def _on(ctx: Context, t, name: str, dtypes, ndim: int):
+    if str(t.dtype) not in dtypes:
+        raise ValueError(f"{name} has type {t.dtype}, expected {' or '.join(dtypes)}")
+    if t.ndim != ndim:
+        raise ValueError(f"{name} has {t.ndim} dimensions, expected {ndim}")
+    if t.device.type != "cuda" or t.device.index != ctx.device:
+        raise ValueError(f"{name} is on {t.device}, the context on cuda:{ctx.device}")
+    return t.data_ptr()
+
+
+def _matrix(ctx: Context, t, name: str, dtypes) -> Tuple[int, int]:
+    """(pointer, row stride) of a 2-d tensor whose rows are contiguous."""
+    p = _on(ctx, t, name, dtypes, 2)
+    (rows, cols), (ld, step) = t.shape, t.stride()
+    if step != 1 and cols > 1 and rows > 0:
+        raise ValueError(f"the rows of {name} are not contiguous (stride {step})")
+    return p, (ld if rows > 1 else max(cols, 1))
+
+
+def _dense(ctx: Context, t, name: str, dtypes, shape) -> Optional[int]:
+    """Pointer of a contiguous tensor of exactly this shape (None stays None)."""
+    if t is None:
+        return None
+    p = _on(ctx, t, name, dtypes, len(shape))
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} is not contiguous")
+    return p
+
+
+_F32, _BF16, _I8, _I32 = ("torch.float32",), ("torch.bfloat16",), ("torch.int8",), ("torch.int32",)
+
+
+def hs_quantize_rows(ctx: Context, x, q, scale, gain=None, eps: float = 1e-6, cu_budget: int = 256,
+                     stream=None) -> None:
+    """x [rows, d] (fp32, bf16 or fp16) -> q int8 [rows, d] and scale fp32 [rows]; gain: bf16 [d] (RMSNorm) or None."""
+    px, ldx = _matrix(ctx, x, "x", _TYPES)
+    pq, ldq = _matrix(ctx, q, "q", _I8)
+    rows, d = x.shape
+    if q.shape != x.shape:
+        raise ValueError(f"q has shape {tuple(q.shape)}, x {tuple(x.shape)}")
+    _check(lib().hs_quantize_rows(ctx.handle, px, _TYPES[str(x.dtype)], ldx, _dense(ctx, gain, "gain", _BF16, (d,)),
+                                  eps, rows, d, pq, ldq, _dense(ctx, scale, "scale", _F32, (rows,)), cu_budget,
+                                  _ptr(stream)))
+
+
+def hs_linear_i8(ctx: Context, a, a_scale, w, w_scale, out, bias=None, cu_budget: int = 256, stream=None) -> None:
+    """out [m, n] = (a int8 [m, k] * a_scale fp32 [m]) (w int8 [n, k] * w_scale fp32 [n])^T + bias bf16 [n]."""
+    pa, lda = _matrix(ctx, a, "a", _I8)
+    pw, ldw = _matrix(ctx, w, "w", _I8)
+    po, ldo = _matrix(ctx, out, "out", _TYPES)
+    (m, k), n = a.shape, w.shape[0]
+    if w.shape[1] != k or tuple(out.shape) != (m, n):
+        raise ValueError(f"a {tuple(a.shape)}, w {tuple(w.shape)} and out {tuple(out.shape)} do not fit")
+    _check(lib().hs_linear_i8(ctx.handle, pa, lda, _dense(ctx, a_scale, "a_scale", _F32, (m,)), pw, ldw,
+                              _dense(ctx, w_scale, "w_scale", _F32, (n,)), _dense(ctx, bias, "bias", _BF16, (n,)),
+                              po, _TYPES[str(out.dtype)], ldo, m, n, k, cu_budget, _ptr(stream)))
+
+
+def hs_logprobs_workspace_size(max_rows: int, vocab: int, top_k: int = 0) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib().hs_logprobs_workspace_size(max_rows, vocab, top_k, ctypes.byref(n)))
+    return int(n.value)
+
+
+def hs_logprobs(ctx: Context, logits, tokens=None, token_logprobs=None, entropy=None, top_logprobs=None,
+                top_tokens=None, cu_budget: int = 256, stream=None, workspace=None,
+                ws_bytes: Optional[int] = None) -> None:
+    """logits [rows, vocab]; tokens int32 and token_logprobs fp32 [rows, n]; entropy fp32 [rows]; top_logprobs fp32 and
+    top_tokens int32 [rows, k].  What is None is not computed."""
+    pz, ld = _matrix(ctx, logits, "logits", _TYPES)
+    rows, vocab = logits.shape
+    if (tokens is None) != (token_logprobs is None) or (top_logprobs is None) != (top_tokens is None):
+        raise ValueError("tokens and token_logprobs, top_logprobs and top_tokens go together")
+    n = 0 if tokens is None else tokens.shape[-1]
+    k = 0 if top_tokens is None else top_tokens.shape[-1]
+    if ws_bytes is None:
+        ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(lib().hs_logprobs(
+        ctx.handle, pz, _TYPES[str(logits.dtype)], ld, rows, vocab, _dense(ctx, tokens, "tokens", _I32, (rows, n)), n,
+        _dense(ctx, token_logprobs, "token_logprobs", _F32, (rows, n)),
+        _dense(ctx, entropy, "entropy", _F32, (rows,)), k,
+        _dense(ctx, top_logprobs, "top_logprobs", _F32, (rows, k)),
+        _dense(ctx, top_tokens, "top_tokens", _I32, (rows, k)), cu_budget, _ptr(stream), _ptr(workspace), ws_bytes))
 
 
 def hs_probe_hw_ids(ctx: Context, stream, n_groups: int, out_ids) -> None:

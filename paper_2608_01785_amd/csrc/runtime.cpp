@@ -7,6 +7,7 @@
 #include <algorithm>
 #include <vector>
 
+#include "context_call.h"
 #include "hs_kernels.h"
 #include "plan.h"
 
@@ -595,6 +596,46 @@ hs_status run_stack(hs_context* ctx, const hs_layer_cfg* cfg, const hs_layer_wei
 }
 
 }  // namespace
+
+namespace hs {
+
+hs_status ContextCall::open(hs_context* ctx, int32_t cu_budget, void* stream) {
+  hs_status st = resolve_stream(ctx, cu_budget, HS_ROLE_SHARED, stream, &stream_);
+  if (st != HS_OK) return st;
+  if (stream) {
+    hipDevice_t dev = -1;
+    HIP_TRY(hipStreamGetDevice(stream_, &dev));
+    if (dev != ctx->device)
+      return fail(HS_ERR_INVALID_ARG, "the stream belongs to device %d, the context to %d", int(dev), ctx->device);
+  }
+  int current = -1;
+  HIP_TRY(hipGetDevice(&current));
+  if (current != ctx->device) {
+    HIP_TRY(hipSetDevice(ctx->device));
+    device_ = current;
+  }
+  // As in run_stack: an earlier call's error is not this one's.
+  (void)hipGetLastError();
+  ctx_ = ctx;
+  return HS_OK;
+}
+
+ContextCall::~ContextCall() {
+  if (device_ >= 0) (void)hipSetDevice(device_);
+}
+
+void ContextCall::timed_begin() {
+  // Launches that a caller captures into a graph are not recorded: their
+  // events would belong to the graph.
+  hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
+  a_ = b_ = nullptr;
+  if (!ctx_->timing || hipStreamIsCapturing(stream_, &cap) != hipSuccess || cap != hipStreamCaptureStatusNone) return;
+  timing_begin(ctx_, stream_, &a_, &b_);
+}
+
+void ContextCall::timed_end(int kind) { timing_end(ctx_, stream_, kind, a_, b_); }
+
+}  // namespace hs
 
 extern "C" {
 

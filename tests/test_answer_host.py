@@ -1,0 +1,157 @@
+"""Refusals of the answering calls: everything invalid fails before any GPU work (no context, fake pointers)."""
+import ctypes
+
+import numpy as np
+import pytest
+
+P = 0x100000   # fake device addresses, far apart and never dereferenced
+
+
+@pytest.fixture(scope="module")
+def b():
+    from paper_2608_01785_amd import binding
+    binding.lib()
+    return binding
+
+
+def quantize(b, **kw):
+    a = dict(x=P, t=0, ldx=64, gain=None, eps=1e-6, rows=4, d=64, q=2 * P, ldq=64, scale=3 * P, cus=256)
+    a.update(kw)
+    st = b.lib().hs_quantize_rows(None, a["x"], a["t"], a["ldx"], a["gain"], a["eps"], a["rows"], a["d"], a["q"],
+                                  a["ldq"], a["scale"], a["cus"], None)
+    return st, b.hs_last_error()
+
+
+def linear(b, **kw):
+    a = dict(a=P, lda=64, sa=2 * P, w=3 * P, ldw=64, sw=4 * P, bias=None, out=5 * P, t=0, ldo=32, m=4, n=32, k=64)
+    a.update(kw)
+    st = b.lib().hs_linear_i8(None, a["a"], a["lda"], a["sa"], a["w"], a["ldw"], a["sw"], a["bias"], a["out"], a["t"],
+                              a["ldo"], a["m"], a["n"], a["k"], 256, None)
+    return st, b.hs_last_error()
+
+
+def logprobs(b, **kw):
+    a = dict(z=P, t=0, ld=64, rows=4, vocab=64, tok=2 * P, nt=1, tlp=3 * P, ent=4 * P, k=5, top=5 * P, tt=6 * P,
+             ws=7 * P, wsb=1 << 30)
+    a.update(kw)
+    st = b.lib().hs_logprobs(None, a["z"], a["t"], a["ld"], a["rows"], a["vocab"], a["tok"], a["nt"], a["tlp"],
+                             a["ent"], a["k"], a["top"], a["tt"], 256, None, a["ws"], a["wsb"])
+    return st, b.hs_last_error()
+
+
+INVALID, UNSUPPORTED = 1, 2
+REFUSED = [
+    (quantize, dict(t=3), INVALID, "type"),
+    (quantize, dict(rows=-1), INVALID, "shape"),
+    (quantize, dict(d=0, ldx=1), INVALID, "shape"),
+    (quantize, dict(x=None), INVALID, "x is null"),
+    (quantize, dict(q=None), INVALID, "q is null"),
+    (quantize, dict(scale=None), INVALID, "scale is null"),
+    (quantize, dict(ldx=63), INVALID, "stride"),
+    (quantize, dict(ldq=63), INVALID, "stride"),
+    (quantize, dict(ldx=(1 << 30) + 1), INVALID, "stride"),
+    (quantize, dict(x=P + 2), INVALID, "aligned"),
+    (quantize, dict(x=P + 1, t=1), INVALID, "aligned"),
+    (quantize, dict(scale=3 * P + 2), INVALID, "aligned"),
+    (quantize, dict(gain=4 * P + 1), INVALID, "aligned"),
+    (quantize, dict(gain=4 * P, eps=0.0), INVALID, "eps"),
+    (quantize, dict(gain=4 * P, eps=float("nan")), INVALID, "eps"),
+    (quantize, dict(gain=4 * P, eps=float("inf")), INVALID, "eps"),
+    (quantize, dict(q=P + 4 * 64 * 4 - 1), INVALID, "overlap"),
+    (quantize, dict(scale=P), INVALID, "overlap"),
+    (quantize, dict(scale=2 * P), INVALID, "overlap"),
+    (quantize, dict(gain=2 * P), INVALID, "overlap"),
+    (linear, dict(t=-1), INVALID, "type"),
+    (linear, dict(m=-1), INVALID, "m -1"),
+    (linear, dict(n=-1), INVALID, "n -1"),
+    (linear, dict(k=0), INVALID, "k 0"),
+    (linear, dict(k=131072, lda=131072, ldw=131072), UNSUPPORTED, "32-bit sums"),
+    (linear, dict(a=None), INVALID, "a is null"),
+    (linear, dict(sa=None), INVALID, "a_scale is null"),
+    (linear, dict(w=None), INVALID, "w is null"),
+    (linear, dict(sw=None), INVALID, "w_scale is null"),
+    (linear, dict(out=None), INVALID, "out is null"),
+    (linear, dict(lda=63), INVALID, "stride"),
+    (linear, dict(ldw=63), INVALID, "stride"),
+    (linear, dict(ldo=31), INVALID, "stride"),
+    (linear, dict(sa=2 * P + 1), INVALID, "aligned"),
+    (linear, dict(bias=6 * P + 1), INVALID, "aligned"),
+    (linear, dict(out=5 * P + 2), INVALID, "aligned"),
+    (linear, dict(out=P), INVALID, "overlap"),
+    (linear, dict(out=4 * P + 124), INVALID, "overlap"),
+    (linear, dict(bias=5 * P), INVALID, "overlap"),
+    (logprobs, dict(t=5), INVALID, "type"),
+    (logprobs, dict(vocab=0), INVALID, "shape"),
+    (logprobs, dict(rows=-2), INVALID, "shape"),
+    (logprobs, dict(k=65), UNSUPPORTED, "top_k"),
+    (logprobs, dict(k=-1), UNSUPPORTED, "top_k"),
+    (logprobs, dict(nt=-1), INVALID, "n_tokens"),
+    (logprobs, dict(ld=63), INVALID, "stride"),
+    (logprobs, dict(z=None), INVALID, "logits is null"),
+    (logprobs, dict(z=P + 1, t=1), INVALID, "aligned"),
+    (logprobs, dict(tok=None), INVALID, "tokens is null"),
+    (logprobs, dict(tlp=None), INVALID, "token_logprobs is null"),
+    (logprobs, dict(top=None), INVALID, "top_logprobs is null"),
+    (logprobs, dict(tt=None), INVALID, "top_tokens is null"),
+    (logprobs, dict(tlp=P), INVALID, "overlap"),
+    (logprobs, dict(ent=3 * P), INVALID, "overlap"),
+    (logprobs, dict(tt=5 * P + 76), INVALID, "overlap"),
+]
+
+
+@pytest.mark.parametrize("i", range(len(REFUSED)))
+def test_refused(b, i):
+    call, kw, status, text = REFUSED[i]
+    st, msg = call(b, **kw)
+    assert st == status and text in msg, (kw, st, msg)
+
+
+@pytest.mark.parametrize("call,kw", [
+    (quantize, {}), (quantize, dict(gain=4 * P)), (quantize, dict(eps=0.0)), (quantize, dict(rows=0, x=None, q=None)),
+    (quantize, dict(x=P + 2, t=2, ldx=65, ldq=67, q=2 * P + 1)), (linear, {}), (linear, dict(bias=6 * P, t=1)),
+    (linear, dict(m=0, a=None, out=None, sa=None)), (linear, dict(n=0, w=None, sw=None, out=None)),
+    (linear, dict(k=131071, lda=131071, ldw=131071, a=100 * P, w=200 * P)),
+    (logprobs, {}), (logprobs, dict(nt=0, tok=None, tlp=None)), (logprobs, dict(k=0, top=None, tt=None)),
+    (logprobs, dict(ent=None)), (logprobs, dict(rows=0, z=None)),
+])
+def test_valid_arguments_reach_the_context(b, call, kw):
+    st, msg = call(b, **kw)
+    assert st == INVALID and msg == "context is null", (st, msg)
+
+
+def test_logprobs_workspace(b):
+    sizes = [b.hs_logprobs_workspace_size(r, 131072, 20) for r in (0, 1, 32, 256, 4096)]
+    assert sizes[0] == 0
+    # A size serves every smaller call.
+    for rows in (1, 7, 32, 100, 256, 1000, 4096):
+        for k in (0, 1, 20, 64):
+            need = b.hs_logprobs_workspace_size(rows, 131072, k)
+            if need == 0:
+                continue
+            st, msg = logprobs(b, rows=rows, vocab=131072, ld=131072, k=k, tok=1 << 40, tlp=2 << 40, ent=3 << 40,
+                               top=4 << 40, tt=5 << 40, ws=6 << 40, wsb=need - 1)
+            assert st == b.HS_ERR_WORKSPACE and "needed" in msg, (rows, k, msg)
+            st, msg = logprobs(b, rows=rows, vocab=131072, ld=131072, k=k, tok=1 << 40, tlp=2 << 40, ent=3 << 40,
+                               top=4 << 40, tt=5 << 40, ws=None, wsb=0)
+            assert st == b.HS_ERR_WORKSPACE and "null" in msg, (rows, k, msg)
+            for fewer in (1, rows // 2, rows - 1):
+                assert b.hs_logprobs_workspace_size(fewer, 131072, k) <= need
+    for bad in ((-1, 10, 0), (1, 0, 0)):
+        with pytest.raises(b.HorizonError):
+            b.hs_logprobs_workspace_size(*bad)
+    assert b.lib().hs_logprobs_workspace_size(1, 1, 0, None) == INVALID
+
+
+def test_binding_refuses_tensors_that_do_not_fit(b):
+    import torch
+
+    class Ctx:
+        handle, device = None, 0
+
+    x = torch.zeros(4, 8)
+    with pytest.raises(ValueError, match="is on cpu"):
+        b.hs_quantize_rows(Ctx, x, x.to(torch.int8), torch.zeros(4))
+    with pytest.raises(ValueError, match="type"):
+        b.hs_quantize_rows(Ctx, x.double(), x.to(torch.int8), torch.zeros(4))
+    with pytest.raises(ValueError, match="dimensions"):
+        b.hs_logprobs(Ctx, x[0])
