@@ -4,17 +4,25 @@
 //   H = log S - T / S,  T = sum e^(z - m) (z - m)
 // Alternatives are ordered by logit, equal ones by the lower token.
 //
-// Every lane keeps a running (m, S, F, T) of its elements; F is S without the
-// largest element's own 1, so that log S = log1p(F) keeps its digits where
-// one token has nearly all the probability.  A 4 KB chunk of a row sits in
-// one wavefront's registers: its maximum first, then one rescaling of the
-// sums, then e^(z - m) of each element.
+// A wavefront keeps a running m, and each of its lanes the sums of its elements
+// against it: S, T, and F, which is S without the elements at m themselves, so
+// that log S = log1p(F) keeps its digits where one token has nearly all the
+// probability.  A 4 KB chunk of a row sits in the wavefront's registers: its
+// maximum first, then e^(z - m) of each element.  Vector instructions bound it
+// (the exponential alone takes four issue slots), so the usual chunk, all of
+// it below m, takes the shortest form: y = z log2(e) - M in one operation with
+// M = m log2(e) rounded, whose rounding error is a factor common to the
+// chunk's sums.  Only a chunk that reaches m (one in c of the first c) keeps
+// F apart and takes exact differences.
 //
-// Alternatives: a wavefront keeps its 64 best keys (order of the value, then
-// the lower token) sorted over its lanes.  A chunk whose maximum does not
-// exceed the k-th best is done; otherwise the elements that do go to a buffer
-// in LDS, and every 64 of them are sorted and merged.  The first chunk's lane
-// maxima give a first bound: their k-th largest.
+// Alternatives: the block's wavefronts sort their lanes' maxima of the first
+// chunk and agree on a value that at least top_k elements reach.  A chunk
+// whose maximum stays below it is done, and elements that reach it leave their
+// key (order of the value, then the lower token) in the wavefront's
+// buffer in LDS.  Every 64 keys are sorted over the lanes and merged into a
+// list of the 64 best, which raises the bound; most rows end before that.
+// What is left, little more than top_k keys, is ranked by counting the larger
+// ones.
 #include "answer_device.h"
 #include "answer_kernels.h"
 
@@ -22,6 +30,7 @@ namespace hs {
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kLowest = -3.4028234663852886e38f;  // running maximum before any element
 constexpr float kInf = __builtin_inff();
 constexpr float kFar = -200.0f;  // e^-200 is 0 in fp32: differences are clamped here where 0 * -inf could arise
@@ -29,21 +38,25 @@ constexpr float kFar = -200.0f;  // e^-200 is 0 in fp32: differences are clamped
 // ---------------------------------------------------------------- running sums
 
 struct Sums {
-  float m, s, f, t;  // maximum, S, S without the maximum's own 1, T
+  float m, s, f, t;  // maximum, S, S without the elements at the maximum, T
 };
 
 __device__ __forceinline__ float exp_of(float d) { return exp2_raw(d * kLog2e); }
 
-__device__ __forceinline__ Sums join(const Sums& a, const Sums& b) {
-  Sums r;
-  r.m = fmaxf(a.m, b.m);
-  const float da = fmaxf(a.m - r.m, kFar), db = fmaxf(b.m - r.m, kFar);
-  const float fa = exp_of(da), fb = exp_of(db);
-  const float sa = a.s * fa, sb = b.s * fb;
-  r.s = sa + sb;
-  r.f = (a.m < r.m ? sa : a.f) + (b.m < r.m ? sb : b.f);
-  r.t = fmaf(sa, da, fa * a.t) + fmaf(sb, db, fb * b.t);
-  return r;
+// The sums against a maximum m >= a.m.
+__device__ __forceinline__ void rescale(Sums& a, float m) {
+  const float d = fmaxf(a.m - m, kFar), f = exp_of(d), s = a.s * f;
+  a.f = a.m < m ? s : a.f;
+  a.t = fmaf(s, d, f * a.t);
+  a.s = s;
+  a.m = m;
+}
+
+__device__ __forceinline__ Sums join(Sums a, Sums b) {
+  const float m = fmaxf(a.m, b.m);
+  rescale(a, m);
+  rescale(b, m);
+  return Sums{m, a.s + b.s, a.f + b.f, a.t + b.t};
 }
 
 // ---------------------------------------------------------------- lanes
@@ -78,17 +91,20 @@ __device__ __forceinline__ uint64_t xor_lane(uint64_t v) {
   return (uint64_t(xor_lane<J>(uint32_t(v >> 32))) << 32) | xor_lane<J>(uint32_t(v));
 }
 
-template <int J>
-__device__ __forceinline__ Sums join_lanes(const Sums& a) {
-  return join(a, Sums{xor_lane<J>(a.m), xor_lane<J>(a.s), xor_lane<J>(a.f), xor_lane<J>(a.t)});
+template <typename V, typename F>
+__device__ __forceinline__ V reduce_wave(V v, F f) {
+  v = f(v, xor_lane<1>(v));
+  v = f(v, xor_lane<2>(v));
+  v = f(v, xor_lane<4>(v));
+  v = f(v, xor_lane<8>(v));
+  v = f(v, xor_lane<16>(v));
+  return f(v, xor_lane<32>(v));
 }
-__device__ __forceinline__ Sums join_wave(Sums a) {
-  a = join_lanes<1>(a);
-  a = join_lanes<2>(a);
-  a = join_lanes<4>(a);
-  a = join_lanes<8>(a);
-  a = join_lanes<16>(a);
-  return join_lanes<32>(a);
+__device__ __forceinline__ float max_wave(float v) {
+  return reduce_wave(v, [](float a, float b) { return fmaxf(a, b); });
+}
+__device__ __forceinline__ float sum_wave(float v) {
+  return reduce_wave(v, [](float a, float b) { return a + b; });
 }
 
 // One stage of a bitonic network over the 64 lanes: lane pairs J apart, the
@@ -139,14 +155,15 @@ __device__ __forceinline__ float value_of(uint64_t key) {
 }
 __device__ __forceinline__ int token_of(uint64_t key) { return int(0xffffffffu - uint32_t(key)); }
 
-constexpr int kBuffer = 128;  // candidates of a wavefront in LDS: 63 left over and 64 new
+constexpr int kBuffer = 128;  // keys of a wavefront in LDS: 63 left over and 64 new
 
 // One wavefront's best keys.
 struct Best {
-  uint64_t list = 0;   // lane i: the i-th best so far
+  uint64_t list = 0;   // lane i: the i-th best of those merged so far
   uint64_t kth;        // a candidate's key must exceed this
   float above;         // so its value must be at least this
-  int count = 0;       // candidates in the buffer
+  int count = 0;       // keys in the buffer
+  bool merged = false;
   int k;
   uint64_t* buf;
 
@@ -156,56 +173,67 @@ struct Best {
     kth = key_of(-kInf, 0);  // above every masked token
     above = kLowest;
   }
-  // Elements still to come have higher tokens than those in the list, so one
-  // that only equals the k-th value loses: the next value up is the least to look at.
-  __device__ __forceinline__ void bound(uint64_t key) {
+  // At least top_k elements reach v.
+  __device__ __forceinline__ void bound(float v) {
+    const uint64_t key = (uint64_t(order_of(v)) << 32) - 1;
     if (key > kth) {
       kth = key;
-      above = value_of(key + (uint64_t(1) << 32));
-    }
-  }
-  // The k-th largest of the first chunk's lane maxima: k elements are at least that.
-  __device__ __forceinline__ void seed(float lane_max) {
-    const float s = sort_wave(lane_max);
-    const float v = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(s), k - 1));
-    if (v > -kInf) {
-      kth = (uint64_t(order_of(v)) << 32) - 1;
       above = v;
     }
   }
-  __device__ __forceinline__ uint64_t kth_of_list() const {
-    return (uint64_t(__builtin_amdgcn_readlane(uint32_t(list >> 32), k - 1)) << 32) |
-           uint32_t(__builtin_amdgcn_readlane(uint32_t(list), k - 1));
-  }
   __device__ __forceinline__ void absorb(uint64_t key) {
     list = merge_lists(list, sort_wave(key));
-    bound(kth_of_list());
+    merged = true;
+    const uint64_t last = (uint64_t(__builtin_amdgcn_readlane(uint32_t(list >> 32), k - 1)) << 32) |
+                          uint32_t(__builtin_amdgcn_readlane(uint32_t(list), k - 1));
+    if (last > kth) {
+      // Elements still to come have higher tokens than those in the list, so
+      // one that only equals the k-th value loses: the next value up is the
+      // least to look at.
+      kth = last;
+      above = value_of(last + (uint64_t(1) << 32));
+    }
   }
   // Every lane offers a key (0: none).
   __device__ __forceinline__ void offer(uint64_t key) {
-    const int lane = threadIdx.x & 63;
     const bool take = key > kth;
     const uint64_t mask = __ballot(take);
-    if (mask == 0) return;
-    const int at = count + __popcll(mask & ((uint64_t(1) << lane) - 1));
+    const int at = count + __builtin_amdgcn_mbcnt_hi(uint32_t(mask >> 32), __builtin_amdgcn_mbcnt_lo(uint32_t(mask), 0));
     if (take) buf[at] = key;
     count += __popcll(mask);
-    if (count >= 64) {
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-      const uint64_t first = buf[lane], rest = buf[64 + lane];
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-      count -= 64;
-      if (lane < count) buf[lane] = rest;
-      absorb(first);
-    }
   }
-  __device__ __forceinline__ void finish() {
+  // Merges the first 64 keys of the buffer, or what there is.
+  __device__ __forceinline__ void settle() {
     const int lane = threadIdx.x & 63;
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    if (count) absorb(lane < count ? buf[lane] : 0);
-    count = 0;
+    const uint64_t first = lane < count ? buf[lane] : 0, rest = buf[64 + lane];
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    count = max(count - 64, 0);
+    if (lane < count) buf[lane] = rest;
+    absorb(first);
+  }
+  // Leaves the wavefront's candidates, at most 127, in the buffer; returns their number.
+  __device__ __forceinline__ int finish() {
+    if (!merged) return count;
+    const int lane = threadIdx.x & 63;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    buf[lane] = list;
+    return min(k, __popcll(__ballot(list != 0)));
   }
 };
+
+// How many of the n keys at p (16-byte aligned) are larger.
+__device__ __forceinline__ int rank_among(const uint64_t* p, int n, uint64_t key) {
+  auto two = [&](int j) {
+    const u32x4 v = *reinterpret_cast<const u32x4*>(p + j);
+    return int((uint64_t(v[1]) << 32 | v[0]) > key) + int((uint64_t(v[3]) << 32 | v[2]) > key);
+  };
+  int r = 0, j = 0;
+  for (; j + 8 <= n; j += 8) r += (two(j) + two(j + 2)) + (two(j + 4) + two(j + 6));
+  for (; j + 2 <= n; j += 2) r += two(j);
+  if (j < n) r += p[j] > key;
+  return r;
+}
 
 // ---------------------------------------------------------------- chunks
 
@@ -235,26 +263,26 @@ struct Chunk {
     for (int l = 0; l < 4; ++l) raw[l] = *reinterpret_cast<const u32x4*>(q + l * 64 * kVec);
   }
   // The same where the chunk reaches past the row [first, last): masked there.
+  // A 16-byte word that the row shares with others is read whole.
   __device__ void load_edge(const T* p, int64_t c, int64_t first, int64_t last) {
+    constexpr uint32_t masked = sizeof(T) == 4 ? 0xff800000u : __is_same(T, uint16_t) ? 0xff80ff80u : 0xfc00fc00u;
 #pragma unroll
     for (int l = 0; l < 4; ++l) {
       const int64_t i = c * kSize + (l * 64 + (threadIdx.x & 63)) * kVec;
-      if (i >= first && i + kVec <= last) {
-        raw[l] = *reinterpret_cast<const u32x4*>(p + i);
-      } else {
-        constexpr uint32_t masked = sizeof(T) == 4 ? 0xff800000u : __is_same(T, uint16_t) ? 0xff80u : 0xfc00u;
-        uint32_t v[4];
+      raw[l] = u32x4{masked, masked, masked, masked};
+      if (i + kVec <= first || i >= last) continue;
+      const u32x4 v = *reinterpret_cast<const u32x4*>(p + i);
+      // Elements lo .. hi - 1 of the word belong to the row.
+      const int lo = int(first > i ? first - i : 0), hi = int(last - i < kVec ? last - i : kVec);
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
-          if constexpr (sizeof(T) == 4) {
-            v[w] = (i + w >= first && i + w < last) ? __float_as_uint(p[i + w]) : masked;
-          } else {
-            const int64_t a = i + 2 * w, b = a + 1;
-            const uint16_t* u = reinterpret_cast<const uint16_t*>(p);
-            v[w] = ((a >= first && a < last) ? u[a] : masked) | (((b >= first && b < last) ? u[b] : masked) << 16);
-          }
-        }
-        raw[l] = u32x4{v[0], v[1], v[2], v[3]};
+      for (int w = 0; w < 4; ++w) {
+        uint32_t keep;
+        if constexpr (sizeof(T) == 4)
+          keep = (w >= lo && w < hi) ? ~0u : 0u;
+        else
+          keep = ((2 * w >= lo && 2 * w < hi) ? 0xffffu : 0u) |
+                 ((2 * w + 1 >= lo && 2 * w + 1 < hi) ? 0xffff0000u : 0u);
+        raw[l][w] = (v[w] & keep) | (masked & ~keep);
       }
     }
   }
@@ -281,57 +309,106 @@ struct Row {
   }
 };
 
-// One chunk's elements into the lane's sums; returns the lane's largest.
-template <typename T>
-__device__ __forceinline__ float accumulate(const Chunk<T>& c, Sums& a) {
-  constexpr int V = Chunk<T>::kVec;
-  float top = c.get(0, 0);
+// A wavefront's sums: m is the same in every lane, the others are the lane's own.
+struct Running {
+  Sums a{kLowest, 0.0f, 0.0f, 0.0f};
+  float scaled = 0.0f;  // M = m log2(e), rounded
+  float delta = 0.0f;   // what the rounding took off: m log2(e) - M
+  float fix = 1.0f;     // 2^-delta
+
+  // The chunk's elements; `top` is its largest over all lanes.
+  template <typename T>
+  __device__ __forceinline__ void add(const Chunk<T>& c, float top) {
+    constexpr int V = Chunk<T>::kVec;
+    float s[4] = {}, f[4] = {}, t[4] = {};
+    // Beyond 1e38 the scaled maximum would leave fp32's range.
+    if (top >= a.m || fabsf(a.m) > 1e38f) {
+      if (top > a.m) {
+        rescale(a, top);
+        scaled = a.m * kLog2e;
+        delta = fmaf(a.m, kLog2e, -scaled);
+        fix = exp2_raw(-delta);
+      }
 #pragma unroll
-  for (int l = 0; l < 4; ++l)
+      for (int l = 0; l < 4; ++l)
 #pragma unroll
-    for (int e = 0; e < V; ++e) top = fmaxf(top, c.get(l, e));
-  const float m = fmaxf(a.m, top);
-  const float d0 = fmaxf(a.m - m, kFar), f0 = exp_of(d0), s0 = a.s * f0;
-  a.f = a.m < m ? s0 : a.f;
-  a.t = fmaf(s0, d0, f0 * a.t);
-  a.m = m;
-  float s[4] = {}, f[4] = {}, t[4] = {};
+        for (int e = 0; e < V; ++e) {
+          const float d = c.get(l, e) - a.m, x = exp_of(d);
+          s[e & 3] += x;
+          f[e & 3] += __builtin_amdgcn_fractf(x);  // 0 where x is 1
+          t[e & 3] = fmaf(x, fmaxf(d, kFar), t[e & 3]);
+        }
+      a.s += (s[0] + s[1]) + (s[2] + s[3]);
+      a.f += (f[0] + f[1]) + (f[2] + f[3]);
+      a.t += (t[0] + t[1]) + (t[2] + t[3]);
+    } else {
 #pragma unroll
-  for (int l = 0; l < 4; ++l)
+      for (int l = 0; l < 4; ++l)
 #pragma unroll
-    for (int e = 0; e < V; ++e) {
-      const float d = c.get(l, e) - m, x = exp_of(d);
-      s[e & 3] += x;
-      f[e & 3] += __builtin_amdgcn_fractf(x);   // 0 where x is 1
-      t[e & 3] = fmaf(x, fmaxf(d, kFar), t[e & 3]);
+        for (int e = 0; e < V; ++e) {
+          const float y = fmaf(c.get(l, e), kLog2e, -scaled), x = exp2_raw(y);
+          s[e & 3] += x;
+          t[e & 3] = fmaf(x, fmaxf(y, 2 * kFar), t[e & 3]);
+        }
+      const float sum = (s[0] + s[1]) + (s[2] + s[3]);
+      const float weighted = fmaf(-delta, sum, (t[0] + t[1]) + (t[2] + t[3]));
+      a.s = fmaf(sum, fix, a.s);
+      a.f = fmaf(sum, fix, a.f);
+      a.t = fmaf(weighted, fix * kLn2, a.t);
     }
-  a.s = s0 + ((s[0] + s[1]) + (s[2] + s[3]));
-  a.f += (f[0] + f[1]) + (f[2] + f[3]);
-  a.t += (t[0] + t[1]) + (t[2] + t[3]);
+  }
+  __device__ __forceinline__ Sums total() const { return Sums{a.m, sum_wave(a.s), sum_wave(a.f), sum_wave(a.t)}; }
+};
+
+// Lane maxima of the four loads.
+template <typename T>
+__device__ __forceinline__ f32x4 tops_of(const Chunk<T>& c) {
+  f32x4 top;
+#pragma unroll
+  for (int l = 0; l < 4; ++l) {
+    top[l] = c.get(l, 0);
+#pragma unroll
+    for (int e = 1; e < Chunk<T>::kVec; ++e) top[l] = fmaxf(top[l], c.get(l, e));
+  }
   return top;
 }
 
-// The chunk's elements that may be among the best.  A lane offers one element
-// at a time, read again from memory (the cache still has it) since registers
-// cannot be indexed.
+// The chunk's elements that may be among the best.  A lane offers one at a
+// time, from a copy of the chunk in LDS since registers cannot be indexed
+// (read again from memory it would wait for the next chunk's loads as well).
+// After the last chunk a list that has been started takes the rest of the
+// buffer.
 template <typename T>
-__device__ __forceinline__ void offer_chunk(const Chunk<T>& c, const Row<T>& row, int i, Best& best) {
+__device__ __forceinline__ void offer_chunk(const Chunk<T>& c, const f32x4& tops, const Row<T>& row, int i, bool last,
+                                            Best& best, u32x4 (*copy)[4]) {
   constexpr int V = Chunk<T>::kVec;
+  const int lane = threadIdx.x & 63;
   uint32_t hits = 0;
 #pragma unroll
-  for (int l = 0; l < 4; ++l)
+  for (int l = 0; l < 4; ++l) {
+    if (!__ballot(tops[l] >= best.above)) continue;
+    copy[lane][l] = c.raw[l];
 #pragma unroll
     for (int e = 0; e < V; ++e) hits |= uint32_t(c.get(l, e) >= best.above) << (l * V + e);
-  while (__ballot(hits != 0)) {
-    uint64_t key = 0;
-    if (hits) {
-      const int j = __builtin_ctz(hits);
-      hits &= hits - 1;
-      const int64_t at = int64_t(i) * Chunk<T>::kSize + ((j / V) * 64 + int(threadIdx.x & 63)) * V + j % V;
-      // Outside the row a chunk holds masked elements.
-      if (at >= row.first && at < row.last) key = key_of(elem(row.p, at), uint32_t(at - row.first));
+  }
+  const int at0 = i * Chunk<T>::kSize + lane * V - int(row.first);  // token of the lane's element 0
+  while (true) {
+    const bool more = __ballot(hits != 0) != 0;
+    if (more) {
+      uint64_t key = 0;
+      if (hits) {
+        const int j = __builtin_ctz(hits);
+        hits &= hits - 1;
+        const float z = elem(reinterpret_cast<const T*>(copy[lane]), j);
+        // Outside the row a chunk holds masked elements.
+        if (z > -kInf) key = key_of(z, at0 + (j / V) * 64 * V + j % V);
+      }
+      best.offer(key);
     }
-    best.offer(key);
+    if (best.count >= 64 || (!more && last && best.merged && best.count > 0))
+      best.settle();
+    else if (!more)
+      break;
   }
 }
 
@@ -339,114 +416,225 @@ __device__ __forceinline__ void offer_chunk(const Chunk<T>& c, const Row<T>& row
 
 __device__ __forceinline__ float log_sum(const Sums& a) { return a.s < 1.5f ? log1pf(a.f) : logf(a.s); }
 
-// One wavefront writes a row's results from its sums and its best keys.
+// A row's log probabilities from its sums.
+struct Answer {
+  float m, log_s;
+  bool bad, none;
+  __device__ __forceinline__ explicit Answer(const Sums& a)
+      : m(a.m), log_s(0.0f), bad(a.s != a.s), none(a.s == 0.0f) {
+    if (!none) log_s = log_sum(a);
+  }
+  __device__ __forceinline__ float logp(float z) const {
+    return bad ? __builtin_nanf("") : z == -kInf ? z : (z - m) - log_s;
+  }
+};
+
+// Given token j of a row and its logit, loaded ahead of the sums.
+struct Given {
+  int tok = -1;
+  float z = 0.0f;
+  template <typename T>
+  __device__ __forceinline__ void load(const LogprobsArgs& a, const T*, int row, int j) {
+    if (j >= a.n_tokens) return;
+    tok = a.tokens[int64_t(row) * a.n_tokens + j];
+    if (tok >= 0 && tok < a.vocab) z = elem(static_cast<const T*>(a.logits) + int64_t(row) * a.ld, tok);
+  }
+  __device__ __forceinline__ void write(const LogprobsArgs& a, int row, int j, const Answer& w) const {
+    if (j < a.n_tokens)
+      a.token_lp[int64_t(row) * a.n_tokens + j] =
+          tok == -1 ? 0.0f : (tok < 0 || tok >= a.vocab) ? __builtin_nanf("") : w.logp(z);
+  }
+};
+
+// One wavefront writes a row's entropy and given tokens; lane j has token j.
 template <typename T>
-__device__ __forceinline__ void write_row(const LogprobsArgs& a, int row, const Sums& sums, uint64_t best) {
+__device__ __forceinline__ void write_row(const LogprobsArgs& a, int row, const Sums& sums, const Answer& w,
+                                          const Given& given) {
   const int lane = threadIdx.x & 63;
-  const bool bad = sums.s != sums.s, none = sums.s == 0.0f;
-  const float nan = __builtin_nanf(""), log_s = none ? 0.0f : log_sum(sums);
-  auto logp = [&](float z) { return bad ? nan : z == -kInf ? z : (z - sums.m) - log_s; };
-  if (lane == 0 && a.entropy) a.entropy[row] = bad ? nan : none ? 0.0f : log_s - sums.t / sums.s;
-  const T* z = static_cast<const T*>(a.logits) + int64_t(row) * a.ld;
-  for (int j = lane; j < a.n_tokens; j += 64) {
-    const int64_t o = int64_t(row) * a.n_tokens + j;
-    const int tok = a.tokens[o];
-    a.token_lp[o] = tok == -1 ? 0.0f : (tok < 0 || tok >= a.vocab) ? nan : logp(elem(z, tok));
+  if (lane == 0 && a.entropy)
+    a.entropy[row] = w.bad ? __builtin_nanf("") : w.none ? 0.0f : w.log_s - sums.t / sums.s;
+  given.write(a, row, lane, w);
+  for (int j = lane + 64; j < a.n_tokens; j += 64) {
+    Given g;
+    g.load(a, static_cast<const T*>(nullptr), row, j);
+    g.write(a, row, j, w);
   }
-  if (lane < a.top_k) {
-    const int64_t o = int64_t(row) * a.top_k + lane;
-    const bool listed = best != 0 && !bad;
-    a.top_tokens[o] = listed ? token_of(best) : -1;
-    a.top_lp[o] = bad ? nan : listed ? logp(value_of(best)) : -kInf;
-  }
+}
+
+// Alternative number `rank` of a row (key 0: none).
+__device__ __forceinline__ void write_top(const LogprobsArgs& a, int row, int rank, uint64_t key, const Answer& w) {
+  const int64_t o = int64_t(row) * a.top_k + rank;
+  a.top_tokens[o] = key != 0 && !w.bad ? token_of(key) : -1;
+  a.top_lp[o] = w.bad ? __builtin_nanf("") : key != 0 ? w.logp(value_of(key)) : -kInf;
 }
 
 __device__ __forceinline__ uint64_t* partial_keys(const LogprobsArgs& a, int64_t blocks) {
   return reinterpret_cast<uint64_t*>(static_cast<f32x4*>(a.part) + blocks);
 }
 
-// The block's wavefronts' sums and lists, joined in wavefront 0.
-template <int W, bool TOP>
-__device__ __forceinline__ void join_block(Sums& sums, uint64_t& list, f32x4* lds_sums, uint64_t (*lds_keys)[kBuffer]) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-  for (int half = W / 2; half > 0; half >>= 1) {
-    if (wave >= half && wave < 2 * half) {
-      if (lane == 0) lds_sums[wave] = f32x4{sums.m, sums.s, sums.f, sums.t};
-      if (TOP) lds_keys[wave][lane] = list;
-    }
-    __syncthreads();
-    if (wave < half) {
-      const f32x4 o = lds_sums[wave + half];
-      sums = join(sums, Sums{o[0], o[1], o[2], o[3]});
-      if (TOP) list = merge_lists(list, lds_keys[wave + half][lane]);
-    }
-  }
-}
-
 // Block (row, split): W wavefronts take the split's chunks in turn.
 template <typename T, int W, bool TOP>
 __global__ __launch_bounds__(64 * W) void logprobs_kernel(LogprobsArgs a, int splits, int chunks_per_split) {
-  __shared__ uint64_t keys[TOP ? W : 1][kBuffer];
-  __shared__ f32x4 lds_sums[W];
+  __shared__ __attribute__((aligned(16))) uint64_t keys[TOP ? W : 1][kBuffer];
+  __shared__ u32x4 copies[TOP ? W : 1][64][4];
+  __shared__ f32x4 all_sums[W];
+  __shared__ float seeds[W][2];
+  __shared__ int counts[W];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t blocks = int64_t(a.rows) * splits;
   const int r = int(blockIdx.x / splits), split = int(blockIdx.x % splits);
   const Row<T> row(a, r);
-  const int end = min(row.chunks, (split + 1) * chunks_per_split);
+  const int begin = split * chunks_per_split, end = min(row.chunks, begin + chunks_per_split);
 
-  Sums sums{kLowest, 0.0f, 0.0f, 0.0f};
+  Running run;
   Best best;
-  if (TOP) best.init(a.top_k, keys[wave]);
-  int i = split * chunks_per_split + wave;
-  bool first = true;
-  Chunk<T> next;
+  if constexpr (TOP) best.init(a.top_k, keys[wave]);
+  Given given;
+  Chunk<T> c, next;
+  int i = begin + wave;
   if (i < end) row.load(next, i);
+  if (wave == 0 && splits == 1) given.load(a, row.p, r, lane);
+  auto lane_top_of = [](const f32x4& t) { return fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3])); };
+  if constexpr (TOP) {
+    // Each of the n wavefronts with a chunk has ceil(top_k / n) lanes at or
+    // above the least of their ceil(top_k / n)-th lane maxima, and one alone
+    // has top_k at or above its top_k-th.
+    float share = kInf, whole = -kInf;  // of a wavefront without a chunk
+    if (i < end) {
+      const int n = min(W, end - begin);
+      const float s = sort_wave(lane_top_of(tops_of(next)));
+      share = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(s), (a.top_k + n - 1) / n - 1));
+      whole = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(s), a.top_k - 1));
+    }
+    if constexpr (W > 1) {
+      if (lane == 0) {
+        seeds[wave][0] = share;
+        seeds[wave][1] = whole;
+      }
+      __syncthreads();
+#pragma unroll
+      for (int w = 0; w < W; ++w) {
+        share = fminf(share, seeds[w][0]);
+        whole = fmaxf(whole, seeds[w][1]);
+      }
+    }
+    best.bound(fmaxf(share, whole));
+  }
   while (i < end) {
-    const Chunk<T> c = next;
+    c = next;
     if (i + W < end) row.load(next, i + W);
-    const float top = accumulate(c, sums);
+    const f32x4 tops = tops_of(c);
+    const float top = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(max_wave(lane_top_of(tops)))));
+    run.add(c, top);
     if constexpr (TOP) {
-      if (first) best.seed(top);
-      if (__ballot(top >= best.above)) offer_chunk(c, row, i, best);
-      first = false;
+      const bool last = i + W >= end;
+      if (top >= best.above || (last && best.merged)) offer_chunk(c, tops, row, i, last, best, copies[wave]);
     }
     i += W;
   }
-  if (TOP) best.finish();
-  sums = join_wave(sums);
-  join_block<W, TOP>(sums, best.list, lds_sums, keys);
-  if (wave != 0) return;
-  if (splits == 1) {
-    write_row<T>(a, r, sums, TOP ? best.list : 0);
-    return;
+
+  Sums sums = run.total();
+  int n = 0;
+  if constexpr (TOP) n = best.finish();
+  if (lane == 0) {
+    all_sums[wave] = f32x4{sums.m, sums.s, sums.f, sums.t};
+    counts[wave] = n;
   }
-  if (lane == 0) static_cast<f32x4*>(a.part)[blockIdx.x] = f32x4{sums.m, sums.s, sums.f, sums.t};
-  if (TOP && lane < a.top_k) partial_keys(a, blocks)[int64_t(blockIdx.x) * a.top_k + lane] = best.list;
+  __syncthreads();
+#pragma unroll 1
+  for (int w = 0; w < W; ++w)
+    if (w != wave) {
+      const f32x4 o = all_sums[w];
+      sums = join(sums, Sums{o[0], o[1], o[2], o[3]});
+    }
+  const Answer answer(sums);
+  if (wave == 0) {
+    if (splits == 1)
+      write_row<T>(a, r, sums, answer, given);
+    else if (lane == 0)
+      static_cast<f32x4*>(a.part)[blockIdx.x] = f32x4{sums.m, sums.s, sums.f, sums.t};
+  }
+  if constexpr (TOP) {
+    uint64_t* part = splits == 1 ? nullptr : partial_keys(a, int64_t(a.rows) * splits) + int64_t(blockIdx.x) * a.top_k;
+    auto put = [&](int rank, uint64_t key) {
+      if (splits == 1)
+        write_top(a, r, rank, key, answer);
+      else
+        part[rank] = key;
+    };
+    int total = 0;
+#pragma unroll
+    for (int w = 0; w < W; ++w) total += counts[w];
+    for (int j = lane; j < n; j += 64) {
+      const uint64_t key = keys[wave][j];
+      int rank = 0;
+#pragma unroll 1
+      for (int w = 0; w < W; ++w) rank += rank_among(keys[w], counts[w], key);
+      if (rank < a.top_k) put(rank, key);
+    }
+    if (wave == 0 && lane >= total && lane < a.top_k) put(lane, 0);
+  }
 }
 
-// A row's partial results: lane i takes split i's sums, the wavefronts the
-// lists in turn.
+// A row's partial results: lane i takes split i's sums; of the splits' sorted
+// keys those that can be among the best (by the same bound as above, with
+// splits in the place of wavefronts) are ranked.
 template <typename T, bool TOP>
 __global__ __launch_bounds__(256) void join_kernel(LogprobsArgs a, int splits) {
-  __shared__ uint64_t keys[TOP ? 4 : 1][kBuffer];
-  __shared__ f32x4 lds_sums[4];
+  __shared__ __attribute__((aligned(16))) uint64_t keys[TOP ? kLogprobsMaxSplits * kLogprobsMaxTop : 2];
+  __shared__ int count;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = blockIdx.x;
   const int64_t base = int64_t(r) * splits;
+  const int n_keys = TOP ? splits * a.top_k : 0;
+  const uint64_t* src = partial_keys(a, int64_t(a.rows) * splits) + base * a.top_k;
+  // Every load that depends on none other first.
   Sums sums{kLowest, 0.0f, 0.0f, 0.0f};
-  if (wave == 0 && lane < splits) {
+  uint32_t share = ~0u, whole = 0;  // the keys' orders
+  if (lane < splits) {
     const f32x4 v = static_cast<const f32x4*>(a.part)[base + lane];
     sums = Sums{v[0], v[1], v[2], v[3]};
+    if constexpr (TOP) {
+      share = uint32_t(src[lane * a.top_k + (a.top_k + splits - 1) / splits - 1] >> 32);
+      whole = uint32_t(src[lane * a.top_k + a.top_k - 1] >> 32);
+    }
   }
-  sums = join_wave(sums);
-  uint64_t list = 0;
-  if (TOP) {
-    const uint64_t* src = partial_keys(a, int64_t(a.rows) * splits) + base * a.top_k;
-    for (int i = wave; i < splits; i += 4)
-      list = merge_lists(list, lane < a.top_k ? src[int64_t(i) * a.top_k + lane] : 0);
+  constexpr int kAhead = 4;
+  uint64_t mine[kAhead];
+#pragma unroll
+  for (int q = 0; q < kAhead; ++q) {
+    const int j = threadIdx.x + 256 * q;
+    mine[q] = j < n_keys ? src[j] : 0;
   }
-  join_block<4, TOP>(sums, list, lds_sums, keys);
-  if (wave == 0) write_row<T>(a, r, sums, list);
+  Given given;
+  if (wave == 0) given.load(a, static_cast<const T*>(nullptr), r, lane);
+  if constexpr (TOP) {
+    if (threadIdx.x == 0) count = 0;
+    share = reduce_wave(share, [](uint32_t x, uint32_t y) { return min(x, y); });
+    whole = reduce_wave(whole, [](uint32_t x, uint32_t y) { return max(x, y); });
+    const uint64_t bound = uint64_t(max(max(share, whole), 1u)) << 32;
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < kAhead; ++q)
+      if (mine[q] >= bound) keys[atomicAdd(&count, 1)] = mine[q];
+    for (int j = threadIdx.x + 256 * kAhead; j < n_keys; j += 256) {
+      const uint64_t key = src[j];
+      if (key >= bound) keys[atomicAdd(&count, 1)] = key;
+    }
+  }
+  const float m = max_wave(sums.m);
+  rescale(sums, m);
+  sums = Sums{m, sum_wave(sums.s), sum_wave(sums.f), sum_wave(sums.t)};
+  const Answer answer(sums);
+  if (wave == 0) write_row<T>(a, r, sums, answer, given);
+  if constexpr (TOP) {
+    __syncthreads();
+    const int n = count;
+    for (int j = threadIdx.x; j < n; j += 256) {
+      const uint64_t key = keys[j];
+      const int rank = rank_among(keys, n, key);
+      if (rank < a.top_k) write_top(a, r, rank, key, answer);
+    }
+    if (int(threadIdx.x) >= n && int(threadIdx.x) < a.top_k) write_top(a, r, threadIdx.x, 0, answer);
+  }
 }
 
 template <typename T, bool TOP>
