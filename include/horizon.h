@@ -460,6 +460,7 @@ hs_status hs_quantize_rows(hs_context* ctx, const void* x, int32_t x_type, int64
  *   a    int8 [m, k] with a_scale fp32 [m] (tokens);
  *   w    int8 [n, k] with w_scale fp32 [n] (channels; [out, in] like all weights);
  *   bias bf16 [n] or NULL;  out [m, n] of out_type.
+ * Row strides of a and w are at most 2^22 (else HS_ERR_UNSUPPORTED).
  * The sum is exact (k <= 131071, else HS_ERR_UNSUPPORTED); then
  * fp32(sum) * fp32(a_scale * w_scale) + bias, each step rounded to fp32, and one
  * rounding to out_type (beyond its range: infinity).  The result does not depend

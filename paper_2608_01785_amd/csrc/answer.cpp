@@ -103,6 +103,9 @@ hs_status hs_linear_i8(hs_context* ctx, const void* a, int64_t lda, const float*
   if (m < 0 || n < 0 || k < 1) return hs::fail(HS_ERR_INVALID_ARG, "m %d, n %d, k %d", m, n, k);
   if (k > hs::kLinearI8MaxK)
     return hs::fail(HS_ERR_UNSUPPORTED, "k %d: 32-bit sums hold %d products", k, hs::kLinearI8MaxK);
+  if (lda > hs::kLinearI8MaxStride || ldw > hs::kLinearI8MaxStride)
+    return hs::fail(HS_ERR_UNSUPPORTED, "row strides %lld and %lld: operands allow %lld", (long long)lda,
+                    (long long)ldw, (long long)hs::kLinearI8MaxStride);
   const size_t osz = type_size(out_type);
   const Span sa = rows_of("a", a, m, k, lda, 1), sw = rows_of("w", w, n, k, ldw, 1);
   const Span sas = rows_of("a_scale", a_scale, m, 1, 1, 4), sws = rows_of("w_scale", w_scale, n, 1, 1, 4);

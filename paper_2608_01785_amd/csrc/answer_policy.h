@@ -8,6 +8,7 @@ namespace hs {
 
 constexpr int kLogprobsMaxTop = 64;       // alternatives a row can list: one per lane of a wavefront
 constexpr int kLinearI8MaxK = 131071;     // (-128)^2 k stays below 2^31
+constexpr int64_t kLinearI8MaxStride = int64_t(1) << 22;  // 256 rows of an operand stay within 32-bit offsets
 
 // hs_logprobs: a row's elements go through wavefronts in chunks of 4 KB (one
 // wavefront's registers); `waves` wavefronts form a block, and a row is split

@@ -66,6 +66,8 @@ REFUSED = [
     (linear, dict(n=-1), INVALID, "n -1"),
     (linear, dict(k=0), INVALID, "k 0"),
     (linear, dict(k=131072, lda=131072, ldw=131072), UNSUPPORTED, "32-bit sums"),
+    (linear, dict(lda=(1 << 22) + 1), UNSUPPORTED, "strides"),
+    (linear, dict(ldw=(1 << 22) + 1), UNSUPPORTED, "strides"),
     (linear, dict(a=None), INVALID, "a is null"),
     (linear, dict(sa=None), INVALID, "a_scale is null"),
     (linear, dict(w=None), INVALID, "w is null"),
