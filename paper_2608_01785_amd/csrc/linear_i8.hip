@@ -8,12 +8,23 @@
 // The MFMA is issued as C^T = W A^T: every lane of a 32 x 32 accumulator owns
 // one row of a and four consecutive channels per register group.
 //
-// A block of WN x WM waves computes tiles of 32 NS WN channels x 32 MT WM rows;
-// K advances in stages of 128 bytes, one cache line of every row, through two
-// LDS buffers, fetched two to three stages ahead into registers.  The grid is
-// persistent and the stages of a block's tiles form one sequence: the last
-// stages of a tile already fetch the next one's first, and its epilogue runs
-// under those loads.
+// A block of WN x WM waves computes tiles of 32 NS WN channels x 32 MT WM rows.
+// K advances in stages of 64 bytes; half of the waves fetch the channels, half
+// the rows, with 16-byte loads into a ring of registers:
+//   stage t is loaded during stage t - 4, written to LDS buffer t % 2 in the
+//   first half of stage t - 1 and multiplied during stage t.
+// One barrier per stage, between its two 32-wide halves, after each wave's
+// writes of stage t + 1 and fragment reads of stage t have completed: it makes
+// the writes visible to the second half's reads of stage t + 1 and retires
+// every read of the buffer that the next stage overwrites.  Stages past the
+// end of k, up to a multiple of four, are zeros.
+//
+// The grid is persistent and the stages of a block's tiles form one sequence:
+// the last four stages of a tile already fetch the next one's first four, and
+// its epilogue runs under those loads.  An epilogue reads no memory: a tile's
+// scales and bias come into LDS during the epilogue before it (stores count
+// against the same completion counter as loads, so a load between them would
+// wait for them; with such loads an epilogue took 18 us).
 #include "answer_kernels.h"
 #include "horizon.h"
 #include "hs_device.h"
@@ -24,19 +35,19 @@ namespace {
 typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
 typedef int32_t i32x16 __attribute__((ext_vector_type(16)));
 
-constexpr int BK = 128;       // bytes of K per stage: 8 chunks of 16
-constexpr int kKk = BK / 32;  // MFMA steps per stage
+constexpr int BK = 64;      // bytes of K per stage: 4 chunks of 16
+constexpr int kUnroll = 4;  // stages per loop body
 constexpr int kGroupM = 4;
 
 __device__ __forceinline__ i32x16 mfma32_i8(const u32x4& a, const u32x4& b, const i32x16& c) {
   return __builtin_amdgcn_mfma_i32_32x32x32_i8(__builtin_bit_cast(i32x4, a), __builtin_bit_cast(i32x4, b), c, 0, 0, 0);
 }
 
-// 16-byte chunk c of tile row r sits at physical chunk c ^ ...: a pass of 16
-// lanes reads one logical chunk of eight even and eight odd rows, and odd rows
-// start on bank 32, so bits 1 .. 3 of r permute the chunks; bit 0 keeps the
-// writes of two rows in different halves.
-__device__ __forceinline__ int phys(int r, int c) { return c ^ ((r >> 1) & 7) ^ ((r & 1) << 2); }
+// 16-byte chunk c of tile row r sits at physical chunk c ^ swz(r).  A 16-lane
+// pass of fragment reads covers rows r0 .. r0 + 15 at one logical chunk;
+// (r & 3, c ^ swz(r)) is then distinct for all 16 rows, so the pass touches
+// each of the 64 banks once.
+__device__ __forceinline__ int swz(int r) { return ((r >> 1) ^ (r >> 2)) & 3; }
 
 // ---------------------------------------------------------------- epilogue
 
@@ -54,89 +65,110 @@ struct OutOf<HS_TYPE_F16> {
 };
 
 // The documented roundings of one output, none of them fused.
-__device__ __forceinline__ float scaled(int32_t sum, float a_scale, float w_scale) {
+__device__ __forceinline__ float output(int32_t sum, float a_scale, float w_scale, bool with_bias, float bias) {
 #pragma clang fp contract(off)
   const float s = a_scale * w_scale;
-  return float(sum) * s;
-}
-__device__ __forceinline__ float biased(float v, uint16_t bias) {
-#pragma clang fp contract(off)
-  return v + bf2f(bias);
+  const float v = float(sum) * s;
+  return with_bias ? v + bias : v;
 }
 
-// Four consecutive channels n .. n + 3 of one row.  WIDE: the address of a
-// multiple of four channels is aligned for one store.
-template <int TYPE, bool WIDE>
-__device__ __forceinline__ void store4(const LinearI8Args& a, int m, int n, const i32x4& sum, float a_scale,
-                                       const f32x4& ws, const float* b) {
-  using T = typename OutOf<TYPE>::T;
-  T* p = static_cast<T*>(a.out) + int64_t(m) * a.ldo + n;
-  float v[4];
+// Four consecutive values from p on, of which the first `left` exist.
+template <typename T>
+__device__ __forceinline__ void store_each(T* p, const float (&v)[4], int left) {
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
-#pragma clang fp contract(off)
-    v[e] = scaled(sum[e], a_scale, ws[e]);
-    if (a.bias) v[e] = v[e] + b[e];
-  }
-  if (WIDE && n + 4 <= a.n) {
-    typedef T T4 __attribute__((ext_vector_type(4)));
-    *reinterpret_cast<T4*>(p) = T4{T(v[0]), T(v[1]), T(v[2]), T(v[3])};
-  } else {
+  for (int e = 0; e < 4; ++e)
+    if (e < left) p[e] = T(v[e]);
+}
+
+template <typename T>
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+  typedef T T2 __attribute__((ext_vector_type(2)));
+  typedef float f2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector((f2{lo, hi}), T2));
+}
+
+// Channels 0 .. 15 of a 16-channel run of one row, of which the first `left`
+// exist: the low lane of the pair (lane, lane + 32) holds 0 .. 3 in `lo` and
+// 8 .. 11 in `hi`, the high lane (h = 1) the four after each.  WIDE: p is
+// aligned to 16 bytes; 16-bit values change lanes so that each lane stores 16
+// bytes.  Both lanes of the pair must be active.
+template <typename T, bool WIDE>
+__device__ __forceinline__ void store_run(T* p, int h, const float (&lo)[4], const float (&hi)[4], int left) {
+  if constexpr (sizeof(T) == 2) {
+    if (WIDE && left >= 16) {
+      const uint32_t a[2] = {pack2<T>(lo[0], lo[1]), pack2<T>(lo[2], lo[3])};
+      const uint32_t b[2] = {pack2<T>(hi[0], hi[1]), pack2<T>(hi[2], hi[3])};
+      u32x4 v;
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (n + e < a.n) p[e] = T(v[e]);
+      for (int d = 0; d < 2; ++d) {
+        // Lanes 32 .. 63 of the first operand against lanes 0 .. 31 of the second.
+        const auto s = __builtin_amdgcn_permlane32_swap(a[d], b[d], false, false);
+        v[d] = s[0];
+        v[2 + d] = s[1];
+      }
+      *reinterpret_cast<u32x4*>(p + 8 * h) = v;
+      return;
+    }
+  } else if (WIDE && left >= 16) {
+    *reinterpret_cast<f32x4*>(p + 4 * h) = f32x4{lo[0], lo[1], lo[2], lo[3]};
+    *reinterpret_cast<f32x4*>(p + 8 + 4 * h) = f32x4{hi[0], hi[1], hi[2], hi[3]};
+    return;
   }
+  store_each(p + 4 * h, lo, left - 4 * h);
+  store_each(p + 8 + 4 * h, hi, left - 8 - 4 * h);
 }
 
 // ---------------------------------------------------------------- tiles
 
-// Operand rows of one tile: the 16-byte chunk (lane & 7) of rows
-// (lane >> 3) + 8 (wave + WAVES l).
+// One wave's share of an operand's rows: the 16-byte chunk (lane & 3) of rows
+// row0 + (lane >> 2) + 16 l.
 //   ALIGNED: base, row stride and k are multiples of 16.  A buffer resource
-//   over the tile's rows: what lies past the last row or past k reads zero.
+//   over the rows: what lies past the last row or past k reads zero.
 //   Otherwise: byte addresses, rows past the last read it again (they are
 //   never stored) and the chunk that holds the end of k is read from 16 bytes
 //   before that end and shifted.
-template <bool ALIGNED, int WAVES, int L>
+template <bool ALIGNED, int L>
 struct Operand {
   const int8_t* base;
   __amdgpu_buffer_rsrc_t res;
-  uint32_t off, off_tail;  // ALIGNED: load 0's offset, and in the stage that holds the end of k
-  uint32_t offs[ALIGNED ? 1 : L];
+  uint32_t off[ALIGNED ? 1 : L];
 
   __device__ __forceinline__ void set(const int8_t* p, int64_t ld, int row0, int rows, int k) {
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int r = 8 * wave + (lane >> 3), c = lane & 7;
-    const int left = rows - row0;
-    base = p + int64_t(row0) * ld;
+    const int r = (threadIdx.x & 63) >> 2, c = threadIdx.x & 3;
     if constexpr (ALIGNED) {
-      const int span = min(left, 8 * WAVES * L);
+      // A wave without rows keeps one (never stored).
+      const int first = min(row0, rows - 1), span = min(rows - first, 16 * L);
+      base = p + int64_t(first) * ld;
       res = make_rsrc(base, uint32_t(span - 1) * uint32_t(ld) + uint32_t(k));
-      off = uint32_t(r) * uint32_t(ld) + uint32_t(c * 16);
-      off_tail = c * 16 < (k & (BK - 1)) ? off : 0x80000000u;
+      off[0] = uint32_t(r) * uint32_t(ld) + uint32_t(c * 16);
     } else {
+      base = p;
+      const int first = min(row0, rows - 1);
+      base = p + int64_t(first) * ld;
 #pragma unroll
-      for (int l = 0; l < L; ++l) offs[l] = uint32_t(min(r + 8 * WAVES * l, left - 1)) * uint32_t(ld) + uint32_t(c * 16);
+      for (int l = 0; l < L; ++l) off[l] = uint32_t(min(r + 16 * l, rows - 1 - first)) * uint32_t(ld) + uint32_t(c * 16);
     }
   }
   __device__ __forceinline__ u32x4 load(int l, int stage, int64_t ld, int k) const {
     const int whole = k / BK;  // stages without the end of k
     if constexpr (ALIGNED) {
-      const uint32_t v = stage < whole ? off : stage > whole ? 0x80000000u : off_tail;
-      const uint32_t s = uint32_t(min(stage, (k - 1) / BK)) * BK + uint32_t(8 * WAVES * l) * uint32_t(ld);
+      uint32_t v = off[0];
+      // Past k: an offset outside the resource, which reads zero.
+      if (stage >= whole && stage * BK + int(threadIdx.x & 3) * 16 >= k) v = 0x80000000u;
+      const uint32_t s = uint32_t(min(stage, (k - 1) / BK)) * BK + uint32_t(16 * l) * uint32_t(ld);
       return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(res, v, s, 0));
     } else {
       u32x4 v = {0, 0, 0, 0};
       const int8_t* p = base + int64_t(stage) * BK;
       if (stage < whole) {
-        __builtin_memcpy(&v, p + offs[l], 16);
+        __builtin_memcpy(&v, p + off[l], 16);
         return v;
       }
-      const int n = k - stage * BK - (int(threadIdx.x) & 7) * 16;  // bytes of the chunk that k holds
+      const int n = k - stage * BK - (int(threadIdx.x) & 3) * 16;  // bytes of the chunk that k holds
       if (n >= 16) {
-        __builtin_memcpy(&v, p + offs[l], 16);
+        __builtin_memcpy(&v, p + off[l], 16);
       } else if (n > 0 && k >= 16) {
-        __builtin_memcpy(&v, p + offs[l] - (16 - n), 16);
+        __builtin_memcpy(&v, p + off[l] - (16 - n), 16);
         // Bytes 16 - n .. 15 are the chunk's first n.
         const int words = (16 - n) >> 2, bytes = (16 - n) & 3;
         uint32_t w[5] = {v[0], v[1], v[2], v[3], 0};
@@ -151,7 +183,7 @@ struct Operand {
       } else if (n > 0) {
         uint32_t w[4] = {0, 0, 0, 0};
         for (int i = 0; i < n; ++i) {
-          const uint32_t b = uint32_t(uint8_t(p[offs[l] + i])) << (8 * (i & 3));
+          const uint32_t b = uint32_t(uint8_t(p[off[l] + i])) << (8 * (i & 3));
 #pragma unroll
           for (int j = 0; j < 4; ++j) w[j] |= (i >> 2) == j ? b : 0u;
         }
@@ -164,13 +196,17 @@ struct Operand {
 
 template <int TYPE, bool ALIGNED, bool WIDE, int WN, int WM, int NS, int MT>
 __global__ __launch_bounds__(WN * WM * 64, WN * WM == 8 ? 1 : 2) void linear_kernel(LinearI8Args a) {
-  constexpr int kWaves = WN * WM;
+  constexpr int kWaves = WN * WM, kHalf = kWaves / 2;
   constexpr int BN = 32 * NS * WN, BM = 32 * MT * WM;
-  constexpr int kWBytes = BN * BK, kABytes = BM * BK;
-  constexpr int kStage = kWBytes + kABytes;
-  constexpr int WL = BN / (8 * kWaves), AL = BM / (8 * kWaves);  // 1 KB loads per wave and stage
-  static_assert(WL * 8 * kWaves == BN && AL * 8 * kWaves == BM, "tile split");
+  static_assert(BN == BM && BN % (16 * kHalf) == 0, "tile split");
+  constexpr int L = BN / (16 * kHalf);  // 1 KB loads per wave and stage
+  constexpr int kTile = BN * BK;
+  constexpr int kStage = 2 * kTile;     // channels, then rows
   __shared__ __attribute__((aligned(1024))) uint8_t smem[2 * kStage];
+  // w_scale, bias and a_scale of a tile; the next tile's beside it.
+  constexpr int kFactors = 2 * BN + BM, kThreads = kWaves * 64, kPer = (kFactors + kThreads - 1) / kThreads;
+  __shared__ __attribute__((aligned(16))) float factors[2][kFactors];
+  using T = typename OutOf<TYPE>::T;
 
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -191,84 +227,66 @@ __global__ __launch_bounds__(WN * WM * 64, WN * WM == 8 ? 1 : 2) void linear_ker
   int tile = xcd_remap(blockIdx.x, G);
   if (tile >= n_tiles) return;
 
-  const int KT = (a.k + BK - 1) / BK, KP = (KT + 1) & ~1;  // stages of a tile, to an even number
-  // The stage to be loaded next: its tile's operands and its number in it.
-  Operand<ALIGNED, kWaves, WL> wop;
-  Operand<ALIGNED, kWaves, AL> aop;
-  int load_tile = tile, load_kt = 0;
-  auto set_ops = [&](int t) {
+  const int KP = ((a.k + BK - 1) / BK + kUnroll - 1) / kUnroll * kUnroll;  // stages of a tile
+  // The first half of the waves loads channels, the second rows.
+  const bool w_wave = wave < kHalf;
+  const int8_t* src = w_wave ? a.w : a.a;
+  const int64_t ld = w_wave ? a.ldw : a.lda;
+  const int rows = w_wave ? a.n : a.m, wave_row = wave % kHalf * 16 * L;
+  Operand<ALIGNED, L> op;
+  auto set_op = [&](int t) {
     int tm, tn;
     coords(t, tm, tn);
-    wop.set(a.w, a.ldw, tn * BN, a.n, a.k);
-    aop.set(a.a, a.lda, tm * BM, a.m, a.k);
+    op.set(src, ld, (w_wave ? tn * BN : tm * BM) + wave_row, rows, a.k);
   };
-  set_ops(tile);
-  // After a tile's last stage come the next tile's; past the last tile the
-  // loads repeat its first stages (in bounds, never used).
-  auto advance = [&] {
-    if (++load_kt == KP) {
-      load_kt = 0;
-      if (load_tile + G < n_tiles) {
-        load_tile += G;
-        set_ops(load_tile);
-      }
-    }
-  };
+  set_op(tile);
 
-  constexpr int NM = NS * MT, NR = NS + MT, NL = WL + AL;
-  u32x4 gr[2][NL];
-  auto load = [&](int slot, int l) {
-    gr[slot][l] = l < WL ? wop.load(l < WL ? l : 0, load_kt, a.ldw, a.k) : aop.load(l < WL ? 0 : l - WL, load_kt, a.lda, a.k);
-  };
-  const uint32_t st_row = 8 * wave + (lane >> 3);
-  const uint32_t st_off = st_row * BK + phys(st_row, lane & 7) * 16;  // the row's bits 0 .. 3 are every load's
+  constexpr int NM = NS * MT, NR = NS + MT;
+  u32x4 ring[kUnroll][L];  // stage t in slot t % 4
+  const uint32_t st_off = (w_wave ? 0u : uint32_t(kTile)) + uint32_t((wave_row + (lane >> 2)) * BK) +
+                          uint32_t(((lane & 3) ^ swz(lane >> 2)) * 16);
   auto put = [&](int buf, int slot, int l) {
-    const uint32_t at = l < WL ? uint32_t(l * 8 * kWaves * BK) : uint32_t(kWBytes + (l - WL) * 8 * kWaves * BK);
-    *reinterpret_cast<u32x4*>(smem + buf * kStage + at + st_off) = gr[slot][l];
+    *reinterpret_cast<u32x4*>(smem + buf * kStage + l * 16 * BK + st_off) = ring[slot][l];
   };
   struct Frag {
     u32x4 w[NS], a[MT];
   };
   Frag f[2];
-  // Fragment x (0 .. NR - 1, rows first) of step kk.
+  // Fragment x (0 .. NR - 1, rows first) of half kk.
   auto read = [&](int buf, int kk, int x, Frag& d) {
-    const uint8_t* p = smem + buf * kStage + fr * BK + phys(fr, 2 * kk + fh) * 16;
+    const uint8_t* p = smem + buf * kStage + fr * BK + (((kk * 2 + fh) ^ swz(fr)) * 16);
     if (x < MT)
-      d.a[x < MT ? x : 0] = *reinterpret_cast<const u32x4*>(p + kWBytes + (wm * MT + x) * 32 * BK);
+      d.a[x < MT ? x : 0] = *reinterpret_cast<const u32x4*>(p + kTile + (wm * MT + x) * 32 * BK);
     else
       d.w[x < MT ? 0 : x - MT] = *reinterpret_cast<const u32x4*>(p + (wn * NS + x - MT) * 32 * BK);
   };
 
-  // Stages 0 and 1 into the register slots, 0 on to LDS, 2 into its slot.
+  // Factor tid + kThreads i of a tile.
+  auto factor = [&](int t, int i) {
+    int tm, tn;
+    coords(t, tm, tn);
+    const int x = tid + kThreads * i;
+    if (x < BN) return a.w_scale[min(tn * BN + x, a.n - 1)];
+    if (x < 2 * BN) return a.bias ? bf2f(a.bias[min(tn * BN + x - BN, a.n - 1)]) : 0.0f;
+    return x < kFactors ? a.a_scale[min(tm * BM + x - 2 * BN, a.m - 1)] : 0.0f;
+  };
 #pragma unroll
-  for (int t = 0; t < 2; ++t) {
-#pragma unroll
-    for (int l = 0; l < NL; ++l) load(t, l);
-    advance();
+  for (int i = 0; i < kPer; ++i) {
+    const float v = factor(tile, i);
+    if (tid + kThreads * i < kFactors) factors[0][tid + kThreads * i] = v;
   }
-  __builtin_amdgcn_sched_barrier(0);
+
 #pragma unroll
-  for (int l = 0; l < NL; ++l) put(0, 0, l);
+  for (int t = 0; t < kUnroll; ++t)
 #pragma unroll
-  for (int l = 0; l < NL; ++l) load(0, l);
-  advance();
-  __builtin_amdgcn_sched_barrier(0);
+    for (int l = 0; l < L; ++l) ring[t][l] = op.load(l, t, ld, a.k);
+#pragma unroll
+  for (int l = 0; l < L; ++l) put(0, 0, l);
   asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
-#pragma unroll
-  for (int x = 0; x < NR; ++x) read(0, 0, x, f[0]);
-  __builtin_amdgcn_sched_barrier(0);
 
-  // Stage t multiplies buffer t % 2, writes stage t + 1 to the other one in its
-  // first two steps and loads stage t + 3 into the registers that held it in
-  // the middle two.  Each step's fragments are read during the step before.
-  // One barrier per stage, inside the last step, whose fragments have been
-  // read by then: it follows every wave's writes of stage t + 1 (whose first
-  // fragments are read next) and its reads of buffer t % 2 (which the next
-  // stage overwrites).  Every MFMA is issued with its share of the LDS accesses
-  // and loads, pinned by scheduling barriers, since a wave issues in order.
-  constexpr int H = (NL + 1) / 2, HB = NM / 2;
+  int parity = 0;
   while (true) {
     i32x16 acc[NS][MT];
 #pragma unroll
@@ -277,71 +295,88 @@ __global__ __launch_bounds__(WN * WM * 64, WN * WM == 8 ? 1 : 2) void linear_ker
       for (int j = 0; j < MT; ++j)
 #pragma unroll
         for (int r = 0; r < 16; ++r) acc[i][j][r] = 0;
-
-    for (int kt = 0; kt < KP; kt += 2) {
+    const bool more = tile + G < n_tiles;
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
+    for (int x = 0; x < NR; ++x) read(0, 0, x, f[0]);
+    for (int kt = 0; kt < KP; kt += kUnroll) {
+      const bool last = kt + kUnroll == KP;
+      if (last && more) set_op(tile + G);
+      // Past a tile's last stage come the next tile's first four; after the
+      // last tile its own again (in bounds, never used).
+      const int kl = last ? 0 : kt + kUnroll;
 #pragma unroll
-        for (int kk = 0; kk < kKk; ++kk) {
-          const bool last = kk + 1 == kKk;
-          const int nw = kk == 0 ? H : kk == 1 ? NL - H : 0;  // writes: 0 .. H - 1, then the rest
-          const int nl = kk == 1 ? H : kk == 2 ? NL - H : 0;  // loads likewise, one step later
+      for (int u = 0; u < kUnroll; ++u) {
+        // A wave issues in order: every MFMA is pinned to its share of the LDS
+        // accesses and loads, writes before loads since the barrier waits for them.
 #pragma unroll
-          for (int q = 0; q < NM; ++q) {
-            if (last && q == HB) {
-              asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-              __builtin_amdgcn_s_barrier();
-              asm volatile("" ::: "memory");
-            }
-            if (!last) {
+        for (int q = 0; q < NM; ++q) {
 #pragma unroll
-              for (int x = q * NR / NM; x < (q + 1) * NR / NM; ++x) read(u, kk + 1, x, f[(kk + 1) & 1]);
-            } else if (q >= HB) {
+          for (int x = q * NR / NM; x < (q + 1) * NR / NM; ++x) read(u & 1, 1, x, f[1]);
+          constexpr int HB = NM > 1 ? NM / 2 : 1;
+          if (q < HB) {
 #pragma unroll
-              for (int x = (q - HB) * NR / (NM - HB); x < (q - HB + 1) * NR / (NM - HB); ++x) read(1 - u, 0, x, f[0]);
-            }
-#pragma unroll
-            for (int x = q * nw / NM; x < (q + 1) * nw / NM; ++x) put(1 - u, 1 - u, kk * H + x);
-            const int i = q / MT, j = q % MT;
-            acc[i][j] = mfma32_i8(f[kk & 1].w[i], f[kk & 1].a[j], acc[i][j]);
-#pragma unroll
-            for (int x = q * nl / NM; x < (q + 1) * nl / NM; ++x) load(1 - u, (kk - 1) * H + x);
-            __builtin_amdgcn_sched_barrier(0);
+            for (int x = q * L / HB; x < (q + 1) * L / HB; ++x) put((u + 1) & 1, (u + 1) & 3, x);
           }
+          acc[q / MT][q % MT] = mfma32_i8(f[0].w[q / MT], f[0].a[q % MT], acc[q / MT][q % MT]);
+          if (q >= NM - HB) {
+#pragma unroll
+            for (int x = (q - NM + HB) * L / HB; x < (q - NM + HB + 1) * L / HB; ++x) ring[u][x] = op.load(x, kl + u, ld, a.k);
+          }
+          __builtin_amdgcn_sched_barrier(0);
         }
-        advance();
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+#pragma unroll
+        for (int q = 0; q < NM; ++q) {
+          if (u + 1 < kUnroll || !last) {
+#pragma unroll
+            for (int x = q * NR / NM; x < (q + 1) * NR / NM; ++x) read((u + 1) & 1, 0, x, f[0]);
+          }
+          acc[q / MT][q % MT] = mfma32_i8(f[1].w[q / MT], f[1].a[q % MT], acc[q / MT][q % MT]);
+          __builtin_amdgcn_sched_barrier(0);
+        }
       }
     }
 
+    // The factors were written before a barrier of this tile's stages, and
+    // the other half was last read before them.
+    float next[kPer];
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) next[i] = more ? factor(tile + G, i) : 0.0f;
     int tm, tn;
     coords(tile, tm, tn);
-    const int n0 = tn * BN + wn * NS * 32 + 4 * fh, m0 = tm * BM + wm * MT * 32 + fr;
-    float a_scale[MT];
+    const int n0 = tn * BN + wn * NS * 32, m0 = tm * BM + wm * MT * 32 + fr;
+    const float* fac = factors[parity] + wn * NS * 32 + 4 * fh;
 #pragma unroll
-    for (int j = 0; j < MT; ++j) a_scale[j] = a.a_scale[min(m0 + j * 32, a.m - 1)];
+    for (int j = 0; j < MT; ++j) {
+      const int m = m0 + j * 32;
+      const float a_scale = factors[parity][2 * BN + wm * MT * 32 + fr + j * 32];
+      if (m < a.m) {
+        T* row = static_cast<T*>(a.out) + int64_t(m) * a.ldo + n0;
 #pragma unroll
-    for (int i = 0; i < NS; ++i)
+        for (int i = 0; i < NS; ++i)
 #pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const int n = n0 + i * 32 + 8 * g;
-        f32x4 ws;
-        float b[4];
+          for (int p = 0; p < 2; ++p) {
+            float v[2][4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int c = min(n + e, a.n - 1);
-          ws[e] = a.w_scale[c];
-          b[e] = a.bias ? bf2f(a.bias[c]) : 0.0f;
-        }
+            for (int h = 0; h < 2; ++h) {
+              const f32x4 ws = *reinterpret_cast<const f32x4*>(fac + i * 32 + 16 * p + 8 * h);
+              const f32x4 b = *reinterpret_cast<const f32x4*>(fac + BN + i * 32 + 16 * p + 8 * h);
 #pragma unroll
-        for (int j = 0; j < MT; ++j) {
-          const i32x16& c = acc[i][j];
-          if (m0 + j * 32 < a.m)
-            store4<TYPE, WIDE>(a, m0 + j * 32, n, i32x4{c[4 * g], c[4 * g + 1], c[4 * g + 2], c[4 * g + 3]},
-                               a_scale[j], ws, b);
-        }
+              for (int e = 0; e < 4; ++e)
+                v[h][e] = output(acc[i][j][8 * p + 4 * h + e], a_scale, ws[e], a.bias != nullptr, b[e]);
+            }
+            store_run<T, WIDE>(row + i * 32 + 16 * p, fh, v[0], v[1], a.n - (n0 + i * 32 + 16 * p));
+          }
       }
+    }
+    if (!more) break;
+    parity ^= 1;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i)
+      if (tid + kThreads * i < kFactors) factors[parity][tid + kThreads * i] = next[i];
     tile += G;
-    if (tile >= n_tiles) break;
   }
 }
 
@@ -357,11 +392,11 @@ hipError_t launch_tiles(const LinearI8Args& a, int blocks, hipStream_t s) {
 
 template <int TYPE>
 hipError_t launch_type(const LinearI8Args& a, int cus, hipStream_t s) {
-  const size_t size = TYPE == HS_TYPE_F32 ? 4 : 2;
+  constexpr size_t size = sizeof(typename OutOf<TYPE>::T);
   const uintptr_t in = reinterpret_cast<uintptr_t>(a.a) | reinterpret_cast<uintptr_t>(a.w) | uintptr_t(a.lda) |
                        uintptr_t(a.ldw) | uintptr_t(a.k);
   const uintptr_t out = reinterpret_cast<uintptr_t>(a.out) | uintptr_t(a.ldo) * size;
-  const bool aligned = in % 16 == 0, wide = out % (4 * size) == 0;
+  const bool aligned = in % 16 == 0, wide = out % 16 == 0;
   if (!aligned) return launch_tiles<TYPE, false, false, 2, 2, 2, 2>(a, 2 * cus, s);
   if (!wide) return launch_tiles<TYPE, true, false, 2, 2, 2, 2>(a, 2 * cus, s);
   const int64_t big = int64_t((a.m + 255) / 256) * ((a.n + 255) / 256);
