@@ -29,6 +29,8 @@
 #include "horizon.h"
 #include "hs_device.h"
 
+#include <type_traits>
+
 namespace hs {
 namespace {
 
@@ -213,19 +215,40 @@ __global__ __launch_bounds__(WN * WM * 64, WN * WM == 8 ? 1 : 2) void linear_ker
   const int wn = wave % WN, wm = wave / WN;
   const int fr = lane & 31, fh = lane >> 5;
 
-  // Tiles in groups of kGroupM row tiles, rows fastest; round r gives block b
-  // tile r G + b, with the blocks of an XCD on a contiguous range.
-  const int tiles_m = (a.m + BM - 1) / BM, tiles_n = (a.n + BN - 1) / BN;
-  const int n_tiles = tiles_m * tiles_n, G = gridDim.x;
+  // Tiles in groups of kGroupM row tiles, rows fastest; a unit is a tile, or
+  // half its rows where MT is even:
+  //   - the tiles of a last row of tiles that holds at most half of them come
+  //     after all others, as one half unit each;
+  //   - when the last round of the others would leave more than half of the
+  //     blocks idle (counting those halves), its tiles are split into two.
+  const int tiles_m = (a.m + BM - 1) / BM, tiles_n = (a.n + BN - 1) / BN, G = gridDim.x;
+  constexpr bool kHalves = MT % 2 == 0;
+  const bool short_last = kHalves && a.m - (tiles_m - 1) * BM <= BM / 2;
+  const int whole_m = short_last ? tiles_m - 1 : tiles_m;
+  const int n_whole = whole_m * tiles_n, n_short = short_last ? tiles_n : 0;
+  const int full_units = n_whole / G * G, tail = n_whole - full_units;
+  const bool split_tail = kHalves && tail > 0 && 2 * tail + n_short <= G;
+  const int n_first = split_tail ? full_units + 2 * tail : n_whole, n_units = n_first + n_short;
   const int per_group = kGroupM * tiles_n;
-  auto coords = [&](int t, int& tm, int& tn) {
-    const int first_m = t / per_group * kGroupM;
-    const int gsize = min(tiles_m - first_m, kGroupM);
-    tm = first_m + t % per_group % gsize;
-    tn = t % per_group / gsize;
+  struct Unit {
+    int tm, tn, half;  // half: -1 the whole tile, else its first or second half
   };
-  int tile = xcd_remap(blockIdx.x, G);
-  if (tile >= n_tiles) return;
+  auto unit_at = [&](int u) {
+    if (u >= n_first) return Unit{tiles_m - 1, u - n_first, 0};
+    const bool split = split_tail && u >= full_units;
+    const int t = split ? full_units + (u - full_units) / 2 : u;
+    const int first_m = t / per_group * kGroupM;
+    const int gsize = min(whole_m - first_m, kGroupM);
+    return Unit{first_m + t % per_group % gsize, t % per_group / gsize, split ? (u - full_units) % 2 : -1};
+  };
+  // Round r gives block b unit r G + b, in odd rounds r G + G - 1 - b: the
+  // blocks left without a full unit take the first halves.  The blocks of an
+  // XCD stay on a contiguous range.
+  const int b = xcd_remap(blockIdx.x, G);
+  auto unit_of = [&](int r) { return r * G + ((r & 1) ? G - 1 - b : b); };
+  int round = 0;
+  if (unit_of(0) >= n_units) return;
+  Unit unit = unit_at(unit_of(0));
 
   const int KP = ((a.k + BK - 1) / BK + kUnroll - 1) / kUnroll * kUnroll;  // stages of a tile
   // The first half of the waves loads channels, the second rows.
@@ -234,14 +257,13 @@ __global__ __launch_bounds__(WN * WM * 64, WN * WM == 8 ? 1 : 2) void linear_ker
   const int64_t ld = w_wave ? a.ldw : a.lda;
   const int rows = w_wave ? a.n : a.m, wave_row = wave % kHalf * 16 * L;
   Operand<ALIGNED, L> op;
-  auto set_op = [&](int t) {
-    int tm, tn;
-    coords(t, tm, tn);
-    op.set(src, ld, (w_wave ? tn * BN : tm * BM) + wave_row, rows, a.k);
+  auto set_op = [&](const Unit& u) {
+    int row0 = w_wave ? u.tn * BN + wave_row : u.tm * BM + wave_row;
+    if (!w_wave && u.half >= 0) row0 = wave_row < BM / 2 ? row0 + u.half * (BM / 2) : rows;
+    op.set(src, ld, row0, rows, a.k);
   };
-  set_op(tile);
+  set_op(unit);
 
-  constexpr int NM = NS * MT, NR = NS + MT;
   u32x4 ring[kUnroll][L];  // stage t in slot t % 4
   const uint32_t st_off = (w_wave ? 0u : uint32_t(kTile)) + uint32_t((wave_row + (lane >> 2)) * BK) +
                           uint32_t(((lane & 3) ^ swz(lane >> 2)) * 16);
@@ -252,27 +274,26 @@ __global__ __launch_bounds__(WN * WM * 64, WN * WM == 8 ? 1 : 2) void linear_ker
     u32x4 w[NS], a[MT];
   };
   Frag f[2];
-  // Fragment x (0 .. NR - 1, rows first) of half kk.
-  auto read = [&](int buf, int kk, int x, Frag& d) {
+  // Fragment x (rows first) of 32-wide half kk, with JT row subtiles per wave.
+  auto read = [&](auto jt, int buf, int kk, int x, Frag& d) {
+    constexpr int JT = decltype(jt)::value;
     const uint8_t* p = smem + buf * kStage + fr * BK + (((kk * 2 + fh) ^ swz(fr)) * 16);
-    if (x < MT)
-      d.a[x < MT ? x : 0] = *reinterpret_cast<const u32x4*>(p + kTile + (wm * MT + x) * 32 * BK);
+    if (x < JT)
+      d.a[x < JT ? x : 0] = *reinterpret_cast<const u32x4*>(p + kTile + (wm * JT + x) * 32 * BK);
     else
-      d.w[x < MT ? 0 : x - MT] = *reinterpret_cast<const u32x4*>(p + (wn * NS + x - MT) * 32 * BK);
+      d.w[x < JT ? 0 : x - JT] = *reinterpret_cast<const u32x4*>(p + (wn * NS + x - JT) * 32 * BK);
   };
 
-  // Factor tid + kThreads i of a tile.
-  auto factor = [&](int t, int i) {
-    int tm, tn;
-    coords(t, tm, tn);
+  // Factor tid + kThreads i of a unit's tile.
+  auto factor = [&](const Unit& u, int i) {
     const int x = tid + kThreads * i;
-    if (x < BN) return a.w_scale[min(tn * BN + x, a.n - 1)];
-    if (x < 2 * BN) return a.bias ? bf2f(a.bias[min(tn * BN + x - BN, a.n - 1)]) : 0.0f;
-    return x < kFactors ? a.a_scale[min(tm * BM + x - 2 * BN, a.m - 1)] : 0.0f;
+    if (x < BN) return a.w_scale[min(u.tn * BN + x, a.n - 1)];
+    if (x < 2 * BN) return a.bias ? bf2f(a.bias[min(u.tn * BN + x - BN, a.n - 1)]) : 0.0f;
+    return x < kFactors ? a.a_scale[min(u.tm * BM + x - 2 * BN, a.m - 1)] : 0.0f;
   };
 #pragma unroll
   for (int i = 0; i < kPer; ++i) {
-    const float v = factor(tile, i);
+    const float v = factor(unit, i);
     if (tid + kThreads * i < kFactors) factors[0][tid + kThreads * i] = v;
   }
 
@@ -295,64 +316,73 @@ __global__ __launch_bounds__(WN * WM * 64, WN * WM == 8 ? 1 : 2) void linear_ker
       for (int j = 0; j < MT; ++j)
 #pragma unroll
         for (int r = 0; r < 16; ++r) acc[i][j][r] = 0;
-    const bool more = tile + G < n_tiles;
+    const bool more = unit_of(round + 1) < n_units;
+    const Unit next_unit = more ? unit_at(unit_of(round + 1)) : unit;
+    auto k_loop = [&](auto jt) {
+      constexpr int JT = decltype(jt)::value;
+      constexpr int NM = NS * JT, NR = NS + JT, HB = NM > 1 ? NM / 2 : 1;
 #pragma unroll
-    for (int x = 0; x < NR; ++x) read(0, 0, x, f[0]);
-    for (int kt = 0; kt < KP; kt += kUnroll) {
-      const bool last = kt + kUnroll == KP;
-      if (last && more) set_op(tile + G);
-      // Past a tile's last stage come the next tile's first four; after the
-      // last tile its own again (in bounds, never used).
-      const int kl = last ? 0 : kt + kUnroll;
+      for (int x = 0; x < NR; ++x) read(jt, 0, 0, x, f[0]);
+      for (int kt = 0; kt < KP; kt += kUnroll) {
+        const bool last = kt + kUnroll == KP;
+        if (last && more) set_op(next_unit);
+        // Past a unit's last stage come the next one's first four; after the
+        // last unit its own again (in bounds, never used).
+        const int kl = last ? 0 : kt + kUnroll;
 #pragma unroll
-      for (int u = 0; u < kUnroll; ++u) {
-        // A wave issues in order: every MFMA is pinned to its share of the LDS
-        // accesses and loads, writes before loads since the barrier waits for them.
+        for (int u = 0; u < kUnroll; ++u) {
+          // A wave issues in order: every MFMA is pinned to its share of the
+          // LDS accesses and loads, writes before loads since the barrier
+          // waits for them.
 #pragma unroll
-        for (int q = 0; q < NM; ++q) {
+          for (int q = 0; q < NM; ++q) {
 #pragma unroll
-          for (int x = q * NR / NM; x < (q + 1) * NR / NM; ++x) read(u & 1, 1, x, f[1]);
-          constexpr int HB = NM > 1 ? NM / 2 : 1;
-          if (q < HB) {
+            for (int x = q * NR / NM; x < (q + 1) * NR / NM; ++x) read(jt, u & 1, 1, x, f[1]);
+            if (q < HB) {
 #pragma unroll
-            for (int x = q * L / HB; x < (q + 1) * L / HB; ++x) put((u + 1) & 1, (u + 1) & 3, x);
+              for (int x = q * L / HB; x < (q + 1) * L / HB; ++x) put((u + 1) & 1, (u + 1) & 3, x);
+            }
+            acc[q / JT][q % JT] = mfma32_i8(f[0].w[q / JT], f[0].a[q % JT], acc[q / JT][q % JT]);
+            if (q >= NM - HB) {
+#pragma unroll
+              for (int x = (q - NM + HB) * L / HB; x < (q - NM + HB + 1) * L / HB; ++x)
+                ring[u][x] = op.load(x, kl + u, ld, a.k);
+            }
+            __builtin_amdgcn_sched_barrier(0);
           }
-          acc[q / MT][q % MT] = mfma32_i8(f[0].w[q / MT], f[0].a[q % MT], acc[q / MT][q % MT]);
-          if (q >= NM - HB) {
+          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+          __builtin_amdgcn_s_barrier();
+          asm volatile("" ::: "memory");
 #pragma unroll
-            for (int x = (q - NM + HB) * L / HB; x < (q - NM + HB + 1) * L / HB; ++x) ring[u][x] = op.load(x, kl + u, ld, a.k);
+          for (int q = 0; q < NM; ++q) {
+            if (u + 1 < kUnroll || !last) {
+#pragma unroll
+              for (int x = q * NR / NM; x < (q + 1) * NR / NM; ++x) read(jt, (u + 1) & 1, 0, x, f[0]);
+            }
+            acc[q / JT][q % JT] = mfma32_i8(f[1].w[q / JT], f[1].a[q % JT], acc[q / JT][q % JT]);
+            __builtin_amdgcn_sched_barrier(0);
           }
-          __builtin_amdgcn_sched_barrier(0);
-        }
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
-#pragma unroll
-        for (int q = 0; q < NM; ++q) {
-          if (u + 1 < kUnroll || !last) {
-#pragma unroll
-            for (int x = q * NR / NM; x < (q + 1) * NR / NM; ++x) read((u + 1) & 1, 0, x, f[0]);
-          }
-          acc[q / MT][q % MT] = mfma32_i8(f[1].w[q / MT], f[1].a[q % MT], acc[q / MT][q % MT]);
-          __builtin_amdgcn_sched_barrier(0);
         }
       }
-    }
+    };
+    if (!kHalves || unit.half < 0)
+      k_loop(std::integral_constant<int, MT>{});
+    else
+      k_loop(std::integral_constant<int, kHalves ? MT / 2 : MT>{});
 
     // The factors were written before a barrier of this tile's stages, and
     // the other half was last read before them.
     float next[kPer];
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) next[i] = more ? factor(tile + G, i) : 0.0f;
-    int tm, tn;
-    coords(tile, tm, tn);
-    const int n0 = tn * BN + wn * NS * 32, m0 = tm * BM + wm * MT * 32 + fr;
+    for (int i = 0; i < kPer; ++i) next[i] = more ? factor(next_unit, i) : 0.0f;
+    const int n0 = unit.tn * BN + wn * NS * 32, nj = unit.half < 0 ? MT : MT / 2;
+    const int row0 = (unit.half < 0 ? 0 : unit.half * (BM / 2)) + wm * nj * 32 + fr;  // within the tile
     const float* fac = factors[parity] + wn * NS * 32 + 4 * fh;
 #pragma unroll
     for (int j = 0; j < MT; ++j) {
-      const int m = m0 + j * 32;
-      const float a_scale = factors[parity][2 * BN + wm * MT * 32 + fr + j * 32];
-      if (m < a.m) {
+      const int m = unit.tm * BM + row0 + j * 32;
+      if (j < nj && m < a.m) {
+        const float a_scale = factors[parity][2 * BN + row0 + j * 32];
         T* row = static_cast<T*>(a.out) + int64_t(m) * a.ldo + n0;
 #pragma unroll
         for (int i = 0; i < NS; ++i)
@@ -362,10 +392,10 @@ __global__ __launch_bounds__(WN * WM * 64, WN * WM == 8 ? 1 : 2) void linear_ker
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
               const f32x4 ws = *reinterpret_cast<const f32x4*>(fac + i * 32 + 16 * p + 8 * h);
-              const f32x4 b = *reinterpret_cast<const f32x4*>(fac + BN + i * 32 + 16 * p + 8 * h);
+              const f32x4 bs = *reinterpret_cast<const f32x4*>(fac + BN + i * 32 + 16 * p + 8 * h);
 #pragma unroll
               for (int e = 0; e < 4; ++e)
-                v[h][e] = output(acc[i][j][8 * p + 4 * h + e], a_scale, ws[e], a.bias != nullptr, b[e]);
+                v[h][e] = output(acc[i][j][8 * p + 4 * h + e], a_scale, ws[e], a.bias != nullptr, bs[e]);
             }
             store_run<T, WIDE>(row + i * 32 + 16 * p, fh, v[0], v[1], a.n - (n0 + i * 32 + 16 * p));
           }
@@ -376,7 +406,8 @@ __global__ __launch_bounds__(WN * WM * 64, WN * WM == 8 ? 1 : 2) void linear_ker
 #pragma unroll
     for (int i = 0; i < kPer; ++i)
       if (tid + kThreads * i < kFactors) factors[parity][tid + kThreads * i] = next[i];
-    tile += G;
+    unit = next_unit;
+    ++round;
   }
 }
 
