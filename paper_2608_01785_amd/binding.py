@@ -33,7 +33,6 @@ SYMBOLS = (
 )
 HS_WEIGHTS_BF16, HS_WEIGHTS_F16 = 0, 1
 HS_TYPE_F32, HS_TYPE_BF16, HS_TYPE_F16 = 0, 1, 2
-_TYPES = {"torch.float32": HS_TYPE_F32, "torch.bfloat16": HS_TYPE_BF16, "torch.float16": HS_TYPE_F16}
 
 KERNEL_KINDS = {"rmsnorm": 0, "qkv": 1, "attention": 2, "decode_attn": 3, "o_proj": 4, "gate_up": 5,
                 "down": 6, "rope_table": 7, "modulation": 8, "ln_mod": 9, "mlp_up": 10, "mlp_down": 11,
@@ -573,65 +572,89 @@ def hs_dit_forward(ctx: Context, cfg, weights, x_in, x_out, cond, seq_offsets, c
 
 # The calls below take torch tensors and read types, sizes and strides off them, so a
 # tensor that does not fit is a ValueError here, before the library sees a pointer.
+# A decode step makes them per token: what they read is read once, and the message
+# is put together only for a refusal.
 
-def _on(ctx: Context, t, name: str, dtypes, ndim: int):
-    if str(t.dtype) not in dtypes:
-        raise ValueError(f"{name} has type {t.dtype}, expected {' or '.join(dtypes)}")
-    if t.ndim != ndim:
-        raise ValueError(f"{name} has {t.ndim} dimensions, expected {ndim}")
-    if t.device.type != "cuda" or t.device.index != ctx.device:
-        raise ValueError(f"{name} is on {t.device}, the context on cuda:{ctx.device}")
-    return t.data_ptr()
+class _Kinds:
+    """torch dtype -> HS_TYPE_* (or 0) of what an argument accepts; filled on first use."""
+    rows: Dict[object, int] = {}
+    f32: Dict[object, int] = {}
+    bf16: Dict[object, int] = {}
+    i8: Dict[object, int] = {}
+    i32: Dict[object, int] = {}
+
+    @classmethod
+    def fill(cls) -> None:
+        import torch
+        cls.rows.update({torch.float32: HS_TYPE_F32, torch.bfloat16: HS_TYPE_BF16, torch.float16: HS_TYPE_F16})
+        for kinds, t in ((cls.f32, torch.float32), (cls.bf16, torch.bfloat16), (cls.i8, torch.int8),
+                         (cls.i32, torch.int32)):
+            kinds[t] = 0
 
 
-def _matrix(ctx: Context, t, name: str, dtypes) -> Tuple[int, int]:
-    """(pointer, row stride) of a 2-d tensor whose rows are contiguous."""
-    p = _on(ctx, t, name, dtypes, 2)
-    (rows, cols), (ld, step) = t.shape, t.stride()
+def _refuse(ctx: Context, t, name: str, kinds, ndim: int) -> None:
+    if t.dtype not in kinds:
+        raise ValueError(f"{name} has type {t.dtype}, expected {' or '.join(str(k) for k in kinds)}")
+    if t.dim() != ndim:
+        raise ValueError(f"{name} has {t.dim()} dimensions, expected {ndim}")
+    raise ValueError(f"{name} is on {t.device}, the context on cuda:{ctx.device}")
+
+
+def _matrix(ctx: Context, t, name: str, kinds) -> Tuple[int, int, int, int]:
+    """(pointer, row stride, rows, columns) of a 2-d tensor whose rows are contiguous."""
+    if t.dtype not in kinds or t.dim() != 2 or t.get_device() != ctx.device:
+        _refuse(ctx, t, name, kinds, 2)
+    rows, cols = t.shape
+    ld, step = t.stride()
     if step != 1 and cols > 1 and rows > 0:
         raise ValueError(f"the rows of {name} are not contiguous (stride {step})")
-    return p, (ld if rows > 1 else max(cols, 1))
+    return t.data_ptr(), (ld if rows > 1 else max(cols, 1)), rows, cols
 
 
-def _dense(ctx: Context, t, name: str, dtypes, shape) -> Optional[int]:
+def _dense(ctx: Context, t, name: str, kinds, *shape) -> Optional[int]:
     """Pointer of a contiguous tensor of exactly this shape (None stays None)."""
     if t is None:
         return None
-    p = _on(ctx, t, name, dtypes, len(shape))
-    if tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if t.dtype not in kinds or t.dim() != len(shape) or t.get_device() != ctx.device:
+        _refuse(ctx, t, name, kinds, len(shape))
+    if t.shape != shape:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {shape}")
     if not t.is_contiguous():
         raise ValueError(f"{name} is not contiguous")
-    return p
-
-
-_F32, _BF16, _I8, _I32 = ("torch.float32",), ("torch.bfloat16",), ("torch.int8",), ("torch.int32",)
+    return t.data_ptr()
 
 
 def hs_quantize_rows(ctx: Context, x, q, scale, gain=None, eps: float = 1e-6, cu_budget: int = 256,
                      stream=None) -> None:
     """x [rows, d] (fp32, bf16 or fp16) -> q int8 [rows, d] and scale fp32 [rows]; gain: bf16 [d] (RMSNorm) or None."""
-    px, ldx = _matrix(ctx, x, "x", _TYPES)
-    pq, ldq = _matrix(ctx, q, "q", _I8)
-    rows, d = x.shape
-    if q.shape != x.shape:
-        raise ValueError(f"q has shape {tuple(q.shape)}, x {tuple(x.shape)}")
-    _check(lib().hs_quantize_rows(ctx.handle, px, _TYPES[str(x.dtype)], ldx, _dense(ctx, gain, "gain", _BF16, (d,)),
-                                  eps, rows, d, pq, ldq, _dense(ctx, scale, "scale", _F32, (rows,)), cu_budget,
-                                  _ptr(stream)))
+    if not _Kinds.rows:
+        _Kinds.fill()
+    px, ldx, rows, d = _matrix(ctx, x, "x", _Kinds.rows)
+    pq, ldq, *q_shape = _matrix(ctx, q, "q", _Kinds.i8)
+    if q_shape != [rows, d]:
+        raise ValueError(f"q has shape {tuple(q_shape)}, x ({rows}, {d})")
+    status = lib().hs_quantize_rows(ctx.handle, px, _Kinds.rows[x.dtype], ldx,
+                                    _dense(ctx, gain, "gain", _Kinds.bf16, d), eps, rows, d, pq, ldq,
+                                    _dense(ctx, scale, "scale", _Kinds.f32, rows), cu_budget, _ptr(stream))
+    if status:
+        _check(status)
 
 
 def hs_linear_i8(ctx: Context, a, a_scale, w, w_scale, out, bias=None, cu_budget: int = 256, stream=None) -> None:
     """out [m, n] = (a int8 [m, k] * a_scale fp32 [m]) (w int8 [n, k] * w_scale fp32 [n])^T + bias bf16 [n]."""
-    pa, lda = _matrix(ctx, a, "a", _I8)
-    pw, ldw = _matrix(ctx, w, "w", _I8)
-    po, ldo = _matrix(ctx, out, "out", _TYPES)
-    (m, k), n = a.shape, w.shape[0]
-    if w.shape[1] != k or tuple(out.shape) != (m, n):
-        raise ValueError(f"a {tuple(a.shape)}, w {tuple(w.shape)} and out {tuple(out.shape)} do not fit")
-    _check(lib().hs_linear_i8(ctx.handle, pa, lda, _dense(ctx, a_scale, "a_scale", _F32, (m,)), pw, ldw,
-                              _dense(ctx, w_scale, "w_scale", _F32, (n,)), _dense(ctx, bias, "bias", _BF16, (n,)),
-                              po, _TYPES[str(out.dtype)], ldo, m, n, k, cu_budget, _ptr(stream)))
+    if not _Kinds.rows:
+        _Kinds.fill()
+    pa, lda, m, k = _matrix(ctx, a, "a", _Kinds.i8)
+    pw, ldw, n, wk = _matrix(ctx, w, "w", _Kinds.i8)
+    po, ldo, om, on = _matrix(ctx, out, "out", _Kinds.rows)
+    if wk != k or om != m or on != n:
+        raise ValueError(f"a ({m}, {k}), w ({n}, {wk}) and out ({om}, {on}) do not fit")
+    status = lib().hs_linear_i8(ctx.handle, pa, lda, _dense(ctx, a_scale, "a_scale", _Kinds.f32, m), pw, ldw,
+                                _dense(ctx, w_scale, "w_scale", _Kinds.f32, n),
+                                _dense(ctx, bias, "bias", _Kinds.bf16, n), po, _Kinds.rows[out.dtype], ldo, m, n, k,
+                                cu_budget, _ptr(stream))
+    if status:
+        _check(status)
 
 
 def hs_logprobs_workspace_size(max_rows: int, vocab: int, top_k: int = 0) -> int:
@@ -645,20 +668,23 @@ def hs_logprobs(ctx: Context, logits, tokens=None, token_logprobs=None, entropy=
                 ws_bytes: Optional[int] = None) -> None:
     """logits [rows, vocab]; tokens int32 and token_logprobs fp32 [rows, n]; entropy fp32 [rows]; top_logprobs fp32 and
     top_tokens int32 [rows, k].  What is None is not computed."""
-    pz, ld = _matrix(ctx, logits, "logits", _TYPES)
-    rows, vocab = logits.shape
+    if not _Kinds.rows:
+        _Kinds.fill()
+    pz, ld, rows, vocab = _matrix(ctx, logits, "logits", _Kinds.rows)
     if (tokens is None) != (token_logprobs is None) or (top_logprobs is None) != (top_tokens is None):
         raise ValueError("tokens and token_logprobs, top_logprobs and top_tokens go together")
     n = 0 if tokens is None else tokens.shape[-1]
     k = 0 if top_tokens is None else top_tokens.shape[-1]
     if ws_bytes is None:
-        ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    _check(lib().hs_logprobs(
-        ctx.handle, pz, _TYPES[str(logits.dtype)], ld, rows, vocab, _dense(ctx, tokens, "tokens", _I32, (rows, n)), n,
-        _dense(ctx, token_logprobs, "token_logprobs", _F32, (rows, n)),
-        _dense(ctx, entropy, "entropy", _F32, (rows,)), k,
-        _dense(ctx, top_logprobs, "top_logprobs", _F32, (rows, k)),
-        _dense(ctx, top_tokens, "top_tokens", _I32, (rows, k)), cu_budget, _ptr(stream), _ptr(workspace), ws_bytes))
+        ws_bytes = 0 if workspace is None else workspace.nbytes
+    f32, i32 = _Kinds.f32, _Kinds.i32
+    status = lib().hs_logprobs(
+        ctx.handle, pz, _Kinds.rows[logits.dtype], ld, rows, vocab, _dense(ctx, tokens, "tokens", i32, rows, n), n,
+        _dense(ctx, token_logprobs, "token_logprobs", f32, rows, n), _dense(ctx, entropy, "entropy", f32, rows), k,
+        _dense(ctx, top_logprobs, "top_logprobs", f32, rows, k), _dense(ctx, top_tokens, "top_tokens", i32, rows, k),
+        cu_budget, _ptr(stream), _ptr(workspace), ws_bytes)
+    if status:
+        _check(status)
 
 
 def hs_probe_hw_ids(ctx: Context, stream, n_groups: int, out_ids) -> None:
