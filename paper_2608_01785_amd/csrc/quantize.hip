@@ -7,78 +7,286 @@
 //
 // The row's reciprocal root mean square scales y and a alike, so it cancels in
 // q = rint(127 x g / max |x g|): the integers are a function of exact products
-// and depend on no rounding.
+// (24 + 8 bits) and depend on no rounding.  They are formed in fp32 first: with
+// t = fl(fl(x g) c), c = fl(127 / fl(max |x g|)), four roundings of 2^-24 put t
+// within |t| 2^-22 of its exact value, so rint(t) is the answer unless t lies
+// that close to a border.  Groups with such an element (one row of 3584 in
+// twenty has any) are decided in 64 bits afterwards: 127 x g is exact there (39
+// bits), and its quotient by a (32 bits) is either a border itself, which the
+// division returns exactly, or at least 2^-42 away from it.
+//
+// A row stays in the registers of W wavefronts from its one read to its
+// store.  Rows whose products or squares leave fp32's comfortable range, or
+// are not finite, take a second, plain path in 64 bits.
+//
+// Memory bounds it: 5 bytes an element with fp32 rows against some 15 vector
+// operations.
 #include "answer_device.h"
 #include "answer_kernels.h"
 
 namespace hs {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kVec = 8;            // elements of a lane's group
+constexpr int kGroup = 64 * kVec;  // elements of a wavefront's groups
 
-__device__ __forceinline__ double block_max(double v, double* lds) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v = fmax(v, __shfl_xor(v, o, 64));
-  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
-  __syncthreads();
-  v = fmax(fmax(lds[0], lds[1]), fmax(lds[2], lds[3]));
-  __syncthreads();
-  return v;
-}
+// The largest |value| as fp32 bits: an integer order that also ranks
+// infinities and NaN, on top.
+__device__ __forceinline__ uint32_t magnitude(float v) { return __float_as_uint(v) & 0x7fffffffu; }
 
-__device__ __forceinline__ double block_sum(double v, double* lds) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
-  __syncthreads();
-  v = (lds[0] + lds[1]) + (lds[2] + lds[3]);
-  __syncthreads();
-  return v;
-}
-
-// One block per row, the row read twice, everything in 64 bits.
 template <typename T>
-__global__ __launch_bounds__(kThreads) void quantize_kernel(QuantizeArgs a) {
-  __shared__ double lds[4];
-  for (int row = blockIdx.x; row < a.rows; row += gridDim.x) {
-    const T* x = static_cast<const T*>(a.x) + int64_t(row) * a.ldx;
-    int8_t* q = a.q + int64_t(row) * a.ldq;
-    double top = 0.0, ss = 0.0, bad = 0.0;
-    for (int i = threadIdx.x; i < a.d; i += kThreads) {
-      const double v = elem(x, i);
-      const double y = a.gain ? v * double(bf2f(a.gain[i])) : v;
-      top = fmax(top, fabs(y));
-      ss = fma(v, v, ss);
-      if (!(fabs(y) < __builtin_inf())) bad = 1.0;
-    }
-    top = block_max(top, lds);
-    ss = block_sum(ss, lds);
-    bad = block_max(bad, lds);
-    const bool none = bad != 0.0 || top == 0.0;
-    if (threadIdx.x == 0) {
-      const double r = a.gain ? 1.0 / sqrt(ss / a.d + double(a.eps)) : 1.0;
-      a.scale[row] = bad != 0.0 ? __builtin_nanf("") : float(top * r / 127.0);
-    }
-    for (int i = threadIdx.x; i < a.d; i += kThreads) {
-      const double v = elem(x, i);
-      const double y = a.gain ? v * double(bf2f(a.gain[i])) : v;
-      q[i] = none ? int8_t(0) : int8_t(int(rint(127.0 * y / top)));
+__device__ __forceinline__ double product(const T* x, const uint16_t* gain, int i) {
+  const double v = elem(x, i);
+  return gain ? v * double(bf2f(gain[i])) : v;
+}
+
+// rint(127 y / a) of exact products, ties to even.
+__device__ __forceinline__ int exact_step(double y, double a) { return int(rint(127.0 * y / a)); }
+
+// f over the row's W wavefronts.
+template <int W, typename V, typename F>
+__device__ __forceinline__ V reduce_row(V v, V* lds, F f) {
+  v = reduce_wave(v, f);
+  if constexpr (W > 1) {
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = lds[0];
+#pragma unroll
+    for (int w = 1; w < W; ++w) v = f(v, lds[w]);
+    __syncthreads();
+  }
+  return v;
+}
+
+template <int W>
+struct RowLds {
+  double d[W];
+  float f[W];
+  uint32_t u[W];
+};
+
+// The row from memory, twice, in 64 bits.
+template <typename T, int W>
+__device__ __forceinline__ void plain_row(const QuantizeArgs& a, const T* x, int8_t* q, int row, RowLds<W>& lds) {
+  const int t = W > 1 ? int(threadIdx.x) : int(threadIdx.x & 63);
+  double top = 0.0, ss = 0.0, bad = 0.0;
+#pragma unroll 1
+  for (int i = t; i < a.d; i += 64 * W) {
+    const double v = elem(x, i), y = product(x, a.gain, i);
+    top = fmax(top, fabs(y));
+    ss = fma(v, v, ss);
+    if (!(fabs(y) < __builtin_inf())) bad = 1.0;
+  }
+  auto most = [](double p, double r) { return fmax(p, r); };
+  top = reduce_row<W>(top, lds.d, most);
+  ss = reduce_row<W>(ss, lds.d, [](double p, double r) { return p + r; });
+  bad = reduce_row<W>(bad, lds.d, most);
+  const bool none = bad != 0.0 || top == 0.0;
+  if (t == 0) {
+    const double r = a.gain ? 1.0 / sqrt(ss / a.d + double(a.eps)) : 1.0;
+    a.scale[row] = bad != 0.0 ? __builtin_nanf("") : float(top * r / 127.0);
+  }
+#pragma unroll 1
+  for (int i = t; i < a.d; i += 64 * W) q[i] = none ? int8_t(0) : int8_t(exact_step(product(x, a.gain, i), top));
+}
+
+// Eight elements from p on, aligned as an element is.
+template <typename T>
+__device__ __forceinline__ void load_group(const T* p, float (&v)[kVec]) {
+  u32x4 raw[sizeof(T) * kVec / 16];
+  __builtin_memcpy(raw, p, sizeof(raw));
+#pragma unroll
+  for (int e = 0; e < kVec; ++e) {
+    if constexpr (sizeof(T) == 4) {
+      v[e] = __uint_as_float(raw[e >> 2][e & 3]);
+    } else {
+      const uint32_t w = raw[0][e >> 1];
+      if constexpr (__is_same(T, uint16_t))
+        v[e] = __uint_as_float((e & 1) ? w & 0xffff0000u : w << 16);
+      else
+        v[e] = h2f(uint16_t((e & 1) ? w >> 16 : w & 0xffffu));
     }
   }
+}
+
+__device__ __forceinline__ void store_group(int8_t* p, const int (&r)[kVec]) {
+  uint32_t w[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+    w[h] = (uint32_t(r[4 * h]) & 0xffu) | (uint32_t(r[4 * h + 1]) & 0xffu) << 8 |
+           (uint32_t(r[4 * h + 2]) & 0xffu) << 16 | uint32_t(r[4 * h + 3]) << 24;
+  __builtin_memcpy(p, w, kVec);
+}
+
+// W wavefronts per row, NG groups per lane: d / 8 <= 64 W NG.  Group number n of a
+// row is elements 8 n .. 8 n + 7; what is left of d modulo 8 goes one element
+// to a lane.
+template <typename T, int W, int NG, bool GAIN>
+__global__ __launch_bounds__(W > 1 ? 64 * W : 256) void quantize_kernel(QuantizeArgs a) {
+  constexpr int kRows = W > 1 ? 1 : 4;  // rows of a block
+  constexpr bool kExact = !GAIN && sizeof(T) == 2;
+  __shared__ RowLds<W> lds;
+  const int wave = threadIdx.x >> 6;
+  const int first = W > 1 ? int(threadIdx.x) : int(threadIdx.x & 63);  // the lane's first group; then 64 W on
+  const int n_groups = a.d / kVec, rest = n_groups * kVec + first;
+  const bool has_rest = first < a.d % kVec;
+  for (int row = blockIdx.x * kRows + (W > 1 ? 0 : wave); row < a.rows; row += gridDim.x * kRows) {
+    const T* x = static_cast<const T*>(a.x) + int64_t(row) * a.ldx;
+    int8_t* q = a.q + int64_t(row) * a.ldq;
+    float y[NG][kVec], y_rest = 0.0f;
+#pragma unroll
+    for (int g = 0; g < NG; ++g) {
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) y[g][e] = 0.0f;
+      const int n = first + 64 * W * g;
+      if (n < n_groups) load_group(x + n * kVec, y[g]);
+    }
+    if (has_rest) y_rest = elem(x, rest);
+    float ss = 0.0f;
+    uint32_t top = 0;
+    if constexpr (GAIN) {
+      ss = y_rest * y_rest;
+      if (has_rest) y_rest *= bf2f(a.gain[rest]);
+    }
+    top = magnitude(y_rest);
+#pragma unroll
+    for (int g = 0; g < NG; ++g) {
+      const int n = first + 64 * W * g;
+      if constexpr (GAIN) {
+        float gain[kVec] = {};
+        if (n < n_groups) load_group(a.gain + n * kVec, gain);
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) {
+          ss = fmaf(y[g][e], y[g][e], ss);
+          y[g][e] *= gain[e];
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) top = max(top, magnitude(y[g][e]));
+    }
+    top = reduce_row<W>(top, lds.u, [](uint32_t p, uint32_t r) { return max(p, r); });
+    if constexpr (GAIN) ss = reduce_row<W>(ss, lds.f, [](float p, float r) { return p + r; });
+    const float top32 = __uint_as_float(top);
+    // False also for what is not a number.
+    if (!(top32 > 0x1p-100f && top32 < 0x1p100f && (!GAIN || (ss > 0x1p-80f && ss < 0x1p100f)))) {
+      plain_row<T, W>(a, x, q, row, lds);
+      continue;
+    }
+    if (first == 0) {
+      const double r = GAIN ? 1.0 / sqrt(double(ss) / a.d + double(a.eps)) : 1.0;
+      a.scale[row] = float(double(top32) * r / 127.0);
+    }
+    const float c = 127.0f / top32;
+    // The quotient's rounding to an integer; `near` where it needs another look.
+    //   16-bit values themselves: 127 y is exact and one Newton step rounds the
+    //   quotient correctly.  Its distance from a tie it does not equal is 16
+    //   times that rounding or more (2^-21 at 1/2), so rint() is right; ties
+    //   are common (every y = a / 2).
+    //   Otherwise: |t - rint(t)| and what t may be off by reach 1/2.
+    auto step = [&](float v, float& off) {
+      float t = v * c;
+      if constexpr (kExact) t = fmaf(fmaf(-t, top32, 127.0f * v), c * (1.0f / 127.0f), t);
+      const float i = rintf(t);
+      if constexpr (!kExact) off = fmaxf(off, fmaf(fabsf(t), 0x1.01p-22f, fabsf(t - i)));
+      return int(i);
+    };
+    uint32_t near = 0;  // groups to decide again; bit NG: the rest
+#pragma unroll
+    for (int g = 0; g < NG; ++g) {
+      const int n = first + 64 * W * g;
+      int r[kVec];
+      float off = 0.0f;
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) r[e] = step(y[g][e], off);
+      near |= uint32_t(off >= 0.5f) << g;
+      if (n < n_groups) store_group(q + n * kVec, r);
+    }
+    if (has_rest) {
+      float off = 0.0f;
+      q[rest] = int8_t(step(y_rest, off));
+      near |= uint32_t(off >= 0.5f) << NG;
+    }
+    if constexpr (kExact) continue;
+    uint32_t any = __ballot(near != 0) != 0;
+    if constexpr (W > 1) any = reduce_row<W>(any, lds.u, [](uint32_t p, uint32_t r) { return p | r; });
+    if (!any) continue;
+    // The exact maximum, then the groups in doubt, from memory.
+    double exact = has_rest ? fabs(product(x, a.gain, rest)) : 0.0;
+#pragma unroll 1
+    for (int n = first; n < n_groups; n += 64 * W) {
+      float v[kVec], gain[kVec];
+      load_group(x + n * kVec, v);
+      if constexpr (GAIN) load_group(a.gain + n * kVec, gain);
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) exact = fmax(exact, fabs(GAIN ? double(v[e]) * double(gain[e]) : double(v[e])));
+    }
+    exact = reduce_row<W>(exact, lds.d, [](double p, double r) { return fmax(p, r); });
+    if (near >> NG) q[rest] = int8_t(exact_step(product(x, a.gain, rest), exact));
+    near &= (1u << NG) - 1;
+#pragma unroll 1
+    while (near) {
+      const int n = first + 64 * W * __builtin_ctz(near);
+      near &= near - 1;
+#pragma unroll 1
+      for (int e = 0; e < kVec; ++e) q[n * kVec + e] = int8_t(exact_step(product(x, a.gain, n * kVec + e), exact));
+    }
+  }
+}
+
+// Rows longer than a block's registers.
+template <typename T>
+__global__ __launch_bounds__(256) void quantize_long_kernel(QuantizeArgs a) {
+  __shared__ RowLds<4> lds;
+  for (int row = blockIdx.x; row < a.rows; row += gridDim.x)
+    plain_row<T, 4>(a, static_cast<const T*>(a.x) + int64_t(row) * a.ldx, a.q + int64_t(row) * a.ldq, row, lds);
+}
+
+template <typename T, int W, int NG>
+hipError_t launch(const QuantizeArgs& a, int cus, hipStream_t s) {
+  constexpr int kRows = W > 1 ? 1 : 4, kThreads = W > 1 ? 64 * W : 256;
+  const int64_t blocks = (int64_t(a.rows) + kRows - 1) / kRows;
+  const int64_t most = int64_t(cus) * 16;
+  const unsigned grid = unsigned(blocks < most ? blocks : most);
+  if (a.gain)
+    hipLaunchKernelGGL((quantize_kernel<T, W, NG, true>), dim3(grid), dim3(kThreads), 0, s, a);
+  else
+    hipLaunchKernelGGL((quantize_kernel<T, W, NG, false>), dim3(grid), dim3(kThreads), 0, s, a);
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t launch_type(const QuantizeArgs& a, int cus, hipStream_t s) {
+  // Two groups a lane, with wavefronts enough for the row, keep the most loads
+  // in flight: 10515 x 3584 fp32 takes 38 us in 4 x 2 (5.0 TB/s), 44 in 2 x 4
+  // and 51 in 1 x 8.  Past four wavefronts the joins cost more than more
+  // groups do: 9000 x 4096 fp32 36 us in 4 x 2, 55 in 8 x 2; 3000 x 18944
+  // fp32 80 us in 8 x 5, 86 in 16 x 3, 92 in 4 x 10.  Short rows need one
+  // (30000 x 1024 fp32: 31 us in 1 x 2, 36 in 2 x 1).  Few rows take 6 us in
+  // any of them.
+  const int groups = (a.d / kVec + 63) / 64;  // per wavefront if it were one; the rest rides along
+  if (groups <= 1) return launch<T, 1, 1>(a, cus, s);
+  if (groups <= 2) return launch<T, 1, 2>(a, cus, s);
+  if (groups <= 4) return launch<T, 2, 2>(a, cus, s);
+  if (groups <= 8) return launch<T, 4, 2>(a, cus, s);
+  if (groups <= 16) return launch<T, 4, 4>(a, cus, s);
+  if (groups <= 32) return launch<T, 8, 4>(a, cus, s);
+  if (groups <= 40) return launch<T, 8, 5>(a, cus, s);
+  if (groups <= 64) return launch<T, 16, 4>(a, cus, s);
+  const int grid = a.rows < 16 * cus ? a.rows : 16 * cus;
+  hipLaunchKernelGGL(quantize_long_kernel<T>, dim3(grid), dim3(256), 0, s, a);
+  return hipGetLastError();
 }
 
 }  // namespace
 
 hipError_t launch_quantize(const QuantizeArgs& a, int cus, hipStream_t s) {
   if (a.rows < 1) return hipSuccess;
-  const int grid = a.rows < 16 * cus ? a.rows : 16 * cus;
   switch (a.type) {
-    case HS_TYPE_F32: hipLaunchKernelGGL(quantize_kernel<float>, dim3(grid), dim3(kThreads), 0, s, a); break;
-    case HS_TYPE_BF16: hipLaunchKernelGGL(quantize_kernel<uint16_t>, dim3(grid), dim3(kThreads), 0, s, a); break;
-    case HS_TYPE_F16: hipLaunchKernelGGL(quantize_kernel<_Float16>, dim3(grid), dim3(kThreads), 0, s, a); break;
+    case HS_TYPE_F32: return launch_type<float>(a, cus, s);
+    case HS_TYPE_BF16: return launch_type<uint16_t>(a, cus, s);
+    case HS_TYPE_F16: return launch_type<_Float16>(a, cus, s);
     default: return hipErrorInvalidValue;
   }
-  return hipGetLastError();
 }
 
 }  // namespace hs

@@ -99,7 +99,8 @@ def _check_quantize(env, x, gain, **kw):
 
 QUANT_SHAPES = [(1, 1, 0, 0), (3, 7, 0, 0), (5, 64, 0, 0), (2, 1000, 0, 0), (33, 1024, 0, 0), (257, 512, 8, 0),
                 (9, 3584, 0, 0), (4, 3585, 3, 1), (3, 4097, 0, 0), (6, 4096, 24, 8), (2, 14336, 0, 0),
-                (3, 18944, 8, 0), (2, 18943, 1, 0), (1, 70001, 0, 0), (2, 131072, 16, 16), (1500, 300, 4, 4)]
+                (3, 18944, 8, 0), (2, 18943, 1, 0), (7, 2000, 0, 0), (5, 1537, 1, 1), (3, 8190, 2, 2),
+                (2, 30001, 0, 0), (2, 32775, 1, 0), (1, 70001, 0, 0), (2, 131072, 16, 16), (1500, 300, 4, 4)]
 
 
 @pytest.mark.parametrize("shape", QUANT_SHAPES, ids=str)
