@@ -122,51 +122,51 @@ __device__ __forceinline__ void store_run(T* p, int h, const float (&lo)[4], con
 
 // ---------------------------------------------------------------- tiles
 
-// One wave's share of an operand's rows: the 16-byte chunk (lane & 3) of rows
-// row0 + (lane >> 2) + 16 l.
+// One wave's share of an operand's rows, in stages of C 16-byte chunks of K:
+// load l takes chunk lane % C of row row0 + lane / C + (64 / C) l.
 //   ALIGNED: base, row stride and k are multiples of 16.  A buffer resource
 //   over the rows: what lies past the last row or past k reads zero.
 //   Otherwise: byte addresses, rows past the last read it again (they are
 //   never stored) and the chunk that holds the end of k is read from 16 bytes
 //   before that end and shifted.
-template <bool ALIGNED, int L>
+template <bool ALIGNED, int C, int L>
 struct Operand {
+  static constexpr int kRows = 64 / C, kBytes = 16 * C;  // of a load, and of a row in a stage
   const int8_t* base;
   __amdgpu_buffer_rsrc_t res;
   uint32_t off[ALIGNED ? 1 : L];
 
   __device__ __forceinline__ void set(const int8_t* p, int64_t ld, int row0, int rows, int k) {
-    const int r = (threadIdx.x & 63) >> 2, c = threadIdx.x & 3;
+    const int r = (threadIdx.x & 63) / C, c = threadIdx.x % C;
     if constexpr (ALIGNED) {
       // A wave without rows keeps one (never stored).
-      const int first = min(row0, rows - 1), span = min(rows - first, 16 * L);
+      const int first = min(row0, rows - 1), span = min(rows - first, kRows * L);
       base = p + int64_t(first) * ld;
       res = make_rsrc(base, uint32_t(span - 1) * uint32_t(ld) + uint32_t(k));
       off[0] = uint32_t(r) * uint32_t(ld) + uint32_t(c * 16);
     } else {
-      base = p;
       const int first = min(row0, rows - 1);
       base = p + int64_t(first) * ld;
 #pragma unroll
-      for (int l = 0; l < L; ++l) off[l] = uint32_t(min(r + 16 * l, rows - 1 - first)) * uint32_t(ld) + uint32_t(c * 16);
+      for (int l = 0; l < L; ++l) off[l] = uint32_t(min(r + kRows * l, rows - 1 - first)) * uint32_t(ld) + uint32_t(c * 16);
     }
   }
   __device__ __forceinline__ u32x4 load(int l, int stage, int64_t ld, int k) const {
-    const int whole = k / BK;  // stages without the end of k
+    const int whole = k / kBytes;  // stages without the end of k
     if constexpr (ALIGNED) {
       uint32_t v = off[0];
       // Past k: an offset outside the resource, which reads zero.
-      if (stage >= whole && stage * BK + int(threadIdx.x & 3) * 16 >= k) v = 0x80000000u;
-      const uint32_t s = uint32_t(min(stage, (k - 1) / BK)) * BK + uint32_t(16 * l) * uint32_t(ld);
+      if (stage >= whole && stage * kBytes + int(threadIdx.x % C) * 16 >= k) v = 0x80000000u;
+      const uint32_t s = uint32_t(min(stage, (k - 1) / kBytes)) * kBytes + uint32_t(kRows * l) * uint32_t(ld);
       return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(res, v, s, 0));
     } else {
       u32x4 v = {0, 0, 0, 0};
-      const int8_t* p = base + int64_t(stage) * BK;
+      const int8_t* p = base + int64_t(stage) * kBytes;
       if (stage < whole) {
         __builtin_memcpy(&v, p + off[l], 16);
         return v;
       }
-      const int n = k - stage * BK - (int(threadIdx.x) & 3) * 16;  // bytes of the chunk that k holds
+      const int n = k - stage * kBytes - int(threadIdx.x % C) * 16;  // bytes of the chunk that k holds
       if (n >= 16) {
         __builtin_memcpy(&v, p + off[l], 16);
       } else if (n > 0 && k >= 16) {
@@ -256,7 +256,7 @@ __global__ __launch_bounds__(WN * WM * 64, WN * WM == 8 ? 1 : 2) void linear_ker
   const int8_t* src = w_wave ? a.w : a.a;
   const int64_t ld = w_wave ? a.ldw : a.lda;
   const int rows = w_wave ? a.n : a.m, wave_row = wave % kHalf * 16 * L;
-  Operand<ALIGNED, L> op;
+  Operand<ALIGNED, BK / 16, L> op;
   auto set_op = [&](const Unit& u) {
     int row0 = w_wave ? u.tn * BN + wave_row : u.tm * BM + wave_row;
     if (!w_wave && u.half >= 0) row0 = wave_row < BM / 2 ? row0 + u.half * (BM / 2) : rows;
@@ -411,6 +411,113 @@ __global__ __launch_bounds__(WN * WM * 64, WN * WM == 8 ? 1 : 2) void linear_ker
   }
 }
 
+// ---------------------------------------------------------------- few rows
+
+// At most 32 MT rows: what counts is reading w once, as fast as memory gives
+// it.  A block takes 32 channels and its eight waves share K, wave v the 128
+// bytes of stages v, v + 8, ...: one cache line of every row to a load's eight
+// lanes, two stages of loads in flight per wave.  Each wave turns its lines
+// into MFMA operands through an LDS image of its own, so nothing in the loop
+// waits for another wave; their sums meet in LDS at the end.
+constexpr int kFewWaves = 8;
+
+// Chunk c of row r of a 128-byte-row image sits at c ^ ...: a pass of 16 lanes
+// reads one logical chunk of eight even and eight odd rows, and odd rows start
+// on bank 32, so bits 1 .. 3 of r permute the chunks; bit 0 keeps the writes of
+// two rows in different halves.
+__device__ __forceinline__ int phys(int r, int c) { return c ^ ((r >> 1) & 7) ^ ((r & 1) << 2); }
+
+template <int TYPE, bool ALIGNED, bool WIDE, int MT>
+__global__ __launch_bounds__(kFewWaves * 64, MT == 1 && ALIGNED ? 4 : 2) void few_kernel(LinearI8Args a) {
+  constexpr int kRow = 128, kImage = (1 + MT) * 32 * kRow;
+  constexpr int D = 2;  // stages of loads in flight
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[kFewWaves * kImage];
+  using T = typename OutOf<TYPE>::T;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int fr = lane & 31, fh = lane >> 5;
+  const int n0 = blockIdx.x * 32;
+
+  Operand<ALIGNED, 8, 4> wop;
+  Operand<ALIGNED, 8, 4 * MT> aop;
+  wop.set(a.w, a.ldw, n0, a.n, a.k);
+  aop.set(a.a, a.lda, 0, a.m, a.k);
+  u32x4 w[D][4], x[D][4 * MT];
+  auto load = [&](int slot, int stage) {
+#pragma unroll
+    for (int l = 0; l < 4; ++l) w[slot][l] = wop.load(l, stage, a.ldw, a.k);
+#pragma unroll
+    for (int l = 0; l < 4 * MT; ++l) x[slot][l] = aop.load(l, stage, a.lda, a.k);
+  };
+  uint8_t* image = smem + wave * kImage;
+  const uint32_t put_off = (lane >> 3) * kRow + phys(lane >> 3, lane & 7) * 16;  // rows 8 l + lane / 8: phys repeats with 16
+  const uint32_t put_odd = (lane >> 3) * kRow + phys(8 + (lane >> 3), lane & 7) * 16;
+
+  i32x16 acc[MT];
+#pragma unroll
+  for (int j = 0; j < MT; ++j)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) acc[j][r] = 0;
+  const int stages = (a.k + kRow - 1) / kRow, rounds = (stages + kFewWaves - 1) / kFewWaves;
+#pragma unroll
+  for (int d = 0; d < D; ++d) load(d, wave + d * kFewWaves);
+  for (int i = 0; i < rounds; i += D) {
+#pragma unroll
+    for (int d = 0; d < D; ++d) {
+#pragma unroll
+      for (int l = 0; l < 4; ++l)
+        *reinterpret_cast<u32x4*>(image + l * 8 * kRow + ((l & 1) ? put_odd : put_off)) = w[d][l];
+#pragma unroll
+      for (int l = 0; l < 4 * MT; ++l)
+        *reinterpret_cast<u32x4*>(image + (4 + l) * 8 * kRow + ((l & 1) ? put_odd : put_off)) = x[d][l];
+      load(d, wave + (i + d + D) * kFewWaves);  // zeros past the end of k
+      // The image is this wave's alone, and LDS serves one wave in order.
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+      for (int kk = 0; kk < 4; ++kk) {
+        const uint8_t* p = image + fr * kRow + phys(fr, 2 * kk + fh) * 16;
+        const u32x4 wf = *reinterpret_cast<const u32x4*>(p);
+#pragma unroll
+        for (int j = 0; j < MT; ++j)
+          acc[j] = mfma32_i8(wf, *reinterpret_cast<const u32x4*>(p + (1 + j) * 32 * kRow), acc[j]);
+      }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    }
+  }
+
+  // Sums of four channels and one row per lane: group g of row subtile j is
+  // wave 4 j + g's (MT <= 2).
+  __syncthreads();
+  int32_t* part = reinterpret_cast<int32_t*>(smem);
+#pragma unroll
+  for (int j = 0; j < MT; ++j)
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+      *reinterpret_cast<i32x4*>(part + (((j * 4 + g) * kFewWaves + wave) * 64 + lane) * 4) =
+          i32x4{acc[j][4 * g], acc[j][4 * g + 1], acc[j][4 * g + 2], acc[j][4 * g + 3]};
+  __syncthreads();
+  const int m = (wave >> 2) * 32 + fr, n = n0 + 8 * (wave & 3) + 4 * fh;
+  if (wave >= 4 * MT || m >= a.m || n >= a.n) return;
+  i32x4 sum = {0, 0, 0, 0};
+#pragma unroll
+  for (int v = 0; v < kFewWaves; ++v) sum += *reinterpret_cast<const i32x4*>(part + ((wave * kFewWaves + v) * 64 + lane) * 4);
+  const float a_scale = a.a_scale[m];
+  float v[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const int c = min(n + e, a.n - 1);
+    v[e] = output(sum[e], a_scale, a.w_scale[c], a.bias != nullptr, a.bias ? bf2f(a.bias[c]) : 0.0f);
+  }
+  T* p = static_cast<T*>(a.out) + int64_t(m) * a.ldo + n;
+  if (WIDE && n + 4 <= a.n) {
+    if constexpr (sizeof(T) == 4)
+      *reinterpret_cast<f32x4*>(p) = f32x4{v[0], v[1], v[2], v[3]};
+    else
+      *reinterpret_cast<u32x2*>(p) = u32x2{pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3])};
+  } else {
+    store_each(p, v, a.n - n);
+  }
+}
+
 template <int TYPE, bool ALIGNED, bool WIDE, int WN, int WM, int NS, int MT>
 hipError_t launch_tiles(const LinearI8Args& a, int blocks, hipStream_t s) {
   constexpr int BN = 32 * NS * WN, BM = 32 * MT * WM;
@@ -421,6 +528,16 @@ hipError_t launch_tiles(const LinearI8Args& a, int blocks, hipStream_t s) {
   return hipGetLastError();
 }
 
+template <int TYPE, bool ALIGNED, bool WIDE>
+hipError_t launch_few(const LinearI8Args& a, hipStream_t s) {
+  const dim3 grid((a.n + 31) / 32), block(kFewWaves * 64);
+  if (a.m <= 32)
+    hipLaunchKernelGGL((few_kernel<TYPE, ALIGNED, WIDE, 1>), grid, block, 0, s, a);
+  else
+    hipLaunchKernelGGL((few_kernel<TYPE, ALIGNED, WIDE, 2>), grid, block, 0, s, a);
+  return hipGetLastError();
+}
+
 template <int TYPE>
 hipError_t launch_type(const LinearI8Args& a, int cus, hipStream_t s) {
   constexpr size_t size = sizeof(typename OutOf<TYPE>::T);
@@ -428,6 +545,10 @@ hipError_t launch_type(const LinearI8Args& a, int cus, hipStream_t s) {
                        uintptr_t(a.ldw) | uintptr_t(a.k);
   const uintptr_t out = reinterpret_cast<uintptr_t>(a.out) | uintptr_t(a.ldo) * size;
   const bool aligned = in % 16 == 0, wide = out % 16 == 0;
+  if (a.m <= 64) {
+    if (!aligned) return launch_few<TYPE, false, false>(a, s);
+    return wide ? launch_few<TYPE, true, true>(a, s) : launch_few<TYPE, true, false>(a, s);
+  }
   if (!aligned) return launch_tiles<TYPE, false, false, 2, 2, 2, 2>(a, 2 * cus, s);
   if (!wide) return launch_tiles<TYPE, true, false, 2, 2, 2, 2>(a, 2 * cus, s);
   const int64_t big = int64_t((a.m + 255) / 256) * ((a.n + 255) / 256);
