@@ -9,15 +9,18 @@
 // one row of a and four consecutive channels per register group.
 //
 // A block of WN x WM waves computes tiles of 32 NS WN channels x 32 MT WM rows.
-// K advances in stages of 64 bytes; half of the waves fetch the channels, half
-// the rows, with 16-byte loads into a ring of registers:
-//   stage t is loaded during stage t - 4, written to LDS buffer t % 2 in the
-//   first half of stage t - 1 and multiplied during stage t.
-// One barrier per stage, between its two 32-wide halves, after each wave's
-// writes of stage t + 1 and fragment reads of stage t have completed: it makes
-// the writes visible to the second half's reads of stage t + 1 and retires
-// every read of the buffer that the next stage overwrites.  Stages past the
-// end of k, up to a multiple of four, are zeros.
+// K advances in stages of 128 bytes, one cache line of every row (loads that
+// take 64 bytes of twice the rows cost the address unit as much for half the
+// data: 1024 x 8192 x 8192 in 128 x 128 tiles 88 us against 72).  Half of the
+// waves fetch the channels, half the rows, with 16-byte loads into a ring of
+// registers:
+//   stage t is loaded during stage t - 2, written to LDS buffer t % 2 during
+//   stage t - 1 and multiplied during stage t, in four steps of 32.
+// One barrier per stage, before its last step, after each wave's writes of
+// stage t + 1 and fragment reads of stage t have completed: it makes the writes
+// visible to the last step's reads of stage t + 1 and retires every read of the
+// buffer that the next stage overwrites.  Stages past the end of k, up to an
+// even number, are zeros.
 //
 // The grid is persistent and the stages of a block's tiles form one sequence:
 // the last four stages of a tile already fetch the next one's first four, and
@@ -37,19 +40,22 @@ namespace {
 typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
 typedef int32_t i32x16 __attribute__((ext_vector_type(16)));
 
-constexpr int BK = 64;      // bytes of K per stage: 4 chunks of 16
-constexpr int kUnroll = 4;  // stages per loop body
 constexpr int kGroupM = 4;
 
 __device__ __forceinline__ i32x16 mfma32_i8(const u32x4& a, const u32x4& b, const i32x16& c) {
   return __builtin_amdgcn_mfma_i32_32x32x32_i8(__builtin_bit_cast(i32x4, a), __builtin_bit_cast(i32x4, b), c, 0, 0, 0);
 }
 
-// 16-byte chunk c of tile row r sits at physical chunk c ^ swz(r).  A 16-lane
-// pass of fragment reads covers rows r0 .. r0 + 15 at one logical chunk;
-// (r & 3, c ^ swz(r)) is then distinct for all 16 rows, so the pass touches
-// each of the 64 banks once.
-__device__ __forceinline__ int swz(int r) { return ((r >> 1) ^ (r >> 2)) & 3; }
+// 16-byte chunk c of row r of an LDS image whose rows hold C chunks sits at
+// physical chunk phys<C>(r, c), so that a pass of 16 lanes, which reads one
+// logical chunk of 16 consecutive rows, touches each of the 64 banks once.
+//   C = 4: (r & 3, phys) is distinct for all 16 rows.
+//   C = 8: odd rows start on bank 32, so bits 1 .. 3 of r permute the chunks;
+//   bit 0 keeps the writes of two rows in different halves.
+template <int C>
+__device__ __forceinline__ int phys(int r, int c) {
+  return C == 4 ? c ^ (((r >> 1) ^ (r >> 2)) & 3) : c ^ ((r >> 1) & 7) ^ ((r & 1) << 2);
+}
 
 // ---------------------------------------------------------------- epilogue
 
@@ -91,13 +97,13 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
 
 // Channels 0 .. 15 of a 16-channel run of one row, of which the first `left`
 // exist: the low lane of the pair (lane, lane + 32) holds 0 .. 3 in `lo` and
-// 8 .. 11 in `hi`, the high lane (h = 1) the four after each.  WIDE: p is
+// 8 .. 11 in `hi`, the high lane (h = 1) the four after each.  wide: p is
 // aligned to 16 bytes; 16-bit values change lanes so that each lane stores 16
 // bytes.  Both lanes of the pair must be active.
-template <typename T, bool WIDE>
-__device__ __forceinline__ void store_run(T* p, int h, const float (&lo)[4], const float (&hi)[4], int left) {
+template <typename T>
+__device__ __forceinline__ void store_run(T* p, int h, const float (&lo)[4], const float (&hi)[4], int left, bool wide) {
   if constexpr (sizeof(T) == 2) {
-    if (WIDE && left >= 16) {
+    if (wide && left >= 16) {
       const uint32_t a[2] = {pack2<T>(lo[0], lo[1]), pack2<T>(lo[2], lo[3])};
       const uint32_t b[2] = {pack2<T>(hi[0], hi[1]), pack2<T>(hi[2], hi[3])};
       u32x4 v;
@@ -111,7 +117,7 @@ __device__ __forceinline__ void store_run(T* p, int h, const float (&lo)[4], con
       *reinterpret_cast<u32x4*>(p + 8 * h) = v;
       return;
     }
-  } else if (WIDE && left >= 16) {
+  } else if (wide && left >= 16) {
     *reinterpret_cast<f32x4*>(p + 4 * h) = f32x4{lo[0], lo[1], lo[2], lo[3]};
     *reinterpret_cast<f32x4*>(p + 8 + 4 * h) = f32x4{hi[0], hi[1], hi[2], hi[3]};
     return;
@@ -196,12 +202,15 @@ struct Operand {
   }
 };
 
-template <int TYPE, bool ALIGNED, bool WIDE, int WN, int WM, int NS, int MT>
+template <int TYPE, bool ALIGNED, int C, int WN, int WM, int NS, int MT>
 __global__ __launch_bounds__(WN * WM * 64, WN * WM == 8 ? 1 : 2) void linear_kernel(LinearI8Args a) {
   constexpr int kWaves = WN * WM, kHalf = kWaves / 2;
   constexpr int BN = 32 * NS * WN, BM = 32 * MT * WM;
+  constexpr int BK = 16 * C, kSteps = C / 2;  // bytes of K per stage, and its steps
+  constexpr int kUnroll = 16 / C;             // stages per loop body
+  constexpr int kLoadRows = 64 / C;           // rows of a load
   static_assert(BN == BM && BN % (16 * kHalf) == 0, "tile split");
-  constexpr int L = BN / (16 * kHalf);  // 1 KB loads per wave and stage
+  constexpr int L = BN / (kLoadRows * kHalf);  // 1 KB loads per wave and stage
   constexpr int kTile = BN * BK;
   constexpr int kStage = 2 * kTile;     // channels, then rows
   __shared__ __attribute__((aligned(1024))) uint8_t smem[2 * kStage];
@@ -255,8 +264,8 @@ __global__ __launch_bounds__(WN * WM * 64, WN * WM == 8 ? 1 : 2) void linear_ker
   const bool w_wave = wave < kHalf;
   const int8_t* src = w_wave ? a.w : a.a;
   const int64_t ld = w_wave ? a.ldw : a.lda;
-  const int rows = w_wave ? a.n : a.m, wave_row = wave % kHalf * 16 * L;
-  Operand<ALIGNED, BK / 16, L> op;
+  const int rows = w_wave ? a.n : a.m, wave_row = wave % kHalf * kLoadRows * L;
+  Operand<ALIGNED, C, L> op;
   auto set_op = [&](const Unit& u) {
     int row0 = w_wave ? u.tn * BN + wave_row : u.tm * BM + wave_row;
     if (!w_wave && u.half >= 0) row0 = wave_row < BM / 2 ? row0 + u.half * (BM / 2) : rows;
@@ -264,20 +273,25 @@ __global__ __launch_bounds__(WN * WM * 64, WN * WM == 8 ? 1 : 2) void linear_ker
   };
   set_op(unit);
 
-  u32x4 ring[kUnroll][L];  // stage t in slot t % 4
-  const uint32_t st_off = (w_wave ? 0u : uint32_t(kTile)) + uint32_t((wave_row + (lane >> 2)) * BK) +
-                          uint32_t(((lane & 3) ^ swz(lane >> 2)) * 16);
+  u32x4 ring[kUnroll][L];  // stage t in slot t % kUnroll
+  // Load l holds image rows wave_row + kLoadRows l + lane / C; phys() repeats
+  // with 16 of them.
+  const int put_row = wave_row + lane / C;
+  const uint32_t put_at = (w_wave ? 0u : uint32_t(kTile)) + uint32_t(put_row * BK);
+  const uint32_t put_chunk[2] = {uint32_t(phys<C>(put_row, lane % C) * 16),
+                                 uint32_t(phys<C>(put_row + kLoadRows, lane % C) * 16)};
   auto put = [&](int buf, int slot, int l) {
-    *reinterpret_cast<u32x4*>(smem + buf * kStage + l * 16 * BK + st_off) = ring[slot][l];
+    *reinterpret_cast<u32x4*>(smem + buf * kStage + l * kLoadRows * BK + put_at +
+                              put_chunk[kLoadRows < 16 ? l & 1 : 0]) = ring[slot][l];
   };
   struct Frag {
     u32x4 w[NS], a[MT];
   };
   Frag f[2];
-  // Fragment x (rows first) of 32-wide half kk, with JT row subtiles per wave.
+  // Fragment x (rows first) of step kk, with JT row subtiles per wave.
   auto read = [&](auto jt, int buf, int kk, int x, Frag& d) {
     constexpr int JT = decltype(jt)::value;
-    const uint8_t* p = smem + buf * kStage + fr * BK + (((kk * 2 + fh) ^ swz(fr)) * 16);
+    const uint8_t* p = smem + buf * kStage + fr * BK + phys<C>(fr, kk * 2 + fh) * 16;
     if (x < JT)
       d.a[x < JT ? x : 0] = *reinterpret_cast<const u32x4*>(p + kTile + (wm * JT + x) * 32 * BK);
     else
@@ -320,47 +334,53 @@ __global__ __launch_bounds__(WN * WM * 64, WN * WM == 8 ? 1 : 2) void linear_ker
     const Unit next_unit = more ? unit_at(unit_of(round + 1)) : unit;
     auto k_loop = [&](auto jt) {
       constexpr int JT = decltype(jt)::value;
-      constexpr int NM = NS * JT, NR = NS + JT, HB = NM > 1 ? NM / 2 : 1;
+      constexpr int NM = NS * JT, NR = NS + JT;
 #pragma unroll
       for (int x = 0; x < NR; ++x) read(jt, 0, 0, x, f[0]);
       for (int kt = 0; kt < KP; kt += kUnroll) {
         const bool last = kt + kUnroll == KP;
         if (last && more) set_op(next_unit);
-        // Past a unit's last stage come the next one's first four; after the
+        // Past a unit's last stage come the next one's first ones; after the
         // last unit its own again (in bounds, never used).
         const int kl = last ? 0 : kt + kUnroll;
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u) {
-          // A wave issues in order: every MFMA is pinned to its share of the
-          // LDS accesses and loads, writes before loads since the barrier
-          // waits for them.
+          const int buf = u & 1;
 #pragma unroll
-          for (int q = 0; q < NM; ++q) {
+          for (int kk = 0; kk < kSteps; ++kk) {
+            // A wave issues in order: every MFMA is pinned to its share of the
+            // LDS accesses and loads.  The steps before the barrier write
+            // stage t + 1 first, then load into the registers that held stage t.
+            constexpr int kSlots = (kSteps - 1) * NM, kPutEnd = kSlots > 1 ? kSlots / 2 : 1;
+            constexpr int kLoadBegin = kSlots > 1 ? kSlots - kPutEnd : 0;
 #pragma unroll
-            for (int x = q * NR / NM; x < (q + 1) * NR / NM; ++x) read(jt, u & 1, 1, x, f[1]);
-            if (q < HB) {
+            for (int q = 0; q < NM; ++q) {
+              const int slot = kk * NM + q;
+              if (kk + 1 < kSteps) {
 #pragma unroll
-              for (int x = q * L / HB; x < (q + 1) * L / HB; ++x) put((u + 1) & 1, (u + 1) & 3, x);
+                for (int x = q * NR / NM; x < (q + 1) * NR / NM; ++x) read(jt, buf, kk + 1, x, f[(kk + 1) & 1]);
+                if (slot < kPutEnd) {
+#pragma unroll
+                  for (int x = slot * L / kPutEnd; x < (slot + 1) * L / kPutEnd; ++x) put(1 - buf, (u + 1) % kUnroll, x);
+                }
+              } else if (u + 1 < kUnroll || !last) {
+#pragma unroll
+                for (int x = q * NR / NM; x < (q + 1) * NR / NM; ++x) read(jt, 1 - buf, 0, x, f[0]);
+              }
+              acc[q / JT][q % JT] = mfma32_i8(f[kk & 1].w[q / JT], f[kk & 1].a[q % JT], acc[q / JT][q % JT]);
+              if (kk + 1 < kSteps && slot >= kLoadBegin) {
+                constexpr int kN = kSlots - kLoadBegin;
+#pragma unroll
+                for (int x = (slot - kLoadBegin) * L / kN; x < (slot - kLoadBegin + 1) * L / kN; ++x)
+                  ring[u][x] = op.load(x, kl + u, ld, a.k);
+              }
+              __builtin_amdgcn_sched_barrier(0);
             }
-            acc[q / JT][q % JT] = mfma32_i8(f[0].w[q / JT], f[0].a[q % JT], acc[q / JT][q % JT]);
-            if (q >= NM - HB) {
-#pragma unroll
-              for (int x = (q - NM + HB) * L / HB; x < (q - NM + HB + 1) * L / HB; ++x)
-                ring[u][x] = op.load(x, kl + u, ld, a.k);
+            if (kk + 2 == kSteps) {
+              asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+              __builtin_amdgcn_s_barrier();
+              asm volatile("" ::: "memory");
             }
-            __builtin_amdgcn_sched_barrier(0);
-          }
-          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-          __builtin_amdgcn_s_barrier();
-          asm volatile("" ::: "memory");
-#pragma unroll
-          for (int q = 0; q < NM; ++q) {
-            if (u + 1 < kUnroll || !last) {
-#pragma unroll
-              for (int x = q * NR / NM; x < (q + 1) * NR / NM; ++x) read(jt, (u + 1) & 1, 0, x, f[0]);
-            }
-            acc[q / JT][q % JT] = mfma32_i8(f[1].w[q / JT], f[1].a[q % JT], acc[q / JT][q % JT]);
-            __builtin_amdgcn_sched_barrier(0);
           }
         }
       }
@@ -397,7 +417,7 @@ __global__ __launch_bounds__(WN * WM * 64, WN * WM == 8 ? 1 : 2) void linear_ker
               for (int e = 0; e < 4; ++e)
                 v[h][e] = output(acc[i][j][8 * p + 4 * h + e], a_scale, ws[e], a.bias != nullptr, bs[e]);
             }
-            store_run<T, WIDE>(row + i * 32 + 16 * p, fh, v[0], v[1], a.n - (n0 + i * 32 + 16 * p));
+            store_run(row + i * 32 + 16 * p, fh, v[0], v[1], a.n - (n0 + i * 32 + 16 * p), a.wide);
           }
       }
     }
@@ -421,13 +441,7 @@ __global__ __launch_bounds__(WN * WM * 64, WN * WM == 8 ? 1 : 2) void linear_ker
 // waits for another wave; their sums meet in LDS at the end.
 constexpr int kFewWaves = 8;
 
-// Chunk c of row r of a 128-byte-row image sits at c ^ ...: a pass of 16 lanes
-// reads one logical chunk of eight even and eight odd rows, and odd rows start
-// on bank 32, so bits 1 .. 3 of r permute the chunks; bit 0 keeps the writes of
-// two rows in different halves.
-__device__ __forceinline__ int phys(int r, int c) { return c ^ ((r >> 1) & 7) ^ ((r & 1) << 2); }
-
-template <int TYPE, bool ALIGNED, bool WIDE, int MT>
+template <int TYPE, bool ALIGNED, int MT>
 __global__ __launch_bounds__(kFewWaves * 64, MT == 1 && ALIGNED ? 4 : 2) void few_kernel(LinearI8Args a) {
   constexpr int kRow = 128, kImage = (1 + MT) * 32 * kRow;
   constexpr int D = 2;  // stages of loads in flight
@@ -449,8 +463,8 @@ __global__ __launch_bounds__(kFewWaves * 64, MT == 1 && ALIGNED ? 4 : 2) void fe
     for (int l = 0; l < 4 * MT; ++l) x[slot][l] = aop.load(l, stage, a.lda, a.k);
   };
   uint8_t* image = smem + wave * kImage;
-  const uint32_t put_off = (lane >> 3) * kRow + phys(lane >> 3, lane & 7) * 16;  // rows 8 l + lane / 8: phys repeats with 16
-  const uint32_t put_odd = (lane >> 3) * kRow + phys(8 + (lane >> 3), lane & 7) * 16;
+  const uint32_t put_off = (lane >> 3) * kRow + phys<8>(lane >> 3, lane & 7) * 16;  // rows 8 l + lane / 8: phys repeats with 16
+  const uint32_t put_odd = (lane >> 3) * kRow + phys<8>(8 + (lane >> 3), lane & 7) * 16;
 
   i32x16 acc[MT];
 #pragma unroll
@@ -474,7 +488,7 @@ __global__ __launch_bounds__(kFewWaves * 64, MT == 1 && ALIGNED ? 4 : 2) void fe
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
       for (int kk = 0; kk < 4; ++kk) {
-        const uint8_t* p = image + fr * kRow + phys(fr, 2 * kk + fh) * 16;
+        const uint8_t* p = image + fr * kRow + phys<8>(fr, 2 * kk + fh) * 16;
         const u32x4 wf = *reinterpret_cast<const u32x4*>(p);
 #pragma unroll
         for (int j = 0; j < MT; ++j)
@@ -508,7 +522,7 @@ __global__ __launch_bounds__(kFewWaves * 64, MT == 1 && ALIGNED ? 4 : 2) void fe
     v[e] = output(sum[e], a_scale, a.w_scale[c], a.bias != nullptr, a.bias ? bf2f(a.bias[c]) : 0.0f);
   }
   T* p = static_cast<T*>(a.out) + int64_t(m) * a.ldo + n;
-  if (WIDE && n + 4 <= a.n) {
+  if (a.wide && n + 4 <= a.n) {
     if constexpr (sizeof(T) == 4)
       *reinterpret_cast<f32x4*>(p) = f32x4{v[0], v[1], v[2], v[3]};
     else
@@ -518,44 +532,44 @@ __global__ __launch_bounds__(kFewWaves * 64, MT == 1 && ALIGNED ? 4 : 2) void fe
   }
 }
 
-template <int TYPE, bool ALIGNED, bool WIDE, int WN, int WM, int NS, int MT>
+template <int TYPE, bool ALIGNED, int C, int WN, int WM, int NS, int MT>
 hipError_t launch_tiles(const LinearI8Args& a, int blocks, hipStream_t s) {
   constexpr int BN = 32 * NS * WN, BM = 32 * MT * WM;
   const int64_t tiles = int64_t((a.m + BM - 1) / BM) * ((a.n + BN - 1) / BN);
   if (tiles > (int64_t(1) << 30)) return hipErrorInvalidValue;
   const int grid = int(tiles < blocks ? tiles : blocks);
-  hipLaunchKernelGGL((linear_kernel<TYPE, ALIGNED, WIDE, WN, WM, NS, MT>), dim3(grid), dim3(WN * WM * 64), 0, s, a);
+  hipLaunchKernelGGL((linear_kernel<TYPE, ALIGNED, C, WN, WM, NS, MT>), dim3(grid), dim3(WN * WM * 64), 0, s, a);
   return hipGetLastError();
 }
 
-template <int TYPE, bool ALIGNED, bool WIDE>
-hipError_t launch_few(const LinearI8Args& a, hipStream_t s) {
-  const dim3 grid((a.n + 31) / 32), block(kFewWaves * 64);
-  if (a.m <= 32)
-    hipLaunchKernelGGL((few_kernel<TYPE, ALIGNED, WIDE, 1>), grid, block, 0, s, a);
-  else
-    hipLaunchKernelGGL((few_kernel<TYPE, ALIGNED, WIDE, 2>), grid, block, 0, s, a);
-  return hipGetLastError();
+template <int TYPE, bool ALIGNED>
+hipError_t launch_choice(const LinearI8Args& a, int choice, int cus, hipStream_t s) {
+  const dim3 few((a.n + 31) / 32);
+  switch (choice) {
+    case kLinearI8Few32:
+      hipLaunchKernelGGL((few_kernel<TYPE, ALIGNED, 1>), few, dim3(kFewWaves * 64), 0, s, a);
+      return hipGetLastError();
+    case kLinearI8Few64:
+      hipLaunchKernelGGL((few_kernel<TYPE, ALIGNED, 2>), few, dim3(kFewWaves * 64), 0, s, a);
+      return hipGetLastError();
+    case kLinearI8Tile64: return launch_tiles<TYPE, ALIGNED, 8, 2, 2, 1, 1>(a, 4 * cus, s);
+    case kLinearI8Tile128: return launch_tiles<TYPE, ALIGNED, 8, 2, 2, 2, 2>(a, 2 * cus, s);
+    default:
+      if constexpr (ALIGNED)
+        return launch_tiles<TYPE, ALIGNED, 8, 2, 4, 4, 2>(a, cus, s);
+      else
+        return launch_tiles<TYPE, ALIGNED, 8, 2, 2, 2, 2>(a, 2 * cus, s);
+  }
 }
 
 template <int TYPE>
-hipError_t launch_type(const LinearI8Args& a, int cus, hipStream_t s) {
+hipError_t launch_type(LinearI8Args a, int cus, hipStream_t s) {
   constexpr size_t size = sizeof(typename OutOf<TYPE>::T);
   const uintptr_t in = reinterpret_cast<uintptr_t>(a.a) | reinterpret_cast<uintptr_t>(a.w) | uintptr_t(a.lda) |
                        uintptr_t(a.ldw) | uintptr_t(a.k);
-  const uintptr_t out = reinterpret_cast<uintptr_t>(a.out) | uintptr_t(a.ldo) * size;
-  const bool aligned = in % 16 == 0, wide = out % 16 == 0;
-  if (a.m <= 64) {
-    if (!aligned) return launch_few<TYPE, false, false>(a, s);
-    return wide ? launch_few<TYPE, true, true>(a, s) : launch_few<TYPE, true, false>(a, s);
-  }
-  if (!aligned) return launch_tiles<TYPE, false, false, 2, 2, 2, 2>(a, 2 * cus, s);
-  if (!wide) return launch_tiles<TYPE, true, false, 2, 2, 2, 2>(a, 2 * cus, s);
-  const int64_t big = int64_t((a.m + 255) / 256) * ((a.n + 255) / 256);
-  if (big >= 2 * cus) return launch_tiles<TYPE, true, true, 2, 4, 4, 2>(a, cus, s);
-  const int64_t mid = int64_t((a.m + 127) / 128) * ((a.n + 127) / 128);
-  if (mid >= cus) return launch_tiles<TYPE, true, true, 2, 2, 2, 2>(a, 2 * cus, s);
-  return launch_tiles<TYPE, true, true, 2, 2, 1, 1>(a, 4 * cus, s);
+  a.wide = (reinterpret_cast<uintptr_t>(a.out) | uintptr_t(a.ldo) * size) % 16 == 0;
+  const int choice = linear_i8_choice(a.m, a.n, a.k, cus);
+  return in % 16 == 0 ? launch_choice<TYPE, true>(a, choice, cus, s) : launch_choice<TYPE, false>(a, choice, cus, s);
 }
 
 }  // namespace
