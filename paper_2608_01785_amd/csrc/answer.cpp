@@ -118,7 +118,7 @@ hs_status hs_linear_i8(hs_context* ctx, const void* a, int64_t lda, const float*
   HS_TRY(check_matrix(so, n ? m : 0, n, ldo, osz));
   for (const Span& in : {sa, sw, sas, sws, sb}) HS_TRY(check_disjoint(so, in));
   hs::LinearI8Args g{static_cast<const int8_t*>(a), lda, a_scale, static_cast<const int8_t*>(w), ldw, w_scale,
-                     static_cast<const uint16_t*>(bias), out, out_type, ldo, m, n, k, false};
+                     static_cast<const uint16_t*>(bias), out, out_type, ldo, m, n, k};
   return run(ctx, cu_budget, stream, m == 0 || n == 0, HS_KERNEL_LINEAR_I8,
              [&](hipStream_t s) { return hs::launch_linear_i8(g, cu_budget, s); });
 }

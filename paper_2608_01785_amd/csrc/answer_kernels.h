@@ -34,7 +34,6 @@ struct LinearI8Args {
   int out_type;           // HS_TYPE_*
   int64_t ldo;
   int m, n, k;
-  bool wide;              // set by the launcher: output rows start on 16 bytes
 };
 hipError_t launch_linear_i8(const LinearI8Args& a, int cus, hipStream_t s);
 

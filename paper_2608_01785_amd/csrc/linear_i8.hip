@@ -97,33 +97,30 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
 
 // Channels 0 .. 15 of a 16-channel run of one row, of which the first `left`
 // exist: the low lane of the pair (lane, lane + 32) holds 0 .. 3 in `lo` and
-// 8 .. 11 in `hi`, the high lane (h = 1) the four after each.  wide: p is
-// aligned to 16 bytes; 16-bit values change lanes so that each lane stores 16
-// bytes.  Both lanes of the pair must be active.
+// 8 .. 11 in `hi`, the high lane (h = 1) the four after each.  16-bit values
+// change lanes so that each lane stores 16 bytes, which need no more alignment
+// than an element.  Both lanes of the pair must be active.
 template <typename T>
-__device__ __forceinline__ void store_run(T* p, int h, const float (&lo)[4], const float (&hi)[4], int left, bool wide) {
-  if constexpr (sizeof(T) == 2) {
-    if (wide && left >= 16) {
-      const uint32_t a[2] = {pack2<T>(lo[0], lo[1]), pack2<T>(lo[2], lo[3])};
-      const uint32_t b[2] = {pack2<T>(hi[0], hi[1]), pack2<T>(hi[2], hi[3])};
-      u32x4 v;
+__device__ __forceinline__ void store_run(T* p, int h, const float (&lo)[4], const float (&hi)[4], int left) {
+  if (left < 16) {
+    store_each(p + 4 * h, lo, left - 4 * h);
+    store_each(p + 8 + 4 * h, hi, left - 8 - 4 * h);
+  } else if constexpr (sizeof(T) == 2) {
+    const uint32_t a[2] = {pack2<T>(lo[0], lo[1]), pack2<T>(lo[2], lo[3])};
+    const uint32_t b[2] = {pack2<T>(hi[0], hi[1]), pack2<T>(hi[2], hi[3])};
+    u32x4 v;
 #pragma unroll
-      for (int d = 0; d < 2; ++d) {
-        // Lanes 32 .. 63 of the first operand against lanes 0 .. 31 of the second.
-        const auto s = __builtin_amdgcn_permlane32_swap(a[d], b[d], false, false);
-        v[d] = s[0];
-        v[2 + d] = s[1];
-      }
-      *reinterpret_cast<u32x4*>(p + 8 * h) = v;
-      return;
+    for (int d = 0; d < 2; ++d) {
+      // Lanes 32 .. 63 of the first operand against lanes 0 .. 31 of the second.
+      const auto s = __builtin_amdgcn_permlane32_swap(a[d], b[d], false, false);
+      v[d] = s[0];
+      v[2 + d] = s[1];
     }
-  } else if (wide && left >= 16) {
-    *reinterpret_cast<f32x4*>(p + 4 * h) = f32x4{lo[0], lo[1], lo[2], lo[3]};
-    *reinterpret_cast<f32x4*>(p + 8 + 4 * h) = f32x4{hi[0], hi[1], hi[2], hi[3]};
-    return;
+    __builtin_memcpy(p + 8 * h, &v, 16);
+  } else {
+    __builtin_memcpy(p + 4 * h, lo, 16);
+    __builtin_memcpy(p + 8 + 4 * h, hi, 16);
   }
-  store_each(p + 4 * h, lo, left - 4 * h);
-  store_each(p + 8 + 4 * h, hi, left - 8 - 4 * h);
 }
 
 // ---------------------------------------------------------------- tiles
@@ -417,7 +414,7 @@ __global__ __launch_bounds__(WN * WM * 64, WN * WM == 8 ? 1 : 2) void linear_ker
               for (int e = 0; e < 4; ++e)
                 v[h][e] = output(acc[i][j][8 * p + 4 * h + e], a_scale, ws[e], a.bias != nullptr, bs[e]);
             }
-            store_run(row + i * 32 + 16 * p, fh, v[0], v[1], a.n - (n0 + i * 32 + 16 * p), a.wide);
+            store_run(row + i * 32 + 16 * p, fh, v[0], v[1], a.n - (n0 + i * 32 + 16 * p));
           }
       }
     }
@@ -522,13 +519,13 @@ __global__ __launch_bounds__(kFewWaves * 64, MT == 1 && ALIGNED ? 4 : 2) void fe
     v[e] = output(sum[e], a_scale, a.w_scale[c], a.bias != nullptr, a.bias ? bf2f(a.bias[c]) : 0.0f);
   }
   T* p = static_cast<T*>(a.out) + int64_t(m) * a.ldo + n;
-  if (a.wide && n + 4 <= a.n) {
-    if constexpr (sizeof(T) == 4)
-      *reinterpret_cast<f32x4*>(p) = f32x4{v[0], v[1], v[2], v[3]};
-    else
-      *reinterpret_cast<u32x2*>(p) = u32x2{pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3])};
-  } else {
+  if (n + 4 > a.n) {
     store_each(p, v, a.n - n);
+  } else if constexpr (sizeof(T) == 4) {
+    __builtin_memcpy(p, v, 16);
+  } else {
+    const u32x2 two = {pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3])};
+    __builtin_memcpy(p, &two, 8);
   }
 }
 
@@ -563,11 +560,9 @@ hipError_t launch_choice(const LinearI8Args& a, int choice, int cus, hipStream_t
 }
 
 template <int TYPE>
-hipError_t launch_type(LinearI8Args a, int cus, hipStream_t s) {
-  constexpr size_t size = sizeof(typename OutOf<TYPE>::T);
+hipError_t launch_type(const LinearI8Args& a, int cus, hipStream_t s) {
   const uintptr_t in = reinterpret_cast<uintptr_t>(a.a) | reinterpret_cast<uintptr_t>(a.w) | uintptr_t(a.lda) |
                        uintptr_t(a.ldw) | uintptr_t(a.k);
-  a.wide = (reinterpret_cast<uintptr_t>(a.out) | uintptr_t(a.ldo) * size) % 16 == 0;
   const int choice = linear_i8_choice(a.m, a.n, a.k, cus);
   return in % 16 == 0 ? launch_choice<TYPE, true>(a, choice, cus, s) : launch_choice<TYPE, false>(a, choice, cus, s);
 }
