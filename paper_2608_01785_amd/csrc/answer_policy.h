@@ -10,33 +10,41 @@ constexpr int kLogprobsMaxTop = 64;       // alternatives a row can list: one pe
 constexpr int kLinearI8MaxK = 131071;     // (-128)^2 k stays below 2^31
 constexpr int64_t kLinearI8MaxStride = int64_t(1) << 22;  // 256 rows of an operand stay within 32-bit offsets
 
-// The kernels of hs_linear_i8: for at most 32 or 64 rows, and tiles.
+// The kernels of hs_linear_i8: for few rows (32 at most, or 64 a block), and tiles.
 enum LinearI8Choice { kLinearI8Few32, kLinearI8Few64, kLinearI8Tile64, kLinearI8Tile128, kLinearI8Tile256 };
 
 // Which of them an [m, k] x [n, k]^T product takes on `cus` compute units.  All
-// give the same bits.
+// give the same bits, so the choice may follow the budget.  The times below
+// are in us, fitted to some 80 products of 1 to 4096 rows on the whole chip.
 //
-// Few rows: the kernels that share K among a block's waves need no channels to
-// fill the chip, the tiles have less to read (and to add up) once there are
-// many.  In us, us of the best tiles: 32 rows 4608 x 3584 6.4, 11.2; 3584 x
-// 18944 18, 46; 37888 x 3584 29.5, 32.6; 65536 x 3584 58, 52.  64 rows: 8.6, 11.2;
-// 26, 46; 14336 x 4096 18.6, 13.7; 65536 x 3584 82, 56.
+// The kernels for few rows share K among a block's waves, so they need no
+// channels to fill the chip; the tiles have less to read and to add up once
+// there are many.  Few rows against the best tiles: 32 rows 4608 x 3584 6.4, 13.9;
+// 3584 x 18944 18, 60; 37888 x 3584 29, 25.  128 rows: 1024 x 4096 7.5, 12; 3584 x
+// 18944 26, 60; 14336 x 4096 34, 19.
 //
-// Tiles: a CU's time is the tiles it gets times a tile's 64-byte stages, in us
-// as fitted to 44 products of 1 to 4096 rows.  Two 128 x 128 tiles side by side
-// on a CU take as long as one after the other; a 256 x 256 stage takes longer the
-// more of the chip works (its clock follows the power).  4096 x 8192 x 8192: 254
-// us in 256s, 350 in 128s, 596 in 64s; 777 x 4096 x 4096: 49, 26, 35; 256 x 4608 x
-// 3584: 41, 21, 16.
+// A CU's time in tiles is the tiles it gets times a tile's 64-byte steps.  128 x
+// 128 tiles side by side on a CU take as long as one after the other; 64 x 64
+// ones hide their latency behind each other; a 256 x 256 step takes longer the
+// more of the chip works, whose clock follows the power.  4096 x 8192 x 8192: 245
+// in 256s, 323 in 128s, 481 in 64s; 777 x 4096 x 4096: 45, 26, 31; 256 x 4608 x
+// 3584: 38, 20, 16.
 inline LinearI8Choice linear_i8_choice(int m, int n, int k, int cus) {
-  if (m <= 32 && n <= 160 * int64_t(cus)) return kLinearI8Few32;
-  if (m <= 64 && n <= 32 * int64_t(cus)) return m <= 32 ? kLinearI8Few32 : kLinearI8Few64;
   auto up = [](int64_t a, int64_t b) { return (a + b - 1) / b; };
-  const float stages = float(up(k, 256)) * 4.0f;
+  const float steps = float(up(k, 256)) * 4.0f, kf = float(k);
   auto rounds = [&](int tile) { return float(up(up(m, tile) * up(n, tile), cus)); };
-  const float t64 = 2.5f + rounds(64) * (0.14f * stages + 0.6f);
-  const float t128 = 3.0f + rounds(128) * (0.335f * stages + 2.0f);
-  // The 256s run in halves at the end (see linear_kernel).
+
+  LinearI8Choice best = kLinearI8Tile64;
+  const float r64 = rounds(64);
+  float cost = 2.5f + steps * (0.12f * r64 > 0.2f ? 0.12f * r64 : 0.2f) + 0.6f * r64;
+  auto offer = [&](LinearI8Choice c, float t) {
+    if (t < cost) {
+      cost = t;
+      best = c;
+    }
+  };
+  offer(kLinearI8Tile128, 3.0f + rounds(128) * (0.305f * steps + 1.3f));
+  // The 256s end in halves (see linear_kernel).
   const int64_t tm = up(m, 256), tn = up(n, 256);
   const bool short_last = m - (tm - 1) * 256 <= 128;
   const int64_t whole = (short_last ? tm - 1 : tm) * tn, halves = short_last ? tn : 0;
@@ -49,9 +57,15 @@ inline LinearI8Choice linear_i8_choice(int m, int n, int k, int cus) {
     const int64_t rest = halves - (tail > 0 ? grid - tail : 0);
     units += rest > 0 ? 0.6f * float(up(rest, grid)) : 0.0f;
   }
-  const float t256 = 6.0f + units * ((0.58f + 0.38f * float(grid) / float(cus)) * stages + 8.0f);
-  if (t256 <= t128 && t256 <= t64) return kLinearI8Tile256;
-  return t128 <= t64 ? kLinearI8Tile128 : kLinearI8Tile64;
+  offer(kLinearI8Tile256, 6.0f + units * ((0.45f + 0.38f * float(grid) / float(cus)) * steps + 8.0f));
+  // One block of the 64s fits a CU, and w comes from memory once in all.
+  const int64_t few = up(n, 32);
+  if (m > 32) offer(kLinearI8Few64, 1.7f + float(up(few * up(m, 64), cus)) * (0.0012f * kf + 2.0f));
+  if (m <= 32) {
+    const float stream = float(n) * kf / (float(cus) * 17000.0f), chain = 0.0008f * kf;
+    offer(kLinearI8Few32, 3.0f + (stream > chain ? stream : chain));
+  }
+  return best;
 }
 
 // hs_logprobs: a row's elements go through wavefronts in chunks of 4 KB (one

@@ -129,9 +129,10 @@ __device__ __forceinline__ void store_run(T* p, int h, const float (&lo)[4], con
 // load l takes chunk lane % C of row row0 + lane / C + (64 / C) l.
 //   ALIGNED: base, row stride and k are multiples of 16.  A buffer resource
 //   over the rows: what lies past the last row or past k reads zero.
-//   Otherwise: byte addresses, rows past the last read it again (they are
-//   never stored) and the chunk that holds the end of k is read from 16 bytes
-//   before that end and shifted.
+//   Otherwise (k >= 16): byte addresses, rows past the last read it again (they
+//   are never stored).  The chunk that holds the end of k is read from 16 bytes
+//   before that end, chunks past it from the row's start, and settle() shifts
+//   and clears them on their way to LDS, so that no load waits for another.
 template <bool ALIGNED, int C, int L>
 struct Operand {
   static constexpr int kRows = 64 / C, kBytes = 16 * C;  // of a load, and of a row in a stage
@@ -151,50 +152,39 @@ struct Operand {
       const int first = min(row0, rows - 1);
       base = p + int64_t(first) * ld;
 #pragma unroll
-      for (int l = 0; l < L; ++l) off[l] = uint32_t(min(r + kRows * l, rows - 1 - first)) * uint32_t(ld) + uint32_t(c * 16);
+      for (int l = 0; l < L; ++l) off[l] = uint32_t(min(r + kRows * l, rows - 1 - first)) * uint32_t(ld);
     }
   }
   __device__ __forceinline__ u32x4 load(int l, int stage, int64_t ld, int k) const {
     const int whole = k / kBytes;  // stages without the end of k
+    const int at = stage * kBytes + int(threadIdx.x % C) * 16;
     if constexpr (ALIGNED) {
       uint32_t v = off[0];
       // Past k: an offset outside the resource, which reads zero.
-      if (stage >= whole && stage * kBytes + int(threadIdx.x % C) * 16 >= k) v = 0x80000000u;
+      if (stage >= whole && at >= k) v = 0x80000000u;
       const uint32_t s = uint32_t(min(stage, (k - 1) / kBytes)) * kBytes + uint32_t(kRows * l) * uint32_t(ld);
       return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(res, v, s, 0));
     } else {
-      u32x4 v = {0, 0, 0, 0};
-      const int8_t* p = base + int64_t(stage) * kBytes;
-      if (stage < whole) {
-        __builtin_memcpy(&v, p + off[l], 16);
-        return v;
-      }
-      const int n = k - stage * kBytes - int(threadIdx.x % C) * 16;  // bytes of the chunk that k holds
-      if (n >= 16) {
-        __builtin_memcpy(&v, p + off[l], 16);
-      } else if (n > 0 && k >= 16) {
-        __builtin_memcpy(&v, p + off[l] - (16 - n), 16);
-        // Bytes 16 - n .. 15 are the chunk's first n.
-        const int words = (16 - n) >> 2, bytes = (16 - n) & 3;
-        uint32_t w[5] = {v[0], v[1], v[2], v[3], 0};
-        for (int i = 0; i < words; ++i) {
-          w[0] = w[1];
-          w[1] = w[2];
-          w[2] = w[3];
-          w[3] = 0;
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = __builtin_amdgcn_alignbyte(w[i + 1], w[i], bytes);
-      } else if (n > 0) {
-        uint32_t w[4] = {0, 0, 0, 0};
-        for (int i = 0; i < n; ++i) {
-          const uint32_t b = uint32_t(uint8_t(p[off[l] + i])) << (8 * (i & 3));
-#pragma unroll
-          for (int j = 0; j < 4; ++j) w[j] |= (i >> 2) == j ? b : 0u;
-        }
-        v = u32x4{w[0], w[1], w[2], w[3]};
-      }
+      u32x4 v;
+      __builtin_memcpy(&v, base + (off[l] + uint32_t(at + 16 <= k ? at : at < k ? k - 16 : 0)), 16);
       return v;
+    }
+  }
+  // The chunk as its stage holds it, from what load() brought.
+  __device__ __forceinline__ u32x4 settle(u32x4 v, int stage, int k) const {
+    if constexpr (ALIGNED) {
+      return v;
+    } else {
+      if (stage < k / kBytes) return v;
+      const int n = k - stage * kBytes - int(threadIdx.x % C) * 16;  // bytes of the chunk that k holds
+      if (n <= 0) return u32x4{0, 0, 0, 0};
+      if (n >= 16) return v;
+      // The chunk's n bytes came last.
+      const int gone = 16 - n;
+      if (gone & 8) v = u32x4{v[2], v[3], 0, 0};
+      if (gone & 4) v = u32x4{v[1], v[2], v[3], 0};
+      return u32x4{__builtin_amdgcn_alignbyte(v[1], v[0], gone & 3), __builtin_amdgcn_alignbyte(v[2], v[1], gone & 3),
+                   __builtin_amdgcn_alignbyte(v[3], v[2], gone & 3), __builtin_amdgcn_alignbyte(0u, v[3], gone & 3)};
     }
   }
 };
@@ -277,9 +267,9 @@ __global__ __launch_bounds__(WN * WM * 64, WN * WM == 8 ? 1 : 2) void linear_ker
   const uint32_t put_at = (w_wave ? 0u : uint32_t(kTile)) + uint32_t(put_row * BK);
   const uint32_t put_chunk[2] = {uint32_t(phys<C>(put_row, lane % C) * 16),
                                  uint32_t(phys<C>(put_row + kLoadRows, lane % C) * 16)};
-  auto put = [&](int buf, int slot, int l) {
+  auto put = [&](int buf, int slot, int l, int stage) {
     *reinterpret_cast<u32x4*>(smem + buf * kStage + l * kLoadRows * BK + put_at +
-                              put_chunk[kLoadRows < 16 ? l & 1 : 0]) = ring[slot][l];
+                              put_chunk[kLoadRows < 16 ? l & 1 : 0]) = op.settle(ring[slot][l], stage, a.k);
   };
   struct Frag {
     u32x4 w[NS], a[MT];
@@ -313,7 +303,7 @@ __global__ __launch_bounds__(WN * WM * 64, WN * WM == 8 ? 1 : 2) void linear_ker
 #pragma unroll
     for (int l = 0; l < L; ++l) ring[t][l] = op.load(l, t, ld, a.k);
 #pragma unroll
-  for (int l = 0; l < L; ++l) put(0, 0, l);
+  for (int l = 0; l < L; ++l) put(0, 0, l, 0);
   asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
@@ -358,7 +348,8 @@ __global__ __launch_bounds__(WN * WM * 64, WN * WM == 8 ? 1 : 2) void linear_ker
                 for (int x = q * NR / NM; x < (q + 1) * NR / NM; ++x) read(jt, buf, kk + 1, x, f[(kk + 1) & 1]);
                 if (slot < kPutEnd) {
 #pragma unroll
-                  for (int x = slot * L / kPutEnd; x < (slot + 1) * L / kPutEnd; ++x) put(1 - buf, (u + 1) % kUnroll, x);
+                  for (int x = slot * L / kPutEnd; x < (slot + 1) * L / kPutEnd; ++x) 
+                    put(1 - buf, (u + 1) % kUnroll, x, u + 1 < kUnroll || !last ? kt + u + 1 : 0);
                 }
               } else if (u + 1 < kUnroll || !last) {
 #pragma unroll
@@ -451,7 +442,8 @@ __global__ __launch_bounds__(kFewWaves * 64, MT == 1 && ALIGNED ? 4 : 2) void fe
   Operand<ALIGNED, 8, 4> wop;
   Operand<ALIGNED, 8, 4 * MT> aop;
   wop.set(a.w, a.ldw, n0, a.n, a.k);
-  aop.set(a.a, a.lda, 0, a.m, a.k);
+  const int m0 = blockIdx.y * 32 * MT;
+  aop.set(a.a, a.lda, m0, a.m, a.k);
   u32x4 w[D][4], x[D][4 * MT];
   auto load = [&](int slot, int stage) {
 #pragma unroll
@@ -474,12 +466,14 @@ __global__ __launch_bounds__(kFewWaves * 64, MT == 1 && ALIGNED ? 4 : 2) void fe
   for (int i = 0; i < rounds; i += D) {
 #pragma unroll
     for (int d = 0; d < D; ++d) {
+      const int stage = wave + (i + d) * kFewWaves;
 #pragma unroll
       for (int l = 0; l < 4; ++l)
-        *reinterpret_cast<u32x4*>(image + l * 8 * kRow + ((l & 1) ? put_odd : put_off)) = w[d][l];
+        *reinterpret_cast<u32x4*>(image + l * 8 * kRow + ((l & 1) ? put_odd : put_off)) = wop.settle(w[d][l], stage, a.k);
 #pragma unroll
       for (int l = 0; l < 4 * MT; ++l)
-        *reinterpret_cast<u32x4*>(image + (4 + l) * 8 * kRow + ((l & 1) ? put_odd : put_off)) = x[d][l];
+        *reinterpret_cast<u32x4*>(image + (4 + l) * 8 * kRow + ((l & 1) ? put_odd : put_off)) =
+            aop.settle(x[d][l], stage, a.k);
       load(d, wave + (i + d + D) * kFewWaves);  // zeros past the end of k
       // The image is this wave's alone, and LDS serves one wave in order.
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -506,7 +500,7 @@ __global__ __launch_bounds__(kFewWaves * 64, MT == 1 && ALIGNED ? 4 : 2) void fe
       *reinterpret_cast<i32x4*>(part + (((j * 4 + g) * kFewWaves + wave) * 64 + lane) * 4) =
           i32x4{acc[j][4 * g], acc[j][4 * g + 1], acc[j][4 * g + 2], acc[j][4 * g + 3]};
   __syncthreads();
-  const int m = (wave >> 2) * 32 + fr, n = n0 + 8 * (wave & 3) + 4 * fh;
+  const int m = m0 + (wave >> 2) * 32 + fr, n = n0 + 8 * (wave & 3) + 4 * fh;
   if (wave >= 4 * MT || m >= a.m || n >= a.n) return;
   i32x4 sum = {0, 0, 0, 0};
 #pragma unroll
@@ -529,6 +523,20 @@ __global__ __launch_bounds__(kFewWaves * 64, MT == 1 && ALIGNED ? 4 : 2) void fe
   }
 }
 
+// Rows of fewer than 16 bytes that are not aligned: one thread an output.
+template <int TYPE>
+__global__ __launch_bounds__(256) void short_kernel(LinearI8Args a) {
+  using T = typename OutOf<TYPE>::T;
+  const int64_t outputs = int64_t(a.m) * a.n;
+  for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < outputs; i += int64_t(gridDim.x) * 256) {
+    const int m = int(i / a.n), n = int(i % a.n);
+    int32_t sum = 0;
+    for (int k = 0; k < a.k; ++k) sum += int32_t(a.a[int64_t(m) * a.lda + k]) * a.w[int64_t(n) * a.ldw + k];
+    static_cast<T*>(a.out)[int64_t(m) * a.ldo + n] =
+        T(output(sum, a.a_scale[m], a.w_scale[n], a.bias != nullptr, a.bias ? bf2f(a.bias[n]) : 0.0f));
+  }
+}
+
 template <int TYPE, bool ALIGNED, int C, int WN, int WM, int NS, int MT>
 hipError_t launch_tiles(const LinearI8Args& a, int blocks, hipStream_t s) {
   constexpr int BN = 32 * NS * WN, BM = 32 * MT * WM;
@@ -541,7 +549,7 @@ hipError_t launch_tiles(const LinearI8Args& a, int blocks, hipStream_t s) {
 
 template <int TYPE, bool ALIGNED>
 hipError_t launch_choice(const LinearI8Args& a, int choice, int cus, hipStream_t s) {
-  const dim3 few((a.n + 31) / 32);
+  const dim3 few((a.n + 31) / 32, choice == kLinearI8Few64 ? (a.m + 63) / 64 : 1);
   switch (choice) {
     case kLinearI8Few32:
       hipLaunchKernelGGL((few_kernel<TYPE, ALIGNED, 1>), few, dim3(kFewWaves * 64), 0, s, a);
@@ -564,7 +572,11 @@ hipError_t launch_type(const LinearI8Args& a, int cus, hipStream_t s) {
   const uintptr_t in = reinterpret_cast<uintptr_t>(a.a) | reinterpret_cast<uintptr_t>(a.w) | uintptr_t(a.lda) |
                        uintptr_t(a.ldw) | uintptr_t(a.k);
   const int choice = linear_i8_choice(a.m, a.n, a.k, cus);
-  return in % 16 == 0 ? launch_choice<TYPE, true>(a, choice, cus, s) : launch_choice<TYPE, false>(a, choice, cus, s);
+  if (in % 16 == 0) return launch_choice<TYPE, true>(a, choice, cus, s);
+  if (a.k >= 16) return launch_choice<TYPE, false>(a, choice, cus, s);
+  const int64_t blocks = (int64_t(a.m) * a.n + 255) / 256;
+  hipLaunchKernelGGL(short_kernel<TYPE>, dim3(unsigned(blocks < 16 * cus ? blocks : 16 * cus)), dim3(256), 0, s, a);
+  return hipGetLastError();
 }
 
 }  // namespace
