@@ -259,6 +259,13 @@ __global__ __launch_bounds__(WN * WM * 64, WN * WM == 8 ? 1 : 2) void linear_ker
     op.set(src, ld, row0, rows, a.k);
   };
   set_op(unit);
+  // Stages of one row of tiles may come in any order (the sums are exact).
+  // Where no other block reads the same channels, each tile starts at another
+  // one: rows a power of two apart would otherwise keep all blocks on the same
+  // memory channels.
+  auto turn_of = [&](const Unit& u) { return tiles_m == 1 ? u.tn * 11 % KP : 0; };
+  int turn = turn_of(unit);
+  auto turned = [&](int stage, int by) { return stage + by < KP ? stage + by : stage + by - KP; };
 
   u32x4 ring[kUnroll][L];  // stage t in slot t % kUnroll
   // Load l holds image rows wave_row + kLoadRows l + lane / C; phys() repeats
@@ -301,9 +308,9 @@ __global__ __launch_bounds__(WN * WM * 64, WN * WM == 8 ? 1 : 2) void linear_ker
 #pragma unroll
   for (int t = 0; t < kUnroll; ++t)
 #pragma unroll
-    for (int l = 0; l < L; ++l) ring[t][l] = op.load(l, t, ld, a.k);
+    for (int l = 0; l < L; ++l) ring[t][l] = op.load(l, turned(t, turn), ld, a.k);
 #pragma unroll
-  for (int l = 0; l < L; ++l) put(0, 0, l, 0);
+  for (int l = 0; l < L; ++l) put(0, 0, l, turn);
   asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
@@ -319,6 +326,7 @@ __global__ __launch_bounds__(WN * WM * 64, WN * WM == 8 ? 1 : 2) void linear_ker
         for (int r = 0; r < 16; ++r) acc[i][j][r] = 0;
     const bool more = unit_of(round + 1) < n_units;
     const Unit next_unit = more ? unit_at(unit_of(round + 1)) : unit;
+    const int next_turn = turn_of(next_unit);
     auto k_loop = [&](auto jt) {
       constexpr int JT = decltype(jt)::value;
       constexpr int NM = NS * JT, NR = NS + JT;
@@ -329,7 +337,7 @@ __global__ __launch_bounds__(WN * WM * 64, WN * WM == 8 ? 1 : 2) void linear_ker
         if (last && more) set_op(next_unit);
         // Past a unit's last stage come the next one's first ones; after the
         // last unit its own again (in bounds, never used).
-        const int kl = last ? 0 : kt + kUnroll;
+        const int kl = last ? 0 : kt + kUnroll, kl_turn = last ? next_turn : turn;
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u) {
           const int buf = u & 1;
@@ -349,7 +357,7 @@ __global__ __launch_bounds__(WN * WM * 64, WN * WM == 8 ? 1 : 2) void linear_ker
                 if (slot < kPutEnd) {
 #pragma unroll
                   for (int x = slot * L / kPutEnd; x < (slot + 1) * L / kPutEnd; ++x) 
-                    put(1 - buf, (u + 1) % kUnroll, x, u + 1 < kUnroll || !last ? kt + u + 1 : 0);
+                    put(1 - buf, (u + 1) % kUnroll, x, u + 1 < kUnroll || !last ? turned(kt + u + 1, turn) : next_turn);
                 }
               } else if (u + 1 < kUnroll || !last) {
 #pragma unroll
@@ -360,7 +368,7 @@ __global__ __launch_bounds__(WN * WM * 64, WN * WM == 8 ? 1 : 2) void linear_ker
                 constexpr int kN = kSlots - kLoadBegin;
 #pragma unroll
                 for (int x = (slot - kLoadBegin) * L / kN; x < (slot - kLoadBegin + 1) * L / kN; ++x)
-                  ring[u][x] = op.load(x, kl + u, ld, a.k);
+                  ring[u][x] = op.load(x, turned(kl + u, kl_turn), ld, a.k);
               }
               __builtin_amdgcn_sched_barrier(0);
             }
@@ -415,6 +423,7 @@ __global__ __launch_bounds__(WN * WM * 64, WN * WM == 8 ? 1 : 2) void linear_ker
     for (int i = 0; i < kPer; ++i)
       if (tid + kThreads * i < kFactors) factors[parity][tid + kThreads * i] = next[i];
     unit = next_unit;
+    turn = next_turn;
     ++round;
   }
 }
@@ -461,12 +470,15 @@ __global__ __launch_bounds__(kFewWaves * 64, MT == 1 && ALIGNED ? 4 : 2) void fe
 #pragma unroll
     for (int r = 0; r < 16; ++r) acc[j][r] = 0;
   const int stages = (a.k + kRow - 1) / kRow, rounds = (stages + kFewWaves - 1) / kFewWaves;
+  // As in linear_kernel, every block starts at another round.
+  const int turn = blockIdx.x * 3 % rounds;
+  auto stage_of = [&](int i) { return i >= rounds ? stages + 1 : wave + (i + turn < rounds ? i + turn : i + turn - rounds) * kFewWaves; };
 #pragma unroll
-  for (int d = 0; d < D; ++d) load(d, wave + d * kFewWaves);
+  for (int d = 0; d < D; ++d) load(d, stage_of(d));
   for (int i = 0; i < rounds; i += D) {
 #pragma unroll
     for (int d = 0; d < D; ++d) {
-      const int stage = wave + (i + d) * kFewWaves;
+      const int stage = stage_of(i + d);
 #pragma unroll
       for (int l = 0; l < 4; ++l)
         *reinterpret_cast<u32x4*>(image + l * 8 * kRow + ((l & 1) ? put_odd : put_off)) = wop.settle(w[d][l], stage, a.k);
@@ -474,7 +486,7 @@ __global__ __launch_bounds__(kFewWaves * 64, MT == 1 && ALIGNED ? 4 : 2) void fe
       for (int l = 0; l < 4 * MT; ++l)
         *reinterpret_cast<u32x4*>(image + (4 + l) * 8 * kRow + ((l & 1) ? put_odd : put_off)) =
             aop.settle(x[d][l], stage, a.k);
-      load(d, wave + (i + d + D) * kFewWaves);  // zeros past the end of k
+      load(d, stage_of(i + d + D));  // zeros past the end of k
       // The image is this wave's alone, and LDS serves one wave in order.
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
