@@ -19,31 +19,37 @@ enum LinearI8Choice { kLinearI8Few32, kLinearI8Few64, kLinearI8Tile64, kLinearI8
 //
 // The kernels for few rows share K among a block's waves, so they need no
 // channels to fill the chip; the tiles have less to read and to add up once
-// there are many.  Few rows against the best tiles: 32 rows 4608 x 3584 6.4, 13.9;
-// 3584 x 18944 18, 60; 37888 x 3584 29, 25.  128 rows: 1024 x 4096 7.5, 12; 3584 x
-// 18944 26, 60; 14336 x 4096 34, 19.
+// there are many.  Few rows against the best tiles: 32 rows 4608 x 3584 6.5, 10.8;
+// 3584 x 18944 18, 43; 65536 x 4096 65, 55.  128 rows: 1024 x 4096 7.5, 12; 3584 x
+// 18944 26, 45; 14336 x 4096 34, 19.
 //
 // A CU's time in tiles is the tiles it gets times a tile's 64-byte steps.  128 x
 // 128 tiles side by side on a CU take as long as one after the other; 64 x 64
 // ones hide their latency behind each other; a 256 x 256 step takes longer the
-// more of the chip works, whose clock follows the power.  4096 x 8192 x 8192: 245
-// in 256s, 323 in 128s, 481 in 64s; 777 x 4096 x 4096: 45, 26, 31; 256 x 4608 x
-// 3584: 38, 20, 16.
+// more of the chip works, whose clock follows the power.  4096 x 8192 x 8192: 235
+// in 256s, 323 in 128s, 477 in 64s; 777 x 4096 x 4096: 45, 26, 31; 256 x 4608 x
+// 3584: 38, 20, 16.  The constants are those of 256 CUs; memory's rate is taken
+// to be shared by them.
 inline LinearI8Choice linear_i8_choice(int m, int n, int k, int cus) {
   auto up = [](int64_t a, int64_t b) { return (a + b - 1) / b; };
-  const float steps = float(up(k, 256)) * 4.0f, kf = float(k);
-  auto rounds = [&](int tile) { return float(up(up(m, tile) * up(n, tile), cus)); };
+  auto larger = [](float a, float b) { return a > b ? a : b; };
+  const float steps = float(up(k, 256)) * 4.0f, kf = float(k), w_bytes = float(n) * kf / float(cus);
+  const int64_t tiles64 = up(m, 64) * up(n, 64);
+  const float r64 = float(up(tiles64, cus)), slots64 = float(tiles64) / float(4 * cus);
+  // Four 64 x 64 tiles run on a CU at a time; a part of a round more stretches
+  // the time of the channels' stream.
+  const float stretch = slots64 > 1.0f ? 0.5f + 0.5f * float(up(tiles64, 4 * cus)) / slots64 : 1.0f;
 
   LinearI8Choice best = kLinearI8Tile64;
-  const float r64 = rounds(64);
-  float cost = 2.5f + steps * (0.12f * r64 > 0.2f ? 0.12f * r64 : 0.2f) + 0.6f * r64;
+  float cost = larger(2.5f + steps * larger(0.145f, 0.12f * r64) + 0.6f * r64, 3.0f + stretch * w_bytes / 20700.0f);
   auto offer = [&](LinearI8Choice c, float t) {
     if (t < cost) {
       cost = t;
       best = c;
     }
   };
-  offer(kLinearI8Tile128, 3.0f + rounds(128) * (0.305f * steps + 1.3f));
+  offer(kLinearI8Tile128, larger(3.0f + float(up(up(m, 128) * up(n, 128), cus)) * (0.305f * steps + 1.3f),
+                                 3.0f + w_bytes / 16500.0f));
   // The 256s end in halves (see linear_kernel).
   const int64_t tm = up(m, 256), tn = up(n, 256);
   const bool short_last = m - (tm - 1) * 256 <= 128;
@@ -57,13 +63,14 @@ inline LinearI8Choice linear_i8_choice(int m, int n, int k, int cus) {
     const int64_t rest = halves - (tail > 0 ? grid - tail : 0);
     units += rest > 0 ? 0.6f * float(up(rest, grid)) : 0.0f;
   }
-  offer(kLinearI8Tile256, 6.0f + units * ((0.45f + 0.38f * float(grid) / float(cus)) * steps + 8.0f));
-  // One block of the 64s fits a CU, and w comes from memory once in all.
+  offer(kLinearI8Tile256, larger(6.0f + units * ((0.45f + 0.38f * float(grid) / float(cus)) * steps + 8.0f),
+                                 3.0f + w_bytes / 19500.0f));
   const int64_t few = up(n, 32);
-  if (m > 32) offer(kLinearI8Few64, 1.7f + float(up(few * up(m, 64), cus)) * (0.0012f * kf + 2.0f));
-  if (m <= 32) {
-    const float stream = float(n) * kf / (float(cus) * 17000.0f), chain = 0.0008f * kf;
-    offer(kLinearI8Few32, 3.0f + (stream > chain ? stream : chain));
+  if (m > 32) {
+    const float rounds = float(up(few * up(m, 64), cus));
+    offer(kLinearI8Few64, larger(1.7f + rounds * (0.0012f * kf + 2.0f), 2.0f + 0.0021f * kf * float(few) / float(cus)));
+  } else {
+    offer(kLinearI8Few32, 3.0f + larger(0.0008f * kf, w_bytes / 17000.0f));
   }
   return best;
 }

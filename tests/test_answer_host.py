@@ -157,3 +157,17 @@ def test_binding_refuses_tensors_that_do_not_fit(b):
         b.hs_quantize_rows(Ctx, x.double(), x.to(torch.int8), torch.zeros(4))
     with pytest.raises(ValueError, match="dimensions"):
         b.hs_logprobs(Ctx, x[0])
+
+
+def test_linear_kernel_rule(b):
+    """Few rows, then larger tiles as there is more to do; what every kernel's GPU test relies on."""
+    kernel = b.lib().hs_linear_i8_kernel
+    few32, few64, t64, t128, t256 = range(5)
+    assert kernel(1, 4608, 3584, 256) == few32 and kernel(32, 3584, 18944, 256) == few32
+    assert kernel(64, 4608, 3584, 256) == few64 and kernel(128, 3584, 18944, 256) == few64
+    assert kernel(128, 14336, 4096, 256) == t64
+    assert kernel(777, 4096, 4096, 256) == t128
+    assert kernel(4096, 8192, 8192, 256) == t256 and kernel(10515, 37888, 3584, 256) == t256
+    for m, n, k in ((1, 1, 1), (1, 1, 131071), (2 ** 20, 2 ** 20, 1), (2 ** 31 - 1, 1, 16), (1, 2 ** 31 - 1, 16)):
+        for cus in (1, 64, 256):
+            assert few32 <= kernel(m, n, k, cus) <= t256
