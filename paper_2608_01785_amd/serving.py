@@ -15,6 +15,12 @@ Each scheduling step k:
    active downstream requests loop on the complementary stream (step 4;
    ``hs_shared_stage_forward``, ``hs_downstream_decode_step``).
 
+With a head (``answer.AnswerHead``) the batch's last prompt rows go on from the
+residual stream to the vocabulary, on the batch's stream and CUs: each request's
+first token with its log probability and entropy, and its alternatives, which
+the loop reads back at the step's end.  They count into the short path's first
+response.
+
 The baseline policy shows every request and runs both stages unmasked on the
 whole chip.  First responses come from GPU events: a short-path request's is
 the end of its prefill step, a long-path request's the end of its
@@ -98,16 +104,24 @@ class StepRecord:
     down_cus: int
 
 
+@dataclasses.dataclass
+class Answer:
+    tokens: List[int]        # the first token (greedy) and its alternatives, by probability
+    logprobs: List[float]
+    entropy: float           # nats
+
+
 class Algorithm1:
     """The loop of Algorithm 1 over one context.
 
     thinker / talker: (shape, device weights, n_layers).  x_pool: bf16 device
     rows [>= token_budget, hidden]; a batch's prompt rows are its first rows.
     requests must be sorted by arrival.  max_ctx: downstream positions per
-    request (one cache page each)."""
+    request (one cache page each).  head: an answer.AnswerHead with top_k >= 1
+    for the shared stage, or None; its results are in answers[rid]."""
 
     def __init__(self, ctx, thinker, talker, requests: List[Request], x_pool, cfg: LoopConfig, max_ctx: int,
-                 x_talker=None, device="cuda"):
+                 x_talker=None, device="cuda", head=None):
         import torch
         from .device_data import DeviceCache
         self.torch, self.ctx, self.cfg = torch, ctx, cfg
@@ -126,6 +140,13 @@ class Algorithm1:
         max_pos = int(max(r.tokens for r in requests))
         self.ws = torch.empty(binding.hs_workspace_size(self.th_shape, cfg.token_budget, n, max_pos),
                               dtype=torch.uint8, device=device)
+        if head is not None and (head.top_k < 1 or head.hidden != self.th_shape.hidden):
+            raise ValueError(f"a head of {head.hidden} columns with {head.top_k} alternatives")
+        self.head = head
+        self.answers: Dict[int, Answer] = {}
+        if head is not None:
+            self.last = torch.empty((n, self.th_shape.hidden), dtype=torch.float32, device=device)
+            self.head_out = head.outputs(n)
         self.max_ctx = max_ctx
         self.cache = DeviceCache(self.tk_layers, n, max_ctx, self.tk_shape.n_kv_heads, self.tk_shape.head_dim, device)
         gen = torch.Generator(device=device)
@@ -180,6 +201,17 @@ class Algorithm1:
         e = self.torch.cuda.Event(enable_timing=True)
         e.record(self._down_stream(s_shared))
         return e
+
+    def _answer(self, offsets: List[int], s_shared: int, stream):
+        """The head over the last prompt row of each request of the batch, on the batch's stream."""
+        n = len(offsets) - 1
+        ends = self.torch.tensor(offsets[1:], pin_memory=True)
+        with self.torch.cuda.stream(stream):
+            ends = ends.to(self.y.device, non_blocking=True)
+            self.torch.index_select(self.y, 0, ends - 1, out=self.last[:n])
+        out = dataclasses.replace(self.head_out, **{k: t[:n] for k, t in vars(self.head_out).items() if t is not None})
+        self.head(self.last[:n], out, cu_budget=s_shared)
+        return out
 
     def _poll(self):
         if self.cfg.pressure == "amdsmi":
@@ -255,6 +287,8 @@ class Algorithm1:
                 t_down0.record(self._down_stream(s_sh))
             binding.hs_shared_stage_forward(self.ctx, self.th_shape, self.th_w, self.x_pool[:tok], self.y[:tok],
                                             offsets, None, None, s_sh, None, self.ws)
+            if self.head is not None:
+                answers = self._answer(offsets, s_sh, stream)
             p_end = torch.cuda.Event(enable_timing=True)
             p_end.record(stream)
             while not p_end.query():
@@ -279,6 +313,10 @@ class Algorithm1:
                 self.issued[cur] += 1
                 self._poll()
         torch.cuda.synchronize()
+        if batch and self.head is not None:
+            lp, tok_ids, ent = (t.tolist() for t in (answers.top_logprobs, answers.top_tokens, answers.entropy))
+            for row, i in enumerate(batch):
+                self.answers[self.reqs[i].rid] = Answer(tok_ids[row], lp[row], ent[row])
         for i in batch:
             self.waiting.remove(i)
             if self.reqs[i].long:
