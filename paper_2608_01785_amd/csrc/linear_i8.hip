@@ -194,7 +194,7 @@ struct Operand {
 };
 
 template <int TYPE, bool ALIGNED, int C, int D, int WN, int WM, int NS, int MT>
-__global__ __launch_bounds__(WN * WM * 64, WN * WM == 8 ? 1 : 2) void linear_kernel(LinearI8Args a) {
+__global__ __launch_bounds__(WN * WM * 64, WN * WM == 8 ? 1 : NS * MT == 1 ? 4 : 2) void linear_kernel(LinearI8Args a) {
   constexpr int kWaves = WN * WM, kHalf = kWaves / 2;
   constexpr int BN = 32 * NS * WN, BM = 32 * MT * WM;
   constexpr int BK = 16 * C, kSteps = C / 2;  // bytes of K per stage, and its steps
@@ -242,11 +242,25 @@ __global__ __launch_bounds__(WN * WM * 64, WN * WM == 8 ? 1 : 2) void linear_ker
     const int gsize = min(whole_m - first_m, kGroupM);
     return Unit{first_m + t % per_group % gsize, t % per_group / gsize, split ? (u - full_units) % 2 : -1};
   };
-  // Round r gives block b unit r G + b, in odd rounds r G + G - 1 - b: the
-  // blocks left without a full unit take the first halves.  The blocks of an
-  // XCD stay on a contiguous range.
-  const int b = xcd_remap(blockIdx.x, G);
-  auto unit_of = [&](int r) { return r * G + ((r & 1) ? G - 1 - b : b); };
+  // The XCD of a block is blockIdx % 8.  Full rounds give every XCD a range of
+  // units side by side, which share operands in its L2, and so does the last
+  // round with its fewer units: each XCD gets an eighth of them (896 x 5120 x
+  // 2048 in 64 x 64 tiles, whose last round has 96 of 1024: 29.2 us with those
+  // on one XCD).  The blocks without a unit there take the first short units.
+  auto of_xcd = [](int count, int x) { return (count - x + kNumXcd - 1) / kNumXcd; };
+  auto before_xcd = [](int count, int x) { return x * (count / kNumXcd) + min(x, count % kNumXcd); };
+  const int xcd = blockIdx.x % kNumXcd, pos = blockIdx.x / kNumXcd;
+  const int full_rounds = n_first / G, rest = n_first % G;
+  const bool busy = pos < of_xcd(rest, xcd);
+  const int block = before_xcd(G, xcd) + pos, busy_at = before_xcd(rest, xcd) + pos;
+  const int short_at = busy ? G - rest + busy_at : block - before_xcd(rest, xcd) - of_xcd(rest, xcd);
+  auto unit_of = [&](int r) {
+    if (r < full_rounds) return r * G + block;
+    r -= full_rounds;
+    if (busy && r == 0) return full_rounds * G + busy_at;
+    const int u = (r - (busy ? 1 : 0)) * G + short_at;
+    return u < n_short ? n_first + u : n_units;
+  };
   int round = 0;
   if (unit_of(0) >= n_units) return;
   Unit unit = unit_at(unit_of(0));

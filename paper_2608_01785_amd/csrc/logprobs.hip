@@ -15,14 +15,16 @@
 // chunk's sums.  Only a chunk that reaches m (one in c of the first c) keeps
 // F apart and takes exact differences.
 //
-// Alternatives: the block's wavefronts sort their lanes' maxima of the first
-// chunk and agree on a value that at least top_k elements reach.  A chunk
-// whose maximum stays below it is done, and elements that reach it leave their
-// key (order of the value, then the lower token) in the wavefront's
-// buffer in LDS.  Every 64 keys are sorted over the lanes and merged into a
-// list of the 64 best, which raises the bound; most rows end before that.
-// What is left, little more than top_k keys, is ranked by counting the larger
-// ones.
+// Alternatives cost the loop over the chunks next to nothing: every lane leaves
+// the maximum of its elements of each chunk in LDS.  At the end 256 maxima of
+// disjoint parts of the row give a value that at least top_k of them reach (and
+// few elements more: 21 to be expected for 20, 74 for 64), the lanes' maxima
+// that reach it name the words to read again, and what reaches it there leaves
+// a key (order of the value, then the lower token).  The keys are ranked by
+// counting the larger ones.  Where too many elements share the last value, as
+// in a row of equal logits, the wavefront goes through its chunks once more:
+// every 64 keys are sorted over the lanes and merged into a list of the 64
+// best, which raises the bound.
 #include "answer_device.h"
 #include "answer_kernels.h"
 
@@ -198,6 +200,30 @@ __device__ __forceinline__ int rank_among(const uint64_t* p, int n, uint64_t key
 
 // ---------------------------------------------------------------- chunks
 
+// The 16-byte word at element i of a row [first, last), masked outside it (a
+// word that the row shares with others is read whole).
+template <typename T>
+__device__ __forceinline__ u32x4 edge_word(const T* p, int64_t i, int64_t first, int64_t last) {
+  constexpr int kVec = 16 / sizeof(T);
+  constexpr uint32_t masked = sizeof(T) == 4 ? 0xff800000u : __is_same(T, uint16_t) ? 0xff80ff80u : 0xfc00fc00u;
+  u32x4 raw = {masked, masked, masked, masked};
+  if (i + kVec <= first || i >= last) return raw;
+  const u32x4 v = *reinterpret_cast<const u32x4*>(p + i);
+  // Elements lo .. hi - 1 of the word belong to the row.
+  const int lo = int(first > i ? first - i : 0), hi = int(last - i < kVec ? last - i : kVec);
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    uint32_t keep;
+    if constexpr (sizeof(T) == 4)
+      keep = (w >= lo && w < hi) ? ~0u : 0u;
+    else
+      keep = ((2 * w >= lo && 2 * w < hi) ? 0xffffu : 0u) |
+             ((2 * w + 1 >= lo && 2 * w + 1 < hi) ? 0xffff0000u : 0u);
+    raw[w] = (v[w] & keep) | (masked & ~keep);
+  }
+  return raw;
+}
+
 template <typename T>
 struct Chunk {
   static constexpr int kVec = 16 / sizeof(T);     // elements of a 16-byte load
@@ -224,28 +250,10 @@ struct Chunk {
     for (int l = 0; l < 4; ++l) raw[l] = *reinterpret_cast<const u32x4*>(q + l * 64 * kVec);
   }
   // The same where the chunk reaches past the row [first, last): masked there.
-  // A 16-byte word that the row shares with others is read whole.
   __device__ void load_edge(const T* p, int64_t c, int64_t first, int64_t last) {
-    constexpr uint32_t masked = sizeof(T) == 4 ? 0xff800000u : __is_same(T, uint16_t) ? 0xff80ff80u : 0xfc00fc00u;
 #pragma unroll
-    for (int l = 0; l < 4; ++l) {
-      const int64_t i = c * kSize + (l * 64 + (threadIdx.x & 63)) * kVec;
-      raw[l] = u32x4{masked, masked, masked, masked};
-      if (i + kVec <= first || i >= last) continue;
-      const u32x4 v = *reinterpret_cast<const u32x4*>(p + i);
-      // Elements lo .. hi - 1 of the word belong to the row.
-      const int lo = int(first > i ? first - i : 0), hi = int(last - i < kVec ? last - i : kVec);
-#pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        uint32_t keep;
-        if constexpr (sizeof(T) == 4)
-          keep = (w >= lo && w < hi) ? ~0u : 0u;
-        else
-          keep = ((2 * w >= lo && 2 * w < hi) ? 0xffffu : 0u) |
-                 ((2 * w + 1 >= lo && 2 * w + 1 < hi) ? 0xffff0000u : 0u);
-        raw[l][w] = (v[w] & keep) | (masked & ~keep);
-      }
-    }
+    for (int l = 0; l < 4; ++l)
+      raw[l] = edge_word(p, c * kSize + (l * 64 + (threadIdx.x & 63)) * kVec, first, last);
   }
 };
 
@@ -433,73 +441,167 @@ __device__ __forceinline__ uint64_t* partial_keys(const LogprobsArgs& a, int64_t
   return reinterpret_cast<uint64_t*>(static_cast<f32x4*>(a.part) + blocks);
 }
 
+// The k-th largest of four values of every lane, rounded towards -inf to 16
+// bits (every step waits for the one before); kLowest where fewer than k are not masked.
+__device__ __forceinline__ float reached_by(const f32x4& v, int k) {
+  uint32_t o[4], t = 0;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) o[q] = order_of(v[q]);
+#pragma unroll
+  for (int b = 31; b >= 16; --b) {
+    const uint32_t c = t | (1u << b);
+    int n = 0;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) n += __popcll(__ballot(o[q] >= c));
+    if (n >= k) t = c;
+  }
+  return t < order_of(kLowest) ? kLowest : value_of(uint64_t(t) << 32);
+}
+
+// What the lanes of a block of W wavefronts leave in LDS of the chunks: so many
+// maxima each.  A wavefront with more chunks than its share of them takes
+// several as one.  16 blocks of one wavefront fit a CU.
+template <int W>
+constexpr int kPeaks = W == 1 ? 32 : 64;
+
+// Keys of the elements that reach `bound`, of the entries (lanes' maxima of
+// `group` chunks) that do, into buf; their number, or more than kBuffer where
+// they are too many (buf then holds nothing of use).
+template <typename T, int W>
+__device__ __forceinline__ int collect(const Row<T>& row, int begin, int end, int group, int entries, float bound,
+                                       const float (*peaks)[64], uint16_t* hits, uint64_t* buf) {
+  constexpr int V = Chunk<T>::kVec;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  auto before = [](uint64_t mask) {
+    return int(__builtin_amdgcn_mbcnt_hi(uint32_t(mask >> 32), __builtin_amdgcn_mbcnt_lo(uint32_t(mask), 0)));
+  };
+  int found = 0, n = 0;
+#pragma unroll 4
+  for (int e = 0; e < entries; ++e) {
+    const bool hit = peaks[e][lane] >= bound;
+    const uint64_t mask = __ballot(hit);
+    if (mask == 0) continue;
+    const int at = found + before(mask);
+    if (hit && at < kBuffer) hits[at] = uint16_t(e * 64 + lane);
+    found += __popcll(mask);
+  }
+  if (found > kBuffer) return found;
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  for (int h = 0; h < found; h += 64) {
+    const int hit = h + lane < found ? hits[h + lane] : -1;
+    for (int g = 0; g < group; ++g) {
+      const int c = begin + wave + W * ((hit >> 6) * group + g);
+      const bool mine = hit >= 0 && c < end;
+      const int64_t i0 = int64_t(c) * Chunk<T>::kSize + (hit & 63) * V;
+      Chunk<T> words;
+#pragma unroll
+      for (int l = 0; l < 4; ++l)
+        words.raw[l] = edge_word(row.p, mine ? i0 + l * 64 * V : row.last, row.first, row.last);
+      uint32_t which = 0;
+#pragma unroll
+      for (int l = 0; l < 4; ++l)
+#pragma unroll
+        for (int e = 0; e < V; ++e) which |= uint32_t(words.get(l, e) >= bound) << (l * V + e);
+      // Nearly always one: read again, since registers cannot be indexed.
+      while (true) {
+        const uint64_t mask = __ballot(which != 0);
+        if (mask == 0) break;
+        const int at = n + before(mask);
+        if (which && at < kBuffer) {
+          const int j = __builtin_ctz(which);
+          const int64_t i = i0 + (j / V) * 64 * V + j % V;
+          buf[at] = key_of(elem(row.p, i), uint32_t(i - row.first));
+        }
+        which &= which - 1;
+        n += __popcll(mask);
+      }
+    }
+  }
+  return n;
+}
+
 // Block (row, split): W wavefronts take the split's chunks in turn.
 template <typename T, int W, bool TOP>
 __global__ __launch_bounds__(64 * W) void logprobs_kernel(LogprobsArgs a, int splits, int chunks_per_split) {
+  constexpr int kOwn = kPeaks<W> / W;  // a wavefront's entries
+  static_assert(kOwn * 64 * sizeof(float) >= 64 * 4 * sizeof(u32x4), "the second look's copy of a chunk takes their place");
   __shared__ __attribute__((aligned(16))) uint64_t keys[TOP ? W : 1][kBuffer];
-  __shared__ u32x4 copies[TOP ? W : 1][64][4];
+  __shared__ __attribute__((aligned(16))) float peaks[TOP ? kPeaks<W> : 1][64];
+  __shared__ __attribute__((aligned(16))) float pool[TOP && W > 1 ? W * 64 : 4];
+  __shared__ uint16_t hits[TOP ? W : 1][kBuffer];
   __shared__ f32x4 all_sums[W];
-  __shared__ float seeds[W][2];
   __shared__ int counts[W];
+  static_assert(W == 1 || W == 4, "four values of every lane make the bound");
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int r = int(blockIdx.x / splits), split = int(blockIdx.x % splits);
   const Row<T> row(a, r);
   const int begin = split * chunks_per_split, end = min(row.chunks, begin + chunks_per_split);
 
   Running run;
-  Best best;
-  if constexpr (TOP) best.init(a.top_k, keys[wave]);
   Given given;
   Chunk<T> c, next;
   int i = begin + wave;
   if (i < end) row.load(next, i);
   if (wave == 0 && splits == 1) given.load(a, row.p, r, lane);
+  const int group = ((end - begin + W - 1) / W + kOwn - 1) / kOwn;
+  float(*own)[64] = peaks + (TOP ? wave * kOwn : 0);
+  f32x4 most = {-kInf, -kInf, -kInf, -kInf};
+  float peak = -kInf;
+  int entry = 0, in_group = 0;
   auto lane_top_of = [](const f32x4& t) { return fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3])); };
-  if constexpr (TOP) {
-    // Each of the n wavefronts with a chunk has ceil(top_k / n) lanes at or
-    // above the least of their ceil(top_k / n)-th lane maxima, and one alone
-    // has top_k at or above its top_k-th.
-    float share = kInf, whole = -kInf;  // of a wavefront without a chunk
-    if (i < end) {
-      const int n = min(W, end - begin);
-      const float s = sort_wave(lane_top_of(tops_of(next)));
-      share = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(s), (a.top_k + n - 1) / n - 1));
-      whole = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(s), a.top_k - 1));
-    }
-    if constexpr (W > 1) {
-      if (lane == 0) {
-        seeds[wave][0] = share;
-        seeds[wave][1] = whole;
-      }
-      __syncthreads();
-#pragma unroll
-      for (int w = 0; w < W; ++w) {
-        share = fminf(share, seeds[w][0]);
-        whole = fmaxf(whole, seeds[w][1]);
-      }
-    }
-    best.bound(fmaxf(share, whole));
-  }
   while (i < end) {
     c = next;
     if (i + W < end) row.load(next, i + W);
     const f32x4 tops = tops_of(c);
-    const float top = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(max_wave(lane_top_of(tops)))));
-    run.add(c, top);
+    const float lane_top = lane_top_of(tops);
+    const float top = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(max_wave(lane_top))));
     if constexpr (TOP) {
-      const bool last = i + W >= end;
-      if (top >= best.above || (last && best.merged)) offer_chunk(c, tops, row, i, last, best, copies[wave]);
+      peak = in_group == 0 ? lane_top : fmaxf(peak, lane_top);
+      own[entry][lane] = peak;
+      if (++in_group == group) {
+        in_group = 0;
+        ++entry;
+      }
+      if constexpr (W == 1) {
+#pragma unroll
+        for (int l = 0; l < 4; ++l) most[l] = fmaxf(most[l], tops[l]);
+      } else {
+        most[0] = fmaxf(most[0], lane_top);
+      }
     }
+    run.add(c, top);
     i += W;
   }
 
   Sums sums = run.total();
+  if (lane == 0) all_sums[wave] = f32x4{sums.m, sums.s, sums.f, sums.t};
   int n = 0;
-  if constexpr (TOP) n = best.finish();
-  if (lane == 0) {
-    all_sums[wave] = f32x4{sums.m, sums.s, sums.f, sums.t};
-    counts[wave] = n;
+  if constexpr (TOP) {
+    if constexpr (W > 1) {
+      pool[threadIdx.x] = most[0];
+      __syncthreads();
+      most = *reinterpret_cast<const f32x4*>(pool + 4 * lane);
+    }
+    const float bound = reached_by(most, a.top_k);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    n = collect<T, W>(row, begin, end, group, entry + (in_group > 0), bound, own, hits[wave], keys[wave]);
+    if (n > kBuffer) {
+      // Too many: all chunks once more.
+      Best best;
+      best.init(a.top_k, keys[wave]);
+      best.bound(bound);
+      u32x4(*copy)[4] = reinterpret_cast<u32x4(*)[4]>(own);
+      for (i = begin + wave; i < end; i += W) {
+        row.load(c, i);
+        const f32x4 tops = tops_of(c);
+        const float top = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(max_wave(lane_top_of(tops)))));
+        const bool last = i + W >= end;
+        if (top >= best.above || (last && best.merged)) offer_chunk(c, tops, row, i, last, best, copy);
+      }
+      n = best.finish();
+    }
   }
+  if (lane == 0) counts[wave] = n;
   __syncthreads();
 #pragma unroll 1
   for (int w = 0; w < W; ++w)
