@@ -16,9 +16,9 @@
 // F apart and takes exact differences.
 //
 // Alternatives cost the loop over the chunks next to nothing: every lane leaves
-// the maximum of its elements of each chunk in LDS.  At the end 256 maxima of
-// disjoint parts of the row give a value that at least top_k of them reach (and
-// few elements more: 21 to be expected for 20, 74 for 64), the lanes' maxima
+// the maximum of its elements of each chunk in LDS.  At the end 64 or 256
+// maxima of disjoint parts of the row give a value that at least top_k of them
+// reach (and few elements more: 24 to be expected for 20), the lanes' maxima
 // that reach it name the words to read again, and what reaches it there leaves
 // a key (order of the value, then the lower token).  The keys are ranked by
 // counting the larger ones.  Where too many elements share the last value, as
@@ -76,7 +76,12 @@ template <int J, typename V>
 __device__ __forceinline__ V stage(V v, bool down) {
   const V o = xor_lane<J>(v);
   const bool keep_large = ((threadIdx.x & J) == 0) == down;
-  return (v > o) == keep_large ? v : o;
+  if constexpr (sizeof(V) == 4) {
+    const V large = max(v, o), small = min(v, o);
+    return keep_large ? large : small;
+  } else {
+    return (v > o) == keep_large ? v : o;
+  }
 }
 template <int J, typename V>
 __device__ __forceinline__ V merge_stages(V v, bool down) {
@@ -441,19 +446,26 @@ __device__ __forceinline__ uint64_t* partial_keys(const LogprobsArgs& a, int64_t
   return reinterpret_cast<uint64_t*>(static_cast<f32x4*>(a.part) + blocks);
 }
 
-// The k-th largest of four values of every lane, rounded towards -inf to 16
-// bits (every step waits for the one before); kLowest where fewer than k are not masked.
+// A value that at least k of four values of every lane reach; kLowest where
+// fewer are not masked.
 __device__ __forceinline__ float reached_by(const f32x4& v, int k) {
   uint32_t o[4], t = 0;
 #pragma unroll
   for (int q = 0; q < 4; ++q) o[q] = order_of(v[q]);
+  if (k <= 32) {
+    // The k-th largest of the lanes' largest: 800 cycles.
+    t = __builtin_amdgcn_readlane(sort_wave(max(max(o[0], o[1]), max(o[2], o[3]))), k - 1);
+  } else {
+    // The k-th largest of all to 16 bits, each step of which waits for the one
+    // before: 2000 cycles, for 85 elements instead of 260 with k = 64.
 #pragma unroll
-  for (int b = 31; b >= 16; --b) {
-    const uint32_t c = t | (1u << b);
-    int n = 0;
+    for (int b = 31; b >= 16; --b) {
+      const uint32_t c = t | (1u << b);
+      int n = 0;
 #pragma unroll
-    for (int q = 0; q < 4; ++q) n += __popcll(__ballot(o[q] >= c));
-    if (n >= k) t = c;
+      for (int q = 0; q < 4; ++q) n += __popcll(__ballot(o[q] >= c));
+      if (n >= k) t = c;
+    }
   }
   return t < order_of(kLowest) ? kLowest : value_of(uint64_t(t) << 32);
 }
@@ -638,9 +650,9 @@ __global__ __launch_bounds__(64 * W) void logprobs_kernel(LogprobsArgs a, int sp
   }
 }
 
-// A row's partial results: lane i takes split i's sums; of the splits' sorted
-// keys those that can be among the best (by the same bound as above, with
-// splits in the place of wavefronts) are ranked.
+// A row's partial results: lane i takes split i's sums.  The lanes share the
+// splits, whose keys are sorted, and the k-th largest of their 64 first keys is
+// the bound for the others; what reaches it is ranked.
 template <typename T, bool TOP>
 __global__ __launch_bounds__(256) void join_kernel(LogprobsArgs a, int splits) {
   __shared__ __attribute__((aligned(16))) uint64_t keys[TOP ? kLogprobsMaxSplits * kLogprobsMaxTop : 2];
@@ -651,14 +663,14 @@ __global__ __launch_bounds__(256) void join_kernel(LogprobsArgs a, int splits) {
   const uint64_t* src = partial_keys(a, int64_t(a.rows) * splits) + base * a.top_k;
   // Every load that depends on none other first.
   Sums sums{kLowest, 0.0f, 0.0f, 0.0f};
-  uint32_t share = ~0u, whole = 0;  // the keys' orders
   if (lane < splits) {
     const f32x4 v = static_cast<const f32x4*>(a.part)[base + lane];
     sums = Sums{v[0], v[1], v[2], v[3]};
-    if constexpr (TOP) {
-      share = uint32_t(src[lane * a.top_k + (a.top_k + splits - 1) / splits - 1] >> 32);
-      whole = uint32_t(src[lane * a.top_k + a.top_k - 1] >> 32);
-    }
+  }
+  uint32_t first = 0;  // its order
+  if constexpr (TOP) {
+    const int share = 64 / splits, from = lane % share;  // lanes a split
+    if (lane / share < splits && from < a.top_k) first = uint32_t(src[lane / share * a.top_k + from] >> 32);
   }
   constexpr int kAhead = 4;
   uint64_t mine[kAhead];
@@ -671,9 +683,8 @@ __global__ __launch_bounds__(256) void join_kernel(LogprobsArgs a, int splits) {
   if (wave == 0) given.load(a, static_cast<const T*>(nullptr), r, lane);
   if constexpr (TOP) {
     if (threadIdx.x == 0) count = 0;
-    share = reduce_wave(share, [](uint32_t x, uint32_t y) { return min(x, y); });
-    whole = reduce_wave(whole, [](uint32_t x, uint32_t y) { return max(x, y); });
-    const uint64_t bound = uint64_t(max(max(share, whole), 1u)) << 32;
+    const uint32_t kth = __builtin_amdgcn_readlane(sort_wave(first), a.top_k - 1);
+    const uint64_t bound = uint64_t(max(kth, 1u)) << 32;  // no key is 0
     __syncthreads();
 #pragma unroll
     for (int q = 0; q < kAhead; ++q)
