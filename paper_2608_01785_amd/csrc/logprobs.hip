@@ -534,7 +534,7 @@ __device__ __forceinline__ int collect(const Row<T>& row, int begin, int end, in
 
 // Block (row, split): W wavefronts take the split's chunks in turn.
 template <typename T, int W, bool TOP>
-__global__ __launch_bounds__(64 * W) void logprobs_kernel(LogprobsArgs a, int splits, int chunks_per_split) {
+__global__ __launch_bounds__(64 * W) void logprobs_kernel(LogprobsArgs a, int splits) {
   constexpr int kOwn = kPeaks<W> / W;  // a wavefront's entries
   static_assert(kOwn * 64 * sizeof(float) >= 64 * 4 * sizeof(u32x4), "the second look's copy of a chunk takes their place");
   __shared__ __attribute__((aligned(16))) uint64_t keys[TOP ? W : 1][kBuffer];
@@ -547,7 +547,7 @@ __global__ __launch_bounds__(64 * W) void logprobs_kernel(LogprobsArgs a, int sp
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int r = int(blockIdx.x / splits), split = int(blockIdx.x % splits);
   const Row<T> row(a, r);
-  const int begin = split * chunks_per_split, end = min(row.chunks, begin + chunks_per_split);
+  const int begin = int(int64_t(row.chunks) * split / splits), end = int(int64_t(row.chunks) * (split + 1) / splits);
 
   Running run;
   Given given;
@@ -592,7 +592,9 @@ __global__ __launch_bounds__(64 * W) void logprobs_kernel(LogprobsArgs a, int sp
     if constexpr (W > 1) {
       pool[threadIdx.x] = most[0];
       __syncthreads();
-      most = *reinterpret_cast<const f32x4*>(pool + 4 * lane);
+      // One wavefront with a chunk is enough for 64 lanes' values.
+#pragma unroll
+      for (int w = 0; w < W; ++w) most[w] = pool[w * 64 + lane];
     }
     const float bound = reached_by(most, a.top_k);
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -716,9 +718,9 @@ hipError_t launch(const LogprobsArgs& a, int cus, hipStream_t s) {
   const LogprobsShape p = logprobs_shape(a.rows, a.vocab, sizeof(T), cus);
   const unsigned grid = unsigned(a.rows) * unsigned(p.splits);
   if (p.waves == 1)
-    hipLaunchKernelGGL((logprobs_kernel<T, 1, TOP>), dim3(grid), dim3(64), 0, s, a, p.splits, p.chunks_per_split);
+    hipLaunchKernelGGL((logprobs_kernel<T, 1, TOP>), dim3(grid), dim3(64), 0, s, a, p.splits);
   else
-    hipLaunchKernelGGL((logprobs_kernel<T, 4, TOP>), dim3(grid), dim3(256), 0, s, a, p.splits, p.chunks_per_split);
+    hipLaunchKernelGGL((logprobs_kernel<T, 4, TOP>), dim3(grid), dim3(256), 0, s, a, p.splits);
   if (p.splits > 1) hipLaunchKernelGGL((join_kernel<T, TOP>), dim3(a.rows), dim3(256), 0, s, a, p.splits);
   return hipGetLastError();
 }
