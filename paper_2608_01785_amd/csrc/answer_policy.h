@@ -23,34 +23,43 @@ enum LinearI8Choice { kLinearI8Few32, kLinearI8Few64, kLinearI8Tile64, kLinearI8
 // 3584 x 18944 18, 43; 65536 x 4096 65, 55.  128 rows: 1024 x 4096 7.5, 12; 3584 x
 // 18944 26, 45; 14336 x 4096 34, 19.
 //
-// A CU's time in tiles is the tiles it gets times a tile's 64-byte steps.  128 x
-// 128 tiles side by side on a CU take as long as one after the other; 64 x 64
-// ones hide their latency behind each other; a 256 x 256 step takes longer the
-// more of the chip works, whose clock follows the power.  4096 x 8192 x 8192: 235
-// in 256s, 323 in 128s, 477 in 64s; 777 x 4096 x 4096: 45, 26, 31; 256 x 4608 x
-// 3584: 38, 20, 16.  The constants are those of 256 CUs; memory's rate is taken
-// to be shared by them.
+// A CU's time in tiles is the tiles it gets times a tile's 64-byte steps.  64 x
+// 64 tiles, four on a CU at a time, hide their latency behind each other; of
+// 128 x 128 tiles it runs two, which take little less than one after the other;
+// a 256 x 256 step takes longer the more of the chip works, whose clock follows
+// the power.  4096 x 8192 x 8192: 235 in 256s, 323 in 128s, 477 in 64s; 777 x
+// 4096 x 4096: 44, 24, 30; 256 x 4608 x 3584: 39, 20, 17.  Over 84 products of 96
+// to 2048 rows the rule loses 0.2 % against the fastest.  The constants are those
+// of 256 CUs; memory's rate is taken to be shared by them.
 inline LinearI8Choice linear_i8_choice(int m, int n, int k, int cus) {
   auto up = [](int64_t a, int64_t b) { return (a + b - 1) / b; };
   auto larger = [](float a, float b) { return a > b ? a : b; };
   const float steps = float(up(k, 256)) * 4.0f, kf = float(k), w_bytes = float(n) * kf / float(cus);
-  const int64_t tiles64 = up(m, 64) * up(n, 64);
-  const float r64 = float(up(tiles64, cus)), slots64 = float(tiles64) / float(4 * cus);
-  // Four 64 x 64 tiles run on a CU at a time; a part of a round more stretches
-  // the time of the channels' stream.
+  const float fcus = float(cus);
+  const int64_t tiles64 = up(m, 64) * up(n, 64), full64 = tiles64 / (4 * cus);
+  const float rest64 = float(up(tiles64 - full64 * 4 * cus, cus)), slots64 = float(tiles64) / (4.0f * fcus);
+  // A part of a round more stretches the time of the channels' stream.
   const float stretch = slots64 > 1.0f ? 0.5f + 0.5f * float(up(tiles64, 4 * cus)) / slots64 : 1.0f;
+  float work64 = 2.5f + float(full64) * (0.44f * steps + 3.0f);
+  if (rest64 > 0.0f) work64 += steps * larger(0.145f, 0.11f * rest64) + 0.75f * rest64 + (full64 > 0 ? 1.0f : 0.0f);
 
   LinearI8Choice best = kLinearI8Tile64;
-  float cost = larger(2.5f + steps * larger(0.145f, 0.12f * r64) + 0.6f * r64, 3.0f + stretch * w_bytes / 20700.0f);
+  float cost = larger(work64, 3.0f + stretch * w_bytes / 20700.0f);
   auto offer = [&](LinearI8Choice c, float t) {
     if (t < cost) {
       cost = t;
       best = c;
     }
   };
-  offer(kLinearI8Tile128, larger(3.0f + float(up(up(m, 128) * up(n, 128), cus)) * (0.305f * steps + 1.3f),
-                                 3.0f + w_bytes / 16500.0f));
-  // The 256s end in halves (see linear_kernel).
+  // Tiles of both kinds: a last row of them that holds at most half its rows
+  // costs half.
+  const int64_t tm128 = up(m, 128), tn128 = up(n, 128);
+  const bool short128 = m - (tm128 - 1) * 128 <= 64;
+  const float rounds128 = (float(tm128) - (short128 ? 0.5f : 0.0f)) * float(tn128) / fcus;
+  const float pairs = float(int64_t(0.5f * rounds128)), rest128 = rounds128 - 2.0f * pairs;
+  const float work128 = 3.0f + pairs * (0.6f * steps + 2.5f) +
+                        (rest128 > 1.0f ? 0.5f * steps + 4.0f : rest128 > 0.0f ? 0.305f * steps + 3.5f : 0.0f);
+  offer(kLinearI8Tile128, larger(work128, 3.0f + w_bytes / 16500.0f));
   const int64_t tm = up(m, 256), tn = up(n, 256);
   const bool short_last = m - (tm - 1) * 256 <= 128;
   const int64_t whole = (short_last ? tm - 1 : tm) * tn, halves = short_last ? tn : 0;
@@ -66,10 +75,10 @@ inline LinearI8Choice linear_i8_choice(int m, int n, int k, int cus) {
   offer(kLinearI8Tile256, larger(6.0f + units * ((0.45f + 0.38f * float(grid) / float(cus)) * steps + 8.0f),
                                  3.0f + w_bytes / 19500.0f));
   const int64_t few = up(n, 32);
-  if (m > 32) {
+  if (m > 32 && up(m, 64) <= 65535) {  // row groups are the grid's second dimension
     const float rounds = float(up(few * up(m, 64), cus));
     offer(kLinearI8Few64, larger(1.7f + rounds * (0.0012f * kf + 2.0f), 2.0f + 0.0021f * kf * float(few) / float(cus)));
-  } else {
+  } else if (m <= 32) {
     offer(kLinearI8Few32, 3.0f + larger(0.0008f * kf, w_bytes / 17000.0f));
   }
   return best;

@@ -136,7 +136,7 @@ __device__ __forceinline__ void store_run(T* p, int h, const float (&lo)[4], con
 //   Otherwise (k >= 16): byte addresses, rows past the last read it again (they
 //   are never stored).  The chunk that holds the end of k is read from 16 bytes
 //   before that end, chunks past it from the row's start, and settle() shifts
-//   and clears them on their way to LDS, so that no load waits for another.
+//   and clears them once they are there, so that no load waits for another.
 template <bool ALIGNED, int C, int L>
 struct Operand {
   static constexpr int kRows = 64 / C, kBytes = 16 * C;  // of a load, and of a row in a stage
@@ -174,12 +174,13 @@ struct Operand {
       return v;
     }
   }
+  // Whether a stage's chunks need settle().
+  __device__ __forceinline__ static bool ends(int stage, int k) { return !ALIGNED && stage >= k / kBytes; }
   // The chunk as its stage holds it, from what load() brought.
   __device__ __forceinline__ u32x4 settle(u32x4 v, int stage, int k) const {
     if constexpr (ALIGNED) {
       return v;
     } else {
-      if (stage < k / kBytes) return v;
       const int n = k - stage * kBytes - int(threadIdx.x % C) * 16;  // bytes of the chunk that k holds
       if (n <= 0) return u32x4{0, 0, 0, 0};
       if (n >= 16) return v;
@@ -293,9 +294,17 @@ __global__ __launch_bounds__(WN * WM * 64, WN * WM == 8 ? 1 : NS * MT == 1 ? 4 :
   const uint32_t put_at = (w_wave ? 0u : uint32_t(kTile)) + uint32_t(put_row * BK);
   const uint32_t put_chunk[2] = {uint32_t(phys<C>(put_row, lane % C) * 16),
                                  uint32_t(phys<C>(put_row + kLoadRows, lane % C) * 16)};
-  auto put = [&](int buf, int slot, int l, int stage) {
+  auto put = [&](int buf, int l, const u32x4& v) {
     *reinterpret_cast<u32x4*>(smem + buf * kStage + l * kLoadRows * BK + put_at +
-                              put_chunk[kLoadRows < 16 ? l & 1 : 0]) = op.settle(ring[slot][l], stage, a.k);
+                              put_chunk[kLoadRows < 16 ? l & 1 : 0]) = v;
+  };
+  // Over what put() wrote of a stage that holds the end of k: one branch a
+  // stage (with one for every chunk 777 x 5001 x 2047 took 34 us, not 31).
+  auto put_end = [&](int buf, int slot, int stage) {
+    if (op.ends(stage, a.k)) {
+#pragma unroll
+      for (int l = 0; l < L; ++l) put(buf, l, op.settle(ring[slot][l], stage, a.k));
+    }
   };
   struct Frag {
     u32x4 w[NS], a[MT];
@@ -329,7 +338,8 @@ __global__ __launch_bounds__(WN * WM * 64, WN * WM == 8 ? 1 : NS * MT == 1 ? 4 :
 #pragma unroll
     for (int l = 0; l < L; ++l) ring[t][l] = op.load(l, turned(t, turn), ld, a.k);
 #pragma unroll
-  for (int l = 0; l < L; ++l) put(0, 0, l, turn);
+  for (int l = 0; l < L; ++l) put(0, l, ring[0][l]);
+  put_end(0, 0, turn);
   asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
@@ -375,8 +385,8 @@ __global__ __launch_bounds__(WN * WM * 64, WN * WM == 8 ? 1 : NS * MT == 1 ? 4 :
                 for (int x = q * NR / NM; x < (q + 1) * NR / NM; ++x) read(jt, buf, kk + 1, x, f[(kk + 1) & 1]);
                 if (slot < kPutEnd) {
 #pragma unroll
-                  for (int x = slot * L / kPutEnd; x < (slot + 1) * L / kPutEnd; ++x) 
-                    put(1 - buf, (u + 1) % kUnroll, x, u + 1 < kUnroll || !last ? turned(kt + u + 1, turn) : next_turn);
+                  for (int x = slot * L / kPutEnd; x < (slot + 1) * L / kPutEnd; ++x)
+                    put(1 - buf, x, ring[(u + 1) % kUnroll][x]);
                 }
               } else if (u + 1 < kUnroll || !last) {
 #pragma unroll
@@ -392,6 +402,8 @@ __global__ __launch_bounds__(WN * WM * 64, WN * WM == 8 ? 1 : NS * MT == 1 ? 4 :
               __builtin_amdgcn_sched_barrier(0);
             }
             if (kk + 2 == kSteps) {
+              put_end(1 - buf, (u + 1) % kUnroll,
+                      u + 1 < kUnroll || !last ? turned(kt + u + 1, turn) : next_turn);
               asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
               __builtin_amdgcn_s_barrier();
               asm volatile("" ::: "memory");
@@ -498,13 +510,19 @@ __global__ __launch_bounds__(kFewWaves * 64, MT == 1 && ALIGNED ? 4 : 2) void fe
 #pragma unroll
     for (int d = 0; d < D; ++d) {
       const int stage = stage_of(i + d);
+      auto put = [&](int l, const u32x4& v) {
+        *reinterpret_cast<u32x4*>(image + l * 8 * kRow + ((l & 1) ? put_odd : put_off)) = v;
+      };
+      if (wop.ends(stage, a.k)) {
 #pragma unroll
-      for (int l = 0; l < 4; ++l)
-        *reinterpret_cast<u32x4*>(image + l * 8 * kRow + ((l & 1) ? put_odd : put_off)) = wop.settle(w[d][l], stage, a.k);
+        for (int l = 0; l < 4; ++l) w[d][l] = wop.settle(w[d][l], stage, a.k);
 #pragma unroll
-      for (int l = 0; l < 4 * MT; ++l)
-        *reinterpret_cast<u32x4*>(image + (4 + l) * 8 * kRow + ((l & 1) ? put_odd : put_off)) =
-            aop.settle(x[d][l], stage, a.k);
+        for (int l = 0; l < 4 * MT; ++l) x[d][l] = aop.settle(x[d][l], stage, a.k);
+      }
+#pragma unroll
+      for (int l = 0; l < 4; ++l) put(l, w[d][l]);
+#pragma unroll
+      for (int l = 0; l < 4 * MT; ++l) put(4 + l, x[d][l]);
       load(d, stage_of(i + d + D));  // zeros past the end of k
       // The image is this wave's alone, and LDS serves one wave in order.
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");

@@ -193,8 +193,8 @@ KERNELS = [(FEW32, 1, 2060, 1024, 256), (FEW32, 31, 1030, 2049, 256), (FEW32, 32
            (FEW64, 33, 130, 1024, 256), (FEW64, 65, 515, 2049, 256), (FEW64, 300, 515, 1040, 256),
            (FEW64, 128, 2060, 2055, 256), (FEW64, 200, 130, 2049, 64),
            (T64, 65, 4100, 1024, 256), (T64, 129, 2060, 255, 64), (T64, 777, 1030, 2049, 256),
-           (T128, 777, 4100, 1024, 256), (T128, 200, 2060, 1033, 64), (T128, 65, 4100, 2049, 64),
-           (T256, 390, 4100, 2049, 64), (T256, 1100, 2060, 2064, 64), (T256, 1100, 2060, 2049, 64)]
+           (T128, 777, 4100, 1024, 256), (T128, 200, 4100, 1033, 64), (T128, 390, 4100, 2049, 64),
+           (T256, 600, 4100, 2049, 64), (T256, 1100, 2060, 2064, 64), (T256, 1100, 2060, 2049, 64)]
 
 
 @pytest.mark.parametrize("case", KERNELS, ids=str)
