@@ -125,8 +125,8 @@ hs_status hs_linear_i8(hs_context* ctx, const void* a, int64_t lda, const float*
 
 // Which kernel hs_linear_i8 takes (see linear_i8_choice).  Internal to the library
 // and its tests (not declared in horizon.h).
-int32_t hs_linear_i8_kernel(int32_t m, int32_t n, int32_t k, int32_t cus) {
-  return hs::linear_i8_choice(m, n, k, cus);
+int32_t hs_linear_i8_kernel(int32_t m, int32_t n, int32_t k, int32_t cus, int32_t aligned) {
+  return hs::linear_i8_choice(m, n, k, cus, aligned != 0);
 }
 
 hs_status hs_logprobs_workspace_size(int32_t max_rows, int32_t vocab, int32_t top_k, size_t* bytes) {

@@ -31,17 +31,22 @@ enum LinearI8Choice { kLinearI8Few32, kLinearI8Few64, kLinearI8Tile64, kLinearI8
 // 4096 x 4096: 44, 24, 30; 256 x 4608 x 3584: 39, 20, 17.  Over 84 products of 96
 // to 2048 rows the rule loses 0.2 % against the fastest.  The constants are those
 // of 256 CUs; memory's rate is taken to be shared by them.
-inline LinearI8Choice linear_i8_choice(int m, int n, int k, int cus) {
+//
+// Rows that are not 16-byte aligned cost the address unit twice as much a load,
+// which the kernels that use a load least feel most: 512 x 4608 x 3583 40 in 64s
+// and 29 in 128s (22 and 21 aligned), 64 x 1024 x 1023 11 for few rows and 8 in
+// 64s (6.5 and 7 aligned).  256s have no registers for their addresses.
+inline LinearI8Choice linear_i8_choice(int m, int n, int k, int cus, bool aligned) {
   auto up = [](int64_t a, int64_t b) { return (a + b - 1) / b; };
   auto larger = [](float a, float b) { return a > b ? a : b; };
-  const float steps = float(up(k, 256)) * 4.0f, kf = float(k), w_bytes = float(n) * kf / float(cus);
-  const float fcus = float(cus);
+  const float steps = float(up(k, 256)) * 4.0f, kf = float(k), fcus = float(cus), w_bytes = float(n) * kf / fcus;
   const int64_t tiles64 = up(m, 64) * up(n, 64), full64 = tiles64 / (4 * cus);
   const float rest64 = float(up(tiles64 - full64 * 4 * cus, cus)), slots64 = float(tiles64) / (4.0f * fcus);
   // A part of a round more stretches the time of the channels' stream.
   const float stretch = slots64 > 1.0f ? 0.5f + 0.5f * float(up(tiles64, 4 * cus)) / slots64 : 1.0f;
-  float work64 = 2.5f + float(full64) * (0.44f * steps + 3.0f);
-  if (rest64 > 0.0f) work64 += steps * larger(0.145f, 0.11f * rest64) + 0.75f * rest64 + (full64 > 0 ? 1.0f : 0.0f);
+  const float each64 = aligned ? 0.11f : 0.21f, alone64 = aligned ? 0.145f : 0.2f;
+  float work64 = 2.5f + float(full64) * (4.0f * each64 * steps + 3.0f);
+  if (rest64 > 0.0f) work64 += steps * larger(alone64, each64 * rest64) + 0.75f * rest64 + (full64 > 0 ? 1.0f : 0.0f);
 
   LinearI8Choice best = kLinearI8Tile64;
   float cost = larger(work64, 3.0f + stretch * w_bytes / 20700.0f);
@@ -57,8 +62,9 @@ inline LinearI8Choice linear_i8_choice(int m, int n, int k, int cus) {
   const bool short128 = m - (tm128 - 1) * 128 <= 64;
   const float rounds128 = (float(tm128) - (short128 ? 0.5f : 0.0f)) * float(tn128) / fcus;
   const float pairs = float(int64_t(0.5f * rounds128)), rest128 = rounds128 - 2.0f * pairs;
-  const float work128 = 3.0f + pairs * (0.6f * steps + 2.5f) +
-                        (rest128 > 1.0f ? 0.5f * steps + 4.0f : rest128 > 0.0f ? 0.305f * steps + 3.5f : 0.0f);
+  const float step128 = aligned ? steps : 1.4f * steps;
+  const float work128 = 3.0f + pairs * (0.6f * step128 + 2.5f) +
+                        (rest128 > 1.0f ? 0.5f * step128 + 4.0f : rest128 > 0.0f ? 0.305f * step128 + 3.5f : 0.0f);
   offer(kLinearI8Tile128, larger(work128, 3.0f + w_bytes / 16500.0f));
   const int64_t tm = up(m, 256), tn = up(n, 256);
   const bool short_last = m - (tm - 1) * 256 <= 128;
@@ -72,14 +78,17 @@ inline LinearI8Choice linear_i8_choice(int m, int n, int k, int cus) {
     const int64_t rest = halves - (tail > 0 ? grid - tail : 0);
     units += rest > 0 ? 0.6f * float(up(rest, grid)) : 0.0f;
   }
-  offer(kLinearI8Tile256, larger(6.0f + units * ((0.45f + 0.38f * float(grid) / float(cus)) * steps + 8.0f),
-                                 3.0f + w_bytes / 19500.0f));
+  if (aligned)
+    offer(kLinearI8Tile256, larger(6.0f + units * ((0.45f + 0.38f * float(grid) / fcus) * steps + 8.0f),
+                                   3.0f + w_bytes / 19500.0f));
   const int64_t few = up(n, 32);
+  const float load = aligned ? 1.0f : 2.0f;
   if (m > 32 && up(m, 64) <= 65535) {  // row groups are the grid's second dimension
     const float rounds = float(up(few * up(m, 64), cus));
-    offer(kLinearI8Few64, larger(1.7f + rounds * (0.0012f * kf + 2.0f), 2.0f + 0.0021f * kf * float(few) / float(cus)));
+    offer(kLinearI8Few64, larger(1.7f + rounds * load * (0.0012f * kf + 2.0f),
+                                 2.0f + load * 0.0021f * kf * float(few) / fcus));
   } else if (m <= 32) {
-    offer(kLinearI8Few32, 3.0f + larger(0.0008f * kf, w_bytes / 17000.0f));
+    offer(kLinearI8Few32, 3.0f + load * larger(0.0008f * kf, w_bytes / 17000.0f));
   }
   return best;
 }

@@ -609,10 +609,8 @@ hipError_t launch_choice(const LinearI8Args& a, int choice, int cus, hipStream_t
     case kLinearI8Tile64: return launch_tiles<TYPE, ALIGNED, 8, 4, 2, 2, 1, 1>(a, 4 * cus, s);
     case kLinearI8Tile128: return launch_tiles<TYPE, ALIGNED, 8, 2, 2, 2, 2, 2>(a, 2 * cus, s);
     default:
-      if constexpr (ALIGNED)
-        return launch_tiles<TYPE, ALIGNED, 8, 2, 2, 4, 4, 2>(a, cus, s);
-      else
-        return launch_tiles<TYPE, ALIGNED, 8, 2, 2, 2, 2, 2>(a, 2 * cus, s);
+      if constexpr (ALIGNED) return launch_tiles<TYPE, ALIGNED, 8, 2, 2, 4, 4, 2>(a, cus, s);
+      return hipErrorInvalidValue;
   }
 }
 
@@ -620,7 +618,7 @@ template <int TYPE>
 hipError_t launch_type(const LinearI8Args& a, int cus, hipStream_t s) {
   const uintptr_t in = reinterpret_cast<uintptr_t>(a.a) | reinterpret_cast<uintptr_t>(a.w) | uintptr_t(a.lda) |
                        uintptr_t(a.ldw) | uintptr_t(a.k);
-  const int choice = linear_i8_choice(a.m, a.n, a.k, cus);
+  const int choice = linear_i8_choice(a.m, a.n, a.k, cus, in % 16 == 0);
   if (in % 16 == 0) return launch_choice<TYPE, true>(a, choice, cus, s);
   if (a.k >= 16) return launch_choice<TYPE, false>(a, choice, cus, s);
   const int64_t blocks = (int64_t(a.m) * a.n + 255) / 256;

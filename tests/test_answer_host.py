@@ -161,13 +161,19 @@ def test_binding_refuses_tensors_that_do_not_fit(b):
 
 def test_linear_kernel_rule(b):
     """Few rows, then larger tiles as there is more to do; what every kernel's GPU test relies on."""
-    kernel = b.lib().hs_linear_i8_kernel
+    def kernel(m, n, k, cus=256, aligned=True):
+        return b.lib().hs_linear_i8_kernel(m, n, k, cus, aligned)
     few32, few64, t64, t128, t256 = range(5)
-    assert kernel(1, 4608, 3584, 256) == few32 and kernel(32, 3584, 18944, 256) == few32
-    assert kernel(64, 4608, 3584, 256) == few64 and kernel(128, 3584, 18944, 256) == few64
-    assert kernel(128, 14336, 4096, 256) == t64
-    assert kernel(777, 4096, 4096, 256) == t128
-    assert kernel(4096, 8192, 8192, 256) == t256 and kernel(10515, 37888, 3584, 256) == t256
+    assert kernel(1, 4608, 3584) == few32 and kernel(32, 3584, 18944) == few32
+    assert kernel(64, 4096, 4096) == few64 and kernel(128, 3584, 18944) == few64
+    assert kernel(128, 14336, 4096) == t64
+    assert kernel(777, 4096, 4096) == t128
+    assert kernel(4096, 8192, 8192) == t256 and kernel(10515, 37888, 3584) == t256
+    assert kernel(4096, 8192, 8192, aligned=False) == t128
+    assert kernel(64, 1024, 1023) == few64 and kernel(64, 1024, 1023, aligned=False) == t64
     for m, n, k in ((1, 1, 1), (1, 1, 131071), (2 ** 20, 2 ** 20, 1), (2 ** 31 - 1, 1, 16), (1, 2 ** 31 - 1, 16)):
         for cus in (1, 64, 256):
-            assert few32 <= kernel(m, n, k, cus) <= t256
+            for aligned in (False, True):
+                assert few32 <= kernel(m, n, k, cus, aligned) <= (t256 if aligned else t128)
+    # The few rows' groups are a grid's second dimension, which ends at 65535.
+    assert kernel(2 ** 23, 32, 8192) != few64 and kernel(2 ** 23, 32, 8192, aligned=False) != few64
