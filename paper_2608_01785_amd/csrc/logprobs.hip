@@ -54,13 +54,6 @@ __device__ __forceinline__ void rescale(Sums& a, float m) {
   a.m = m;
 }
 
-__device__ __forceinline__ Sums join(Sums a, Sums b) {
-  const float m = fmaxf(a.m, b.m);
-  rescale(a, m);
-  rescale(b, m);
-  return Sums{m, a.s + b.s, a.f + b.f, a.t + b.t};
-}
-
 // ---------------------------------------------------------------- lanes
 
 __device__ __forceinline__ float max_wave(float v) {
@@ -246,6 +239,25 @@ struct Chunk {
         return __uint_as_float((e & 1) ? w & 0xffff0000u : w << 16);
       else
         return h2f(uint16_t((e & 1) ? w >> 16 : w & 0xffffu));
+    }
+  }
+  // Element j of the lane, whose j is its own: registers cannot be indexed.
+  __device__ __forceinline__ float pick(int j) const {
+    const int w = sizeof(T) == 4 ? j : j >> 1;
+    auto of_load = [&](const u32x4& v) {
+      const uint32_t lo = (w & 1) ? v[1] : v[0], hi = (w & 1) ? v[3] : v[2];
+      return (w & 2) ? hi : lo;
+    };
+    const uint32_t lo = (w & 4) ? of_load(raw[1]) : of_load(raw[0]), hi = (w & 4) ? of_load(raw[3]) : of_load(raw[2]);
+    const uint32_t v = (w & 8) ? hi : lo;
+    if constexpr (sizeof(T) == 4) {
+      return __uint_as_float(v);
+    } else {
+      const uint32_t half = (j & 1) ? v >> 16 : v & 0xffffu;
+      if constexpr (__is_same(T, uint16_t))
+        return __uint_as_float(half << 16);
+      else
+        return h2f(uint16_t(half));
     }
   }
   // `p`: the row's 16-byte aligned origin; all of chunk c lies in the row.
@@ -506,24 +518,30 @@ __device__ __forceinline__ int collect(const Row<T>& row, int begin, int end, in
       const bool mine = hit >= 0 && c < end;
       const int64_t i0 = int64_t(c) * Chunk<T>::kSize + (hit & 63) * V;
       Chunk<T> words;
+      uint32_t inside = 0;  // elements that the row holds
 #pragma unroll
-      for (int l = 0; l < 4; ++l)
-        words.raw[l] = edge_word(row.p, mine ? i0 + l * 64 * V : row.last, row.first, row.last);
+      for (int l = 0; l < 4; ++l) {
+        const int64_t i = i0 + l * 64 * V;
+        words.raw[l] = u32x4{0, 0, 0, 0};
+        if (mine && i + V > row.first && i < row.last) {
+          words.raw[l] = *reinterpret_cast<const u32x4*>(row.p + i);
+          const int lo = int(max(row.first - i, int64_t(0))), hi = int(min(row.last - i, int64_t(V)));
+          inside |= ((1u << hi) - (1u << lo)) << (l * V);
+        }
+      }
       uint32_t which = 0;
 #pragma unroll
       for (int l = 0; l < 4; ++l)
 #pragma unroll
         for (int e = 0; e < V; ++e) which |= uint32_t(words.get(l, e) >= bound) << (l * V + e);
-      // Nearly always one: read again, since registers cannot be indexed.
-      while (true) {
+      which &= inside;
+      while (true) {  // nearly always one
         const uint64_t mask = __ballot(which != 0);
         if (mask == 0) break;
         const int at = n + before(mask);
-        if (which && at < kBuffer) {
-          const int j = __builtin_ctz(which);
-          const int64_t i = i0 + (j / V) * 64 * V + j % V;
-          buf[at] = key_of(elem(row.p, i), uint32_t(i - row.first));
-        }
+        const int j = __builtin_ctz(which | 0x80000000u);
+        const float z = words.pick(j);
+        if (which && at < kBuffer) buf[at] = key_of(z, uint32_t(i0 + (j / V) * 64 * V + j % V - row.first));
         which &= which - 1;
         n += __popcll(mask);
       }
@@ -617,12 +635,19 @@ __global__ __launch_bounds__(64 * W) void logprobs_kernel(LogprobsArgs a, int sp
   }
   if (lane == 0) counts[wave] = n;
   __syncthreads();
-#pragma unroll 1
-  for (int w = 0; w < W; ++w)
-    if (w != wave) {
-      const f32x4 o = all_sums[w];
-      sums = join(sums, Sums{o[0], o[1], o[2], o[3]});
-    }
+  if constexpr (W > 1) {
+    // Lane l takes wavefront l % 4's.
+    const f32x4 o = all_sums[lane & 3];
+    sums = Sums{o[0], o[1], o[2], o[3]};
+    auto quad = [](float v, auto f) {
+      v = f(v, xor_lane<1>(v));
+      return f(v, xor_lane<2>(v));
+    };
+    auto add = [](float x, float y) { return x + y; };
+    const float m = quad(sums.m, [](float x, float y) { return fmaxf(x, y); });
+    rescale(sums, m);
+    sums = Sums{m, quad(sums.s, add), quad(sums.f, add), quad(sums.t, add)};
+  }
   const Answer answer(sums);
   if (wave == 0) {
     if (splits == 1)
@@ -641,12 +666,17 @@ __global__ __launch_bounds__(64 * W) void logprobs_kernel(LogprobsArgs a, int sp
     int total = 0;
 #pragma unroll
     for (int w = 0; w < W; ++w) total += counts[w];
-    for (int j = lane; j < n; j += 64) {
-      const uint64_t key = keys[wave][j];
-      int rank = 0;
-#pragma unroll 1
-      for (int w = 0; w < W; ++w) rank += rank_among(keys[w], counts[w], key);
-      if (rank < a.top_k) put(rank, key);
+    // W lanes rank a key, each among one wavefront's.
+    const int w = lane % W;
+    for (int j0 = 0; j0 < n; j0 += 64 / W) {
+      const int j = j0 + lane / W;
+      const uint64_t key = keys[wave][min(j, kBuffer - 1)];
+      int rank = j < n ? rank_among(keys[w], counts[w], key) : a.top_k;
+      if constexpr (W > 1) {
+        rank += xor_lane<1>(uint32_t(rank));
+        rank += xor_lane<2>(uint32_t(rank));
+      }
+      if (w == 0 && rank < a.top_k) put(rank, key);
     }
     if (wave == 0 && lane >= total && lane < a.top_k) put(lane, 0);
   }
