@@ -436,8 +436,9 @@ hs_status hs_dit_forward(hs_context* ctx, const hs_dit_cfg* cfg, const hs_dit_we
  *     synchronise, so they can be captured into a graph on the caller's
  *     stream.  The caller's current device is left as it was.
  *   - No rows: HS_OK, nothing is enqueued.  Outputs that overlap an input or
- *     each other, strides below the row length and misaligned pointers are
- *     HS_ERR_INVALID_ARG. */
+ *     each other, strides outside [row length, 2^30] and misaligned pointers are
+ *     HS_ERR_INVALID_ARG; more than 2^30 rows (2^25 of logits) are
+ *     HS_ERR_UNSUPPORTED. */
 enum { HS_TYPE_F32 = 0, HS_TYPE_BF16 = 1, HS_TYPE_F16 = 2 };
 
 /* Rows to 8-bit integers with one scale each:

@@ -10,6 +10,8 @@
 namespace {
 
 constexpr int64_t kMaxStride = int64_t(1) << 30;  // elements between rows: byte extents stay below 2^63
+constexpr int32_t kMaxRows = 1 << 30;             // rows plus a grid's stride stay below 2^31
+constexpr int32_t kLogprobsMaxRows = 1 << 25;     // a wavefront each: a grid holds fewer than 2^32 threads
 
 size_t type_size(int32_t type) { return type == HS_TYPE_F32 ? 4 : 2; }
 
@@ -28,6 +30,11 @@ struct Span {
 
 Span rows_of(const char* name, const void* p, int64_t rows, int64_t cols, int64_t ld, size_t size) {
   return {name, p, rows < 1 ? 0 : (uint64_t(rows - 1) * uint64_t(ld) + uint64_t(cols)) * size};
+}
+
+hs_status check_rows(int32_t rows, int32_t most) {
+  if (rows > most) return hs::fail(HS_ERR_UNSUPPORTED, "%d rows: at most %d", rows, most);
+  return HS_OK;
 }
 
 hs_status check_matrix(const Span& s, int64_t rows, int64_t cols, int64_t ld, size_t size) {
@@ -77,6 +84,7 @@ hs_status hs_quantize_rows(hs_context* ctx, const void* x, int32_t x_type, int64
   hs::clear_error();
   HS_TRY(check_type("x", x_type));
   if (rows < 0 || d < 1) return hs::fail(HS_ERR_INVALID_ARG, "shape [%d, %d]", rows, d);
+  HS_TRY(check_rows(rows, kMaxRows));
   const Span sx = rows_of("x", x, rows, d, ldx, type_size(x_type)), sq = rows_of("q", q, rows, d, ldq, 1);
   const Span ss = rows_of("scale", scale, rows, 1, 1, 4), sg = rows_of("gain", gain, 1, d, d, 2);
   HS_TRY(check_matrix(sx, rows, d, ldx, type_size(x_type)));
@@ -106,6 +114,8 @@ hs_status hs_linear_i8(hs_context* ctx, const void* a, int64_t lda, const float*
   if (lda > hs::kLinearI8MaxStride || ldw > hs::kLinearI8MaxStride)
     return hs::fail(HS_ERR_UNSUPPORTED, "row strides %lld and %lld: operands allow %lld", (long long)lda,
                     (long long)ldw, (long long)hs::kLinearI8MaxStride);
+  HS_TRY(check_rows(m, kMaxRows));
+  HS_TRY(check_rows(n, kMaxRows));
   const size_t osz = type_size(out_type);
   const Span sa = rows_of("a", a, m, k, lda, 1), sw = rows_of("w", w, n, k, ldw, 1);
   const Span sas = rows_of("a_scale", a_scale, m, 1, 1, 4), sws = rows_of("w_scale", w_scale, n, 1, 1, 4);
@@ -135,6 +145,7 @@ hs_status hs_logprobs_workspace_size(int32_t max_rows, int32_t vocab, int32_t to
   if (max_rows < 0 || vocab < 1) return hs::fail(HS_ERR_INVALID_ARG, "shape [%d, %d]", max_rows, vocab);
   if (top_k < 0 || top_k > hs::kLogprobsMaxTop)
     return hs::fail(HS_ERR_UNSUPPORTED, "top_k %d outside [0, %d]", top_k, hs::kLogprobsMaxTop);
+  HS_TRY(check_rows(max_rows, kLogprobsMaxRows));
   *bytes = hs::logprobs_workspace(max_rows, vocab, top_k);
   return HS_OK;
 }

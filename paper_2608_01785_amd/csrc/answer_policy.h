@@ -81,13 +81,16 @@ inline LinearI8Choice linear_i8_choice(int m, int n, int k, int cus, bool aligne
   if (aligned)
     offer(kLinearI8Tile256, larger(6.0f + units * ((0.45f + 0.38f * float(grid) / fcus) * steps + 8.0f),
                                    3.0f + w_bytes / 19500.0f));
+  // A grid's first dimension holds fewer than 2^32 threads, its second 65535
+  // row groups.
   const int64_t few = up(n, 32);
+  const bool fits = few < (1 << 23) && up(m, 64) <= 65535;
   const float load = aligned ? 1.0f : 2.0f;
-  if (m > 32 && up(m, 64) <= 65535) {  // row groups are the grid's second dimension
+  if (m > 32 && fits) {
     const float rounds = float(up(few * up(m, 64), cus));
     offer(kLinearI8Few64, larger(1.7f + rounds * load * (0.0012f * kf + 2.0f),
                                  2.0f + load * 0.0021f * kf * float(few) / fcus));
-  } else if (m <= 32) {
+  } else if (fits) {
     offer(kLinearI8Few32, 3.0f + load * larger(0.0008f * kf, w_bytes / 17000.0f));
   }
   return best;

@@ -175,5 +175,26 @@ def test_linear_kernel_rule(b):
         for cus in (1, 64, 256):
             for aligned in (False, True):
                 assert few32 <= kernel(m, n, k, cus, aligned) <= (t256 if aligned else t128)
+    assert kernel(1, 2 ** 30, 16) >= t64   # more blocks than a grid of the few rows' kernel holds
     # The few rows' groups are a grid's second dimension, which ends at 65535.
     assert kernel(2 ** 23, 32, 8192) != few64 and kernel(2 ** 23, 32, 8192, aligned=False) != few64
+
+
+def test_too_many_rows(b):
+    """Refused before anything is read: row counts beyond what the grids hold."""
+    lib, one = b.lib(), 4096
+    for rows, calls in ((2 ** 30 + 1, ("q", "m", "n")), (2 ** 25 + 1, ("l", "w"))):
+        for call in calls:
+            if call == "q":
+                st = lib.hs_quantize_rows(None, one, b.HS_TYPE_F32, 4, None, 1e-6, rows, 4, one, 4, one, 256, None)
+            elif call in "mn":
+                m, n = (rows, 4) if call == "m" else (4, rows)
+                st = lib.hs_linear_i8(None, one, 16, one, one, 16, one, None, one, b.HS_TYPE_F32, 2 ** 30, m, n, 16, 256,
+                                      None)
+            elif call == "l":
+                st = lib.hs_logprobs(None, one, b.HS_TYPE_F32, 4, rows, 4, None, 0, None, one, 0, None, None, 256, None,
+                                     None, 0)
+            else:
+                st = lib.hs_logprobs_workspace_size(rows, 4, 0, ctypes.byref(ctypes.c_size_t(0)))
+            assert st == b.HS_ERR_UNSUPPORTED, (call, st)
+            assert b"rows" in lib.hs_last_error()
