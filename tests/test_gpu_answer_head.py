@@ -12,7 +12,7 @@ import pytest
 
 from oracle import answer as A
 from tests.gpu_common import log, require_gpu
-from tests.test_gpu_answer import _check_linear, _gen, _linear, _np, _quantize, _t, _view
+from tests.test_gpu_answer import _check_linear, _gen, _linear, _logprobs, _np, _quantize, _t, _view
 from tests.test_gpu_algorithm1 import LADDER, _loop
 
 pytestmark = pytest.mark.gpu
@@ -233,6 +233,31 @@ def test_product_lengths(env, k, m):
         _, av = _view(torch, a, pad, shift, fill=99)
         _, wv = _view(torch, w, pad, shift, fill=-99)
         _check_linear(env, av, sa, wv, sw, "f32")
+
+
+# ---------------------------------------------------------------------------- long rows, many of them
+
+@pytest.mark.parametrize("rows,vocab,cus", [(64, 160001, 64), (512, 40000, 64), (3, 700001, 64)])
+@pytest.mark.parametrize("top", [1, 20, 64])
+def test_alternatives_of_more_chunks_than_a_block_keeps_apart(env, rows, vocab, cus, top):
+    """Rows whole in a block of four wavefronts, in one, and split: maxima of several chunks in one place."""
+    torch, b, ctx = env
+    g = _gen(torch, vocab + top)
+    z = torch.randn(rows, vocab, generator=g, device="cuda") * 3
+    z[1] = 1.25                                              # every logit the same
+    z[2] = torch.randint(0, 3, (vocab,), generator=g, device="cuda").float()   # a third of them the largest
+    if rows > 3:
+        z[3] = -float("inf")
+        z[3, vocab - 40:] = 2.0                              # fewer than 64 unmasked, all at the end
+        z[4, ::7] = 25.0                                     # ties above all others, spread out
+    got = _logprobs((torch, b, ctx), z, None, top, cus=cus)
+    rows_checked = list(range(min(rows, 8))) + ([rows - 1] if rows > 8 else [])
+    ref = A.logprobs(_np(z[rows_checked]), None, top)
+    np.testing.assert_array_equal(got["top_tokens"][rows_checked].cpu().numpy(), ref["top_tokens"])
+    # Every row against a sort by value and then token.
+    lo = torch.sort(z, dim=1, descending=True, stable=True)
+    want = torch.where(lo.values[:, :top].isinf(), -1, lo.indices[:, :top]).int()
+    assert torch.equal(got["top_tokens"], want)
 
 
 # ---------------------------------------------------------------------------- offsets beyond 32 bits
