@@ -42,14 +42,20 @@ inline LinearI8Choice linear_i8_choice(int m, int n, int k, int cus, bool aligne
   const float steps = float(up(k, 256)) * 4.0f, kf = float(k), fcus = float(cus), w_bytes = float(n) * kf / fcus;
   const int64_t tiles64 = up(m, 64) * up(n, 64), full64 = tiles64 / (4 * cus);
   const float rest64 = float(up(tiles64 - full64 * 4 * cus, cus)), slots64 = float(tiles64) / (4.0f * fcus);
-  // A part of a round more stretches the time of the channels' stream.
-  const float stretch = slots64 > 1.0f ? 0.5f + 0.5f * float(up(tiles64, 4 * cus)) / slots64 : 1.0f;
+  // The time of the channels' stream stretches where CUs get unequal numbers of
+  // tiles, by a part of what the largest number is above the mean.
+  auto stretch = [&](int64_t tiles, int64_t places, float part) {
+    return 1.0f + part * (float(up(tiles, places) * places) / float(tiles) - 1.0f);
+  };
   const float each64 = aligned ? 0.11f : 0.21f, alone64 = aligned ? 0.145f : 0.2f;
   float work64 = 2.5f + float(full64) * (4.0f * each64 * steps + 3.0f);
   if (rest64 > 0.0f) work64 += steps * larger(alone64, each64 * rest64) + 0.75f * rest64 + (full64 > 0 ? 1.0f : 0.0f);
 
   LinearI8Choice best = kLinearI8Tile64;
-  float cost = larger(work64, 3.0f + stretch * w_bytes / 20700.0f);
+  // Rows of a tile take from the rate of the channels' stream.
+  auto fill = [&](int tile, float part) { return 1.0f + part * float(m < tile ? m : tile); };
+  float cost = larger(work64, 3.0f + stretch(tiles64, slots64 > 1.0f ? 4 * cus : cus, slots64 > 1.0f ? 0.5f : 0.2f) *
+                                         fill(64, 0.003f) * w_bytes / 20700.0f);
   auto offer = [&](LinearI8Choice c, float t) {
     if (t < cost) {
       cost = t;
@@ -65,7 +71,8 @@ inline LinearI8Choice linear_i8_choice(int m, int n, int k, int cus, bool aligne
   const float step128 = aligned ? steps : 1.4f * steps;
   const float work128 = 3.0f + pairs * (0.6f * step128 + 2.5f) +
                         (rest128 > 1.0f ? 0.5f * step128 + 4.0f : rest128 > 0.0f ? 0.305f * step128 + 3.5f : 0.0f);
-  offer(kLinearI8Tile128, larger(work128, 3.0f + w_bytes / 16500.0f));
+  offer(kLinearI8Tile128, larger(work128, 3.0f + stretch(tm128 * tn128, cus, 0.45f) * fill(128, 0.0018f) *
+                                                     w_bytes / 20700.0f));
   const int64_t tm = up(m, 256), tn = up(n, 256);
   const bool short_last = m - (tm - 1) * 256 <= 128;
   const int64_t whole = (short_last ? tm - 1 : tm) * tn, halves = short_last ? tn : 0;
@@ -80,7 +87,7 @@ inline LinearI8Choice linear_i8_choice(int m, int n, int k, int cus, bool aligne
   }
   if (aligned)
     offer(kLinearI8Tile256, larger(6.0f + units * ((0.45f + 0.38f * float(grid) / fcus) * steps + 8.0f),
-                                   3.0f + w_bytes / 19500.0f));
+                                   3.0f + stretch(tm * tn, cus, 0.4f) * fill(128, 0.0012f) * w_bytes / 20000.0f));
   // A grid's first dimension holds fewer than 2^32 threads, its second 65535
   // row groups.
   const int64_t few = up(n, 32);
@@ -91,7 +98,7 @@ inline LinearI8Choice linear_i8_choice(int m, int n, int k, int cus, bool aligne
     offer(kLinearI8Few64, larger(1.7f + rounds * load * (0.0012f * kf + 2.0f),
                                  2.0f + load * 0.0021f * kf * float(few) / fcus));
   } else if (fits) {
-    offer(kLinearI8Few32, 3.0f + load * larger(0.0008f * kf, w_bytes / 17000.0f));
+    offer(kLinearI8Few32, 3.0f + load * larger(0.0008f * kf, fill(32, 0.008f) * w_bytes / 20700.0f));
   }
   return best;
 }
