@@ -10,7 +10,7 @@ constexpr int kLogprobsMaxTop = 64;       // alternatives a row can list: one pe
 constexpr int kLinearI8MaxK = 131071;     // (-128)^2 k stays below 2^31
 constexpr int64_t kLinearI8MaxStride = int64_t(1) << 22;  // 256 rows of an operand stay within 32-bit offsets
 
-// The kernels of hs_linear_i8: for few rows (32 at most, or 64 a block), and tiles.
+// The kernels of hs_linear_i8: for few rows (32 or 64 a block), and tiles.
 enum LinearI8Choice { kLinearI8Few32, kLinearI8Few64, kLinearI8Tile64, kLinearI8Tile128, kLinearI8Tile256 };
 
 // Which of them an [m, k] x [n, k]^T product takes on `cus` compute units.  All
@@ -21,7 +21,9 @@ enum LinearI8Choice { kLinearI8Few32, kLinearI8Few64, kLinearI8Tile64, kLinearI8
 // channels to fill the chip; the tiles have less to read and to add up once
 // there are many.  Few rows against the best tiles: 32 rows 4608 x 3584 6.5, 10.8;
 // 3584 x 18944 18, 43; 65536 x 4096 65, 55.  128 rows: 1024 x 4096 7.5, 12; 3584 x
-// 18944 26, 45; 14336 x 4096 34, 19.
+// 18944 26, 45; 14336 x 4096 34, 19.  32 rows a block where the blocks fit the
+// chip, 64 where that halves the rounds: 64 rows 3584 x 18944 19.3 against 26.3,
+// 96 rows 1024 x 8192 8.6 against 11.8; 64 rows 8192 x 8192 23.6 against 16.8.
 //
 // A CU's time in tiles is the tiles it gets times a tile's 64-byte steps.  64 x
 // 64 tiles, four on a CU at a time, hide their latency behind each other; of
@@ -91,14 +93,14 @@ inline LinearI8Choice linear_i8_choice(int m, int n, int k, int cus, bool aligne
   // A grid's first dimension holds fewer than 2^32 threads, its second 65535
   // row groups.
   const int64_t few = up(n, 32);
-  const bool fits = few < (1 << 23) && up(m, 64) <= 65535;
-  const float load = aligned ? 1.0f : 2.0f;
-  if (m > 32 && fits) {
-    const float rounds = float(up(few * up(m, 64), cus));
-    offer(kLinearI8Few64, larger(1.7f + rounds * load * (0.0012f * kf + 2.0f),
-                                 2.0f + load * 0.0021f * kf * float(few) / fcus));
-  } else if (fits) {
-    offer(kLinearI8Few32, 3.0f + load * larger(0.0008f * kf, fill(32, 0.008f) * w_bytes / 20700.0f));
+  if (few < (1 << 23) && up(m, 32) <= 65535) {
+    const float load = aligned ? 1.0f : 2.0f;
+    const float rounds32 = float(up(few * up(m, 32), cus)), rounds64 = float(up(few * up(m, 64), cus));
+    offer(kLinearI8Few32, 3.0f + load * larger(rounds32 * (0.00085f * kf + 0.2f),
+                                               (rounds32 > 1.0f && m > 32 ? 1.6f : 1.0f) * fill(32, 0.008f) * w_bytes / 20700.0f));
+    if (m > 32)
+      offer(kLinearI8Few64, larger(1.7f + rounds64 * load * (0.0012f * kf + 2.0f),
+                                   2.0f + load * 0.0021f * kf * float(few) / fcus));
   }
   return best;
 }

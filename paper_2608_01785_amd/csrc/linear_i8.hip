@@ -461,8 +461,8 @@ __global__ __launch_bounds__(WN * WM * 64, WN * WM == 8 ? 1 : NS * MT == 1 ? 4 :
 
 // ---------------------------------------------------------------- few rows
 
-// At most 32 MT rows: what counts is reading w once, as fast as memory gives
-// it.  A block takes 32 channels and its eight waves share K, wave v the 128
+// Few rows, in groups of 32 MT: what counts is reading w once, as fast as memory
+// gives it.  A block takes 32 channels and its eight waves share K, wave v the 128
 // bytes of stages v, v + 8, ...: one cache line of every row to a load's eight
 // lanes, two stages of loads in flight per wave.  Each wave turns its lines
 // into MFMA operands through an LDS image of its own, so nothing in the loop
@@ -598,7 +598,8 @@ hipError_t launch_tiles(const LinearI8Args& a, int blocks, hipStream_t s) {
 
 template <int TYPE, bool ALIGNED>
 hipError_t launch_choice(const LinearI8Args& a, int choice, int cus, hipStream_t s) {
-  const dim3 few((a.n + 31) / 32, choice == kLinearI8Few64 ? (a.m + 63) / 64 : 1);
+  const int few_rows = choice == kLinearI8Few64 ? 64 : 32;
+  const dim3 few((a.n + 31) / 32, (a.m + few_rows - 1) / few_rows);
   switch (choice) {
     case kLinearI8Few32:
       hipLaunchKernelGGL((few_kernel<TYPE, ALIGNED, 1>), few, dim3(kFewWaves * 64), 0, s, a);

@@ -191,11 +191,11 @@ def test_the_serving_loop_answers_every_request(env, policy):
 FEW32, FEW64, T64, T128, T256 = range(5)
 # Kernel, m, n, k, CUs, and whether rows are 16-byte aligned.
 KERNELS = [(FEW32, 1, 2060, 1024, 256, True), (FEW32, 32, 4100, 4112, 64, True), (FEW32, 31, 1030, 2049, 256, False),
-           (FEW32, 20, 2060, 1040, 256, False),
-           (FEW64, 33, 130, 1024, 256, True), (FEW64, 300, 515, 1040, 256, True), (FEW64, 65, 515, 2049, 256, False),
-           (FEW64, 200, 130, 2049, 64, False), (FEW64, 128, 2060, 2064, 256, False),
-           (T64, 65, 4100, 1024, 256, True), (T64, 129, 2060, 256, 64, True), (T64, 777, 1030, 2049, 256, False),
-           (T64, 65, 4100, 1024, 256, False),
+           (FEW32, 20, 2060, 1040, 256, False), (FEW32, 300, 515, 1040, 256, True), (FEW32, 65, 515, 2049, 256, False),
+           (FEW64, 33, 1030, 1040, 64, True), (FEW64, 300, 1030, 2064, 256, True), (FEW64, 100, 515, 2049, 64, False),
+           (FEW64, 128, 2060, 4111, 256, False), (FEW64, 300, 1030, 2064, 256, False),
+           (T64, 300, 4100, 1024, 256, True), (T64, 200, 2060, 256, 64, True), (T64, 777, 1030, 2049, 256, False),
+           (T64, 300, 4100, 1024, 256, False),
            (T128, 777, 4100, 1024, 256, True), (T128, 390, 4100, 2064, 64, True), (T128, 200, 4100, 1033, 64, False),
            (T128, 600, 4100, 2049, 64, False), (T128, 1100, 2060, 2064, 64, False),
            (T256, 600, 4100, 2064, 64, True), (T256, 1100, 2060, 2064, 64, True), (T256, 1500, 2060, 1040, 64, True)]
