@@ -129,6 +129,70 @@ def test_two_heads_with_the_same_weights_at_once(env):
     _check(two, _np(y2), _host(o2))
 
 
+def test_a_captured_head_with_split_rows(env):
+    """Rows long enough to be split over blocks and joined, replayed with new rows between eager passes."""
+    torch, b, ctx = env
+    head = _new_head(env, vocab=70001, max_rows=4)
+    y, out = torch.randn(7, head.hidden, generator=_gen(torch, 1), device="cuda"), head.outputs(7, 1)
+    tokens = torch.randint(0, head.vocab, (7, 1), generator=_gen(torch, 2), device="cuda", dtype=torch.int32)
+    stream = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    head(y, out, tokens, stream=stream.cuda_stream)
+    stream.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        head(y, out, tokens, stream=stream.cuda_stream)
+    for i in range(4):
+        y.copy_(torch.randn(y.shape, generator=_gen(torch, 10 + i), device="cuda"))
+        for t in vars(out).values():
+            t.fill_(-7)
+        head.ws.fill_(255)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        _check(head, _np(y), _host(out), tokens.cpu().numpy())
+        kept = {k: t.clone() for k, t in vars(out).items()}
+        torch.cuda.synchronize()
+        head(y, out, tokens)
+        torch.cuda.synchronize()
+        assert all(torch.equal(t, kept[k]) for k, t in vars(out).items())
+
+
+def test_two_threads_on_one_context(env):
+    """Calls from two host threads at once, each with its own head and stream; a refusal in one is not the other's."""
+    import threading
+    torch, b, ctx = env
+    one = _new_head(env, max_rows=8, vocab=30000)
+    two = one.sharing(max_rows=5)
+    jobs = []
+    for head, rows, role in ((one, 11, b.HS_ROLE_SHARED), (two, 9, b.HS_ROLE_DOWN)):
+        y = torch.randn(rows, head.hidden, generator=_gen(torch, rows), device="cuda")
+        jobs.append((head, y, head.outputs(rows), b.hs_context_stream(ctx, 128, role)))
+    torch.cuda.synchronize()
+    errors = []
+
+    def run(i):
+        try:
+            head, y, out, stream = jobs[i]
+            for n in range(40):
+                head(y, out, cu_budget=128, stream=stream)
+                if i and n % 8 == 0:
+                    with pytest.raises(b.HorizonError, match="carries 128"):
+                        head(y, out, cu_budget=64, stream=stream)
+        except BaseException as e:   # noqa: B902 -- shown by the main thread
+            errors.append(e)
+
+    threads = [threading.Thread(target=run, args=(i,)) for i in (0, 1)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert not errors, errors
+    for head, y, out, _ in jobs:
+        _check(head, _np(y), _host(out))
+
+
 def test_head_refusals(env):
     torch, b, ctx = env
     head = _new_head(env)
