@@ -404,8 +404,9 @@ __device__ __forceinline__ float log_sum(const Sums& a) { return a.s < 1.5f ? lo
 
 // A row's log probabilities from its sums.
 struct Answer {
-  float m, log_s;
-  bool bad, none;
+  float m = 0.0f, log_s = 0.0f;
+  bool bad = false, none = false;
+  __device__ Answer() = default;
   __device__ __forceinline__ explicit Answer(const Sums& a)
       : m(a.m), log_s(0.0f), bad(a.s != a.s), none(a.s == 0.0f) {
     if (!none) log_s = log_sum(a);
@@ -550,8 +551,10 @@ __device__ __forceinline__ int collect(const Row<T>& row, int begin, int end, in
   return n;
 }
 
-// Block (row, split): W wavefronts take the split's chunks in turn.
-template <typename T, int W, bool TOP>
+// Block (split, row): W wavefronts take the split's chunks in turn.  SPLIT: the
+// block's sums and its best keys, sorted, go to the workspace; else the row's
+// results are written.
+template <typename T, int W, bool SPLIT, bool TOP>
 __global__ __launch_bounds__(64 * W) void logprobs_kernel(LogprobsArgs a, int splits) {
   constexpr int kOwn = kPeaks<W> / W;  // a wavefront's entries
   static_assert(kOwn * 64 * sizeof(float) >= 64 * 4 * sizeof(u32x4), "the second look's copy of a chunk takes their place");
@@ -563,16 +566,23 @@ __global__ __launch_bounds__(64 * W) void logprobs_kernel(LogprobsArgs a, int sp
   __shared__ int counts[W];
   static_assert(W == 1 || W == 4, "four values of every lane make the bound");
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int r = int(blockIdx.x / splits), split = int(blockIdx.x % splits);
+  const int r = SPLIT ? blockIdx.y : blockIdx.x;
   const Row<T> row(a, r);
-  const int begin = int(int64_t(row.chunks) * split / splits), end = int(int64_t(row.chunks) * (split + 1) / splits);
+  int begin = 0, end = row.chunks;
+  if constexpr (SPLIT) {
+    // Equal parts: the first ones take a chunk more.
+    const uint32_t split = blockIdx.x, each = uint32_t(row.chunks) / uint32_t(splits);
+    const uint32_t more = uint32_t(row.chunks) - each * uint32_t(splits);
+    begin = int(each * split + min(split, more));
+    end = begin + int(each) + int(split < more);
+  }
 
   Running run;
   Given given;
   Chunk<T> c, next;
   int i = begin + wave;
   if (i < end) row.load(next, i);
-  if (wave == 0 && splits == 1) given.load(a, row.p, r, lane);
+  if (!SPLIT && wave == 0) given.load(a, row.p, r, lane);
   const int group = ((end - begin + W - 1) / W + kOwn - 1) / kOwn;
   float(*own)[64] = peaks + (TOP ? wave * kOwn : 0);
   f32x4 most = {-kInf, -kInf, -kInf, -kInf};
@@ -648,20 +658,21 @@ __global__ __launch_bounds__(64 * W) void logprobs_kernel(LogprobsArgs a, int sp
     rescale(sums, m);
     sums = Sums{m, quad(sums.s, add), quad(sums.f, add), quad(sums.t, add)};
   }
-  const Answer answer(sums);
-  if (wave == 0) {
-    if (splits == 1)
-      write_row<T>(a, r, sums, answer, given);
-    else if (lane == 0)
-      static_cast<f32x4*>(a.part)[blockIdx.x] = f32x4{sums.m, sums.s, sums.f, sums.t};
+  const int64_t part = int64_t(r) * splits + blockIdx.x;  // SPLIT: the block's place
+  Answer answer;
+  if constexpr (SPLIT) {
+    if (threadIdx.x == 0) static_cast<f32x4*>(a.part)[part] = f32x4{sums.m, sums.s, sums.f, sums.t};
+  } else {
+    answer = Answer(sums);
+    if (wave == 0) write_row<T>(a, r, sums, answer, given);
   }
   if constexpr (TOP) {
-    uint64_t* part = splits == 1 ? nullptr : partial_keys(a, int64_t(a.rows) * splits) + int64_t(blockIdx.x) * a.top_k;
+    uint64_t* sorted = partial_keys(a, int64_t(a.rows) * splits) + part * a.top_k;
     auto put = [&](int rank, uint64_t key) {
-      if (splits == 1)
-        write_top(a, r, rank, key, answer);
+      if constexpr (SPLIT)
+        sorted[rank] = key;
       else
-        part[rank] = key;
+        write_top(a, r, rank, key, answer);
     };
     int total = 0;
 #pragma unroll
@@ -746,12 +757,14 @@ __global__ __launch_bounds__(256) void join_kernel(LogprobsArgs a, int splits) {
 template <typename T, bool TOP>
 hipError_t launch(const LogprobsArgs& a, int cus, hipStream_t s) {
   const LogprobsShape p = logprobs_shape(a.rows, a.vocab, sizeof(T), cus);
-  const unsigned grid = unsigned(a.rows) * unsigned(p.splits);
-  if (p.waves == 1)
-    hipLaunchKernelGGL((logprobs_kernel<T, 1, TOP>), dim3(grid), dim3(64), 0, s, a, p.splits);
-  else
-    hipLaunchKernelGGL((logprobs_kernel<T, 4, TOP>), dim3(grid), dim3(256), 0, s, a, p.splits);
-  if (p.splits > 1) hipLaunchKernelGGL((join_kernel<T, TOP>), dim3(a.rows), dim3(256), 0, s, a, p.splits);
+  if (p.splits > 1) {
+    hipLaunchKernelGGL((logprobs_kernel<T, 4, true, TOP>), dim3(p.splits, a.rows), dim3(256), 0, s, a, p.splits);
+    hipLaunchKernelGGL((join_kernel<T, TOP>), dim3(a.rows), dim3(256), 0, s, a, p.splits);
+  } else if (p.waves == 1) {
+    hipLaunchKernelGGL((logprobs_kernel<T, 1, false, TOP>), dim3(a.rows), dim3(64), 0, s, a, 1);
+  } else {
+    hipLaunchKernelGGL((logprobs_kernel<T, 4, false, TOP>), dim3(a.rows), dim3(256), 0, s, a, 1);
+  }
   return hipGetLastError();
 }
 
