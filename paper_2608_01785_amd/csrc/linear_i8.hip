@@ -506,6 +506,20 @@ __global__ __launch_bounds__(kFewWaves * 64, MT == 1 && ALIGNED ? 4 : 2) void fe
   auto stage_of = [&](int i) { return i >= rounds ? stages + 1 : wave + (i + turn < rounds ? i + turn : i + turn - rounds) * kFewWaves; };
 #pragma unroll
   for (int d = 0; d < D; ++d) load(d, stage_of(d));
+  // At the end wave 4 j + g has channel group g of row subtile j (MT <= 2); its
+  // factors come behind the first stages.
+  const int m = m0 + (wave >> 2) * 32 + fr, n = n0 + 8 * (wave & 3) + 4 * fh;
+  const bool mine = wave < 4 * MT && m < a.m && n < a.n;
+  float a_scale = 0.0f, w_scale[4] = {}, bias[4] = {};
+  if (mine) {
+    a_scale = a.a_scale[m];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int c = min(n + e, a.n - 1);
+      w_scale[e] = a.w_scale[c];
+      if (a.bias) bias[e] = bf2f(a.bias[c]);
+    }
+  }
   for (int i = 0; i < rounds; i += D) {
 #pragma unroll
     for (int d = 0; d < D; ++d) {
@@ -538,8 +552,7 @@ __global__ __launch_bounds__(kFewWaves * 64, MT == 1 && ALIGNED ? 4 : 2) void fe
     }
   }
 
-  // Sums of four channels and one row per lane: group g of row subtile j is
-  // wave 4 j + g's (MT <= 2).
+  // Sums of four channels and one row per lane.
   __syncthreads();
   int32_t* part = reinterpret_cast<int32_t*>(smem);
 #pragma unroll
@@ -549,18 +562,13 @@ __global__ __launch_bounds__(kFewWaves * 64, MT == 1 && ALIGNED ? 4 : 2) void fe
       *reinterpret_cast<i32x4*>(part + (((j * 4 + g) * kFewWaves + wave) * 64 + lane) * 4) =
           i32x4{acc[j][4 * g], acc[j][4 * g + 1], acc[j][4 * g + 2], acc[j][4 * g + 3]};
   __syncthreads();
-  const int m = m0 + (wave >> 2) * 32 + fr, n = n0 + 8 * (wave & 3) + 4 * fh;
-  if (wave >= 4 * MT || m >= a.m || n >= a.n) return;
+  if (!mine) return;
   i32x4 sum = {0, 0, 0, 0};
 #pragma unroll
   for (int v = 0; v < kFewWaves; ++v) sum += *reinterpret_cast<const i32x4*>(part + ((wave * kFewWaves + v) * 64 + lane) * 4);
-  const float a_scale = a.a_scale[m];
   float v[4];
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    const int c = min(n + e, a.n - 1);
-    v[e] = output(sum[e], a_scale, a.w_scale[c], a.bias != nullptr, a.bias ? bf2f(a.bias[c]) : 0.0f);
-  }
+  for (int e = 0; e < 4; ++e) v[e] = output(sum[e], a_scale, w_scale[e], a.bias != nullptr, bias[e]);
   T* p = static_cast<T*>(a.out) + int64_t(m) * a.ldo + n;
   if (n + 4 > a.n) {
     store_each(p, v, a.n - n);
