@@ -602,9 +602,10 @@ def _refuse(ctx: Context, t, name: str, kinds, ndim: int) -> None:
 
 def _matrix(ctx: Context, t, name: str, kinds) -> Tuple[int, int, int, int]:
     """(pointer, row stride, rows, columns) of a 2-d tensor whose rows are contiguous."""
-    if t.dtype not in kinds or t.dim() != 2 or t.get_device() != ctx.device:
+    shape = t.shape
+    if t.dtype not in kinds or len(shape) != 2 or t.get_device() != ctx.device:
         _refuse(ctx, t, name, kinds, 2)
-    rows, cols = t.shape
+    rows, cols = shape
     ld, step = t.stride()
     if step != 1 and cols > 1 and rows > 0:
         raise ValueError(f"the rows of {name} are not contiguous (stride {step})")
@@ -615,10 +616,11 @@ def _dense(ctx: Context, t, name: str, kinds, *shape) -> Optional[int]:
     """Pointer of a contiguous tensor of exactly this shape (None stays None)."""
     if t is None:
         return None
-    if t.dtype not in kinds or t.dim() != len(shape) or t.get_device() != ctx.device:
+    size = t.shape
+    if t.dtype not in kinds or len(size) != len(shape) or t.get_device() != ctx.device:
         _refuse(ctx, t, name, kinds, len(shape))
-    if t.shape != shape:
-        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {shape}")
+    if size != shape:
+        raise ValueError(f"{name} has shape {tuple(size)}, expected {shape}")
     if not t.is_contiguous():
         raise ValueError(f"{name} is not contiguous")
     return t.data_ptr()
