@@ -10,8 +10,16 @@ constexpr int kLogprobsMaxTop = 64;       // alternatives a row can list: one pe
 constexpr int kLinearI8MaxK = 131071;     // (-128)^2 k stays below 2^31
 constexpr int64_t kLinearI8MaxStride = int64_t(1) << 22;  // 256 rows of an operand stay within 32-bit offsets
 
-// The kernels of hs_linear_i8: for few rows (32 or 64 a block), and tiles.
-enum LinearI8Choice { kLinearI8Few32, kLinearI8Few64, kLinearI8Tile64, kLinearI8Tile128, kLinearI8Tile256 };
+// The kernels of hs_linear_i8: for few rows (32 or 64 a block, by 32 or 64
+// channels), and tiles.
+enum LinearI8Choice {
+  kLinearI8Few32,
+  kLinearI8Few64,
+  kLinearI8Few64x64,
+  kLinearI8Tile64,
+  kLinearI8Tile128,
+  kLinearI8Tile256
+};
 
 // Which of them an [m, k] x [n, k]^T product takes on `cus` compute units.  All
 // give the same bits, so the choice may follow the budget.  The times below
@@ -22,8 +30,10 @@ enum LinearI8Choice { kLinearI8Few32, kLinearI8Few64, kLinearI8Tile64, kLinearI8
 // there are many.  Few rows against the best tiles: 32 rows 4608 x 3584 6.5, 10.8;
 // 3584 x 18944 18, 43; 65536 x 4096 65, 55.  128 rows: 1024 x 4096 7.5, 12; 3584 x
 // 18944 26, 45; 14336 x 4096 34, 19.  32 rows a block where the blocks fit the
-// chip, 64 where that halves the rounds: 64 rows 3584 x 18944 19.3 against 26.3,
-// 96 rows 1024 x 8192 8.6 against 11.8; 64 rows 8192 x 8192 23.6 against 16.8.
+// chip, 64 where that halves the rounds: 64 rows 3584 x 18944 19 against 25, 100
+// rows 4096 x 4096 10.7 against 9.3.  64 by 64 reads half as much a product and
+// runs alone on its CU, for long sums of more rows: 192 rows 3584 x 18944 36
+// against 49 and 51, and 45 in tiles; 100 rows 8192 x 8192 20 against 42, 30 and 23.
 //
 // A CU's time in tiles is the tiles it gets times a tile's 64-byte steps.  64 x
 // 64 tiles, four on a CU at a time, hide their latency behind each other; of
@@ -37,7 +47,8 @@ enum LinearI8Choice { kLinearI8Few32, kLinearI8Few64, kLinearI8Tile64, kLinearI8
 // Rows that are not 16-byte aligned cost the address unit twice as much a load,
 // which the kernels that use a load least feel most: 512 x 4608 x 3583 40 in 64s
 // and 29 in 128s (22 and 21 aligned), 64 x 1024 x 1023 11 for few rows and 8 in
-// 64s (6.5 and 7 aligned).  256s have no registers for their addresses.
+// 64s (6.7 and 6.2 aligned).  256s have no registers for their addresses, and 64 by
+// 64 for few rows is behind the tiles (256 x 4096 x 4095 22, 18).
 inline LinearI8Choice linear_i8_choice(int m, int n, int k, int cus, bool aligned) {
   auto up = [](int64_t a, int64_t b) { return (a + b - 1) / b; };
   auto larger = [](float a, float b) { return a > b ? a : b; };
@@ -96,11 +107,15 @@ inline LinearI8Choice linear_i8_choice(int m, int n, int k, int cus, bool aligne
   if (few < (1 << 23) && up(m, 32) <= 65535) {
     const float load = aligned ? 1.0f : 2.0f;
     const float rounds32 = float(up(few * up(m, 32), cus)), rounds64 = float(up(few * up(m, 64), cus));
-    offer(kLinearI8Few32, 3.0f + load * larger(rounds32 * (0.00085f * kf + 0.2f),
-                                               (rounds32 > 1.0f && m > 32 ? 1.6f : 1.0f) * fill(32, 0.008f) * w_bytes / 20700.0f));
+    const float read32 = (rounds32 > 1.0f && m > 32 ? 1.6f : 1.0f) * fill(32, 0.008f) * w_bytes / 20700.0f;
+    offer(kLinearI8Few32, larger(5.0f, 3.0f + load * larger(rounds32 * (0.00085f * kf + 0.2f), read32)));
+    const float rounds6464 = float(up(up(n, 64) * up(m, 64), cus));
+    if (m > 32 && aligned)
+      offer(kLinearI8Few64x64, larger(rounds6464 * (0.00165f * kf + 5.0f),
+                                      3.5f + stretch(tiles64, cus, 0.2f) * fill(64, 0.003f) * w_bytes / 20700.0f));
     if (m > 32)
-      offer(kLinearI8Few64, larger(1.7f + rounds64 * load * (0.0012f * kf + 2.0f),
-                                   2.0f + load * 0.0021f * kf * float(few) / fcus));
+      offer(kLinearI8Few64, larger(2.5f + rounds64 * load * (0.0013f * kf + 2.0f),
+                                   2.0f + load * 0.0018f * kf * float(few) / fcus));
   }
   return best;
 }

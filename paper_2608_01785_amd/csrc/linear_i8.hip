@@ -462,32 +462,32 @@ __global__ __launch_bounds__(WN * WM * 64, WN * WM == 8 ? 1 : NS * MT == 1 ? 4 :
 // ---------------------------------------------------------------- few rows
 
 // Few rows, in groups of 32 MT: what counts is reading w once, as fast as memory
-// gives it.  A block takes 32 channels and its eight waves share K, wave v the 128
-// bytes of stages v, v + 8, ...: one cache line of every row to a load's eight
+// gives it.  A block takes 32 NT channels and its eight waves share K, wave v the
+// 128 bytes of stages v, v + 8, ...: one cache line of every row to a load's eight
 // lanes, two stages of loads in flight per wave.  Each wave turns its lines
 // into MFMA operands through an LDS image of its own, so nothing in the loop
 // waits for another wave; their sums meet in LDS at the end.
 constexpr int kFewWaves = 8;
 
-template <int TYPE, bool ALIGNED, int MT>
+template <int TYPE, bool ALIGNED, int MT, int NT>
 __global__ __launch_bounds__(kFewWaves * 64, MT == 1 && ALIGNED ? 4 : 2) void few_kernel(LinearI8Args a) {
-  constexpr int kRow = 128, kImage = (1 + MT) * 32 * kRow;
+  constexpr int kRow = 128, kImage = (NT + MT) * 32 * kRow;
   constexpr int D = 2;  // stages of loads in flight
   __shared__ __attribute__((aligned(1024))) uint8_t smem[kFewWaves * kImage];
   using T = typename OutOf<TYPE>::T;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int fr = lane & 31, fh = lane >> 5;
-  const int n0 = blockIdx.x * 32;
+  const int n0 = blockIdx.x * 32 * NT;
 
-  Operand<ALIGNED, 8, 4> wop;
+  Operand<ALIGNED, 8, 4 * NT> wop;
   Operand<ALIGNED, 8, 4 * MT> aop;
   wop.set(a.w, a.ldw, n0, a.n, a.k);
   const int m0 = blockIdx.y * 32 * MT;
   aop.set(a.a, a.lda, m0, a.m, a.k);
-  u32x4 w[D][4], x[D][4 * MT];
+  u32x4 w[D][4 * NT], x[D][4 * MT];
   auto load = [&](int slot, int stage) {
 #pragma unroll
-    for (int l = 0; l < 4; ++l) w[slot][l] = wop.load(l, stage, a.ldw, a.k);
+    for (int l = 0; l < 4 * NT; ++l) w[slot][l] = wop.load(l, stage, a.ldw, a.k);
 #pragma unroll
     for (int l = 0; l < 4 * MT; ++l) x[slot][l] = aop.load(l, stage, a.lda, a.k);
   };
@@ -495,29 +495,36 @@ __global__ __launch_bounds__(kFewWaves * 64, MT == 1 && ALIGNED ? 4 : 2) void fe
   const uint32_t put_off = (lane >> 3) * kRow + phys<8>(lane >> 3, lane & 7) * 16;  // rows 8 l + lane / 8: phys repeats with 16
   const uint32_t put_odd = (lane >> 3) * kRow + phys<8>(8 + (lane >> 3), lane & 7) * 16;
 
-  i32x16 acc[MT];
+  i32x16 acc[NT][MT];
 #pragma unroll
-  for (int j = 0; j < MT; ++j)
+  for (int i = 0; i < NT; ++i)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) acc[j][r] = 0;
+    for (int j = 0; j < MT; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[i][j][r] = 0;
   const int stages = (a.k + kRow - 1) / kRow, rounds = (stages + kFewWaves - 1) / kFewWaves;
   // As in linear_kernel, every block starts at another round.
   const int turn = blockIdx.x * 3 % rounds;
   auto stage_of = [&](int i) { return i >= rounds ? stages + 1 : wave + (i + turn < rounds ? i + turn : i + turn - rounds) * kFewWaves; };
 #pragma unroll
   for (int d = 0; d < D; ++d) load(d, stage_of(d));
-  // At the end wave 4 j + g has channel group g of row subtile j (MT <= 2); its
-  // factors come behind the first stages.
-  const int m = m0 + (wave >> 2) * 32 + fr, n = n0 + 8 * (wave & 3) + 4 * fh;
-  const bool mine = wave < 4 * MT && m < a.m && n < a.n;
-  float a_scale = 0.0f, w_scale[4] = {}, bias[4] = {};
-  if (mine) {
-    a_scale = a.a_scale[m];
+  // At the end wave v has the groups of four channels v, v + 8, ... of a lane:
+  // group 4 (MT i + j) + g is number g of channel subtile i and row subtile j.
+  // Their factors come behind the first stages.
+  constexpr int kGroups = 4 * MT * NT, kOwn = (kGroups + kFewWaves - 1) / kFewWaves;
+  auto row_of = [&](int o) { return m0 + (wave + kFewWaves * o) / 4 % MT * 32 + fr; };
+  auto channel_of = [&](int o) { return n0 + (wave + kFewWaves * o) / (4 * MT) * 32 + 8 * (wave & 3) + 4 * fh; };
+  auto mine = [&](int o) { return wave + kFewWaves * o < kGroups && row_of(o) < a.m && channel_of(o) < a.n; };
+  float a_scale[kOwn] = {}, w_scale[kOwn][4] = {}, bias[kOwn][4] = {};
+#pragma unroll
+  for (int o = 0; o < kOwn; ++o) {
+    if (!mine(o)) continue;
+    a_scale[o] = a.a_scale[row_of(o)];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const int c = min(n + e, a.n - 1);
-      w_scale[e] = a.w_scale[c];
-      if (a.bias) bias[e] = bf2f(a.bias[c]);
+      const int c = min(channel_of(o) + e, a.n - 1);
+      w_scale[o][e] = a.w_scale[c];
+      if (a.bias) bias[o][e] = bf2f(a.bias[c]);
     }
   }
   for (int i = 0; i < rounds; i += D) {
@@ -529,24 +536,29 @@ __global__ __launch_bounds__(kFewWaves * 64, MT == 1 && ALIGNED ? 4 : 2) void fe
       };
       if (wop.ends(stage, a.k)) {
 #pragma unroll
-        for (int l = 0; l < 4; ++l) w[d][l] = wop.settle(w[d][l], stage, a.k);
+        for (int l = 0; l < 4 * NT; ++l) w[d][l] = wop.settle(w[d][l], stage, a.k);
 #pragma unroll
         for (int l = 0; l < 4 * MT; ++l) x[d][l] = aop.settle(x[d][l], stage, a.k);
       }
 #pragma unroll
-      for (int l = 0; l < 4; ++l) put(l, w[d][l]);
+      for (int l = 0; l < 4 * NT; ++l) put(l, w[d][l]);
 #pragma unroll
-      for (int l = 0; l < 4 * MT; ++l) put(4 + l, x[d][l]);
+      for (int l = 0; l < 4 * MT; ++l) put(4 * NT + l, x[d][l]);
       load(d, stage_of(i + d + D));  // zeros past the end of k
       // The image is this wave's alone, and LDS serves one wave in order.
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
       for (int kk = 0; kk < 4; ++kk) {
         const uint8_t* p = image + fr * kRow + phys<8>(fr, 2 * kk + fh) * 16;
-        const u32x4 wf = *reinterpret_cast<const u32x4*>(p);
+        u32x4 wf[NT], af[MT];
 #pragma unroll
-        for (int j = 0; j < MT; ++j)
-          acc[j] = mfma32_i8(wf, *reinterpret_cast<const u32x4*>(p + (1 + j) * 32 * kRow), acc[j]);
+        for (int i = 0; i < NT; ++i) wf[i] = *reinterpret_cast<const u32x4*>(p + i * 32 * kRow);
+#pragma unroll
+        for (int j = 0; j < MT; ++j) af[j] = *reinterpret_cast<const u32x4*>(p + (NT + j) * 32 * kRow);
+#pragma unroll
+        for (int i = 0; i < NT; ++i)
+#pragma unroll
+          for (int j = 0; j < MT; ++j) acc[i][j] = mfma32_i8(wf[i], af[j], acc[i][j]);
       }
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
@@ -556,27 +568,34 @@ __global__ __launch_bounds__(kFewWaves * 64, MT == 1 && ALIGNED ? 4 : 2) void fe
   __syncthreads();
   int32_t* part = reinterpret_cast<int32_t*>(smem);
 #pragma unroll
-  for (int j = 0; j < MT; ++j)
+  for (int i = 0; i < NT; ++i)
 #pragma unroll
-    for (int g = 0; g < 4; ++g)
-      *reinterpret_cast<i32x4*>(part + (((j * 4 + g) * kFewWaves + wave) * 64 + lane) * 4) =
-          i32x4{acc[j][4 * g], acc[j][4 * g + 1], acc[j][4 * g + 2], acc[j][4 * g + 3]};
+    for (int j = 0; j < MT; ++j)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        *reinterpret_cast<i32x4*>(part + (((4 * (MT * i + j) + g) * kFewWaves + wave) * 64 + lane) * 4) =
+            i32x4{acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
   __syncthreads();
-  if (!mine) return;
-  i32x4 sum = {0, 0, 0, 0};
 #pragma unroll
-  for (int v = 0; v < kFewWaves; ++v) sum += *reinterpret_cast<const i32x4*>(part + ((wave * kFewWaves + v) * 64 + lane) * 4);
-  float v[4];
+  for (int o = 0; o < kOwn; ++o) {
+    if (!mine(o)) continue;
+    const int32_t* from = part + ((wave + kFewWaves * o) * kFewWaves * 64 + lane) * 4;
+    i32x4 sum = {0, 0, 0, 0};
 #pragma unroll
-  for (int e = 0; e < 4; ++e) v[e] = output(sum[e], a_scale, w_scale[e], a.bias != nullptr, bias[e]);
-  T* p = static_cast<T*>(a.out) + int64_t(m) * a.ldo + n;
-  if (n + 4 > a.n) {
-    store_each(p, v, a.n - n);
-  } else if constexpr (sizeof(T) == 4) {
-    __builtin_memcpy(p, v, 16);
-  } else {
-    const u32x2 two = {pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3])};
-    __builtin_memcpy(p, &two, 8);
+    for (int v = 0; v < kFewWaves; ++v) sum += *reinterpret_cast<const i32x4*>(from + v * 64 * 4);
+    float v[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = output(sum[e], a_scale[o], w_scale[o][e], a.bias != nullptr, bias[o][e]);
+    const int n = channel_of(o);
+    T* p = static_cast<T*>(a.out) + int64_t(row_of(o)) * a.ldo + n;
+    if (n + 4 > a.n) {
+      store_each(p, v, a.n - n);
+    } else if constexpr (sizeof(T) == 4) {
+      __builtin_memcpy(p, v, 16);
+    } else {
+      const u32x2 two = {pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3])};
+      __builtin_memcpy(p, &two, 8);
+    }
   }
 }
 
@@ -606,14 +625,18 @@ hipError_t launch_tiles(const LinearI8Args& a, int blocks, hipStream_t s) {
 
 template <int TYPE, bool ALIGNED>
 hipError_t launch_choice(const LinearI8Args& a, int choice, int cus, hipStream_t s) {
-  const int few_rows = choice == kLinearI8Few64 ? 64 : 32;
-  const dim3 few((a.n + 31) / 32, (a.m + few_rows - 1) / few_rows);
+  const int few_rows = choice == kLinearI8Few32 ? 32 : 64, few_channels = choice == kLinearI8Few64x64 ? 64 : 32;
+  const dim3 few((a.n + few_channels - 1) / few_channels, (a.m + few_rows - 1) / few_rows);
   switch (choice) {
     case kLinearI8Few32:
-      hipLaunchKernelGGL((few_kernel<TYPE, ALIGNED, 1>), few, dim3(kFewWaves * 64), 0, s, a);
+      hipLaunchKernelGGL((few_kernel<TYPE, ALIGNED, 1, 1>), few, dim3(kFewWaves * 64), 0, s, a);
       return hipGetLastError();
     case kLinearI8Few64:
-      hipLaunchKernelGGL((few_kernel<TYPE, ALIGNED, 2>), few, dim3(kFewWaves * 64), 0, s, a);
+      hipLaunchKernelGGL((few_kernel<TYPE, ALIGNED, 2, 1>), few, dim3(kFewWaves * 64), 0, s, a);
+      return hipGetLastError();
+    case kLinearI8Few64x64:
+      if constexpr (!ALIGNED) return hipErrorInvalidValue;
+      hipLaunchKernelGGL((few_kernel<TYPE, true, 2, 2>), few, dim3(kFewWaves * 64), 0, s, a);
       return hipGetLastError();
     case kLinearI8Tile64: return launch_tiles<TYPE, ALIGNED, 8, 4, 2, 2, 1, 1>(a, 4 * cus, s);
     case kLinearI8Tile128: return launch_tiles<TYPE, ALIGNED, 8, 2, 2, 2, 2, 2>(a, 2 * cus, s);

@@ -163,10 +163,11 @@ def test_linear_kernel_rule(b):
     """Few rows, then larger tiles as there is more to do; what every kernel's GPU test relies on."""
     def kernel(m, n, k, cus=256, aligned=True):
         return b.lib().hs_linear_i8_kernel(m, n, k, cus, aligned)
-    few32, few64, t64, t128, t256 = range(5)
+    few32, few64, few6464, t64, t128, t256 = range(6)
     assert kernel(1, 4608, 3584) == few32 and kernel(32, 3584, 18944) == few32
     assert kernel(64, 3584, 18944) == few32 and kernel(128, 3584, 18944) == few64
     assert kernel(64, 4608, 3584) == few64
+    assert kernel(192, 3584, 18944) == few6464 and kernel(192, 3584, 18943, aligned=False) == t64
     assert kernel(128, 14336, 4096) == t64
     assert kernel(777, 4096, 4096) == t128
     assert kernel(4096, 8192, 8192) == t256 and kernel(10515, 37888, 3584) == t256

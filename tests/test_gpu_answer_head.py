@@ -252,12 +252,13 @@ def test_the_serving_loop_answers_every_request(env, policy):
 
 # ---------------------------------------------------------------------------- every product kernel
 
-FEW32, FEW64, T64, T128, T256 = range(5)
+FEW32, FEW64, FEW6464, T64, T128, T256 = range(6)
 # Kernel, m, n, k, CUs, and whether rows are 16-byte aligned.
 KERNELS = [(FEW32, 1, 2060, 1024, 256, True), (FEW32, 32, 4100, 4112, 64, True), (FEW32, 31, 1030, 2049, 256, False),
            (FEW32, 20, 2060, 1040, 256, False), (FEW32, 300, 515, 1040, 256, True), (FEW32, 65, 515, 2049, 256, False),
-           (FEW64, 33, 1030, 1040, 64, True), (FEW64, 300, 1030, 2064, 256, True), (FEW64, 100, 515, 2049, 64, False),
-           (FEW64, 128, 2060, 4111, 256, False), (FEW64, 300, 1030, 2064, 256, False),
+           (FEW64, 33, 1030, 4112, 64, True), (FEW64, 300, 1030, 4112, 256, True), (FEW64, 100, 515, 4111, 64, False),
+           (FEW64, 128, 2060, 4111, 256, False), (FEW6464, 100, 1030, 4112, 64, True),
+           (FEW6464, 300, 2060, 4112, 256, True), (FEW6464, 500, 1030, 4112, 256, True),
            (T64, 300, 4100, 1024, 256, True), (T64, 200, 2060, 256, 64, True), (T64, 777, 1030, 2049, 256, False),
            (T64, 300, 4100, 1024, 256, False),
            (T128, 777, 4100, 1024, 256, True), (T128, 390, 4100, 2064, 64, True), (T128, 200, 4100, 1033, 64, False),
