@@ -459,27 +459,30 @@ __device__ __forceinline__ uint64_t* partial_keys(const LogprobsArgs& a, int64_t
   return reinterpret_cast<uint64_t*>(static_cast<f32x4*>(a.part) + blocks);
 }
 
-// A value that at least k of four values of every lane reach; kLowest where
-// fewer are not masked.
-__device__ __forceinline__ float reached_by(const f32x4& v, int k) {
-  uint32_t o[4], t = 0;
+// The k-th largest of the lanes' largest orders: 800 cycles.
+__device__ __forceinline__ uint32_t kth_lane(uint32_t o, int k) {
+  return __builtin_amdgcn_readlane(sort_wave(o), k - 1);
+}
+// The k-th largest of four orders of every lane, its lower 16 bits cleared: each
+// step waits for the one before, 2000 cycles.
+__device__ __forceinline__ uint32_t kth_of_four(const uint32_t (&o)[4], int k) {
+  uint32_t t = 0;
 #pragma unroll
-  for (int q = 0; q < 4; ++q) o[q] = order_of(v[q]);
-  if (k <= 32) {
-    // The k-th largest of the lanes' largest: 800 cycles.
-    t = __builtin_amdgcn_readlane(sort_wave(max(max(o[0], o[1]), max(o[2], o[3]))), k - 1);
-  } else {
-    // The k-th largest of all to 16 bits, each step of which waits for the one
-    // before: 2000 cycles, for 85 elements instead of 260 with k = 64.
+  for (int b = 31; b >= 16; --b) {
+    const uint32_t c = t | (1u << b);
+    int n = 0;
 #pragma unroll
-    for (int b = 31; b >= 16; --b) {
-      const uint32_t c = t | (1u << b);
-      int n = 0;
-#pragma unroll
-      for (int q = 0; q < 4; ++q) n += __popcll(__ballot(o[q] >= c));
-      if (n >= k) t = c;
-    }
+    for (int q = 0; q < 4; ++q) n += __popcll(__ballot(o[q] >= c));
+    if (n >= k) t = c;
   }
+  return t;
+}
+// A value that at least k of four values of every lane reach; kLowest where
+// fewer are not masked.  With k = 64 a bound from the lanes' largest leaves 260
+// elements, one from all four 85.
+__device__ __forceinline__ float reached_by(const f32x4& v, int k) {
+  const uint32_t o[4] = {order_of(v[0]), order_of(v[1]), order_of(v[2]), order_of(v[3])};
+  const uint32_t t = k <= 32 ? kth_lane(max(max(o[0], o[1]), max(o[2], o[3])), k) : kth_of_four(o, k);
   return t < order_of(kLowest) ? kLowest : value_of(uint64_t(t) << 32);
 }
 
@@ -694,8 +697,8 @@ __global__ __launch_bounds__(64 * W) void logprobs_kernel(LogprobsArgs a, int sp
 }
 
 // A row's partial results: lane i takes split i's sums.  The lanes share the
-// splits, whose keys are sorted, and the k-th largest of their 64 first keys is
-// the bound for the others; what reaches it is ranked.
+// splits, whose keys are sorted, and the k-th largest of the first keys that they
+// hold, one or four a lane, is the bound for the others; what reaches it is ranked.
 template <typename T, bool TOP>
 __global__ __launch_bounds__(256) void join_kernel(LogprobsArgs a, int splits) {
   __shared__ __attribute__((aligned(16))) uint64_t keys[TOP ? kLogprobsMaxSplits * kLogprobsMaxTop : 2];
@@ -710,10 +713,16 @@ __global__ __launch_bounds__(256) void join_kernel(LogprobsArgs a, int splits) {
     const f32x4 v = static_cast<const f32x4*>(a.part)[base + lane];
     sums = Sums{v[0], v[1], v[2], v[3]};
   }
-  uint32_t first = 0;  // its order
+  uint32_t first[4] = {};  // orders
+  const int share = 64 / splits;  // lanes a split
+  // One a lane where they are twice as many as the alternatives.
+  const bool one = share * splits >= 2 * a.top_k;
   if constexpr (TOP) {
-    const int share = 64 / splits, from = lane % share;  // lanes a split
-    if (lane / share < splits && from < a.top_k) first = uint32_t(src[lane / share * a.top_k + from] >> 32);
+    const int from = one ? lane % share : lane % share * 4;
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      if (lane / share < splits && from + q < a.top_k && (q == 0 || !one))
+        first[q] = uint32_t(src[lane / share * a.top_k + from + q] >> 32);
   }
   constexpr int kAhead = 4;
   uint64_t mine[kAhead];
@@ -726,7 +735,7 @@ __global__ __launch_bounds__(256) void join_kernel(LogprobsArgs a, int splits) {
   if (wave == 0) given.load(a, static_cast<const T*>(nullptr), r, lane);
   if constexpr (TOP) {
     if (threadIdx.x == 0) count = 0;
-    const uint32_t kth = __builtin_amdgcn_readlane(sort_wave(first), a.top_k - 1);
+    const uint32_t kth = one ? kth_lane(first[0], a.top_k) : kth_of_four(first, a.top_k);
     const uint64_t bound = uint64_t(max(kth, 1u)) << 32;  // no key is 0
     __syncthreads();
 #pragma unroll
