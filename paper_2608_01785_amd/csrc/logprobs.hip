@@ -459,30 +459,27 @@ __device__ __forceinline__ uint64_t* partial_keys(const LogprobsArgs& a, int64_t
   return reinterpret_cast<uint64_t*>(static_cast<f32x4*>(a.part) + blocks);
 }
 
-// The k-th largest of the lanes' largest orders: 800 cycles.
-__device__ __forceinline__ uint32_t kth_lane(uint32_t o, int k) {
-  return __builtin_amdgcn_readlane(sort_wave(o), k - 1);
-}
-// The k-th largest of four orders of every lane, its lower 16 bits cleared: each
-// step waits for the one before, 2000 cycles.
-__device__ __forceinline__ uint32_t kth_of_four(const uint32_t (&o)[4], int k) {
-  uint32_t t = 0;
-#pragma unroll
-  for (int b = 31; b >= 16; --b) {
-    const uint32_t c = t | (1u << b);
-    int n = 0;
-#pragma unroll
-    for (int q = 0; q < 4; ++q) n += __popcll(__ballot(o[q] >= c));
-    if (n >= k) t = c;
-  }
-  return t;
-}
 // A value that at least k of four values of every lane reach; kLowest where
-// fewer are not masked.  With k = 64 a bound from the lanes' largest leaves 260
-// elements, one from all four 85.
+// fewer are not masked.
 __device__ __forceinline__ float reached_by(const f32x4& v, int k) {
-  const uint32_t o[4] = {order_of(v[0]), order_of(v[1]), order_of(v[2]), order_of(v[3])};
-  const uint32_t t = k <= 32 ? kth_lane(max(max(o[0], o[1]), max(o[2], o[3])), k) : kth_of_four(o, k);
+  uint32_t o[4], t = 0;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) o[q] = order_of(v[q]);
+  if (k <= 32) {
+    // The k-th largest of the lanes' largest: 800 cycles.
+    t = __builtin_amdgcn_readlane(sort_wave(max(max(o[0], o[1]), max(o[2], o[3]))), k - 1);
+  } else {
+    // The k-th largest of all to 16 bits, each step of which waits for the one
+    // before: 2000 cycles, for 85 elements instead of 260 with k = 64.
+#pragma unroll
+    for (int b = 31; b >= 16; --b) {
+      const uint32_t c = t | (1u << b);
+      int n = 0;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) n += __popcll(__ballot(o[q] >= c));
+      if (n >= k) t = c;
+    }
+  }
   return t < order_of(kLowest) ? kLowest : value_of(uint64_t(t) << 32);
 }
 
@@ -696,70 +693,64 @@ __global__ __launch_bounds__(64 * W) void logprobs_kernel(LogprobsArgs a, int sp
   }
 }
 
-// A row's partial results: lane i takes split i's sums.  The lanes share the
-// splits, whose keys are sorted, and the k-th largest of the first keys that they
-// hold, one or four a lane, is the bound for the others; what reaches it is ranked.
+// A row's partial results.  Lane i of the last wavefront takes split i's sums; the
+// others merge the splits' sorted keys, a fourth of the splits each, and the
+// first of them what they have (a merge is six stages, some 300 cycles).
+constexpr int kMergers = 4;
+
 template <typename T, bool TOP>
-__global__ __launch_bounds__(256) void join_kernel(LogprobsArgs a, int splits) {
-  __shared__ __attribute__((aligned(16))) uint64_t keys[TOP ? kLogprobsMaxSplits * kLogprobsMaxTop : 2];
-  __shared__ int count;
+__global__ __launch_bounds__(64 * (TOP ? kMergers + 1 : 1)) void join_kernel(LogprobsArgs a, int splits) {
+  __shared__ uint64_t lists[kMergers][64];
+  __shared__ f32x4 shared;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = blockIdx.x;
   const int64_t base = int64_t(r) * splits;
-  const int n_keys = TOP ? splits * a.top_k : 0;
-  const uint64_t* src = partial_keys(a, int64_t(a.rows) * splits) + base * a.top_k;
-  // Every load that depends on none other first.
-  Sums sums{kLowest, 0.0f, 0.0f, 0.0f};
-  if (lane < splits) {
-    const f32x4 v = static_cast<const f32x4*>(a.part)[base + lane];
-    sums = Sums{v[0], v[1], v[2], v[3]};
-  }
-  uint32_t first[4] = {};  // orders
-  const int share = 64 / splits;  // lanes a split
-  // One a lane where they are twice as many as the alternatives.
-  const bool one = share * splits >= 2 * a.top_k;
-  if constexpr (TOP) {
-    const int from = one ? lane % share : lane % share * 4;
-#pragma unroll
-    for (int q = 0; q < 4; ++q)
-      if (lane / share < splits && from + q < a.top_k && (q == 0 || !one))
-        first[q] = uint32_t(src[lane / share * a.top_k + from + q] >> 32);
-  }
-  constexpr int kAhead = 4;
-  uint64_t mine[kAhead];
-#pragma unroll
-  for (int q = 0; q < kAhead; ++q) {
-    const int j = threadIdx.x + 256 * q;
-    mine[q] = j < n_keys ? src[j] : 0;
-  }
-  Given given;
-  if (wave == 0) given.load(a, static_cast<const T*>(nullptr), r, lane);
-  if constexpr (TOP) {
-    if (threadIdx.x == 0) count = 0;
-    const uint32_t kth = one ? kth_lane(first[0], a.top_k) : kth_of_four(first, a.top_k);
-    const uint64_t bound = uint64_t(max(kth, 1u)) << 32;  // no key is 0
-    __syncthreads();
-#pragma unroll
-    for (int q = 0; q < kAhead; ++q)
-      if (mine[q] >= bound) keys[atomicAdd(&count, 1)] = mine[q];
-    for (int j = threadIdx.x + 256 * kAhead; j < n_keys; j += 256) {
-      const uint64_t key = src[j];
-      if (key >= bound) keys[atomicAdd(&count, 1)] = key;
+  uint64_t list = 0;
+  if (!TOP || wave == kMergers) {
+    Sums sums{kLowest, 0.0f, 0.0f, 0.0f};
+    if (lane < splits) {
+      const f32x4 v = static_cast<const f32x4*>(a.part)[base + lane];
+      sums = Sums{v[0], v[1], v[2], v[3]};
     }
+    Given given;
+    given.load(a, static_cast<const T*>(nullptr), r, lane);
+    const float m = max_wave(sums.m);
+    rescale(sums, m);
+    sums = Sums{m, sum_wave(sums.s), sum_wave(sums.f), sum_wave(sums.t)};
+    const Answer answer(sums);
+    write_row<T>(a, r, sums, answer, given);
+    if (TOP && lane == 0) shared = f32x4{answer.m, answer.log_s, float(answer.bad), float(answer.none)};
+  } else if constexpr (TOP) {
+    const uint64_t* src = partial_keys(a, int64_t(a.rows) * splits) + base * a.top_k;
+    // The best key of a split is a list's first, or its last where it is merged into another.
+    auto key = [&](int split, int i) { return split < splits && i < a.top_k ? src[split * a.top_k + i] : 0; };
+    constexpr int kAhead = 4;
+    uint64_t next[kAhead];
+    list = key(wave, lane);
+#pragma unroll
+    for (int q = 0; q < kAhead; ++q) next[q] = key(wave + kMergers * (q + 1), 63 - lane);
+    for (int s = wave + kMergers; s < splits; s += kMergers * kAhead) {
+#pragma unroll
+      for (int q = 0; q < kAhead; ++q) {
+        if (s + kMergers * q >= splits) break;
+        list = merge_stages<32>(list > next[q] ? list : next[q], true);
+        next[q] = key(s + kMergers * (q + kAhead), 63 - lane);
+      }
+    }
+    lists[wave][lane] = list;
   }
-  const float m = max_wave(sums.m);
-  rescale(sums, m);
-  sums = Sums{m, sum_wave(sums.s), sum_wave(sums.f), sum_wave(sums.t)};
-  const Answer answer(sums);
-  if (wave == 0) write_row<T>(a, r, sums, answer, given);
   if constexpr (TOP) {
     __syncthreads();
-    const int n = count;
-    for (int j = threadIdx.x; j < n; j += 256) {
-      const uint64_t key = keys[j];
-      const int rank = rank_among(keys, n, key);
-      if (rank < a.top_k) write_top(a, r, rank, key, answer);
+    if (wave != 0) return;
+    for (int w = 1; w < min(kMergers, splits); ++w) {
+      const uint64_t other = lists[w][63 - lane];
+      list = merge_stages<32>(list > other ? list : other, true);
     }
-    if (int(threadIdx.x) >= n && int(threadIdx.x) < a.top_k) write_top(a, r, threadIdx.x, 0, answer);
+    Answer answer;
+    answer.m = shared[0];
+    answer.log_s = shared[1];
+    answer.bad = shared[2] != 0.0f;
+    answer.none = shared[3] != 0.0f;
+    if (lane < a.top_k) write_top(a, r, lane, list, answer);
   }
 }
 
@@ -768,7 +759,7 @@ hipError_t launch(const LogprobsArgs& a, int cus, hipStream_t s) {
   const LogprobsShape p = logprobs_shape(a.rows, a.vocab, sizeof(T), cus);
   if (p.splits > 1) {
     hipLaunchKernelGGL((logprobs_kernel<T, 4, true, TOP>), dim3(p.splits, a.rows), dim3(256), 0, s, a, p.splits);
-    hipLaunchKernelGGL((join_kernel<T, TOP>), dim3(a.rows), dim3(256), 0, s, a, p.splits);
+    hipLaunchKernelGGL((join_kernel<T, TOP>), dim3(a.rows), dim3(TOP ? 64 * (kMergers + 1) : 64), 0, s, a, p.splits);
   } else if (p.waves == 1) {
     hipLaunchKernelGGL((logprobs_kernel<T, 1, false, TOP>), dim3(a.rows), dim3(64), 0, s, a, 1);
   } else {
