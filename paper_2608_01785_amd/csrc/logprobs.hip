@@ -489,6 +489,39 @@ __device__ __forceinline__ float reached_by(const f32x4& v, int k) {
 template <int W>
 constexpr int kPeaks = W == 1 ? 32 : 64;
 
+__device__ __forceinline__ int lanes_before(uint64_t mask) {
+  return int(__builtin_amdgcn_mbcnt_hi(uint32_t(mask >> 32), __builtin_amdgcn_mbcnt_lo(uint32_t(mask), 0)));
+}
+
+// Bit j: element j of the lane reaches `bound`.
+template <typename T>
+__device__ __forceinline__ uint32_t reaching(const Chunk<T>& c, float bound) {
+  constexpr int V = Chunk<T>::kVec;
+  uint32_t which = 0;
+#pragma unroll
+  for (int l = 0; l < 4; ++l)
+#pragma unroll
+    for (int e = 0; e < V; ++e) which |= uint32_t(c.get(l, e) >= bound) << (l * V + e);
+  return which;
+}
+
+// Keys of the lanes' elements `which` of a chunk, whose element 0 of the lane is
+// `token`, behind the n in buf; their new number, of which kBuffer are there.
+template <typename T>
+__device__ __forceinline__ int leave_keys(const Chunk<T>& c, uint32_t which, int64_t token, uint64_t* buf, int n) {
+  constexpr int V = Chunk<T>::kVec;
+  while (true) {  // nearly always one a lane
+    const uint64_t mask = __ballot(which != 0);
+    if (mask == 0) return n;
+    const int at = n + lanes_before(mask);
+    const int j = __builtin_ctz(which | 0x80000000u);
+    const float z = c.pick(j);
+    if (which && at < kBuffer) buf[at] = key_of(z, uint32_t(token + (j / V) * 64 * V + j % V));
+    which &= which - 1;
+    n += __popcll(mask);
+  }
+}
+
 // Keys of the elements that reach `bound`, of the entries (lanes' maxima of
 // `group` chunks) that do, into buf; their number, or more than kBuffer where
 // they are too many (buf then holds nothing of use).
@@ -497,16 +530,13 @@ __device__ __forceinline__ int collect(const Row<T>& row, int begin, int end, in
                                        const float (*peaks)[64], uint16_t* hits, uint64_t* buf) {
   constexpr int V = Chunk<T>::kVec;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  auto before = [](uint64_t mask) {
-    return int(__builtin_amdgcn_mbcnt_hi(uint32_t(mask >> 32), __builtin_amdgcn_mbcnt_lo(uint32_t(mask), 0)));
-  };
   int found = 0, n = 0;
 #pragma unroll 4
   for (int e = 0; e < entries; ++e) {
     const bool hit = peaks[e][lane] >= bound;
     const uint64_t mask = __ballot(hit);
     if (mask == 0) continue;
-    const int at = found + before(mask);
+    const int at = found + lanes_before(mask);
     if (hit && at < kBuffer) hits[at] = uint16_t(e * 64 + lane);
     found += __popcll(mask);
   }
@@ -530,22 +560,7 @@ __device__ __forceinline__ int collect(const Row<T>& row, int begin, int end, in
           inside |= ((1u << hi) - (1u << lo)) << (l * V);
         }
       }
-      uint32_t which = 0;
-#pragma unroll
-      for (int l = 0; l < 4; ++l)
-#pragma unroll
-        for (int e = 0; e < V; ++e) which |= uint32_t(words.get(l, e) >= bound) << (l * V + e);
-      which &= inside;
-      while (true) {  // nearly always one
-        const uint64_t mask = __ballot(which != 0);
-        if (mask == 0) break;
-        const int at = n + before(mask);
-        const int j = __builtin_ctz(which | 0x80000000u);
-        const float z = words.pick(j);
-        if (which && at < kBuffer) buf[at] = key_of(z, uint32_t(i0 + (j / V) * 64 * V + j % V - row.first));
-        which &= which - 1;
-        n += __popcll(mask);
-      }
+      n = leave_keys(words, reaching(words, bound) & inside, i0 - row.first, buf, n);
     }
   }
   return n;
@@ -626,7 +641,14 @@ __global__ __launch_bounds__(64 * W) void logprobs_kernel(LogprobsArgs a, int sp
     }
     const float bound = reached_by(most, a.top_k);
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    n = collect<T, W>(row, begin, end, group, entry + (in_group > 0), bound, own, hits[wave], keys[wave]);
+    // A wavefront's only chunk is still in registers.
+    if (begin + W >= end)
+      n = begin + wave < end
+              ? leave_keys(c, reaching(c, bound), int64_t(begin + wave) * Chunk<T>::kSize + lane * Chunk<T>::kVec - row.first,
+                           keys[wave], 0)
+              : 0;
+    else
+      n = collect<T, W>(row, begin, end, group, entry + (in_group > 0), bound, own, hits[wave], keys[wave]);
     if (n > kBuffer) {
       // Too many: all chunks once more.
       Best best;
