@@ -12,7 +12,8 @@ import pytest
 
 from oracle import answer as A
 from tests.gpu_common import log, require_gpu
-from tests.test_gpu_answer import _check_linear, _gen, _linear, _logprobs, _np, _quantize, _t, _view
+from tests.test_gpu_answer import _check_linear, _check_quantize, _gen, _linear, _logprobs, _np, _quantize, _t, _view
+from tests.test_gpu_answer import test_quantize_values as _quantize_values
 from tests.test_gpu_algorithm1 import LADDER, _loop
 
 pytestmark = pytest.mark.gpu
@@ -301,6 +302,20 @@ def test_product_lengths(env, k, m):
 
 
 # ---------------------------------------------------------------------------- long rows, many of them
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("norm", [False, True])
+@pytest.mark.parametrize("d", [32776, 40003])
+def test_quantisation_of_rows_beyond_the_registers(env, dtype, norm, d):
+    """Ties, extremes, subnormals, zeros and rows that are not finite, as for short rows; odd strides."""
+    torch, b, ctx = env
+    _quantize_values((torch, b, ctx), dtype, norm, d)
+    g = _gen(torch, d)
+    x = torch.randn(5, d, generator=g, device="cuda").to(_t(torch, dtype))
+    gain = (1 + 0.2 * torch.randn(d, generator=g, device="cuda")).bfloat16() if norm else None
+    _check_quantize((torch, b, ctx), _view(torch, x, 3, 1, fill=7)[1], gain, pad=1, shift=5)
+
+
 
 @pytest.mark.parametrize("rows,vocab,cus", [(64, 160001, 64), (512, 40000, 64), (3, 700001, 64)])
 @pytest.mark.parametrize("top", [1, 20, 64])
