@@ -241,6 +241,86 @@ __global__ __launch_bounds__(W > 1 ? 64 * W : 256) void quantize_kernel(Quantize
   }
 }
 
+// Rows of at most 8 LR elements, LR lanes each: a wavefront has 64 / LR of them.
+// 50000 x 64 fp32 with a gain: 6.8 us, 23 with a wavefront a row; 500000 x 256:
+// 132 us (4.9 TB/s), 203.
+template <typename T, int LR, bool GAIN>
+__global__ __launch_bounds__(256) void quantize_narrow_kernel(QuantizeArgs a) {
+  constexpr int kRows = 256 / LR;  // of a block
+  constexpr bool kExact = !GAIN && sizeof(T) == 2;
+  __shared__ RowLds<1> lds;  // not used by one wavefront
+  auto reduce = [](auto v, auto f) {
+    v = f(v, xor_lane<1>(v));
+    v = f(v, xor_lane<2>(v));
+    v = f(v, xor_lane<4>(v));
+    if constexpr (LR > 8) v = f(v, xor_lane<8>(v));
+    if constexpr (LR > 16) v = f(v, xor_lane<16>(v));
+    return v;
+  };
+  const int first = threadIdx.x % LR, at = first * kVec, rest = a.d / kVec * kVec + first;
+  const bool has_group = at + kVec <= a.d, has_rest = first < a.d % kVec;
+  float gain[kVec] = {}, gain_rest = 0.0f;  // the same for all its rows
+  if constexpr (GAIN) {
+    if (has_group) load_group(a.gain + at, gain);
+    if (has_rest) gain_rest = bf2f(a.gain[rest]);
+  }
+  for (int row0 = blockIdx.x * kRows; row0 < a.rows; row0 += gridDim.x * kRows) {
+    const int row = row0 + int(threadIdx.x) / LR;
+    const bool valid = row < a.rows;
+    const T* x = static_cast<const T*>(a.x) + int64_t(row) * a.ldx;
+    int8_t* q = a.q + int64_t(row) * a.ldq;
+    float v[kVec] = {}, v_rest = 0.0f, ss = 0.0f;
+    if (valid && has_group) load_group(x + at, v);
+    if (valid && has_rest) v_rest = elem(x, rest);
+    auto y = [&](int e) { return GAIN ? v[e] * gain[e] : v[e]; };
+    const float y_rest = GAIN ? v_rest * gain_rest : v_rest;
+    uint32_t top = magnitude(y_rest);
+    if constexpr (GAIN) ss = v_rest * v_rest;
+#pragma unroll
+    for (int e = 0; e < kVec; ++e) {
+      if constexpr (GAIN) ss = fmaf(v[e], v[e], ss);
+      top = max(top, magnitude(y(e)));
+    }
+    top = reduce(top, [](uint32_t p, uint32_t r) { return max(p, r); });
+    if constexpr (GAIN) ss = reduce(ss, [](float p, float r) { return p + r; });
+    const float top32 = __uint_as_float(top), c = 127.0f / top32;
+    const bool fast = valid && comfortable(top32, GAIN, ss);
+    float off = 0.0f;
+    if (fast) {
+      if (first == 0) {
+        const double r = GAIN ? 1.0 / sqrt(double(ss) / a.d + double(a.eps)) : 1.0;
+        a.scale[row] = float(double(top32) * r / 127.0);
+      }
+      int r[kVec];
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) r[e] = fast_step<kExact>(y(e), top32, c, off);
+      if (has_group) store_group(q + at, r);
+      if (has_rest) q[rest] = int8_t(fast_step<kExact>(y_rest, top32, c, off));
+    }
+    if constexpr (!kExact) {
+      if (__ballot(off >= 0.5f)) {
+        // The exact maxima, then the lanes in doubt.
+        double exact = fabs(double(v_rest) * (GAIN ? double(gain_rest) : 1.0));
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) exact = fmax(exact, fabs(double(v[e]) * (GAIN ? double(gain[e]) : 1.0)));
+        exact = reduce(exact, [](double p, double r) { return fmax(p, r); });
+        if (off >= 0.5f) {
+          int r[kVec];
+#pragma unroll
+          for (int e = 0; e < kVec; ++e) r[e] = exact_step(double(v[e]) * (GAIN ? double(gain[e]) : 1.0), exact);
+          if (has_group) store_group(q + at, r);
+          if (has_rest) q[rest] = int8_t(exact_step(double(v_rest) * (GAIN ? double(gain_rest) : 1.0), exact));
+        }
+      }
+    }
+    // The others one after another, a wavefront for each.
+    for (uint64_t slow = __ballot(valid && !fast && first == 0); slow != 0; slow &= slow - 1) {
+      const int other = row0 + (int(threadIdx.x) / 64 * 64 + __builtin_ctzll(slow)) / LR;
+      plain_row<T, 1>(a, static_cast<const T*>(a.x) + int64_t(other) * a.ldx, a.q + int64_t(other) * a.ldq, other, lds);
+    }
+  }
+}
+
 // Rows longer than a block's registers: read twice, the second time from a cache.
 // With the exact maximum at hand a group in doubt is decided at once.  300 x
 // 131072 fp32 with a gain: 77 us, 593 on the plain path.
@@ -324,8 +404,22 @@ hipError_t launch(const QuantizeArgs& a, int cus, hipStream_t s) {
   return hipGetLastError();
 }
 
+template <typename T, int LR>
+hipError_t launch_narrow(const QuantizeArgs& a, int cus, hipStream_t s) {
+  const int64_t blocks = (int64_t(a.rows) * LR + 255) / 256, most = int64_t(cus) * 16;
+  const unsigned grid = unsigned(blocks < most ? blocks : most);
+  if (a.gain)
+    hipLaunchKernelGGL((quantize_narrow_kernel<T, LR, true>), dim3(grid), dim3(256), 0, s, a);
+  else
+    hipLaunchKernelGGL((quantize_narrow_kernel<T, LR, false>), dim3(grid), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
 template <typename T>
 hipError_t launch_type(const QuantizeArgs& a, int cus, hipStream_t s) {
+  if (a.d <= 64) return launch_narrow<T, 8>(a, cus, s);
+  if (a.d <= 128) return launch_narrow<T, 16>(a, cus, s);
+  if (a.d <= 256) return launch_narrow<T, 32>(a, cus, s);
   // Two groups a lane, with wavefronts enough for the row, keep the most loads
   // in flight: 10515 x 3584 fp32 takes 38 us in 4 x 2 (5.0 TB/s), 44 in 2 x 4
   // and 51 in 1 x 8.  Past four wavefronts the joins cost more than more

@@ -305,13 +305,14 @@ def test_product_lengths(env, k, m):
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
 @pytest.mark.parametrize("norm", [False, True])
-@pytest.mark.parametrize("d", [32776, 40003])
-def test_quantisation_of_rows_beyond_the_registers(env, dtype, norm, d):
-    """Ties, extremes, subnormals, zeros and rows that are not finite, as for short rows; odd strides."""
+@pytest.mark.parametrize("d", [8, 63, 64, 65, 100, 128, 129, 250, 256, 257, 32776, 40003])
+def test_quantisation_of_narrow_and_long_rows(env, dtype, norm, d):
+    """Several rows of a wavefront, and rows beyond a block's registers: ties, extremes, subnormals, zeros and rows that
+    are not finite beside ordinary ones; odd strides."""
     torch, b, ctx = env
     _quantize_values((torch, b, ctx), dtype, norm, d)
     g = _gen(torch, d)
-    x = torch.randn(5, d, generator=g, device="cuda").to(_t(torch, dtype))
+    x = torch.randn(5 if d > 1000 else 5003, d, generator=g, device="cuda").to(_t(torch, dtype))
     gain = (1 + 0.2 * torch.randn(d, generator=g, device="cuda")).bfloat16() if norm else None
     _check_quantize((torch, b, ctx), _view(torch, x, 3, 1, fill=7)[1], gain, pad=1, shift=5)
 
