@@ -492,7 +492,8 @@ __global__ __launch_bounds__(kFewWaves * 64, MT == 1 && ALIGNED ? 4 : 2) void fe
     for (int l = 0; l < 4 * MT; ++l) x[slot][l] = aop.load(l, stage, a.lda, a.k);
   };
   uint8_t* image = smem + wave * kImage;
-  const uint32_t put_off = (lane >> 3) * kRow + phys<8>(lane >> 3, lane & 7) * 16;  // rows 8 l + lane / 8: phys repeats with 16
+  // Load l holds rows 8 l + lane / 8, and phys() repeats with 16 rows.
+  const uint32_t put_off = (lane >> 3) * kRow + phys<8>(lane >> 3, lane & 7) * 16;
   const uint32_t put_odd = (lane >> 3) * kRow + phys<8>(8 + (lane >> 3), lane & 7) * 16;
 
   i32x16 acc[NT][MT];
@@ -505,7 +506,10 @@ __global__ __launch_bounds__(kFewWaves * 64, MT == 1 && ALIGNED ? 4 : 2) void fe
   const int stages = (a.k + kRow - 1) / kRow, rounds = (stages + kFewWaves - 1) / kFewWaves;
   // As in linear_kernel, every block starts at another round.
   const int turn = blockIdx.x * 3 % rounds;
-  auto stage_of = [&](int i) { return i >= rounds ? stages + 1 : wave + (i + turn < rounds ? i + turn : i + turn - rounds) * kFewWaves; };
+  auto stage_of = [&](int i) {
+    const int round = i + turn < rounds ? i + turn : i + turn - rounds;
+    return i < rounds ? wave + round * kFewWaves : stages + 1;
+  };
 #pragma unroll
   for (int d = 0; d < D; ++d) load(d, stage_of(d));
   // At the end wave v has the groups of four channels v, v + 8, ... of a lane:

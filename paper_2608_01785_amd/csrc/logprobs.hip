@@ -63,6 +63,11 @@ __device__ __forceinline__ float sum_wave(float v) {
   return reduce_wave(v, [](float a, float b) { return a + b; });
 }
 
+// Lanes of the mask below this one.
+__device__ __forceinline__ int lanes_before(uint64_t mask) {
+  return int(__builtin_amdgcn_mbcnt_hi(uint32_t(mask >> 32), __builtin_amdgcn_mbcnt_lo(uint32_t(mask), 0)));
+}
+
 // One stage of a bitonic network over the 64 lanes: lane pairs J apart, the
 // larger value to the lower lane where `down`.
 template <int J, typename V>
@@ -159,7 +164,7 @@ struct Best {
   __device__ __forceinline__ void offer(uint64_t key) {
     const bool take = key > kth;
     const uint64_t mask = __ballot(take);
-    const int at = count + __builtin_amdgcn_mbcnt_hi(uint32_t(mask >> 32), __builtin_amdgcn_mbcnt_lo(uint32_t(mask), 0));
+    const int at = count + lanes_before(mask);
     if (take) buf[at] = key;
     count += __popcll(mask);
   }
@@ -489,10 +494,6 @@ __device__ __forceinline__ float reached_by(const f32x4& v, int k) {
 template <int W>
 constexpr int kPeaks = W == 1 ? 32 : 64;
 
-__device__ __forceinline__ int lanes_before(uint64_t mask) {
-  return int(__builtin_amdgcn_mbcnt_hi(uint32_t(mask >> 32), __builtin_amdgcn_mbcnt_lo(uint32_t(mask), 0)));
-}
-
 // Bit j: element j of the lane reaches `bound`.
 template <typename T>
 __device__ __forceinline__ uint32_t reaching(const Chunk<T>& c, float bound) {
@@ -572,7 +573,8 @@ __device__ __forceinline__ int collect(const Row<T>& row, int begin, int end, in
 template <typename T, int W, bool SPLIT, bool TOP>
 __global__ __launch_bounds__(64 * W) void logprobs_kernel(LogprobsArgs a, int splits) {
   constexpr int kOwn = kPeaks<W> / W;  // a wavefront's entries
-  static_assert(kOwn * 64 * sizeof(float) >= 64 * 4 * sizeof(u32x4), "the second look's copy of a chunk takes their place");
+  // The second look's copy of a chunk takes their place.
+  static_assert(kOwn * 64 * sizeof(float) >= 64 * 4 * sizeof(u32x4), "peaks hold a chunk");
   __shared__ __attribute__((aligned(16))) uint64_t keys[TOP ? W : 1][kBuffer];
   __shared__ __attribute__((aligned(16))) float peaks[TOP ? kPeaks<W> : 1][64];
   __shared__ __attribute__((aligned(16))) float pool[TOP && W > 1 ? W * 64 : 4];
@@ -641,14 +643,13 @@ __global__ __launch_bounds__(64 * W) void logprobs_kernel(LogprobsArgs a, int sp
     }
     const float bound = reached_by(most, a.top_k);
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    // A wavefront's only chunk is still in registers.
-    if (begin + W >= end)
-      n = begin + wave < end
-              ? leave_keys(c, reaching(c, bound), int64_t(begin + wave) * Chunk<T>::kSize + lane * Chunk<T>::kVec - row.first,
-                           keys[wave], 0)
-              : 0;
-    else
+    if (begin + W < end) {
       n = collect<T, W>(row, begin, end, group, entry + (in_group > 0), bound, own, hits[wave], keys[wave]);
+    } else if (begin + wave < end) {
+      // The wavefront's only chunk is still in registers.
+      const int64_t at = int64_t(begin + wave) * Chunk<T>::kSize + lane * Chunk<T>::kVec;
+      n = leave_keys(c, reaching(c, bound), at - row.first, keys[wave], 0);
+    }
     if (n > kBuffer) {
       // Too many: all chunks once more.
       Best best;

@@ -1,4 +1,5 @@
-"""The text head over residual rows, in passes and inside the serving loop; every product kernel by its rule; long strides.
+"""The text head over residual rows, in passes and inside the serving loop; every product kernel by its rule; long
+strides; narrow and long rows.
 
 Bounds (u = 2^-24): a row's scale is within 78 u, so a logit z, the product of an exact sum with two scales, is
 within 160 u |z| of the float64 chain with the weights' scales as stored, and a log probability within twice the
