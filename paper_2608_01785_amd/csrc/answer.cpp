@@ -139,6 +139,11 @@ int32_t hs_linear_i8_kernel(int32_t m, int32_t n, int32_t k, int32_t cus, int32_
   return hs::linear_i8_choice(m, n, k, cus, aligned != 0);
 }
 
+// The blocks a row is split over by hs_logprobs (see logprobs_shape), as internal.
+int32_t hs_logprobs_splits(int32_t rows, int32_t vocab, int32_t elem_bytes, int32_t cus) {
+  return hs::logprobs_shape(rows, vocab, elem_bytes, cus).splits;
+}
+
 hs_status hs_logprobs_workspace_size(int32_t max_rows, int32_t vocab, int32_t top_k, size_t* bytes) {
   hs::clear_error();
   if (!bytes) return hs::fail(HS_ERR_INVALID_ARG, "output pointer is null");

@@ -200,3 +200,28 @@ def test_too_many_rows(b):
                 st = lib.hs_logprobs_workspace_size(rows, 4, 0, ctypes.byref(ctypes.c_size_t(0)))
             assert st == b.HS_ERR_UNSUPPORTED, (call, st)
             assert b"rows" in lib.hs_last_error()
+
+
+def test_workspace_covers_every_split(b):
+    """A block's 16 bytes of sums and its keys fit the size given for these rows or more, whatever the budget and type."""
+    rng = np.random.default_rng(5)
+    seen = 0
+    for _ in range(4000):
+        rows = int(rng.integers(1, rng.choice([4, 40, 300, 3000])))
+        vocab, top = int(2 ** rng.uniform(0, 20)), int(rng.integers(0, 65))
+        splits = b.lib().hs_logprobs_splits(rows, vocab, int(rng.choice([2, 4])), int(rng.integers(1, 257)))
+        assert 1 <= splits <= 64
+        if splits > 1:
+            seen += 1
+            need = rows * splits * (16 + 8 * top)
+            assert need <= b.hs_logprobs_workspace_size(rows, vocab, top)
+            assert need <= b.hs_logprobs_workspace_size(rows + int(rng.integers(0, 500)), vocab, top)
+    assert seen > 300
+
+
+def test_split_rule(b):
+    """Rows are split where they leave compute units idle and are long enough for a second kernel."""
+    def splits(rows, vocab, bytes_, cus=256):
+        return b.lib().hs_logprobs_splits(rows, vocab, bytes_, cus)
+    assert splits(1, 131072, 2) > 8 and splits(64, 131072, 2) == 4 and splits(64, 131072, 2, 64) == 1
+    assert splits(257, 131072, 2) == 1 and splits(1, 1000, 4) == 1 and splits(128, 32000, 4) == 1
