@@ -11,9 +11,10 @@
 // t = fl(fl(x g) c), c = fl(127 / fl(max |x g|)), four roundings of 2^-24 put t
 // within |t| 2^-22 of its exact value, so rint(t) is the answer unless t lies
 // that close to a border.  Groups with such an element (one row of 3584 in
-// twenty has any) are decided in 64 bits afterwards: 127 x g is exact there (39
-// bits), and its quotient by a (32 bits) is either a border itself, which the
-// division returns exactly, or at least 2^-42 away from it.
+// twenty has any, of bf16 rows with a gain one in six, mostly ties) are decided
+// in 64 bits afterwards: 127 x g is exact there (39 bits), and so are the borders
+// (i + 1/2) a it is compared with.  Products of 16-bit values and rows without a
+// gain are exact in fp32 already; fp32 rows with one are read again.
 //
 // A row stays in the registers of W wavefronts from its one read to its
 // store.  Rows whose products or squares leave fp32's comfortable range, or
@@ -59,6 +60,20 @@ __device__ __forceinline__ int fast_step(float v, float top, float c, float& off
   return int(i);
 }
 
+// rint(127 y / top) of an exact product y (32 bits or less), ties to even, from
+// fast_step's guess: 127 |y| is compared with (i +- 1/2) top, which are exact.
+__device__ __forceinline__ int exact_round(double y, double top, float c) {
+  const double a = 127.0 * fabs(y);
+  double i = rintf(fabsf(float(y)) * c);
+  const bool odd = int(i) & 1;
+  const double hi = (i + 0.5) * top, lo = (i - 0.5) * top;
+  if (a > hi || (a == hi && odd))
+    i += 1.0;
+  else if (a < lo || (a == lo && odd))
+    i -= 1.0;
+  return int(y < 0.0 ? -i : i);
+}
+
 // Whether fast_step may take a row: false also for what is not a number.
 __device__ __forceinline__ bool comfortable(float top, bool with_gain, float ss) {
   return top > 0x1p-100f && top < 0x1p100f && (!with_gain || (ss > 0x1p-80f && ss < 0x1p100f));
@@ -82,8 +97,11 @@ __device__ __forceinline__ V reduce_row(V v, V* lds, F f) {
 template <int W>
 struct RowLds {
   double d[W];
-  float f[W];
   uint32_t u[W];
+  // Of quantize_kernel, rows in turn in one half and the other: a wavefront
+  // that writes a half has passed a barrier behind its last reads.
+  uint32_t top[2][W], near[2][W];
+  float ss[2][W];
 };
 
 // The row from memory, twice, in 64 bits.
@@ -146,12 +164,14 @@ template <typename T, int W, int NG, bool GAIN>
 __global__ __launch_bounds__(W > 1 ? 64 * W : 256) void quantize_kernel(QuantizeArgs a) {
   constexpr int kRows = W > 1 ? 1 : 4;  // rows of a block
   constexpr bool kExact = !GAIN && sizeof(T) == 2;
+  constexpr bool kLocal = !(GAIN && sizeof(T) == 4);  // products and their maximum are exact in fp32
   __shared__ RowLds<W> lds;
   const int wave = threadIdx.x >> 6;
   const int first = W > 1 ? int(threadIdx.x) : int(threadIdx.x & 63);  // the lane's first group; then 64 W on
   const int n_groups = a.d / kVec, rest = n_groups * kVec + first;
   const bool has_rest = first < a.d % kVec;
-  for (int row = blockIdx.x * kRows + (W > 1 ? 0 : wave); row < a.rows; row += gridDim.x * kRows) {
+  int half = 0;
+  for (int row = blockIdx.x * kRows + (W > 1 ? 0 : wave); row < a.rows; row += gridDim.x * kRows, half ^= 1) {
     const T* x = static_cast<const T*>(a.x) + int64_t(row) * a.ldx;
     int8_t* q = a.q + int64_t(row) * a.ldq;
     float y[NG][kVec], y_rest = 0.0f;
@@ -185,8 +205,22 @@ __global__ __launch_bounds__(W > 1 ? 64 * W : 256) void quantize_kernel(Quantize
 #pragma unroll
       for (int e = 0; e < kVec; ++e) top = max(top, magnitude(y[g][e]));
     }
-    top = reduce_row<W>(top, lds.u, [](uint32_t p, uint32_t r) { return max(p, r); });
-    if constexpr (GAIN) ss = reduce_row<W>(ss, lds.f, [](float p, float r) { return p + r; });
+    top = reduce_wave(top, [](uint32_t p, uint32_t r) { return max(p, r); });
+    if constexpr (GAIN) ss = reduce_wave(ss, [](float p, float r) { return p + r; });
+    if constexpr (W > 1) {
+      if ((threadIdx.x & 63) == 0) {
+        lds.top[half][wave] = top;
+        lds.ss[half][wave] = ss;
+      }
+      __syncthreads();
+      top = lds.top[half][0];
+      ss = lds.ss[half][0];
+#pragma unroll
+      for (int w = 1; w < W; ++w) {
+        top = max(top, lds.top[half][w]);
+        ss += lds.ss[half][w];
+      }
+    }
     const float top32 = __uint_as_float(top);
     if (!comfortable(top32, GAIN, ss)) {
       plain_row<T, W>(a, x, q, row, lds);
@@ -197,7 +231,6 @@ __global__ __launch_bounds__(W > 1 ? 64 * W : 256) void quantize_kernel(Quantize
       a.scale[row] = float(double(top32) * r / 127.0);
     }
     const float c = 127.0f / top32;
-    auto step = [&](float v, float& off) { return fast_step<kExact>(v, top32, c, off); };
     uint32_t near = 0;  // groups to decide again; bit NG: the rest
 #pragma unroll
     for (int g = 0; g < NG; ++g) {
@@ -205,38 +238,53 @@ __global__ __launch_bounds__(W > 1 ? 64 * W : 256) void quantize_kernel(Quantize
       int r[kVec];
       float off = 0.0f;
 #pragma unroll
-      for (int e = 0; e < kVec; ++e) r[e] = step(y[g][e], off);
+      for (int e = 0; e < kVec; ++e) r[e] = fast_step<kExact>(y[g][e], top32, c, off);
       near |= uint32_t(off >= 0.5f) << g;
       if (n < n_groups) store_group(q + n * kVec, r);
     }
     if (has_rest) {
       float off = 0.0f;
-      q[rest] = int8_t(step(y_rest, off));
+      q[rest] = int8_t(fast_step<kExact>(y_rest, top32, c, off));
       near |= uint32_t(off >= 0.5f) << NG;
     }
     if constexpr (kExact) continue;
-    uint32_t any = __ballot(near != 0) != 0;
-    if constexpr (W > 1) any = reduce_row<W>(any, lds.u, [](uint32_t p, uint32_t r) { return p | r; });
-    if (!any) continue;
-    // The exact maximum, then the groups in doubt, from memory.
-    double exact = has_rest ? fabs(product(x, a.gain, rest)) : 0.0;
-#pragma unroll 1
-    for (int n = first; n < n_groups; n += 64 * W) {
-      float v[kVec], gain[kVec];
-      load_group(x + n * kVec, v);
-      if constexpr (GAIN) load_group(a.gain + n * kVec, gain);
+    double exact = top32;
+    if constexpr (!kLocal) {
+      uint32_t any = __ballot(near != 0) != 0;
+      if constexpr (W > 1) {
+        if ((threadIdx.x & 63) == 0) lds.near[half][wave] = any;
+        __syncthreads();
 #pragma unroll
-      for (int e = 0; e < kVec; ++e) exact = fmax(exact, fabs(GAIN ? double(v[e]) * double(gain[e]) : double(v[e])));
+        for (int w = 0; w < W; ++w) any |= lds.near[half][w];
+      }
+      if (!any) continue;
+      // The exact maximum.
+      exact = has_rest ? fabs(product(x, a.gain, rest)) : 0.0;
+#pragma unroll 1
+      for (int n = first; n < n_groups; n += 64 * W) {
+        float v[kVec], gain[kVec];
+        load_group(x + n * kVec, v);
+        load_group(a.gain + n * kVec, gain);
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) exact = fmax(exact, fabs(double(v[e]) * double(gain[e])));
+      }
+      exact = reduce_row<W>(exact, lds.d, [](double p, double r) { return fmax(p, r); });
     }
-    exact = reduce_row<W>(exact, lds.d, [](double p, double r) { return fmax(p, r); });
-    if (near >> NG) q[rest] = int8_t(exact_step(product(x, a.gain, rest), exact));
+    // The groups in doubt, from memory.
+    if (near >> NG) q[rest] = int8_t(exact_round(product(x, a.gain, rest), exact, c));
     near &= (1u << NG) - 1;
 #pragma unroll 1
     while (near) {
       const int n = first + 64 * W * __builtin_ctz(near);
       near &= near - 1;
-#pragma unroll 1
-      for (int e = 0; e < kVec; ++e) q[n * kVec + e] = int8_t(exact_step(product(x, a.gain, n * kVec + e), exact));
+      float v[kVec], gain[kVec];
+      int r[kVec];
+      load_group(x + n * kVec, v);
+      if constexpr (GAIN) load_group(a.gain + n * kVec, gain);
+#pragma unroll
+      for (int e = 0; e < kVec; ++e)
+        r[e] = exact_round(GAIN ? double(v[e]) * double(gain[e]) : double(v[e]), exact, c);
+      store_group(q + n * kVec, r);
     }
   }
 }
@@ -384,7 +432,7 @@ __global__ __launch_bounds__(512) void quantize_long_kernel(QuantizeArgs a) {
       if (off >= 0.5f)
 #pragma unroll
         for (int e = 0; e < kVec; ++e)
-          i[e] = exact_step(GAIN ? double(v[e]) * double(gain[e]) : double(v[e]), exact);
+          i[e] = exact_round(GAIN ? double(v[e]) * double(gain[e]) : double(v[e]), exact, c);
       store_group(q + n * kVec, i);
     }
     if (has_rest) q[rest] = int8_t(exact_step(product(x, a.gain, rest), exact));
