@@ -469,12 +469,12 @@ hipError_t launch_type(const QuantizeArgs& a, int cus, hipStream_t s) {
   if (a.d <= 128) return launch_narrow<T, 16>(a, cus, s);
   if (a.d <= 256) return launch_narrow<T, 32>(a, cus, s);
   // Two groups a lane, with wavefronts enough for the row, keep the most loads
-  // in flight: 10515 x 3584 fp32 takes 38 us in 4 x 2 (5.0 TB/s), 44 in 2 x 4
+  // in flight: 10515 x 3584 fp32 takes 37 us in 4 x 2 (5.1 TB/s), 44 in 2 x 4
   // and 51 in 1 x 8.  Past four wavefronts the joins cost more than more
   // groups do: 9000 x 4096 fp32 36 us in 4 x 2, 55 in 8 x 2; 3000 x 18944
-  // fp32 80 us in 8 x 5, 86 in 16 x 3, 92 in 4 x 10.  Short rows need one
-  // (30000 x 1024 fp32: 31 us in 1 x 2, 36 in 2 x 1).  Few rows take 6 us in
-  // any of them.
+  // fp32 72 us in 8 x 5, 86 in 16 x 3, 92 in 4 x 10 (both with three barriers
+  // a row more, which were 8 us in 8 x 5).  Short rows need one (30000 x 1024
+  // fp32: 31 us in 1 x 2, 36 in 2 x 1).  Few rows take 6 us in any of them.
   const int groups = (a.d / kVec + 63) / 64;  // per wavefront if it were one; the rest rides along
   if (groups <= 1) return launch<T, 1, 1>(a, cus, s);
   if (groups <= 2) return launch<T, 1, 2>(a, cus, s);
