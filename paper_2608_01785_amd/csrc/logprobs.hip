@@ -12,8 +12,8 @@
 // (the exponential alone takes four issue slots), so the usual chunk, all of
 // it below m, takes the shortest form: y = z log2(e) - M in one operation with
 // M = m log2(e) rounded, whose rounding error is a factor common to the
-// chunk's sums.  Only a chunk that reaches m (one in c of the first c) keeps
-// F apart and takes exact differences.
+// chunk's sums.  Only a chunk that reaches m (one in c of the first c), or comes
+// under an m beyond 2^20, keeps F apart and takes exact differences.
 //
 // Alternatives cost the loop over the chunks next to nothing: every lane leaves
 // the maximum of its elements of each chunk in LDS.  At the end 64 or 256
@@ -36,6 +36,10 @@ constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kLowest = -3.4028234663852886e38f;  // running maximum before any element
 constexpr float kInf = __builtin_inff();
 constexpr float kFar = -200.0f;  // e^-200 is 0 in fp32: differences are clamped here where 0 * -inf could arise
+// Maxima up to here take the short form of a lower chunk: what rounding m log2(e)
+// takes off is then at most 2^-4, and its power of two next to 1.  It grows with
+// m, past 2^128 from |m| of some 10^9 on, and such a factor times a sum of 0 is NaN.
+constexpr float kFarMaximum = 0x1p20f;
 
 // ---------------------------------------------------------------- running sums
 
@@ -312,8 +316,7 @@ struct Running {
   __device__ __forceinline__ void add(const Chunk<T>& c, float top) {
     constexpr int V = Chunk<T>::kVec;
     float s[4] = {}, f[4] = {}, t[4] = {};
-    // Beyond 1e38 the scaled maximum would leave fp32's range.
-    if (top >= a.m || fabsf(a.m) > 1e38f) {
+    if (top >= a.m || fabsf(a.m) > kFarMaximum) {
       if (top > a.m) {
         rescale(a, top);
         scaled = a.m * kLog2e;

@@ -1,0 +1,61 @@
+"""The answering operators where values, counts and layouts leave the ordinary range, against the float64 reference.
+
+Bounds are those derived beside the operators' own tests.
+"""
+import numpy as np
+import pytest
+
+from tests.gpu_common import require_gpu
+from tests.test_gpu_answer import _check_logprobs, _gen, _t
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def env():
+    torch = require_gpu()
+    from paper_2608_01785_amd import binding
+    ctx = binding.Context(0, budgets=(64, 256))
+    yield torch, binding, ctx
+    torch.cuda.synchronize()
+    ctx.close()
+
+
+# Rows, vocab, CUs: rows whole in a block of four wavefronts, whole in one, and split, with several 4 KB chunks a
+# wavefront in each.
+LAYOUTS = {"four": (40, 20011, 64), "one": (520, 9001, 64), "split": (8, 131072, 64)}
+
+
+def _check_layout(b, name, dtype):
+    rows, vocab, cus = LAYOUTS[name]
+    splits = b.lib().hs_logprobs_splits(rows, vocab, 4 if dtype == "f32" else 2, cus)
+    assert (splits > 1) == (name == "split") and (rows >= 8 * cus) == (name == "one")
+    return rows, vocab, cus
+
+
+@pytest.mark.parametrize("layout", LAYOUTS)
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_large_maxima_before_lower_chunks(env, layout, dtype):
+    """Finite logits of any size: a first chunk that holds the maximum, and chunks far below it or masked."""
+    torch, b, ctx = env
+    rows, vocab, cus = _check_layout(b, layout, dtype)
+    tops = [s * v for v in (2.0 ** 20, 2.0 ** 20 + 2.0 ** 15, 1e7, 5e9, 1e10, 2e10, 1e12, 1e15, 1e30, 1.5e30)
+            for s in (1, -1)]
+    g = _gen(torch, rows)
+    z = torch.randn(rows, vocab, generator=g, device="cuda") * 3
+    for r in range(rows):
+        # Rows in turn over the maxima; eight rows take eight of them, from the fifth on.
+        m = tops[(r + (6 if rows < len(tops) else 0)) % len(tops)]
+        if m < 0:
+            z[r] = -float("inf") if r % 4 < 2 else 4 * m      # masked, or far below
+        z[r, 5] = m
+        z[r, 9::vocab // 3] = m                               # and ties in later chunks
+        z[r, 11] = m - 2 * abs(m) * 2.0 ** -20                # a near value, where the type has one
+    tokens = torch.randint(0, vocab, (rows, 4), generator=g, device="cuda", dtype=torch.int32)
+    tokens[:, 0], tokens[:, 1] = 5, 11
+    _check_logprobs(env, z.to(_t(torch, dtype)), tokens, 20, cus=cus)
+    # The maximum alone.
+    for r in range(rows):
+        m = float(z[r, 5])
+        z[r, 9::vocab // 3] = 2 * m if m < 0 else 0.0
+    _check_logprobs(env, z.to(_t(torch, dtype)), tokens, 20, cus=cus)
