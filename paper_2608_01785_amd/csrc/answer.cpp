@@ -139,6 +139,15 @@ int32_t hs_linear_i8_kernel(int32_t m, int32_t n, int32_t k, int32_t cus, int32_
   return hs::linear_i8_choice(m, n, k, cus, aligned != 0);
 }
 
+// One 16-byte load of an aligned operand (see linear_i8_load): its vector and scalar
+// byte offsets and the resource's bytes, as internal.
+void hs_linear_i8_load(int32_t lane, int32_t l, int32_t stage, int32_t span, int64_t ld, int32_t k, uint32_t out[3]) {
+  const hs::LinearI8Load at = hs::linear_i8_load(hs::linear_i8_offset(lane, ld), lane, l, stage, ld, k);
+  out[0] = at.vector;
+  out[1] = at.scalar;
+  out[2] = hs::linear_i8_records(span, ld, k);
+}
+
 // The blocks a row is split over by hs_logprobs (see logprobs_shape), as internal.
 int32_t hs_logprobs_splits(int32_t rows, int32_t vocab, int32_t elem_bytes, int32_t cus) {
   return hs::logprobs_shape(rows, vocab, elem_bytes, cus).splits;

@@ -10,6 +10,32 @@ constexpr int kLogprobsMaxTop = 64;       // alternatives a row can list: one pe
 constexpr int kLinearI8MaxK = 131071;     // (-128)^2 k stays below 2^31
 constexpr int64_t kLinearI8MaxStride = int64_t(1) << 22;  // 256 rows of an operand stay within 32-bit offsets
 
+// How hs_linear_i8 reads 16-byte aligned operands: in stages of one 128-byte
+// line of K, eight rows to a load, 16 bytes to a lane, through a buffer resource
+// that ends with the k bytes of the last of `span` rows.  The vector offset is
+// what the resource's end is checked against; a scalar offset may or may not
+// count.  So rows and what lies past k are told apart by the vector offset alone,
+// and the scalar offset is the stage's, which stays inside the row.
+struct LinearI8Load {
+  uint32_t vector, scalar;  // byte offsets
+};
+constexpr int kLinearI8Line = 128;
+constexpr uint32_t linear_i8_records(int span, int64_t ld, int k) {
+  return uint32_t(span - 1) * uint32_t(ld) + uint32_t(k);
+}
+// A lane's place in load 0 of stage 0.
+constexpr uint32_t linear_i8_offset(int lane, int64_t ld) {
+  return uint32_t(lane / 8) * uint32_t(ld) + uint32_t(lane % 8 * 16);
+}
+// Load l (rows 8 l .. 8 l + 7) of a stage.  Past k it reads zeros: 2^31 is beyond
+// any resource, with up to 63 rows of stride kLinearI8MaxStride on top as well.
+constexpr LinearI8Load linear_i8_load(uint32_t offset, int lane, int l, int stage, int64_t ld, int k) {
+  const bool past = stage >= k / kLinearI8Line && stage * kLinearI8Line + lane % 8 * 16 >= k;
+  const int last = (k - 1) / kLinearI8Line;
+  return LinearI8Load{(past ? 0x80000000u : offset) + uint32_t(8 * l) * uint32_t(ld),
+                      uint32_t(stage < last ? stage : last) * uint32_t(kLinearI8Line)};
+}
+
 // The kernels of hs_linear_i8: for few rows (32 or 64 a block, by 32 or 64
 // channels), and tiles.
 enum LinearI8Choice {

@@ -132,7 +132,8 @@ __device__ __forceinline__ void store_run(T* p, int h, const float (&lo)[4], con
 // One wave's share of an operand's rows, in stages of C 16-byte chunks of K:
 // load l takes chunk lane % C of row row0 + lane / C + (64 / C) l.
 //   ALIGNED: base, row stride and k are multiples of 16.  A buffer resource
-//   over the rows: what lies past the last row or past k reads zero.
+//   over the rows: what lies past the last row or past k reads zero
+//   (linear_i8_load).
 //   Otherwise (k >= 16): byte addresses, rows past the last read it again (they
 //   are never stored).  The chunk that holds the end of k is read from 16 bytes
 //   before that end, chunks past it from the row's start, and settle() shifts
@@ -140,35 +141,31 @@ __device__ __forceinline__ void store_run(T* p, int h, const float (&lo)[4], con
 template <bool ALIGNED, int C, int L>
 struct Operand {
   static constexpr int kRows = 64 / C, kBytes = 16 * C;  // of a load, and of a row in a stage
+  static_assert(kBytes == kLinearI8Line, "linear_i8_load's layout");
   const int8_t* base;
   __amdgpu_buffer_rsrc_t res;
   uint32_t off[ALIGNED ? 1 : L];
 
   __device__ __forceinline__ void set(const int8_t* p, int64_t ld, int row0, int rows, int k) {
-    const int r = (threadIdx.x & 63) / C, c = threadIdx.x % C;
     if constexpr (ALIGNED) {
       // A wave without rows keeps one (never stored).
       const int first = min(row0, rows - 1), span = min(rows - first, kRows * L);
       base = p + int64_t(first) * ld;
-      res = make_rsrc(base, uint32_t(span - 1) * uint32_t(ld) + uint32_t(k));
-      off[0] = uint32_t(r) * uint32_t(ld) + uint32_t(c * 16);
+      res = make_rsrc(base, linear_i8_records(span, ld, k));
+      off[0] = linear_i8_offset(threadIdx.x & 63, ld);
     } else {
-      const int first = min(row0, rows - 1);
+      const int first = min(row0, rows - 1), r = (threadIdx.x & 63) / C;
       base = p + int64_t(first) * ld;
 #pragma unroll
       for (int l = 0; l < L; ++l) off[l] = uint32_t(min(r + kRows * l, rows - 1 - first)) * uint32_t(ld);
     }
   }
   __device__ __forceinline__ u32x4 load(int l, int stage, int64_t ld, int k) const {
-    const int whole = k / kBytes;  // stages without the end of k
-    const int at = stage * kBytes + int(threadIdx.x % C) * 16;
     if constexpr (ALIGNED) {
-      uint32_t v = off[0];
-      // Past k: an offset outside the resource, which reads zero.
-      if (stage >= whole && at >= k) v = 0x80000000u;
-      const uint32_t s = uint32_t(min(stage, (k - 1) / kBytes)) * kBytes + uint32_t(kRows * l) * uint32_t(ld);
-      return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(res, v, s, 0));
+      const LinearI8Load at = linear_i8_load(off[0], threadIdx.x & 63, l, stage, ld, k);
+      return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(res, at.vector, at.scalar, 0));
     } else {
+      const int at = stage * kBytes + int(threadIdx.x % C) * 16;
       u32x4 v;
       __builtin_memcpy(&v, base + (off[l] + uint32_t(at + 16 <= k ? at : at < k ? k - 16 : 0)), 16);
       return v;

@@ -225,3 +225,28 @@ def test_split_rule(b):
         return b.lib().hs_logprobs_splits(rows, vocab, bytes_, cus)
     assert splits(1, 131072, 2) > 8 and splits(64, 131072, 2) == 4 and splits(64, 131072, 2, 64) == 1
     assert splits(257, 131072, 2) == 1 and splits(1, 1000, 4) == 1 and splits(128, 32000, 4) == 1
+
+
+@pytest.mark.parametrize("ld,k", [(16, 16), (128, 128), (160, 144), (1040, 1040), (4096, 2064), (1 << 22, 512),
+                                  (1 << 22, 131056)])
+def test_aligned_product_loads_stay_in_the_operand(b, ld, k):
+    """Every 16-byte load either lies in a row's k bytes, or its vector offset alone is past the resource's end: what a
+    scalar offset counts for in that check does not matter."""
+    out = (ctypes.c_uint32 * 3)()
+    load = b.lib().hs_linear_i8_load
+    load.argtypes = [ctypes.c_int32] * 4 + [ctypes.c_int64, ctypes.c_int32, ctypes.POINTER(ctypes.c_uint32)]
+    load.restype = None
+    last = (k - 1) // 128
+    stages = sorted({0, 1, 2, last // 2, last - 1, last, last + 1, last + 9} & set(range(last + 10)))
+    for span in (1, 2, 7, 8, 9, 31, 63, 64):
+        for stage in stages:
+            for lane in range(64):
+                for l in range(8):
+                    load(lane, l, stage, span, ld, k, out)
+                    vector, scalar, records = out
+                    row, at = 8 * l + lane // 8, 128 * stage + 16 * (lane % 8)
+                    assert records == (span - 1) * ld + k and scalar < k
+                    if row < span and at < k:
+                        assert vector + scalar == row * ld + at and vector + scalar + 16 <= records
+                    else:
+                        assert vector >= records, (span, stage, lane, l)

@@ -6,7 +6,8 @@ import numpy as np
 import pytest
 
 from tests.gpu_common import require_gpu
-from tests.test_gpu_answer import _check_logprobs, _gen, _t
+from tests.test_gpu_answer import _check_logprobs, _gen, _linear, _t
+from tests.test_gpu_answer_head import KERNELS
 
 pytestmark = pytest.mark.gpu
 
@@ -59,3 +60,25 @@ def test_large_maxima_before_lower_chunks(env, layout, dtype):
         m = float(z[r, 5])
         z[r, 9::vocab // 3] = 2 * m if m < 0 else 0.0
     _check_logprobs(env, z.to(_t(torch, dtype)), tokens, 20, cus=cus)
+
+
+@pytest.mark.parametrize("case", [c for c in KERNELS if c[5]], ids=str)
+def test_aligned_operands_of_the_largest_stride(env, case):
+    """Rows 4 MB apart, the last ones in a tile that they do not fill, against the same rows side by side."""
+    torch, b, ctx = env
+    kind, m, n, k, cus, _ = case
+    assert b.lib().hs_linear_i8_kernel(m, n, k, cus, True) == kind
+    g = _gen(torch, m + n + k)
+    a = torch.randint(-128, 128, (m, k), generator=g, device="cuda", dtype=torch.int8)
+    w = torch.randint(-128, 128, (n, k), generator=g, device="cuda", dtype=torch.int8)
+    sa, sw = torch.rand(m, generator=g, device="cuda"), torch.rand(n, generator=g, device="cuda")
+    near = _linear(env, a, sa, w, sw, "f32", cus=cus)
+
+    def spread(t):
+        v = torch.empty((t.shape[0] - 1) * 2 ** 22 + t.shape[1], dtype=torch.int8, device="cuda")
+        v = v.as_strided(t.shape, (2 ** 22, 1))
+        v.copy_(t)
+        return v
+
+    assert torch.equal(_linear(env, spread(a), sa, spread(w), sw, "f32", cus=cus), near)
+    torch.cuda.empty_cache()
