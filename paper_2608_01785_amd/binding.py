@@ -626,6 +626,26 @@ def _dense(ctx: Context, t, name: str, kinds, *shape) -> Optional[int]:
     return t.data_ptr()
 
 
+def _workspace(ctx: Context, t, n_bytes: Optional[int]) -> Tuple[Optional[int], int]:
+    """(pointer, bytes) of a workspace: a contiguous tensor of any type (its bytes, or fewer where n_bytes says so), a
+    device address with n_bytes, or None."""
+    if t is None:
+        return None, n_bytes or 0
+    if isinstance(t, int):
+        if n_bytes is None:
+            raise ValueError("a workspace address needs ws_bytes")
+        return t, n_bytes
+    if t.get_device() != ctx.device:
+        raise ValueError(f"workspace is on {t.device}, the context on cuda:{ctx.device}")
+    if not t.is_contiguous():
+        raise ValueError("workspace is not contiguous")
+    if n_bytes is None:
+        return t.data_ptr(), t.nbytes
+    if n_bytes > t.nbytes:
+        raise ValueError(f"workspace has {t.nbytes} bytes, ws_bytes is {n_bytes}")
+    return t.data_ptr(), n_bytes
+
+
 def hs_quantize_rows(ctx: Context, x, q, scale, gain=None, eps: float = 1e-6, cu_budget: int = 256,
                      stream=None) -> None:
     """x [rows, d] (fp32, bf16 or fp16) -> q int8 [rows, d] and scale fp32 [rows]; gain: bf16 [d] (RMSNorm) or None."""
@@ -677,14 +697,13 @@ def hs_logprobs(ctx: Context, logits, tokens=None, token_logprobs=None, entropy=
         raise ValueError("tokens and token_logprobs, top_logprobs and top_tokens go together")
     n = 0 if tokens is None else tokens.shape[-1]
     k = 0 if top_tokens is None else top_tokens.shape[-1]
-    if ws_bytes is None:
-        ws_bytes = 0 if workspace is None else workspace.nbytes
+    ws, ws_bytes = _workspace(ctx, workspace, ws_bytes)
     f32, i32 = _Kinds.f32, _Kinds.i32
     status = lib().hs_logprobs(
         ctx.handle, pz, _Kinds.rows[logits.dtype], ld, rows, vocab, _dense(ctx, tokens, "tokens", i32, rows, n), n,
         _dense(ctx, token_logprobs, "token_logprobs", f32, rows, n), _dense(ctx, entropy, "entropy", f32, rows), k,
         _dense(ctx, top_logprobs, "top_logprobs", f32, rows, k), _dense(ctx, top_tokens, "top_tokens", i32, rows, k),
-        cu_budget, _ptr(stream), _ptr(workspace), ws_bytes)
+        cu_budget, _ptr(stream), ws, ws_bytes)
     if status:
         _check(status)
 

@@ -250,3 +250,31 @@ def test_aligned_product_loads_stay_in_the_operand(b, ld, k):
                         assert vector + scalar == row * ld + at and vector + scalar + 16 <= records
                     else:
                         assert vector >= records, (span, stage, lane, l)
+
+
+def test_binding_refuses_workspaces_that_do_not_fit(b):
+    """Before the library sees a pointer: on the host or another device, with gaps, of fewer bytes than claimed."""
+    import torch
+
+    class Host:
+        handle, device = None, -1   # CPU tensors report device -1
+
+    class Gpu:
+        handle, device = None, 0
+
+    z, e = torch.zeros(2, 70000), torch.zeros(2)
+    need = b.hs_logprobs_workspace_size(2, 70000, 0)
+    ws = torch.zeros(need, dtype=torch.uint8)
+    with pytest.raises(ValueError, match="workspace is on cpu"):
+        b._workspace(Gpu, ws, None)
+    for bad, n, text in ((ws[::2], None, "not contiguous"), (ws[:1].expand(need), None, "not contiguous"),
+                         (ws, need + 1, "ws_bytes is"), (0x1000, None, "needs ws_bytes")):
+        with pytest.raises(ValueError, match=text):
+            b.hs_logprobs(Host, z, entropy=e, workspace=bad, ws_bytes=n)
+    for good, n in ((ws, None), (ws, need), (ws.view(torch.int32) if need % 4 == 0 else ws, None), (0x1000, need)):
+        with pytest.raises(b.HorizonError, match="context is null"):
+            b.hs_logprobs(Host, z, entropy=e, workspace=good, ws_bytes=n)
+    for short, n in ((ws[:need - 1], None), (ws, need - 1), (None, None)):
+        with pytest.raises(b.HorizonError) as err:
+            b.hs_logprobs(Host, z, entropy=e, workspace=short, ws_bytes=n)
+        assert err.value.status == b.HS_ERR_WORKSPACE

@@ -82,3 +82,13 @@ def test_aligned_operands_of_the_largest_stride(env, case):
 
     assert torch.equal(_linear(env, spread(a), sa, spread(w), sw, "f32", cus=cus), near)
     torch.cuda.empty_cache()
+
+
+def test_workspaces_elsewhere_are_refused(env):
+    torch, b, ctx = env
+    z, e = torch.randn(2, 70000, device="cuda"), torch.empty(2, device="cuda")
+    need = b.hs_logprobs_workspace_size(2, 70000, 0)
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    for bad, text in ((ws.cpu(), "workspace is on cpu"), (ws[:1].expand(need), "not contiguous")):
+        with pytest.raises(ValueError, match=text):
+            b.hs_logprobs(ctx, z, entropy=e, workspace=bad)
