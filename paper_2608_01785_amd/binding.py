@@ -600,6 +600,11 @@ def _refuse(ctx: Context, t, name: str, kinds, ndim: int) -> None:
     raise ValueError(f"{name} is on {t.device}, the context on cuda:{ctx.device}")
 
 
+# Counts are 32 bits wide in the ABI.  Larger ones are passed as the largest, which every call refuses, and not
+# without their upper bits.
+_INT32_MAX = 2 ** 31 - 1
+
+
 def _matrix(ctx: Context, t, name: str, kinds) -> Tuple[int, int, int, int]:
     """(pointer, row stride, rows, columns) of a 2-d tensor whose rows are contiguous."""
     shape = t.shape
@@ -609,6 +614,8 @@ def _matrix(ctx: Context, t, name: str, kinds) -> Tuple[int, int, int, int]:
     ld, step = t.stride()
     if step != 1 and cols > 1 and rows > 0:
         raise ValueError(f"the rows of {name} are not contiguous (stride {step})")
+    if rows > _INT32_MAX or cols > _INT32_MAX:
+        rows, cols = min(rows, _INT32_MAX), min(cols, _INT32_MAX)
     return t.data_ptr(), (ld if rows > 1 else max(cols, 1)), rows, cols
 
 
@@ -619,7 +626,7 @@ def _dense(ctx: Context, t, name: str, kinds, *shape) -> Optional[int]:
     size = t.shape
     if t.dtype not in kinds or len(size) != len(shape) or t.get_device() != ctx.device:
         _refuse(ctx, t, name, kinds, len(shape))
-    if size != shape:
+    if size != shape and tuple(min(n, _INT32_MAX) for n in size) != shape:
         raise ValueError(f"{name} has shape {tuple(size)}, expected {shape}")
     if not t.is_contiguous():
         raise ValueError(f"{name} is not contiguous")
@@ -681,6 +688,7 @@ def hs_linear_i8(ctx: Context, a, a_scale, w, w_scale, out, bias=None, cu_budget
 
 def hs_logprobs_workspace_size(max_rows: int, vocab: int, top_k: int = 0) -> int:
     n = ctypes.c_size_t(0)
+    max_rows, vocab, top_k = (min(v, _INT32_MAX) for v in (max_rows, vocab, top_k))
     _check(lib().hs_logprobs_workspace_size(max_rows, vocab, top_k, ctypes.byref(n)))
     return int(n.value)
 
@@ -695,8 +703,8 @@ def hs_logprobs(ctx: Context, logits, tokens=None, token_logprobs=None, entropy=
     pz, ld, rows, vocab = _matrix(ctx, logits, "logits", _Kinds.rows)
     if (tokens is None) != (token_logprobs is None) or (top_logprobs is None) != (top_tokens is None):
         raise ValueError("tokens and token_logprobs, top_logprobs and top_tokens go together")
-    n = 0 if tokens is None else tokens.shape[-1]
-    k = 0 if top_tokens is None else top_tokens.shape[-1]
+    n = 0 if tokens is None else min(tokens.shape[-1], _INT32_MAX)
+    k = 0 if top_tokens is None else min(top_tokens.shape[-1], _INT32_MAX)
     ws, ws_bytes = _workspace(ctx, workspace, ws_bytes)
     f32, i32 = _Kinds.f32, _Kinds.i32
     status = lib().hs_logprobs(

@@ -278,3 +278,33 @@ def test_binding_refuses_workspaces_that_do_not_fit(b):
         with pytest.raises(b.HorizonError) as err:
             b.hs_logprobs(Host, z, entropy=e, workspace=short, ws_bytes=n)
         assert err.value.status == b.HS_ERR_WORKSPACE
+
+
+def test_binding_refuses_counts_beyond_32_bits(b):
+    """2^32 rows (columns, tokens, alternatives) and some are not passed as some.  Meta tensors: no memory."""
+    import torch
+
+    class Ctx:
+        handle, device = None, -1   # as CPU and meta tensors report
+
+    def meta(*shape, dtype=torch.float32):
+        return torch.empty(shape, dtype=dtype, device="meta")
+
+    n, i8, i32 = 2 ** 32 + 4, torch.int8, torch.int32
+    with pytest.raises(b.HorizonError, match="rows: at most"):
+        b.hs_quantize_rows(Ctx, meta(n, 8), meta(n, 8, dtype=i8), meta(n))
+    with pytest.raises(b.HorizonError, match="rows: at most"):
+        b.hs_logprobs(Ctx, meta(n, 8), entropy=meta(n))
+    for m, w, k in ((n, 8, 16), (8, n, 16), (8, 8, n)):
+        with pytest.raises(b.HorizonError, match="rows: at most|32-bit sums|row strides"):
+            b.hs_linear_i8(Ctx, meta(m, k, dtype=i8), meta(m), meta(w, k, dtype=i8), meta(w), meta(m, w))
+    with pytest.raises(b.HorizonError, match="top_k"):
+        b.hs_logprobs(Ctx, meta(2, 8), top_logprobs=meta(2, n), top_tokens=meta(2, n, dtype=i32))
+    for counts in ((n, 8, 0), (8, n, 0), (8, 8, n)):
+        if counts[1] == n:
+            assert b.hs_logprobs_workspace_size(*counts) >= b.hs_logprobs_workspace_size(8, 2 ** 30, 0)
+        else:
+            with pytest.raises(b.HorizonError, match="rows: at most|top_k"):
+                b.hs_logprobs_workspace_size(*counts)
+    st, msg = logprobs(b, nt=2 ** 31 - 1)   # what 2^31 given tokens a row and more are passed as
+    assert st == INVALID and "tokens: row stride" in msg
