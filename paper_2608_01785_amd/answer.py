@@ -79,8 +79,8 @@ class AnswerHead:
             raise ValueError(f"y has shape {tuple(y.shape)}, expected (rows, {self.hidden})")
         rows = y.shape[0]
         for name, t in (("tokens", tokens), *vars(out).items()):
-            if t is not None and t.shape[0] != rows:
-                raise ValueError(f"{name} has {t.shape[0]} rows, y {rows}")
+            if t is not None and t.shape[:1] != (rows,):
+                raise ValueError(f"{name} has {t.shape[0] if t.shape else 'no'} rows, y {rows}")
         for first in range(0, rows, self.max_rows):
             part = slice(first, min(first + self.max_rows, rows))
             n = part.stop - first

@@ -703,8 +703,8 @@ def hs_logprobs(ctx: Context, logits, tokens=None, token_logprobs=None, entropy=
     pz, ld, rows, vocab = _matrix(ctx, logits, "logits", _Kinds.rows)
     if (tokens is None) != (token_logprobs is None) or (top_logprobs is None) != (top_tokens is None):
         raise ValueError("tokens and token_logprobs, top_logprobs and top_tokens go together")
-    n = 0 if tokens is None else min(tokens.shape[-1], _INT32_MAX)
-    k = 0 if top_tokens is None else min(top_tokens.shape[-1], _INT32_MAX)
+    n = 0 if tokens is None or not tokens.shape else min(tokens.shape[-1], _INT32_MAX)
+    k = 0 if top_tokens is None or not top_tokens.shape else min(top_tokens.shape[-1], _INT32_MAX)
     ws, ws_bytes = _workspace(ctx, workspace, ws_bytes)
     f32, i32 = _Kinds.f32, _Kinds.i32
     status = lib().hs_logprobs(

@@ -65,3 +65,13 @@ def test_refusals():
         _head(top_k=65)
     with pytest.raises(binding.HorizonError, match="context is null"):
         head(y, out)
+
+
+def test_tensors_without_rows_are_refused():
+    head = _head(max_rows=3, top_k=2)
+    y, out = torch.zeros(4, 8), head.outputs(4)
+    with pytest.raises(ValueError, match="tokens has no rows, y 4"):
+        head(y, out, torch.tensor(1, dtype=torch.int32))
+    out.entropy = torch.tensor(0.0)
+    with pytest.raises(ValueError, match="entropy has no rows, y 4"):
+        head(y, out)

@@ -308,3 +308,19 @@ def test_binding_refuses_counts_beyond_32_bits(b):
                 b.hs_logprobs_workspace_size(*counts)
     st, msg = logprobs(b, nt=2 ** 31 - 1)   # what 2^31 given tokens a row and more are passed as
     assert st == INVALID and "tokens: row stride" in msg
+
+
+def test_binding_refuses_tensors_without_dimensions(b):
+    import torch
+
+    class Ctx:
+        handle, device = None, -1
+
+    z, one = torch.zeros(2, 8), torch.tensor(3, dtype=torch.int32)
+    with pytest.raises(ValueError, match="tokens has 0 dimensions"):
+        b.hs_logprobs(Ctx, z, tokens=one, token_logprobs=torch.zeros(2, 1))
+    with pytest.raises(ValueError, match="top_tokens has 0 dimensions|top_logprobs has shape"):
+        b.hs_logprobs(Ctx, z, top_tokens=one, top_logprobs=torch.zeros(2, 1))
+    for bad in (torch.tensor(1.0), torch.zeros(2)):
+        with pytest.raises(ValueError, match="dimensions"):
+            b.hs_logprobs(Ctx, bad)
