@@ -210,7 +210,8 @@ class Algorithm1:
             ends = ends.to(self.y.device, non_blocking=True)
             self.torch.index_select(self.y, 0, ends - 1, out=self.last[:n])
         out = dataclasses.replace(self.head_out, **{k: t[:n] for k, t in vars(self.head_out).items() if t is not None})
-        self.head(self.last[:n], out, cu_budget=s_shared)
+        # The batch's stream itself: a head made on another context has streams of its own.
+        self.head(self.last[:n], out, cu_budget=s_shared, stream=stream.cuda_stream)
         return out
 
     def _poll(self):

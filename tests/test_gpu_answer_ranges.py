@@ -6,8 +6,9 @@ import numpy as np
 import pytest
 
 from tests.gpu_common import require_gpu
-from tests.test_gpu_answer import _check_logprobs, _gen, _linear, _t
-from tests.test_gpu_answer_head import KERNELS
+from tests.test_gpu_algorithm1 import LADDER
+from tests.test_gpu_answer import _check_logprobs, _gen, _linear, _np, _t
+from tests.test_gpu_answer_head import KERNELS, _check, _loop_with, _new_head
 
 pytestmark = pytest.mark.gpu
 
@@ -92,3 +93,28 @@ def test_workspaces_elsewhere_are_refused(env):
     for bad, text in ((ws.cpu(), "workspace is on cpu"), (ws[:1].expand(need), "not contiguous")):
         with pytest.raises(ValueError, match=text):
             b.hs_logprobs(ctx, z, entropy=e, workspace=bad)
+
+
+def test_the_serving_loop_takes_a_head_of_another_context(env):
+    """The head's work belongs on the batch's stream, whatever levels and streams the head's own context has."""
+    torch, b, ctx = env
+    loop_ctx = b.Context(0, budgets=LADDER + (256,))
+    head = _new_head(env, max_rows=3)            # a context without the ladder
+    loop, reqs, _, _ = _loop_with((torch, b, loop_ctx), "joint", head, n_req=6, seed=6)
+    loop.begin()
+    try:
+        for _ in range(200):
+            rec = loop.step()
+            if rec is None:
+                break
+            if rec.batch:
+                y = _np(loop.y[torch.tensor(rec.offsets[1:], device="cuda") - 1])
+                got = [loop.answers[reqs[i].rid] for i in rec.batch]
+                _check(head, y, {"entropy": np.array([a.entropy for a in got]),
+                                 "top_tokens": np.array([a.tokens for a in got]),
+                                 "top_logprobs": np.array([a.logprobs for a in got])})
+    finally:
+        loop.close()
+    assert sorted(loop.answers) == sorted(r.rid for r in reqs)
+    torch.cuda.synchronize()
+    loop_ctx.close()
