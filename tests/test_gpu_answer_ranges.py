@@ -5,9 +5,10 @@ Bounds are those derived beside the operators' own tests.
 import numpy as np
 import pytest
 
+from oracle import answer as A
 from tests.gpu_common import require_gpu
 from tests.test_gpu_algorithm1 import LADDER
-from tests.test_gpu_answer import _check_logprobs, _gen, _linear, _np, _t
+from tests.test_gpu_answer import U, _check_logprobs, _close, _gen, _linear, _np, _t
 from tests.test_gpu_answer_head import KERNELS, _check, _loop_with, _new_head
 
 pytestmark = pytest.mark.gpu
@@ -118,3 +119,67 @@ def test_the_serving_loop_takes_a_head_of_another_context(env):
     assert sorted(loop.answers) == sorted(r.rid for r in reqs)
     torch.cuda.synchronize()
     loop_ctx.close()
+
+
+# ---------------------------------------------------------------------------- paths of the head and of long lists
+
+def _check_answers(got, z, tokens, top):
+    """Log probabilities of exactly these logits, within the bounds of the operators' own tests."""
+    ref = A.logprobs(z, tokens, top)
+    np.testing.assert_array_equal(got["top_tokens"].cpu().numpy(), ref["top_tokens"])
+    n = 32 + -(-z.shape[1] // 2048) + 40
+    s, t1, t2 = ref["s"], ref["t1"], ref["t2"]
+    log_s = ((n + 4) * s / (1 + s) + 3 * t1 + 2 * np.log1p(s)) * U
+    for name, key in (("token_logprobs", "token"), ("top_logprobs", "top")):
+        size = np.where(np.isfinite(ref[key]), np.abs(ref[key]), 0)
+        _close(name, got[name], ref[key], log_s[:, None] + 4 * U * size + z.shape[1] * 2.0 ** -126)
+    _close("entropy", got["entropy"], ref["entropy"],
+           ((n + 8) * (t1 + s / (1 + s)) + 3 * t2 + 4 * ref["entropy"]) * U + 128 * z.shape[1] * 2.0 ** -126)
+
+
+@pytest.mark.parametrize("with_bias", [False, True])
+@pytest.mark.parametrize("logits", ["f32", "bf16", "f16"])
+def test_head_steps_one_after_another(env, logits, with_bias):
+    """Each step of a pass against the reference of the step before it, so 16-bit logits hide nothing of what follows."""
+    torch, b, ctx = env
+    vocab, rows = 2501, 13
+    g = _gen(torch, 77)
+    bias = torch.randn(vocab, generator=g, device="cuda").bfloat16() if with_bias else None
+    head = _new_head(env, vocab=vocab, max_rows=16, bias=bias, logits=_t(torch, logits))
+    assert (head.bias is not None) == with_bias
+    y = torch.randn(rows, head.hidden, generator=g, device="cuda") * 30
+    y[2] = 0.0
+    y[3, 5] = float("nan")
+    tokens = torch.randint(-1, vocab, (rows, 3), generator=g, device="cuda", dtype=torch.int32)
+    out = head.outputs(rows, 3)
+    torch.cuda.synchronize()
+    head(y, out, tokens)
+    torch.cuda.synchronize()
+    q, _ = A.quantize_rows(_np(y), _np(head.gain), 1e-6)
+    np.testing.assert_array_equal(head.q[:rows].cpu().numpy(), q)
+    z = A.linear_i8(q, head.q_scale[:rows].cpu().numpy(), head.w.cpu().numpy(), head.w_scale.cpu().numpy(),
+                    None if bias is None else bias.float().cpu().numpy())
+    z = torch.from_numpy(z).to(head.logits.dtype)
+    same = (head.logits[:rows].cpu() == z) | (head.logits[:rows].cpu().isnan() & z.isnan())
+    assert bool(same.all())
+    _check_answers(vars(out), z.double().numpy(), tokens.cpu().numpy(), head.top_k)
+
+
+@pytest.mark.parametrize("layout", LAYOUTS)
+@pytest.mark.parametrize("dtype", ["f32", "f16"])
+@pytest.mark.parametrize("given", [64, 65, 130])
+def test_more_given_tokens_than_lanes(env, layout, dtype, given):
+    """Lists of given tokens beyond a wavefront's lanes, with -1 and tokens outside the vocabulary among the later ones."""
+    torch, b, ctx = env
+    rows, vocab, cus = _check_layout(b, layout, dtype)
+    g = _gen(torch, given)
+    z = (torch.randn(rows, vocab, generator=g, device="cuda") * 3).to(_t(torch, dtype))
+    z[1] = -float("inf")
+    z[2, 7] = float("nan")
+    tokens = torch.randint(0, vocab, (rows, given), generator=g, device="cuda", dtype=torch.int32)
+    tokens[:, -1], tokens[:, given // 2] = -1, -1
+    tokens[::2, -2], tokens[1::2, -2] = vocab, -7
+    if given > 65:
+        tokens[:, 64], tokens[:, 127], tokens[:, 128] = vocab + 5, 0, -1
+    _check_logprobs(env, z, tokens, 20, cus=cus)
+    _check_logprobs(env, z, tokens, 0, cus=cus)
