@@ -16,6 +16,12 @@
 // (i + 1/2) a it is compared with.  Products of 16-bit values and rows without a
 // gain are exact in fp32 already; fp32 rows with one are read again.
 //
+// The scale takes the largest product as fp32 and the sum of squares in fp32: at
+// most 8 NG + W + 6 roundings on a square's way, halved by the root, and two more,
+// 15 half steps for 3584 columns (the tests hold it to that).  64-bit sums would be
+// two more instructions an element of a kernel that memory bounds.  Rows beyond a
+// block's registers, whose sums are longer, have 64 bits.
+//
 // A row stays in the registers of W wavefronts from its one read to its
 // store.  Rows whose products or squares leave fp32's comfortable range, or
 // are not finite, take a second, plain path in 64 bits.

@@ -8,7 +8,7 @@ import pytest
 from oracle import answer as A
 from tests.gpu_common import require_gpu
 from tests.test_gpu_algorithm1 import LADDER
-from tests.test_gpu_answer import U, _check_logprobs, _close, _gen, _linear, _np, _t
+from tests.test_gpu_answer import EPS, U, _check_logprobs, _close, _gen, _linear, _np, _quantize, _t
 from tests.test_gpu_answer_head import KERNELS, _check, _loop_with, _new_head
 
 pytestmark = pytest.mark.gpu
@@ -183,3 +183,43 @@ def test_more_given_tokens_than_lanes(env, layout, dtype, given):
         tokens[:, 64], tokens[:, 127], tokens[:, 128] = vocab + 5, 0, -1
     _check_logprobs(env, z, tokens, 20, cus=cus)
     _check_logprobs(env, z, tokens, 0, cus=cus)
+
+
+# ---------------------------------------------------------------------------- how near the scales are
+
+def _scale_bound(d, dtype, norm):
+    """Half steps of fp32 that a row's scale may be off by.
+
+    Without a gain: the last rounding.  With one: that, the rounding of an fp32 row's largest product, and half of what
+    the sum of squares is off by, since its root is taken.  A square passes the additions of its lane (8 a group and
+    the rest's product), 3 to 6 levels of lanes and the other wavefronts; beyond 32768 columns sums are 64 bits but
+    for a group's 8."""
+    if not norm:
+        return 1
+    product = 1 if dtype == "f32" else 0
+    if d > 32768 + 7:
+        return 1 + 8 / 2
+    if d <= 256:
+        return 1 + product + (8 + 1 + (3 if d <= 64 else 4 if d <= 128 else 5)) / 2
+    per_wave = -(-(d // 8) // 64)
+    w, ng = next(v for most, v in ((1, (1, 1)), (2, (1, 2)), (4, (2, 2)), (8, (4, 2)), (16, (4, 4)), (32, (8, 4)),
+                                   (40, (8, 5)), (64, (16, 4))) if per_wave <= most)
+    return 1 + product + (8 * ng + 1 + 6 + w - 1) / 2
+
+
+@pytest.mark.parametrize("d", [64, 100, 256, 500, 1024, 1500, 3584, 8192, 16384, 18944, 30001, 40000])
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("norm", [False, True])
+def test_scales_are_as_near_as_their_roundings(env, d, dtype, norm):
+    """Ordinary rows, rows of one value (whose sums are all off to the same side) and rows of a few large ones."""
+    torch, b, ctx = env
+    g = _gen(torch, d)
+    x = torch.randn(48, d, generator=g, device="cuda")
+    x[16:32] = torch.rand(16, 1, generator=g, device="cuda") + 0.1
+    x[32:] *= 1 + 30 * (torch.rand(d, generator=g, device="cuda") < 0.003)
+    x = x.to(_t(torch, dtype))
+    gain = (1 + 0.3 * torch.randn(d, generator=g, device="cuda")).bfloat16() if norm else None
+    q, s = _quantize(env, x, gain)
+    _, ref = A.quantize_rows(_np(x), None if gain is None else _np(gain), float(np.float32(EPS)))
+    off = np.abs(s.double().cpu().numpy() / ref - 1) / U
+    assert off.max() <= _scale_bound(d, dtype, norm) * (1 + 1e-5), off.max()
