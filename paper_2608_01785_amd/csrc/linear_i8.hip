@@ -24,8 +24,8 @@
 // memory's latency, have registers for D = 4: 128 x 4608 x 3584 11.4 us against 14.0.
 //
 // The grid is persistent and the stages of a block's tiles form one sequence:
-// the last four stages of a tile already fetch the next one's first four, and
-// its epilogue runs under those loads.  An epilogue reads no memory: a tile's
+// the last D stages of a tile already fetch the next one's first D (four of the 64
+// x 64 tiles, two of the others), and its epilogue runs under those loads.  An epilogue reads no memory: a tile's
 // scales and bias come into LDS during the epilogue before it (stores count
 // against the same completion counter as loads, so a load between them would
 // wait for them; with such loads an epilogue took 18 us).
@@ -50,16 +50,15 @@ __device__ __forceinline__ i32x16 mfma32_i8(const u32x4& a, const u32x4& b, cons
   return __builtin_amdgcn_mfma_i32_32x32x32_i8(__builtin_bit_cast(i32x4, a), __builtin_bit_cast(i32x4, b), c, 0, 0, 0);
 }
 
-// 16-byte chunk c of row r of an LDS image whose rows hold C chunks sits at
-// physical chunk phys<C>(r, c), so that a pass of 16 lanes, which reads one
-// logical chunk of 16 consecutive rows, touches each of the 64 banks once.
-//   C = 4: (r & 3, phys) is distinct for all 16 rows.
-//   C = 8: odd rows start on bank 32, so bits 1 .. 3 of r permute the chunks;
-//   bit 0 keeps the writes of two rows in different halves.
-template <int C>
-__device__ __forceinline__ int phys(int r, int c) {
-  return C == 4 ? c ^ (((r >> 1) ^ (r >> 2)) & 3) : c ^ ((r >> 1) & 7) ^ ((r & 1) << 2);
-}
+// A stage holds one 128-byte line of K of every row, in 16-byte chunks; a load of
+// 64 lanes takes eight rows of it.
+constexpr int kLine = kLinearI8Line, kChunks = kLine / 16, kLoadRows = 64 / kChunks;
+
+// Chunk c of row r of an LDS image of lines sits at physical chunk phys(r, c), so
+// that a pass of 16 lanes, which reads one logical chunk of 16 consecutive rows,
+// touches each of the 64 banks once: odd rows start on bank 32, so bits 1 .. 3 of
+// r permute the chunks, and bit 0 keeps the writes of two rows in different halves.
+__device__ __forceinline__ int phys(int r, int c) { return c ^ ((r >> 1) & 7) ^ ((r & 1) << 2); }
 
 // ---------------------------------------------------------------- epilogue
 
@@ -129,8 +128,8 @@ __device__ __forceinline__ void store_run(T* p, int h, const float (&lo)[4], con
 
 // ---------------------------------------------------------------- tiles
 
-// One wave's share of an operand's rows, in stages of C 16-byte chunks of K:
-// load l takes chunk lane % C of row row0 + lane / C + (64 / C) l.
+// One wave's share of an operand's rows: load l of a stage takes chunk lane % 8 of
+// row row0 + lane / 8 + 8 l.
 //   ALIGNED: base, row stride and k are multiples of 16.  A buffer resource
 //   over the rows: what lies past the last row or past k reads zero
 //   (linear_i8_load).
@@ -138,10 +137,8 @@ __device__ __forceinline__ void store_run(T* p, int h, const float (&lo)[4], con
 //   are never stored).  The chunk that holds the end of k is read from 16 bytes
 //   before that end, chunks past it from the row's start, and settle() shifts
 //   and clears them once they are there, so that no load waits for another.
-template <bool ALIGNED, int C, int L>
+template <bool ALIGNED, int L>
 struct Operand {
-  static constexpr int kRows = 64 / C, kBytes = 16 * C;  // of a load, and of a row in a stage
-  static_assert(kBytes == kLinearI8Line, "linear_i8_load's layout");
   const int8_t* base;
   __amdgpu_buffer_rsrc_t res;
   uint32_t off[ALIGNED ? 1 : L];
@@ -149,15 +146,15 @@ struct Operand {
   __device__ __forceinline__ void set(const int8_t* p, int64_t ld, int row0, int rows, int k) {
     if constexpr (ALIGNED) {
       // A wave without rows keeps one (never stored).
-      const int first = min(row0, rows - 1), span = min(rows - first, kRows * L);
+      const int first = min(row0, rows - 1), span = min(rows - first, kLoadRows * L);
       base = p + int64_t(first) * ld;
       res = make_rsrc(base, linear_i8_records(span, ld, k));
       off[0] = linear_i8_offset(threadIdx.x & 63, ld);
     } else {
-      const int first = min(row0, rows - 1), r = (threadIdx.x & 63) / C;
+      const int first = min(row0, rows - 1), r = (threadIdx.x & 63) / kChunks;
       base = p + int64_t(first) * ld;
 #pragma unroll
-      for (int l = 0; l < L; ++l) off[l] = uint32_t(min(r + kRows * l, rows - 1 - first)) * uint32_t(ld);
+      for (int l = 0; l < L; ++l) off[l] = uint32_t(min(r + kLoadRows * l, rows - 1 - first)) * uint32_t(ld);
     }
   }
   __device__ __forceinline__ u32x4 load(int l, int stage, int64_t ld, int k) const {
@@ -165,20 +162,20 @@ struct Operand {
       const LinearI8Load at = linear_i8_load(off[0], threadIdx.x & 63, l, stage, ld, k);
       return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(res, at.vector, at.scalar, 0));
     } else {
-      const int at = stage * kBytes + int(threadIdx.x % C) * 16;
+      const int at = stage * kLine + int(threadIdx.x % kChunks) * 16;
       u32x4 v;
       __builtin_memcpy(&v, base + (off[l] + uint32_t(at + 16 <= k ? at : at < k ? k - 16 : 0)), 16);
       return v;
     }
   }
   // Whether a stage's chunks need settle().
-  __device__ __forceinline__ static bool ends(int stage, int k) { return !ALIGNED && stage >= k / kBytes; }
+  __device__ __forceinline__ static bool ends(int stage, int k) { return !ALIGNED && stage >= k / kLine; }
   // The chunk as its stage holds it, from what load() brought.
   __device__ __forceinline__ u32x4 settle(u32x4 v, int stage, int k) const {
     if constexpr (ALIGNED) {
       return v;
     } else {
-      const int n = k - stage * kBytes - int(threadIdx.x % C) * 16;  // bytes of the chunk that k holds
+      const int n = k - stage * kLine - int(threadIdx.x % kChunks) * 16;  // bytes of the chunk that k holds
       if (n <= 0) return u32x4{0, 0, 0, 0};
       if (n >= 16) return v;
       // The chunk's n bytes came last.
@@ -191,14 +188,13 @@ struct Operand {
   }
 };
 
-template <int TYPE, bool ALIGNED, int C, int D, int WN, int WM, int NS, int MT>
+template <int TYPE, bool ALIGNED, int D, int WN, int WM, int NS, int MT>
 __global__ __launch_bounds__(WN * WM * 64, WN * WM == 8 ? 1 : NS * MT == 1 ? 4 : 2) void linear_kernel(LinearI8Args a) {
   constexpr int kWaves = WN * WM, kHalf = kWaves / 2;
   constexpr int BN = 32 * NS * WN, BM = 32 * MT * WM;
-  constexpr int BK = 16 * C, kSteps = C / 2;  // bytes of K per stage, and its steps
+  constexpr int BK = kLine, kSteps = BK / 32;  // bytes of K per stage, and its steps
   constexpr int kUnroll = D;                  // stages in flight, and per loop body
   static_assert(D % 2 == 0, "a body's buffers alternate");
-  constexpr int kLoadRows = 64 / C;           // rows of a load
   static_assert(BN == BM && BN % (16 * kHalf) == 0, "tile split");
   constexpr int L = BN / (kLoadRows * kHalf);  // 1 KB loads per wave and stage
   constexpr int kTile = BN * BK;
@@ -269,7 +265,7 @@ __global__ __launch_bounds__(WN * WM * 64, WN * WM == 8 ? 1 : NS * MT == 1 ? 4 :
   const int8_t* src = w_wave ? a.w : a.a;
   const int64_t ld = w_wave ? a.ldw : a.lda;
   const int rows = w_wave ? a.n : a.m, wave_row = wave % kHalf * kLoadRows * L;
-  Operand<ALIGNED, C, L> op;
+  Operand<ALIGNED, L> op;
   auto set_op = [&](const Unit& u) {
     int row0 = w_wave ? u.tn * BN + wave_row : u.tm * BM + wave_row;
     if (!w_wave && u.half >= 0) row0 = wave_row < BM / 2 ? row0 + u.half * (BM / 2) : rows;
@@ -285,15 +281,15 @@ __global__ __launch_bounds__(WN * WM * 64, WN * WM == 8 ? 1 : NS * MT == 1 ? 4 :
   auto turned = [&](int stage, int by) { return stage + by < KP ? stage + by : stage + by - KP; };
 
   u32x4 ring[kUnroll][L];  // stage t in slot t % kUnroll
-  // Load l holds image rows wave_row + kLoadRows l + lane / C; phys() repeats
-  // with 16 of them.
-  const int put_row = wave_row + lane / C;
+  // Load l holds image rows wave_row + 8 l + lane / 8; phys() repeats with 16 of
+  // them.
+  const int put_row = wave_row + lane / kChunks;
   const uint32_t put_at = (w_wave ? 0u : uint32_t(kTile)) + uint32_t(put_row * BK);
-  const uint32_t put_chunk[2] = {uint32_t(phys<C>(put_row, lane % C) * 16),
-                                 uint32_t(phys<C>(put_row + kLoadRows, lane % C) * 16)};
+  const uint32_t put_chunk[2] = {uint32_t(phys(put_row, lane % kChunks) * 16),
+                                 uint32_t(phys(put_row + kLoadRows, lane % kChunks) * 16)};
   auto put = [&](int buf, int l, const u32x4& v) {
     *reinterpret_cast<u32x4*>(smem + buf * kStage + l * kLoadRows * BK + put_at +
-                              put_chunk[kLoadRows < 16 ? l & 1 : 0]) = v;
+                              put_chunk[l & 1]) = v;
   };
   // Over what put() wrote of a stage that holds the end of k: one branch a
   // stage (with one for every chunk 777 x 5001 x 2047 took 34 us, not 31).
@@ -310,7 +306,7 @@ __global__ __launch_bounds__(WN * WM * 64, WN * WM == 8 ? 1 : NS * MT == 1 ? 4 :
   // Fragment x (rows first) of step kk, with JT row subtiles per wave.
   auto read = [&](auto jt, int buf, int kk, int x, Frag& d) {
     constexpr int JT = decltype(jt)::value;
-    const uint8_t* p = smem + buf * kStage + fr * BK + phys<C>(fr, kk * 2 + fh) * 16;
+    const uint8_t* p = smem + buf * kStage + fr * BK + phys(fr, kk * 2 + fh) * 16;
     if (x < JT)
       d.a[x < JT ? x : 0] = *reinterpret_cast<const u32x4*>(p + kTile + (wm * JT + x) * 32 * BK);
     else
@@ -372,8 +368,7 @@ __global__ __launch_bounds__(WN * WM * 64, WN * WM == 8 ? 1 : NS * MT == 1 ? 4 :
             // A wave issues in order: every MFMA is pinned to its share of the
             // LDS accesses and loads.  The steps before the barrier write
             // stage t + 1 first, then load into the registers that held stage t.
-            constexpr int kSlots = (kSteps - 1) * NM, kPutEnd = kSlots > 1 ? kSlots / 2 : 1;
-            constexpr int kLoadBegin = kSlots > 1 ? kSlots - kPutEnd : 0;
+            constexpr int kSlots = (kSteps - 1) * NM, kPutEnd = kSlots / 2, kLoadBegin = kSlots - kPutEnd;
 #pragma unroll
             for (int q = 0; q < NM; ++q) {
               const int slot = kk * NM + q;
@@ -476,8 +471,8 @@ __global__ __launch_bounds__(kFewWaves * 64, MT == 1 && ALIGNED ? 4 : 2) void fe
   const int fr = lane & 31, fh = lane >> 5;
   const int n0 = blockIdx.x * 32 * NT;
 
-  Operand<ALIGNED, 8, 4 * NT> wop;
-  Operand<ALIGNED, 8, 4 * MT> aop;
+  Operand<ALIGNED, 4 * NT> wop;
+  Operand<ALIGNED, 4 * MT> aop;
   wop.set(a.w, a.ldw, n0, a.n, a.k);
   const int m0 = blockIdx.y * 32 * MT;
   aop.set(a.a, a.lda, m0, a.m, a.k);
@@ -490,8 +485,8 @@ __global__ __launch_bounds__(kFewWaves * 64, MT == 1 && ALIGNED ? 4 : 2) void fe
   };
   uint8_t* image = smem + wave * kImage;
   // Load l holds rows 8 l + lane / 8, and phys() repeats with 16 rows.
-  const uint32_t put_off = (lane >> 3) * kRow + phys<8>(lane >> 3, lane & 7) * 16;
-  const uint32_t put_odd = (lane >> 3) * kRow + phys<8>(8 + (lane >> 3), lane & 7) * 16;
+  const uint32_t put_off = (lane >> 3) * kRow + phys(lane >> 3, lane & 7) * 16;
+  const uint32_t put_odd = (lane >> 3) * kRow + phys(8 + (lane >> 3), lane & 7) * 16;
 
   i32x16 acc[NT][MT];
 #pragma unroll
@@ -550,7 +545,7 @@ __global__ __launch_bounds__(kFewWaves * 64, MT == 1 && ALIGNED ? 4 : 2) void fe
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
       for (int kk = 0; kk < 4; ++kk) {
-        const uint8_t* p = image + fr * kRow + phys<8>(fr, 2 * kk + fh) * 16;
+        const uint8_t* p = image + fr * kRow + phys(fr, 2 * kk + fh) * 16;
         u32x4 wf[NT], af[MT];
 #pragma unroll
         for (int i = 0; i < NT; ++i) wf[i] = *reinterpret_cast<const u32x4*>(p + i * 32 * kRow);
@@ -614,13 +609,13 @@ __global__ __launch_bounds__(256) void short_kernel(LinearI8Args a) {
   }
 }
 
-template <int TYPE, bool ALIGNED, int C, int D, int WN, int WM, int NS, int MT>
+template <int TYPE, bool ALIGNED, int D, int WN, int WM, int NS, int MT>
 hipError_t launch_tiles(const LinearI8Args& a, int blocks, hipStream_t s) {
   constexpr int BN = 32 * NS * WN, BM = 32 * MT * WM;
   const int64_t tiles = int64_t((a.m + BM - 1) / BM) * ((a.n + BN - 1) / BN);
   if (tiles > (int64_t(1) << 30)) return hipErrorInvalidValue;
   const int grid = int(tiles < blocks ? tiles : blocks);
-  hipLaunchKernelGGL((linear_kernel<TYPE, ALIGNED, C, D, WN, WM, NS, MT>), dim3(grid), dim3(WN * WM * 64), 0, s, a);
+  hipLaunchKernelGGL((linear_kernel<TYPE, ALIGNED, D, WN, WM, NS, MT>), dim3(grid), dim3(WN * WM * 64), 0, s, a);
   return hipGetLastError();
 }
 
@@ -639,10 +634,10 @@ hipError_t launch_choice(const LinearI8Args& a, int choice, int cus, hipStream_t
       if constexpr (!ALIGNED) return hipErrorInvalidValue;
       hipLaunchKernelGGL((few_kernel<TYPE, true, 2, 2>), few, dim3(kFewWaves * 64), 0, s, a);
       return hipGetLastError();
-    case kLinearI8Tile64: return launch_tiles<TYPE, ALIGNED, 8, 4, 2, 2, 1, 1>(a, 4 * cus, s);
-    case kLinearI8Tile128: return launch_tiles<TYPE, ALIGNED, 8, 2, 2, 2, 2, 2>(a, 2 * cus, s);
+    case kLinearI8Tile64: return launch_tiles<TYPE, ALIGNED, 4, 2, 2, 1, 1>(a, 4 * cus, s);
+    case kLinearI8Tile128: return launch_tiles<TYPE, ALIGNED, 2, 2, 2, 2, 2>(a, 2 * cus, s);
     default:
-      if constexpr (ALIGNED) return launch_tiles<TYPE, ALIGNED, 8, 2, 2, 4, 4, 2>(a, cus, s);
+      if constexpr (ALIGNED) return launch_tiles<TYPE, ALIGNED, 2, 2, 4, 4, 2>(a, cus, s);
       return hipErrorInvalidValue;
   }
 }
