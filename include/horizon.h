@@ -21,17 +21,19 @@
  *     reuse them at once).  Streams are hipStream_t passed as void*.
  *   - bf16 means IEEE bfloat16 and fp16 IEEE binary16, stored as 16-bit words.
  *   - Precision: token rows and weights are bf16 in memory; every contraction
- *     runs on fp16 MFMA operands with fp32 accumulation (weights are converted
- *     bf16 -> fp16 on load, exact for magnitudes in [2^-14, 65504]); the
- *     residual stream is fp32; intermediate activations and the key/value
- *     cache are fp16 (finite values saturate at +-65504).
+ *     of the layers runs on fp16 MFMA operands with fp32 accumulation (weights
+ *     are converted bf16 -> fp16 on load, exact for magnitudes in
+ *     [2^-14, 65504]); the residual stream is fp32; intermediate activations
+ *     and the key/value cache are fp16 (finite values saturate at +-65504).
+ *     hs_linear_i8 alone takes 8-bit integers, whose sums are exact.
  *   - Weight matrices are [out, in] row-major, so y = x * W^T.
  *   - Every function returns an hs_status.  No C++ exception crosses the
  *     ABI.  On any error other than HS_ERR_HIP nothing has been enqueued.
  *     hs_last_error() returns a thread-local message for the last failure.
  *   - Compute calls are asynchronous with respect to their stream; device
  *     faults surface at the caller's next synchronisation.
- *   - A context is not thread-safe; use one per host thread.
+ *   - A context is not thread-safe; use one per host thread.  Calls that only
+ *     read it say so (hs_quantize_rows, hs_linear_i8, hs_logprobs).
  */
 #ifndef HORIZON_H_
 #define HORIZON_H_
@@ -435,6 +437,9 @@ hs_status hs_dit_forward(hs_context* ctx, const hs_dit_cfg* cfg, const hs_dit_we
  *   - The calls allocate nothing, stage nothing on the host and never
  *     synchronise, so they can be captured into a graph on the caller's
  *     stream.  The caller's current device is left as it was.
+ *   - They only read the context while its timing is off (hs_timing_enable), so
+ *     several host threads may make them on one context at a time, as long as
+ *     none makes any other call on it; with timing on, one thread at a time.
  *   - No rows: HS_OK, nothing is enqueued.  Outputs that overlap an input or
  *     each other, strides outside [row length, 2^30] and misaligned pointers are
  *     HS_ERR_INVALID_ARG; more than 2^30 rows (2^25 of logits) are

@@ -6,7 +6,9 @@ head's weights in 8 bits (made once from bf16 by the library's quantiser) with
 the buffers of one pass, and runs the three calls over any number of rows, in
 passes of ``max_rows``.  It allocates nothing and never synchronises after its
 construction.  Passes share the buffers, so two calls that may overlap need a
-head each (they may share the weights: ``sharing``).
+head each (they may share the weights: ``sharing``).  Keep a head, its outputs
+and its rows until the stream has passed their last call: torch does not see the
+library's streams and would give their memory away.
 """
 from __future__ import annotations
 
