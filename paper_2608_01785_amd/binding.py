@@ -614,7 +614,7 @@ def _matrix(ctx: Context, t, name: str, kinds) -> Tuple[int, int, int, int]:
     ld, step = t.stride()
     if step != 1 and cols > 1 and rows > 0:
         raise ValueError(f"the rows of {name} are not contiguous (stride {step})")
-    if rows > _INT32_MAX or cols > _INT32_MAX:
+    if (rows | cols) >> 31:
         rows, cols = min(rows, _INT32_MAX), min(cols, _INT32_MAX)
     return t.data_ptr(), (ld if rows > 1 else max(cols, 1)), rows, cols
 
@@ -638,7 +638,7 @@ def _workspace(ctx: Context, t, n_bytes: Optional[int]) -> Tuple[Optional[int], 
     device address with n_bytes, or None."""
     if t is None:
         return None, n_bytes or 0
-    if isinstance(t, int):
+    if type(t) is int:
         if n_bytes is None:
             raise ValueError("a workspace address needs ws_bytes")
         return t, n_bytes
@@ -646,11 +646,12 @@ def _workspace(ctx: Context, t, n_bytes: Optional[int]) -> Tuple[Optional[int], 
         raise ValueError(f"workspace is on {t.device}, the context on cuda:{ctx.device}")
     if not t.is_contiguous():
         raise ValueError("workspace is not contiguous")
-    if n_bytes is None:
-        return t.data_ptr(), t.nbytes
-    if n_bytes > t.nbytes:
-        raise ValueError(f"workspace has {t.nbytes} bytes, ws_bytes is {n_bytes}")
-    return t.data_ptr(), n_bytes
+    size = t.nbytes
+    if n_bytes is not None:
+        if n_bytes > size:
+            raise ValueError(f"workspace has {size} bytes, ws_bytes is {n_bytes}")
+        size = n_bytes
+    return t.data_ptr(), size
 
 
 def hs_quantize_rows(ctx: Context, x, q, scale, gain=None, eps: float = 1e-6, cu_budget: int = 256,
@@ -703,15 +704,23 @@ def hs_logprobs(ctx: Context, logits, tokens=None, token_logprobs=None, entropy=
     pz, ld, rows, vocab = _matrix(ctx, logits, "logits", _Kinds.rows)
     if (tokens is None) != (token_logprobs is None) or (top_logprobs is None) != (top_tokens is None):
         raise ValueError("tokens and token_logprobs, top_logprobs and top_tokens go together")
-    n = 0 if tokens is None or not tokens.shape else min(tokens.shape[-1], _INT32_MAX)
-    k = 0 if top_tokens is None or not top_tokens.shape else min(top_tokens.shape[-1], _INT32_MAX)
+    n = k = 0
+    try:
+        if tokens is not None:
+            n = tokens.shape[-1]
+        if top_tokens is not None:
+            k = top_tokens.shape[-1]
+    except IndexError:   # no dimensions: refused with the others below
+        pass
+    if (n | k) >> 31:
+        n, k = min(n, _INT32_MAX), min(k, _INT32_MAX)
     ws, ws_bytes = _workspace(ctx, workspace, ws_bytes)
     f32, i32 = _Kinds.f32, _Kinds.i32
     status = lib().hs_logprobs(
         ctx.handle, pz, _Kinds.rows[logits.dtype], ld, rows, vocab, _dense(ctx, tokens, "tokens", i32, rows, n), n,
         _dense(ctx, token_logprobs, "token_logprobs", f32, rows, n), _dense(ctx, entropy, "entropy", f32, rows), k,
         _dense(ctx, top_logprobs, "top_logprobs", f32, rows, k), _dense(ctx, top_tokens, "top_tokens", i32, rows, k),
-        cu_budget, _ptr(stream), ws, ws_bytes)
+        cu_budget, stream and _ptr(stream), ws, ws_bytes)
     if status:
         _check(status)
 
