@@ -223,3 +223,27 @@ def test_scales_are_as_near_as_their_roundings(env, d, dtype, norm):
     _, ref = A.quantize_rows(_np(x), None if gain is None else _np(gain), float(np.float32(EPS)))
     off = np.abs(s.double().cpu().numpy() / ref - 1) / U
     assert off.max() <= _scale_bound(d, dtype, norm) * (1 + 1e-5), off.max()
+
+
+@pytest.mark.parametrize("layout", LAYOUTS)
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_signalling_nans(env, layout, dtype):
+    """A NaN of either kind and sign anywhere in a row, beside ordinary logits and in a masked row."""
+    torch, b, ctx = env
+    rows, vocab, cus = _check_layout(b, layout, dtype)
+    t = _t(torch, dtype)
+    word = torch.int32 if dtype == "f32" else torch.int16
+    quiet, signalling = {"f32": (0x7fc00000, 0x7f800001), "bf16": (0x7fc0, 0x7f81), "f16": (0x7e00, 0x7c01)}[dtype]
+    sign = torch.iinfo(word).min
+    z = (torch.randn(rows, vocab, generator=_gen(torch, 3), device="cuda") * 3).to(t)
+    bits = z.view(word)
+    for r in range(7):
+        if r >= 4:
+            z[r] = -float("inf")
+        bits[r, (0, vocab - 1, vocab // 2, 4999)[r % 4]] = (signalling, signalling + sign, quiet + sign, signalling)[r % 4]
+    tokens = torch.randint(0, vocab, (rows, 2), generator=_gen(torch, 4), device="cuda", dtype=torch.int32)
+    got = _check_logprobs(env, z, tokens, 20, cus=cus)
+    assert bool(got["entropy"][:7].isnan().all()) and not bool(got["entropy"][7:].isnan().any())
+    q, s = _quantize(env, z[:, :5003], None)
+    at = torch.isnan(z[:, :5003]).any(1) | torch.isinf(z[:, :5003]).any(1)
+    assert torch.equal(torch.isnan(s), at) and not bool(q[at].any()) and int(at.sum()) >= 5
