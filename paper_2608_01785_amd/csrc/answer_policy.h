@@ -66,9 +66,12 @@ enum LinearI8Choice {
 // 128 x 128 tiles it runs two, which take little less than one after the other;
 // a 256 x 256 step takes longer the more of the chip works, whose clock follows
 // the power.  4096 x 8192 x 8192: 235 in 256s, 323 in 128s, 477 in 64s; 777 x
-// 4096 x 4096: 44, 24, 30; 256 x 4608 x 3584: 39, 20, 17.  Over 84 products of 96
-// to 2048 rows the rule loses 0.2 % against the fastest.  The constants are those
-// of 256 CUs; memory's rate is taken to be shared by them.
+// 4096 x 4096: 44, 24, 30; 256 x 4608 x 3584: 39, 20, 17.  Over 143 products of 1
+// to 1024 rows the rule loses 0.8 % against the fastest (192 x 37888 x 3584 most: 63
+// in 128s, 48 in 256s).  The constants are those of 256 CUs, of which every CU
+// is taken to have its share of memory's rate.  64 CUs reach half of it and not a
+// fourth, so on part of the chip the rule loses more: 3 % on 128 CUs, 7 % on 64,
+// there 48 x 14336 x 4096 47 for few rows against 27 in 64s.
 //
 // Rows that are not 16-byte aligned cost the address unit twice as much a load,
 // which the kernels that use a load least feel most: 512 x 4608 x 3583 40 in 64s
