@@ -25,10 +25,11 @@
 //
 // The grid is persistent and the stages of a block's tiles form one sequence:
 // the last D stages of a tile already fetch the next one's first D (four of the 64
-// x 64 tiles, two of the others), and its epilogue runs under those loads.  An epilogue reads no memory: a tile's
-// scales and bias come into LDS during the epilogue before it (stores count
-// against the same completion counter as loads, so a load between them would
-// wait for them; with such loads an epilogue took 18 us).
+// x 64 tiles, two of the others), and its epilogue runs under those loads.  An
+// epilogue reads no memory: a tile's scales and bias come into LDS during the
+// epilogue before it (stores count against the same completion counter as loads,
+// so a load between them would wait for them; with such loads an epilogue took 18
+// us).
 //
 // Large products are bound by power: 8192^3 takes 460 to 490 us (2.3 PFLOP/s)
 // with normally distributed values and 354 with zeros.
