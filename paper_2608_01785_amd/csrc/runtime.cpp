@@ -1297,6 +1297,7 @@ hs_status hs_timing_enable(hs_context* ctx, int32_t enable) {
       HIP_TRY(hipEventCreate(&e));
       ctx->ev_pool.push_back(e);
     }
+    ctx->recs.reserve(kTimingPairs);  // a timed call allocates nothing and cannot throw
   }
   if (enable && !ctx->clock_buf) HIP_TRY(hipMalloc(&ctx->clock_buf, kTimingPairs * 4 * sizeof(uint64_t)));
   // Finish outstanding records before their events can be recorded again.
