@@ -363,8 +363,8 @@ def _buffers(st):
     else:
         hq, hkv, dh = HEADS[case["heads"]]
         st["out"] = new((case["seqs"], hq * dh), TYPES[case["dtype"]])
-        size = binding.hs_prefix_attention_workspace_size(hq, hkv, dh, case["seqs"], case["groups"],
-                                                          st["max_prefix"], st["max_rest"])
+        size = binding.hs_prefix_attention_workspace_size(hq, hkv, dh, case["seqs"], st["max_prefix"],
+                                                          st["max_rest"])
     st["ws"] = new(max(1, size), torch.uint8)
     torch.cuda.synchronize()
     return st["out"]
