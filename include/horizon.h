@@ -33,7 +33,8 @@
  *   - Compute calls are asynchronous with respect to their stream; device
  *     faults surface at the caller's next synchronisation.
  *   - A context is not thread-safe; use one per host thread.  Calls that only
- *     read it say so (hs_quantize_rows, hs_linear_i8, hs_logprobs).
+ *     read it say so (hs_quantize_rows, hs_linear_i8, hs_logprobs,
+ *     hs_beam_select, hs_cache_copy, hs_prefix_attention).
  */
 #ifndef HORIZON_H_
 #define HORIZON_H_
@@ -502,6 +503,146 @@ hs_status hs_logprobs(hs_context* ctx, const void* logits, int32_t type, int64_t
                       float* top_logprobs, int32_t* top_tokens, int32_t cu_budget, void* stream, void* workspace,
                       size_t ws_bytes);
 
+/* ------------------------------------------------------------------------
+ * Decoding on a shared cache: selection over beams, pages that sequences share,
+ * and attention that reads a shared prefix once.  hs_beam_select, hs_cache_copy
+ * and hs_prefix_attention take cu_budget and stream, validate, enqueue and read
+ * the context as the three calls above do; they can be captured too.
+ *
+ * A step of beam search: hs_downstream_decode_step_prefix (or
+ * hs_downstream_decode_step), the head, hs_beam_select; then on the host
+ * hs_pages_fork with the parents, hs_pages_reserve for the next row, and
+ * hs_cache_copy with the copies that it names. */
+
+/* Workspace bytes of hs_beam_select for at most max_groups groups. */
+hs_status hs_beam_select_workspace_size(int32_t max_groups, int32_t beams, int32_t vocab, int32_t n_select,
+                                        size_t* bytes);
+
+/* The n_select best continuations of every group of beams, over its beams b and
+ * the vocabulary:  value(b, t) = scores[b] + z[b, t] - log sum_j e^z[b, j].
+ *   logits        [groups * beams, vocab] of `type`, row stride ld; -inf marks a
+ *                 masked token (no continuation);
+ *   scores        fp32 [groups, beams]; a beam at -inf (or NaN) is empty and
+ *                 proposes nothing;
+ *   finished      uint8 [groups, beams] or NULL: a beam with a non-zero entry
+ *                 proposes end_token alone, at its own score;
+ *   end_token     in [0, vocab), or -1: none (finished must be NULL then);
+ *   out_scores    fp32, out_parents and out_tokens int32 [groups, n_select]: the
+ *                 values, the beams (0 .. beams - 1) and the tokens, best first;
+ *   out_finished  uint8 [groups, n_select] or NULL: 1 where the parent had
+ *                 finished or the token is end_token.
+ * beams and n_select are at most 64.  The order is the value's, then the lower
+ * beam, then the lower token; a beam's own continuations go by logit (-0 equals
+ * +0).  Sums of exponentials are fp32; from them on values are compared in 64 bits
+ * and rounded once.  Where there are fewer continuations the rest holds -inf, -1,
+ * -1, 0.  A row with a NaN or +inf has no distribution and no continuation.
+ * Rows of empty and finished beams are not read.
+ * workspace: hs_beam_select_workspace_size() bytes for this shape or a larger
+ * max_groups, 16-byte aligned; reuse as for hs_logprobs. */
+hs_status hs_beam_select(hs_context* ctx, const void* logits, int32_t type, int64_t ld, int32_t groups, int32_t beams,
+                         int32_t vocab, const float* scores, const uint8_t* finished, int32_t end_token,
+                         int32_t n_select, float* out_scores, int32_t* out_parents, int32_t* out_tokens,
+                         uint8_t* out_finished, int32_t cu_budget, void* stream, void* workspace, size_t ws_bytes);
+
+/* Copies within a cache, in each of n_layers layers: positions [0, positions[i])
+ * of slot src[i] to the same positions of slot dst[i], keys and values.
+ *   kv         block_table is not read; k[l] and v[l] 16-byte aligned;
+ *   src, dst, positions  host arrays [n_copies], kept by the launches themselves
+ *              (a captured call repeats them); positions NULL: whole slots.
+ * Values move in tiles of 32 positions, so a copy takes positions[i] rounded up
+ * to 32 (what the source holds there is copied too); 0 copies nothing.
+ * A slot may be the source of several copies; a destination is no other copy's
+ * destination and no copy's source (HS_ERR_INVALID_ARG).  A slot of a layer is
+ * at most 2^33 bytes, n_kv_heads at most 1024. */
+hs_status hs_cache_copy(hs_context* ctx, const hs_kv_cache* kv, int32_t n_layers, int32_t n_kv_heads, int32_t head_dim,
+                        const int32_t* src, const int32_t* dst, const int32_t* positions, int32_t n_copies,
+                        int32_t cu_budget, void* stream);
+
+/* Workspace bytes of hs_prefix_attention for at most n_seqs rows and these bounds
+ * (any grouping and budget). */
+hs_status hs_prefix_attention_workspace_size(int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t n_seqs,
+                                             int32_t max_prefix, int32_t max_rest, size_t* bytes);
+
+/* Attention of one row a sequence over one layer of a paged cache, where groups
+ * of sequences share their first positions (a system prompt, a document, the
+ * prompt of a request's beams):
+ *   o[i, h] = softmax(q[i, h] K^T / sqrt(head_dim)) V
+ * over the keys [0, prefix) of row i's group, read once for all its rows from the
+ * pages of its first row, and the keys [prefix, lens[i]) of row i's own pages.
+ *   q, out         `type` HS_TYPE_F16 or HS_TYPE_BF16 [n_seqs, n_q_heads, head_dim],
+ *                  row strides ldq, ldo (of q: a multiple of 8, q 16-byte aligned);
+ *   k, v           the layer's keys and values (hs_kv_cache: n_slots slots of
+ *                  page_positions positions), 16-byte aligned;
+ *   block_table    int32 [n_seqs, pages_per_seq] device;
+ *   lens           int32 [n_seqs] device: keys of each row, its prefix included;
+ *   group_offsets  int32 [n_groups + 1] device, non-decreasing from 0 to n_seqs:
+ *                  group g has rows group_offsets[g] .. group_offsets[g + 1] - 1;
+ *   prefix_lens    int32 [n_groups] device, 0 for none;
+ *   max_prefix, max_rest  bounds of prefix_lens and of lens - prefix, which size the
+ *                  launches (close bounds are fast ones).
+ * n_groups 0: no row has a prefix.  head_dim 64 or 128.  A row without keys gives 0.
+ * A row with prefix or lens - prefix negative or beyond its bound, or with keys
+ * beyond the table, gives NaN, and so does one that needs a slot outside
+ * [0, n_slots); entries that no key needs are not read.  Other group_offsets than
+ * described leave rows undefined, but nothing outside the arguments is touched.
+ * Products take fp16 operands (bf16 q converts exactly for magnitudes in
+ * [2^-14, 65504]) and weights rounded to fp16; scores, statistics and sums are fp32.
+ * workspace: hs_prefix_attention_workspace_size() bytes, 16-byte aligned; reuse as
+ * for hs_logprobs. */
+hs_status hs_prefix_attention(hs_context* ctx, const void* q, int32_t type, int64_t ldq, void* out, int64_t ldo,
+                              int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, const void* k, const void* v,
+                              int32_t n_slots, int32_t page_positions, const int32_t* block_table,
+                              int32_t pages_per_seq, const int32_t* lens, int32_t n_seqs,
+                              const int32_t* group_offsets, const int32_t* prefix_lens, int32_t n_groups,
+                              int32_t max_prefix, int32_t max_rest, int32_t cu_budget, void* stream, void* workspace,
+                              size_t ws_bytes);
+
+/* Which page holds what: the block tables of the sequences that share a cache's
+ * pages.  Host only; it moves no data but names the copies that hs_cache_copy has
+ * to make, on the stream of the step and before the step.
+ * A sequence 0 .. max_seqs - 1 has a length and the pages that hold it, at most
+ * pages_per_seq; a page belongs to as many sequences as list it, and is free
+ * without any.  Every call leaves the state as it was when it fails. */
+typedef struct hs_pages hs_pages;
+
+/* n_pages pages of page_positions positions (a positive multiple of 64), all
+ * free; every sequence is empty. */
+hs_status hs_pages_create(int32_t n_pages, int32_t page_positions, int32_t max_seqs, int32_t pages_per_seq,
+                          hs_pages** out);
+hs_status hs_pages_destroy(hs_pages* pages);
+
+/* Room for add[i] >= 0 more positions of each sequence seqs[i] (distinct), which
+ * its length then counts: free pages, the lowest first, and for a partly filled last page
+ * that other sequences list too a page of its own, the copy of which goes to
+ * src/dst/positions (host, each with room for n entries; *n_copies of them are
+ * written).  Sequences are served in order, so the last that lists a page keeps
+ * it.  HS_ERR_WORKSPACE: not enough free pages. */
+hs_status hs_pages_reserve(hs_pages* pages, const int32_t* seqs, const int32_t* add, int32_t n, int32_t* src,
+                           int32_t* dst, int32_t* positions, int32_t* n_copies);
+
+/* All at once: sequence seqs[i] (distinct) becomes what parents[i] was before the
+ * call, sharing its pages; parents[i] -1: empty.  Pages that nobody lists any more
+ * become free. */
+hs_status hs_pages_fork(hs_pages* pages, const int32_t* seqs, const int32_t* parents, int32_t n);
+
+/* Moves the highest pages in use to the lowest free ones until the pages in use
+ * are 0 .. used - 1, and names the copies (src/dst/positions with room for
+ * `room` entries; at most `room` pages move, so a pass may stop earlier).  A
+ * moved page keeps its place in every sequence that lists it; positions counts what
+ * the longest of them holds there. */
+hs_status hs_pages_compact(hs_pages* pages, int32_t room, int32_t* src, int32_t* dst, int32_t* positions,
+                           int32_t* n_copies);
+
+/* The block table [n][pages_per_seq] (unreached entries 0) and lengths [n] of some
+ * sequences; either may be NULL. */
+hs_status hs_pages_table(const hs_pages* pages, const int32_t* seqs, int32_t n, int32_t* table, int32_t* lens);
+
+/* Positions in whole pages that all of the n >= 1 sequences share from position 0
+ * on: a prefix_lens entry of a group of them.  0 for an empty sequence. */
+hs_status hs_pages_shared(const hs_pages* pages, const int32_t* seqs, int32_t n, int32_t* positions);
+
+hs_status hs_pages_free_count(const hs_pages* pages, int32_t* n_free);
+
 /* Topology probe: launches n_groups work-groups on `stream` (NULL = the
  * context's full-budget stream); each writes, into out_ids (device, uint32
  * [n_groups * 4]): XCC id, shader engine, CU id, and the low 32 bits of the
@@ -541,7 +682,10 @@ enum {
   HS_KERNEL_QUANTIZE = 12,    /* hs_quantize_rows */
   HS_KERNEL_LINEAR_I8 = 13,   /* hs_linear_i8 */
   HS_KERNEL_LOGPROBS = 14,    /* hs_logprobs */
-  HS_KERNEL_KINDS = 15
+  HS_KERNEL_BEAM_SELECT = 15, /* hs_beam_select */
+  HS_KERNEL_CACHE_COPY = 16,  /* hs_cache_copy */
+  HS_KERNEL_PREFIX_ATTN = 17, /* hs_prefix_attention, and the decode step's */
+  HS_KERNEL_KINDS = 18
 };
 
 hs_status hs_timing_enable(hs_context* ctx, int32_t enable);

@@ -30,13 +30,17 @@ SYMBOLS = (
     "hs_controller_create", "hs_controller_step", "hs_controller_destroy", "hs_pressure_sample",
     "hs_temporal_create", "hs_temporal_step", "hs_temporal_destroy",
     "hs_quantize_rows", "hs_linear_i8", "hs_logprobs_workspace_size", "hs_logprobs",
+    "hs_beam_select_workspace_size", "hs_beam_select", "hs_cache_copy", "hs_prefix_attention_workspace_size",
+    "hs_prefix_attention", "hs_pages_create", "hs_pages_destroy", "hs_pages_reserve", "hs_pages_fork",
+    "hs_pages_compact", "hs_pages_table", "hs_pages_shared", "hs_pages_free_count",
 )
 HS_WEIGHTS_BF16, HS_WEIGHTS_F16 = 0, 1
 HS_TYPE_F32, HS_TYPE_BF16, HS_TYPE_F16 = 0, 1, 2
 
 KERNEL_KINDS = {"rmsnorm": 0, "qkv": 1, "attention": 2, "decode_attn": 3, "o_proj": 4, "gate_up": 5,
                 "down": 6, "rope_table": 7, "modulation": 8, "ln_mod": 9, "mlp_up": 10, "mlp_down": 11,
-                "quantize": 12, "linear_i8": 13, "logprobs": 14}
+                "quantize": 12, "linear_i8": 13, "logprobs": 14, "beam_select": 15, "cache_copy": 16,
+                "prefix_attn": 17}
 
 
 class LayerCfg(ctypes.Structure):
@@ -186,6 +190,21 @@ def lib() -> ctypes.CDLL:
             "hs_linear_i8": [vp, vp, i64, vp, vp, i64, vp, vp, vp, i32, i64, i32, i32, i32, i32, vp],
             "hs_logprobs_workspace_size": [i32, i32, i32, ctypes.POINTER(ctypes.c_size_t)],
             "hs_logprobs": [vp, vp, i32, i64, i32, i32, vp, i32, vp, vp, i32, vp, vp, i32, vp, vp, ctypes.c_size_t],
+            "hs_beam_select_workspace_size": [i32, i32, i32, i32, ctypes.POINTER(ctypes.c_size_t)],
+            "hs_beam_select": [vp, vp, i32, i64, i32, i32, i32, vp, vp, i32, i32, vp, vp, vp, vp, i32, vp, vp,
+                               ctypes.c_size_t],
+            "hs_cache_copy": [vp, ctypes.POINTER(KvCache), i32, i32, i32, i32p, i32p, i32p, i32, i32, vp],
+            "hs_prefix_attention_workspace_size": [i32, i32, i32, i32, i32, i32, ctypes.POINTER(ctypes.c_size_t)],
+            "hs_prefix_attention": [vp, vp, i32, i64, vp, i64, i32, i32, i32, vp, vp, i32, i32, vp, i32, vp, i32, vp,
+                                    vp, i32, i32, i32, i32, vp, vp, ctypes.c_size_t],
+            "hs_pages_create": [i32, i32, i32, i32, ctypes.POINTER(vp)],
+            "hs_pages_destroy": [vp],
+            "hs_pages_reserve": [vp, i32p, i32p, i32, i32p, i32p, i32p, i32p],
+            "hs_pages_fork": [vp, i32p, i32p, i32],
+            "hs_pages_compact": [vp, i32, i32p, i32p, i32p, i32p],
+            "hs_pages_table": [vp, i32p, i32, i32p, i32p],
+            "hs_pages_shared": [vp, i32p, i32, i32p],
+            "hs_pages_free_count": [vp, i32p],
         }
         for name, args in sigs.items():
             fn = getattr(L, name)
@@ -582,14 +601,18 @@ class _Kinds:
     bf16: Dict[object, int] = {}
     i8: Dict[object, int] = {}
     i32: Dict[object, int] = {}
+    u8: Dict[object, int] = {}
+    halves: Dict[object, int] = {}
+    f16: Dict[object, int] = {}
 
     @classmethod
     def fill(cls) -> None:
         import torch
         cls.rows.update({torch.float32: HS_TYPE_F32, torch.bfloat16: HS_TYPE_BF16, torch.float16: HS_TYPE_F16})
         for kinds, t in ((cls.f32, torch.float32), (cls.bf16, torch.bfloat16), (cls.i8, torch.int8),
-                         (cls.i32, torch.int32)):
+                         (cls.i32, torch.int32), (cls.u8, torch.uint8), (cls.f16, torch.float16)):
             kinds[t] = 0
+        cls.halves.update({torch.bfloat16: HS_TYPE_BF16, torch.float16: HS_TYPE_F16})
 
 
 def _refuse(ctx: Context, t, name: str, kinds, ndim: int) -> None:
@@ -723,6 +746,184 @@ def hs_logprobs(ctx: Context, logits, tokens=None, token_logprobs=None, entropy=
         cu_budget, stream and _ptr(stream), ws, ws_bytes)
     if status:
         _check(status)
+
+
+def hs_beam_select_workspace_size(max_groups: int, beams: int, vocab: int, n_select: int) -> int:
+    n = ctypes.c_size_t(0)
+    args = (min(v, _INT32_MAX) for v in (max_groups, beams, vocab, n_select))
+    _check(lib().hs_beam_select_workspace_size(*args, ctypes.byref(n)))
+    return int(n.value)
+
+
+def hs_beam_select(ctx: Context, logits, scores, out_scores, out_parents, out_tokens, finished=None, out_finished=None,
+                   end_token: int = -1, cu_budget: int = 256, stream=None, workspace=None,
+                   ws_bytes: Optional[int] = None) -> None:
+    """logits [groups * beams, vocab], scores fp32 and finished uint8 [groups, beams] -> out_scores fp32, out_parents and
+    out_tokens int32, out_finished uint8 [groups, n_select]; what is None is not used."""
+    if not _Kinds.rows:
+        _Kinds.fill()
+    pz, ld, rows, vocab = _matrix(ctx, logits, "logits", _Kinds.rows)
+    for t, name, kinds in ((scores, "scores", _Kinds.f32), (out_scores, "out_scores", _Kinds.f32)):
+        if t.dim() != 2:
+            _refuse(ctx, t, name, kinds, 2)
+    groups, beams = scores.shape
+    if groups * beams != rows:
+        raise ValueError(f"logits has {rows} rows, scores {groups} x {beams}")
+    select = min(out_scores.shape[1], _INT32_MAX)
+    f32, i32, u8 = _Kinds.f32, _Kinds.i32, _Kinds.u8
+    ws, ws_bytes = _workspace(ctx, workspace, ws_bytes)
+    status = lib().hs_beam_select(
+        ctx.handle, pz, _Kinds.rows[logits.dtype], ld, groups, beams, vocab,
+        _dense(ctx, scores, "scores", f32, groups, beams), _dense(ctx, finished, "finished", u8, groups, beams),
+        end_token, select, _dense(ctx, out_scores, "out_scores", f32, groups, select),
+        _dense(ctx, out_parents, "out_parents", i32, groups, select),
+        _dense(ctx, out_tokens, "out_tokens", i32, groups, select),
+        _dense(ctx, out_finished, "out_finished", u8, groups, select), cu_budget, stream and _ptr(stream), ws, ws_bytes)
+    if status:
+        _check(status)
+
+
+def _cache_layers(ctx: Context, k, v, n_slots: int, max_ctx: int) -> Tuple[int, int]:
+    """(key/value heads, head size) of a cache's layers: k[l] fp16 [n_slots, hkv, max_ctx, dh], v[l] the same in value
+    tiles [n_slots, hkv, max_ctx / 32, dh, 32]."""
+    if len(k) != len(v) or not k:
+        raise ValueError(f"{len(k)} layers of keys, {len(v)} of values")
+    if k[0].dim() != 4:
+        _refuse(ctx, k[0], "k", _Kinds.f16, 4)
+    hkv, dh = k[0].shape[1], k[0].shape[3]
+    for kl, vl in zip(k, v):
+        _dense(ctx, kl, "k", _Kinds.f16, n_slots, hkv, max_ctx, dh)
+        _dense(ctx, vl, "v", _Kinds.f16, n_slots, hkv, max_ctx // 32, dh, 32)
+    return hkv, dh
+
+
+def hs_cache_copy(ctx: Context, kv, src, dst, positions=None, cu_budget: int = 256, stream=None) -> None:
+    """kv: (k, v, n_slots, max_ctx[, block table]) as for the decode step, of tensors; src, dst, positions: host lists,
+    positions None for whole slots."""
+    if not _Kinds.rows:
+        _Kinds.fill()
+    k, v, n_slots, max_ctx = kv[:4]
+    hkv, dh = _cache_layers(ctx, k, v, n_slots, max_ctx)
+    n = len(src)
+    if len(dst) != n or (positions is not None and len(positions) != n):
+        raise ValueError(f"{n} sources, {len(dst)} destinations"
+                         + ("" if positions is None else f", {len(positions)} numbers of positions"))
+    _check(lib().hs_cache_copy(ctx.handle, ctypes.byref(_kv_struct((k, v, n_slots, max_ctx))), len(k), hkv, dh,
+                               _i32_array(src), _i32_array(dst), _i32_array(positions), n, cu_budget, _ptr(stream)))
+
+
+def hs_prefix_attention_workspace_size(n_q_heads: int, n_kv_heads: int, head_dim: int, n_seqs: int, max_prefix: int,
+                                       max_rest: int) -> int:
+    n = ctypes.c_size_t(0)
+    args = (min(v, _INT32_MAX) for v in (n_q_heads, n_kv_heads, head_dim, n_seqs, max_prefix, max_rest))
+    _check(lib().hs_prefix_attention_workspace_size(*args, ctypes.byref(n)))
+    return int(n.value)
+
+
+def hs_prefix_attention(ctx: Context, q, out, k, v, block_table, lens, group_offsets, prefix_lens, max_prefix: int,
+                        max_rest: int, cu_budget: int = 256, stream=None, workspace=None,
+                        ws_bytes: Optional[int] = None) -> None:
+    """q and out (fp16 or bf16) [n_seqs, n_q_heads * head_dim]; k and v: one layer of a cache; block_table int32
+    [n_seqs, pages_per_seq], lens int32 [n_seqs], group_offsets int32 [n_groups + 1], prefix_lens int32 [n_groups],
+    all on the device (group_offsets and prefix_lens None: no prefixes)."""
+    if not _Kinds.rows:
+        _Kinds.fill()
+    pq, ldq, n, cols = _matrix(ctx, q, "q", _Kinds.halves)
+    po, ldo, *o_shape = _matrix(ctx, out, "out", {q.dtype: 0})
+    if o_shape != [n, cols]:
+        raise ValueError(f"out has shape {tuple(o_shape)}, q ({n}, {cols})")
+    if k.dim() != 4:
+        _refuse(ctx, k, "k", _Kinds.f16, 4)
+    n_slots, hkv, page, dh = k.shape
+    _cache_layers(ctx, (k,), (v,), n_slots, page)
+    if dh < 1 or cols % dh:
+        raise ValueError(f"q has {cols} columns, the cache heads of {dh}")
+    if block_table.dim() != 2:
+        _refuse(ctx, block_table, "block_table", _Kinds.i32, 2)
+    per_seq = block_table.shape[1]
+    if (group_offsets is None) != (prefix_lens is None):
+        raise ValueError("group_offsets and prefix_lens go together")
+    groups = 0
+    if prefix_lens is not None:
+        if prefix_lens.dim() != 1:
+            _refuse(ctx, prefix_lens, "prefix_lens", _Kinds.i32, 1)
+        groups = prefix_lens.shape[0]
+    i32 = _Kinds.i32
+    ws, ws_bytes = _workspace(ctx, workspace, ws_bytes)
+    status = lib().hs_prefix_attention(
+        ctx.handle, pq, _Kinds.halves[q.dtype], ldq, po, ldo, cols // dh, hkv, dh, k.data_ptr(), v.data_ptr(), n_slots,
+        page, _dense(ctx, block_table, "block_table", i32, n, per_seq), per_seq, _dense(ctx, lens, "lens", i32, n), n,
+        _dense(ctx, group_offsets, "group_offsets", i32, groups + 1),
+        _dense(ctx, prefix_lens, "prefix_lens", i32, groups), groups, min(max_prefix, _INT32_MAX),
+        min(max_rest, _INT32_MAX), cu_budget, stream and _ptr(stream), ws, ws_bytes)
+    if status:
+        _check(status)
+
+
+class Pages:
+    """Owns an ``hs_pages`` handle: which pages of a cache the sequences list (host only).
+
+    Calls that move data return (src, dst, positions) for ``hs_cache_copy``."""
+
+    def __init__(self, n_pages: int, page_positions: int, max_seqs: int, pages_per_seq: int):
+        self.handle = None
+        h = ctypes.c_void_p()
+        _check(lib().hs_pages_create(n_pages, page_positions, max_seqs, pages_per_seq, ctypes.byref(h)))
+        self.handle = h
+        self.pages_per_seq = pages_per_seq
+
+    def _copies(self, room: int, call) -> Tuple[List[int], List[int], List[int]]:
+        lists = [(ctypes.c_int32 * max(room, 1))() for _ in range(3)]
+        n = ctypes.c_int32(0)
+        _check(call(*lists, ctypes.byref(n)))
+        return tuple(list(x[:n.value]) for x in lists)
+
+    def reserve(self, seqs, add):
+        if len(seqs) != len(add):
+            raise ValueError(f"{len(seqs)} sequences, {len(add)} numbers of positions")
+        return self._copies(len(seqs), lambda *out: lib().hs_pages_reserve(
+            self.handle, _i32_array(seqs), _i32_array(add), len(seqs), *out))
+
+    def fork(self, seqs, parents) -> None:
+        if len(seqs) != len(parents):
+            raise ValueError(f"{len(seqs)} sequences, {len(parents)} parents")
+        _check(lib().hs_pages_fork(self.handle, _i32_array(seqs), _i32_array(parents), len(seqs)))
+
+    def release(self, seqs) -> None:
+        self.fork(seqs, [-1] * len(seqs))
+
+    def compact(self, room: int):
+        return self._copies(room, lambda *out: lib().hs_pages_compact(self.handle, room, *out))
+
+    def table(self, seqs) -> Tuple[np.ndarray, np.ndarray]:
+        """(block table [n, pages_per_seq], lengths [n])."""
+        table = np.zeros((len(seqs), self.pages_per_seq), np.int32)
+        lens = np.zeros(len(seqs), np.int32)
+        as_i32 = ctypes.POINTER(ctypes.c_int32)
+        _check(lib().hs_pages_table(self.handle, _i32_array(seqs), len(seqs), table.ctypes.data_as(as_i32),
+                                    lens.ctypes.data_as(as_i32)))
+        return table, lens
+
+    def shared(self, seqs) -> int:
+        n = ctypes.c_int32(0)
+        _check(lib().hs_pages_shared(self.handle, _i32_array(seqs), len(seqs), ctypes.byref(n)))
+        return int(n.value)
+
+    def free_count(self) -> int:
+        n = ctypes.c_int32(0)
+        _check(lib().hs_pages_free_count(self.handle, ctypes.byref(n)))
+        return int(n.value)
+
+    def close(self) -> None:
+        if self.handle is not None:
+            lib().hs_pages_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):  # pragma: no cover
+        try:
+            self.close()
+        except Exception:
+            pass
 
 
 def hs_probe_hw_ids(ctx: Context, stream, n_groups: int, out_ids) -> None:

@@ -1,0 +1,185 @@
+// The best continuations of a group of beams, over beams b and vocabulary t:
+//   value(b, t) = score[b] + z[b, t] - log sum_j e^z[b, j]
+// Order: the value, then the lower beam, then the lower token; within a row, the
+// logit's own order, which its values share.
+//
+// Two launches.  The scan of hs_logprobs (logits_scan.h) reads every row once and
+// leaves, for each block of it, the sums behind the logarithm and the keys of its
+// `select` best logits: no continuation outside a row's `select` best can be among
+// the group's.  The join, a block per group, takes the logarithm of each beam's sum,
+// merges the beam's sorted lists to one, and ranks the beams' candidates against
+// each other.  The scan's read of the logits bounds the call; ended and empty beams
+// are not read.
+//
+// Values are held in 64 bits from the scan's fp32 sums on: continuations of two
+// beams that lie closer than the 2^-20 that fp32 resolves at -10 are common among
+// the many near a selection's border, and their order decides whole sequences.
+#include "decoding_kernels.h"
+#include "logits_scan.h"
+
+namespace hs {
+namespace {
+
+using namespace scan;
+
+constexpr int kJoinWaves = 16;
+
+__device__ __forceinline__ double first_lane(double v) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  const uint32_t lo = __builtin_amdgcn_readfirstlane(uint32_t(u)), hi = __builtin_amdgcn_readfirstlane(uint32_t(u >> 32));
+  return __builtin_bit_cast(double, (uint64_t(hi) << 32) | lo);
+}
+
+// Block: one group.  `team` wavefronts share a beam.
+__global__ __launch_bounds__(64 * kJoinWaves) void beam_join_kernel(BeamArgs a, LogprobsArgs scanned, int splits,
+                                                                    int team) {
+  __shared__ uint64_t lists[kJoinWaves][64];
+  __shared__ int counts[kBeamMaxBeams];
+  extern __shared__ double values[];                                   // [beams][select]
+  int32_t* tokens = reinterpret_cast<int32_t*>(values + a.beams * a.select);  // [beams][select]
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int teams = int(blockDim.x >> 6) / team, member = wave % team;
+  const int k = a.select;
+  const int64_t row0 = int64_t(blockIdx.x) * a.beams;
+  for (int b0 = 0; b0 < a.beams; b0 += teams) {
+    const int b = b0 + wave / team;
+    const bool mine = b < a.beams;
+    const int64_t row = row0 + b;
+    const bool ended = mine && a.finished && a.finished[row] != 0;
+    const float score = mine ? a.scores[row] : -kInf;
+    const bool live = mine && !ended && score > -kInf;
+    uint64_t list = 0;
+    if (live) {
+      const uint64_t* src = partial_keys(scanned, int64_t(scanned.rows) * splits) + row * splits * k;
+      // The best key of a split is a list's first, or its last where it is merged into another.
+      auto key = [&](int split, int i) { return split < splits && i < k ? src[int64_t(split) * k + i] : 0; };
+      list = key(member, lane);
+      uint64_t next = key(member + team, 63 - lane);
+      for (int s = member + team; s < splits; s += team) {
+        const uint64_t other = next;
+        next = key(s + team, 63 - lane);
+        list = merge_stages<32>(list > other ? list : other, true);
+      }
+    }
+    if (team > 1) {
+      lists[wave][lane] = list;
+      __syncthreads();
+    }
+    if (mine && member == 0) {
+      int n = 0;
+      if (live) {
+        for (int w = 1; w < min(team, splits); ++w) {
+          const uint64_t other = lists[wave + w][63 - lane];
+          list = merge_stages<32>(list > other ? list : other, true);
+        }
+        Sums sums{kLowest, 0.0f, 0.0f, 0.0f};
+        if (lane < splits) {
+          const f32x4 v = static_cast<const f32x4*>(a.part)[row * splits + lane];
+          sums = Sums{v[0], v[1], v[2], v[3]};
+        }
+        // The splits' sums against the row's maximum; F without the elements at it.
+        const float m = max_wave(sums.m);
+        const double f = exp(fmax(double(sums.m) - double(m), -700.0));
+        double s = double(sums.s) * f, rest = sums.m < m ? s : double(sums.f);
+        s = reduce_wave(s, [](double x, double y) { return x + y; });
+        rest = reduce_wave(rest, [](double x, double y) { return x + y; });
+        // One lane's for all: a product contracted into the first sum rounds differently
+        // on either side of a lane pair.
+        const double log_sum = first_lane(double(m) + (s < 1.5 ? log1p(rest) : log(s)));
+        // A row without a distribution (NaN, +inf, all masked) has no continuation.
+        const uint64_t some = s > 0.0 ? __ballot(lane < k && list != 0) : 0;
+        n = __popcll(some);
+        if (lane < n) {
+          values[b * k + lane] = double(score) + (double(value_of(list)) - log_sum);
+          tokens[b * k + lane] = token_of(list);
+        }
+      } else if (ended && score > -kInf) {
+        n = 1;
+        if (lane == 0) {
+          values[b * k] = double(score);
+          tokens[b * k] = a.end_token;
+        }
+      }
+      if (lane == 0) counts[b] = n;
+    }
+    __syncthreads();
+  }
+  // The lists are sorted: a candidate's rank is its place in its own and, by
+  // bisection, the number of larger values in each other (of equal ones, those of
+  // lower beams).
+  int total = 0;
+  for (int b = 0; b < a.beams; ++b) total += counts[b];
+  const int64_t out0 = int64_t(blockIdx.x) * k;
+  for (int c = threadIdx.x; c < a.beams * k; c += blockDim.x) {
+    const int b = c / k, i = c - b * k;
+    if (i >= counts[b]) continue;
+    const double v = values[c];
+    int rank = i;
+    for (int o = 0; o < a.beams && rank < k; ++o) {
+      if (o == b) continue;
+      int lo = 0, hi = counts[o];
+      while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        const double w = values[o * k + mid];
+        if (w > v || (w == v && o < b))
+          lo = mid + 1;
+        else
+          hi = mid;
+      }
+      rank += lo;
+    }
+    if (rank >= k) continue;
+    a.out_scores[out0 + rank] = float(v);
+    a.out_parents[out0 + rank] = b;
+    a.out_tokens[out0 + rank] = tokens[c];
+    if (a.out_finished)
+      a.out_finished[out0 + rank] = (a.finished && a.finished[row0 + b] != 0) || (a.end_token >= 0 && tokens[c] == a.end_token);
+  }
+  for (int r = total + int(threadIdx.x); r < k; r += blockDim.x) {
+    a.out_scores[out0 + r] = -kInf;
+    a.out_parents[out0 + r] = -1;
+    a.out_tokens[out0 + r] = -1;
+    if (a.out_finished) a.out_finished[out0 + r] = 0;
+  }
+}
+
+template <typename T>
+hipError_t launch(const BeamArgs& a, int cus, hipStream_t s) {
+  BeamScanArgs p{};
+  p.logits = a.logits;
+  p.type = a.type;
+  p.ld = a.ld;
+  p.rows = a.groups * a.beams;
+  p.vocab = a.vocab;
+  p.top_k = a.select;
+  p.part = a.part;
+  p.scores = a.scores;
+  p.finished = a.finished;
+  const LogprobsShape shape = logprobs_shape(p.rows, p.vocab, sizeof(T), cus);
+  if (shape.waves == 1)
+    hipLaunchKernelGGL((logprobs_kernel<T, 1, true, true, BeamScanArgs>), dim3(p.rows * shape.splits), dim3(64), 0, s, p,
+                       shape.splits);
+  else
+    hipLaunchKernelGGL((logprobs_kernel<T, 4, true, true, BeamScanArgs>), dim3(p.rows * shape.splits), dim3(256), 0, s, p,
+                       shape.splits);
+  int team = a.beams < kJoinWaves ? kJoinWaves / a.beams : 1;
+  if (team > shape.splits) team = shape.splits;
+  const int waves = a.beams * team < kJoinWaves ? a.beams * team : kJoinWaves / team * team;
+  hipLaunchKernelGGL(beam_join_kernel, dim3(a.groups), dim3(64 * waves), size_t(a.beams) * a.select * 12, s, a, p,
+                     shape.splits, team);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_beam_select(const BeamArgs& a, int cus, hipStream_t s) {
+  if (a.groups < 1) return hipSuccess;
+  switch (a.type) {
+    case HS_TYPE_F32: return launch<float>(a, cus, s);
+    case HS_TYPE_BF16: return launch<uint16_t>(a, cus, s);
+    case HS_TYPE_F16: return launch<_Float16>(a, cus, s);
+    default: return hipErrorInvalidValue;
+  }
+}
+
+}  // namespace hs

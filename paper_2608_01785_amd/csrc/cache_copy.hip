@@ -1,0 +1,52 @@
+// Copies within a key/value cache: the first positions of one slot to another, in
+// every layer.
+//
+// The first n positions of a head, n rounded up to whole value tiles, are one
+// contiguous run in the keys and one in the values, 2 n dh bytes each: a copy is
+// 2 heads layers runs between two slots.  A block moves a segment of a run, every
+// thread a few 16-byte words, all loaded before the first is stored.  Memory bounds
+// it, at two bytes moved for each copied.
+#include "decoding_kernels.h"
+#include "hs_device.h"
+
+namespace hs {
+namespace {
+
+constexpr int kCopyThreads = 256;
+constexpr int kCopyWords = kCopySegment / (kCopyThreads * 16);  // of a thread
+
+__global__ __launch_bounds__(kCopyThreads) void cache_copy_kernel(CacheCopyArgs a) {
+  // x: (segment, head); y: (layer, keys or values); z: copy.
+  const CacheCopyArgs::Copy c = a.copies[blockIdx.z];
+  const uint32_t segments = copy_segments(a.max_tiles, a.dh);
+  const int segment = blockIdx.x % segments, head = blockIdx.x / segments;
+  const int64_t first = int64_t(segment) * kCopySegment, bytes = int64_t(c.tiles) * 64 * a.dh;
+  if (first >= bytes) return;
+  uint16_t* base = (blockIdx.y & 1) ? a.v[blockIdx.y >> 1] : a.k[blockIdx.y >> 1];
+  uint8_t* p = reinterpret_cast<uint8_t*>(base) + head * a.head_bytes + first;
+  const int64_t slot = a.head_bytes * a.heads;
+  const uint8_t* src = p + c.src * slot;
+  uint8_t* dst = p + c.dst * slot;
+  const int left = int(min(bytes - first, int64_t(kCopySegment)));
+  u32x4 w[kCopyWords];
+#pragma unroll
+  for (int i = 0; i < kCopyWords; ++i) {
+    const int at = (i * kCopyThreads + int(threadIdx.x)) * 16;
+    if (at < left) w[i] = *reinterpret_cast<const u32x4*>(src + at);
+  }
+#pragma unroll
+  for (int i = 0; i < kCopyWords; ++i) {
+    const int at = (i * kCopyThreads + int(threadIdx.x)) * 16;
+    if (at < left) *reinterpret_cast<u32x4*>(dst + at) = w[i];
+  }
+}
+
+}  // namespace
+
+hipError_t launch_cache_copy(const CacheCopyArgs& a, int, hipStream_t s) {
+  if (a.n_copies < 1) return hipSuccess;
+  hipLaunchKernelGGL(cache_copy_kernel, dim3(copy_segments(a.max_tiles, a.dh) * a.heads, 2 * a.layers, a.n_copies), dim3(kCopyThreads), 0, s, a);
+  return hipGetLastError();
+}
+
+}  // namespace hs

@@ -1,0 +1,97 @@
+// Splits and sizes of the kernels for decoding on a shared cache, shared by their
+// launchers, the workspace sizes and the tests.  Pure C++; no HIP types.
+#pragma once
+
+#include <stddef.h>
+#include <stdint.h>
+
+#include "answer_policy.h"
+
+namespace hs {
+
+// hs_beam_select: beams of a group and selected continuations at most; the join
+// holds beams * select candidates in LDS (48 KB at most) and its lists of keys
+// cover a wavefront.
+constexpr int kBeamMaxBeams = 64;
+constexpr int kBeamMaxSelect = kLogprobsMaxTop;
+
+// Workspace bytes of a call of at most max_rows rows on any budget and type: a
+// partial result for every block of a row, of which there is one, or where rows
+// are split as many as hs_logprobs takes.
+inline size_t beam_workspace(int64_t max_rows, int64_t vocab, int select) {
+  const size_t whole = size_t(max_rows) * logprobs_partial_bytes(select);
+  const size_t split = logprobs_workspace(max_rows, vocab, select);
+  return whole > split ? whole : split;
+}
+
+// hs_cache_copy: layers and copies of one launch (kernel arguments hold 4 KB).
+constexpr int kCopyLayers = 32;
+constexpr int kCopyList = 240;
+constexpr int kCopySegment = 16384;  // bytes of a block
+// Segments of a head's run of so many value tiles (2^33 bytes at most: 2^19).
+constexpr uint32_t copy_segments(int tiles, int dh) {
+  return uint32_t((int64_t(tiles) * 64 * dh + kCopySegment - 1) / kCopySegment);
+}
+
+// hs_prefix_attention: which rows go through one block together, and how the keys
+// are split over blocks.
+struct PrefixShape {
+  int prefix_rows;    // rows (query heads of a group's sequences) of a block: 16 or 32
+  int prefix_tiles;   // row tiles of all groups together, at most
+  int prefix_keys;    // keys of a block
+  int prefix_splits;  // blocks over the longest prefix
+  int rest_keys, rest_splits;
+};
+
+constexpr int kPrefixMaxSplits = 64;  // of a prefix, and of what a row has to itself
+constexpr int kPrefixKeys = 128;      // a block's keys are a multiple: a tile for each wavefront
+
+inline int64_t prefix_up(int64_t n, int64_t to) { return (n + to - 1) / to; }
+
+// Keys of a block where `blocks` blocks share each split of `keys` keys.
+inline int prefix_split_keys(int64_t keys, int64_t blocks, int cus) {
+  if (keys < 1) return kPrefixKeys;
+  int64_t splits = prefix_up(4 * int64_t(cus), blocks < 1 ? 1 : blocks);
+  if (splits > kPrefixMaxSplits) splits = kPrefixMaxSplits;
+  int64_t each = prefix_up(prefix_up(keys, splits), kPrefixKeys) * kPrefixKeys;
+  const int64_t least = 2 * kPrefixKeys;
+  if (each < least) each = least;
+  return int(each);
+}
+
+inline PrefixShape prefix_shape(int n_seqs, int n_groups, int max_prefix, int max_rest, int hq, int hkv, int cus) {
+  const int64_t per_head = hq / hkv, rows = int64_t(n_seqs) * per_head;
+  PrefixShape s{};
+  s.prefix_rows = rows <= 16 * int64_t(n_groups) ? 16 : 32;
+  s.prefix_tiles = max_prefix > 0 ? int(rows / s.prefix_rows + n_groups) : 0;
+  s.prefix_keys = prefix_split_keys(max_prefix, prefix_up(rows, s.prefix_rows) * hkv, cus);
+  s.prefix_splits = int(prefix_up(max_prefix, s.prefix_keys));
+  s.rest_keys = prefix_split_keys(max_rest, int64_t(n_seqs) * hkv, cus);
+  s.rest_splits = int(prefix_up(max_rest, s.rest_keys));
+  return s;
+}
+
+// Blocks of a launch: of the prefixes, then of what rows have to themselves.
+inline int64_t prefix_blocks(const PrefixShape& s, int n_seqs, int hkv) {
+  return (int64_t(s.prefix_tiles) * s.prefix_splits + int64_t(n_seqs) * s.rest_splits) * hkv;
+}
+
+// A partial state: dh unnormalised outputs, and the maximum and sum behind them.
+inline size_t prefix_part_bytes(int dh) { return size_t(4 * dh + 8); }
+
+// Workspace bytes for at most n_seqs rows, on any budget.  Fewer rows or groups, a
+// smaller bound and fewer CUs never take more partial states than this: `blocks`
+// blocks take at most 4 cus / blocks + 1 splits, and each block holds prefix_rows
+// (rest: per_head) states of a split.
+inline size_t prefix_workspace(int n_seqs, int max_prefix, int max_rest, int hq, int hkv, int dh) {
+  const int64_t rows = int64_t(n_seqs) * hq;
+  auto states = [&](int64_t keys, int64_t of_block) {
+    int64_t splits = prefix_up(keys, 2 * kPrefixKeys);
+    if (splits > kPrefixMaxSplits) splits = kPrefixMaxSplits;
+    const int64_t shared = 4 * 256 * of_block + rows, each = rows * splits;
+    return splits < 1 ? 0 : each < shared ? each : shared;
+  };
+  return size_t(states(max_prefix, 32) + states(max_rest, hq / hkv)) * prefix_part_bytes(dh);
+}
+
+}  // namespace hs
