@@ -36,7 +36,7 @@ constexpr uint32_t copy_segments(int tiles, int dh) {
 // hs_prefix_attention: which rows go through one block together, and how the keys
 // are split over blocks.
 struct PrefixShape {
-  int prefix_rows;    // rows (query heads of a group's sequences) of a block: 16 or 32
+  int prefix_rows;    // rows (query heads of a group's sequences) of a block: 16, 32 or 128
   int prefix_tiles;   // row tiles of all groups together, at most
   int prefix_keys;    // keys of a block
   int prefix_splits;  // blocks over the longest prefix
@@ -49,9 +49,9 @@ constexpr int kPrefixKeys = 128;      // a block's keys are a multiple: a tile f
 inline int64_t prefix_up(int64_t n, int64_t to) { return (n + to - 1) / to; }
 
 // Keys of a block where `blocks` blocks share each split of `keys` keys.
-inline int prefix_split_keys(int64_t keys, int64_t blocks, int cus) {
+inline int prefix_split_keys(int64_t keys, int64_t blocks, int cus, int per_cu) {
   if (keys < 1) return kPrefixKeys;
-  int64_t splits = prefix_up(4 * int64_t(cus), blocks < 1 ? 1 : blocks);
+  int64_t splits = prefix_up(per_cu * int64_t(cus), blocks < 1 ? 1 : blocks);
   if (splits > kPrefixMaxSplits) splits = kPrefixMaxSplits;
   int64_t each = prefix_up(prefix_up(keys, splits), kPrefixKeys) * kPrefixKeys;
   const int64_t least = 2 * kPrefixKeys;
@@ -62,11 +62,11 @@ inline int prefix_split_keys(int64_t keys, int64_t blocks, int cus) {
 inline PrefixShape prefix_shape(int n_seqs, int n_groups, int max_prefix, int max_rest, int hq, int hkv, int cus) {
   const int64_t per_head = hq / hkv, rows = int64_t(n_seqs) * per_head;
   PrefixShape s{};
-  s.prefix_rows = rows <= 16 * int64_t(n_groups) ? 16 : 32;
+  s.prefix_rows = rows <= 16 * int64_t(n_groups) ? 16 : rows <= 64 * int64_t(n_groups) ? 32 : 128;
   s.prefix_tiles = max_prefix > 0 ? int(rows / s.prefix_rows + n_groups) : 0;
-  s.prefix_keys = prefix_split_keys(max_prefix, prefix_up(rows, s.prefix_rows) * hkv, cus);
+  s.prefix_keys = prefix_split_keys(max_prefix, prefix_up(rows, s.prefix_rows) * hkv, cus, s.prefix_rows == 128 ? 2 : 4);
   s.prefix_splits = int(prefix_up(max_prefix, s.prefix_keys));
-  s.rest_keys = prefix_split_keys(max_rest, int64_t(n_seqs) * hkv, cus);
+  s.rest_keys = prefix_split_keys(max_rest, int64_t(n_seqs) * hkv, cus, 4);
   s.rest_splits = int(prefix_up(max_rest, s.rest_keys));
   return s;
 }
@@ -88,10 +88,10 @@ inline size_t prefix_workspace(int n_seqs, int max_prefix, int max_rest, int hq,
   auto states = [&](int64_t keys, int64_t of_block) {
     int64_t splits = prefix_up(keys, 2 * kPrefixKeys);
     if (splits > kPrefixMaxSplits) splits = kPrefixMaxSplits;
-    const int64_t shared = 4 * 256 * of_block + rows, each = rows * splits;
+    const int64_t shared = 256 * of_block + rows, each = rows * splits;
     return splits < 1 ? 0 : each < shared ? each : shared;
   };
-  return size_t(states(max_prefix, 32) + states(max_rest, hq / hkv)) * prefix_part_bytes(dh);
+  return size_t(states(max_prefix, 2 * 128) + states(max_rest, 4 * (hq / hkv))) * prefix_part_bytes(dh);
 }
 
 }  // namespace hs

@@ -16,9 +16,13 @@
 // passes them through an LDS image of its own into MFMA layout, S^T = K Q^T and
 // O^T = V^T P^T, with a running softmax.
 //
+// Where a group has more columns than such a unit, the tile is that of prefill attention
+// (attention_tile.h): 128 columns, 32 a wavefront, which share 64-key tiles in LDS.
+//
 // What the device arrays say is checked here: a slot outside the cache is read as
 // zeros and makes its rows NaN, and no range leaves the table.
 #include "answer_device.h"
+#include "attention_tile.h"
 #include "decode_policy.h"
 #include "decoding_kernels.h"
 
@@ -357,11 +361,229 @@ __device__ __forceinline__ void unit(const PrefixArgs& a, int lo, int m0, int n_
   }
 }
 
+template <bool C, typename A, typename B>
+struct Choose {
+  using type = A;
+};
+template <typename A, typename B>
+struct Choose<false, A, B> {
+  using type = B;
+};
+
+// The same for up to 128 columns: wavefront w takes columns 32 w .. 32 w + 31 over all
+// keys, whose tiles of 64 pass through LDS for all of them.  k_lo is a tile's start.
+template <int DH>
+struct WideSmem {
+  static constexpr int kTile = BKV * DH * 2;
+  static constexpr int kRow = 64 + 4;  // a state's 64 dimensions; 16 columns apart in banks
+  union {
+    uint8_t tile[2][2][kTile];         // [stage][keys, values]
+    float out[4][32][kRow];
+  };
+};
+
+template <int DH, typename T>
+__device__ __forceinline__ void wide_unit(const PrefixArgs& a, int lo, int m0, int n_cols, int head, int owner,
+                                          int k_lo, int k_hi, int split, int splits, WideSmem<DH>& sm) {
+  constexpr int KROW = DH * 2, KCH = DH / 8;
+  constexpr int LOADS = BKV * KCH / kThreads;  // of a thread, keys and values alike
+  constexpr int NDS = DH / 32;
+  const int tid = threadIdx.x, lane = tid & 63, wave = first_lane(tid >> 6);
+  const int fr = lane & 31, fh = lane >> 5;
+  const int G = a.hq / a.hkv;
+  const int64_t head_elems = int64_t(a.page) * DH, slot_elems = head_elems * a.hkv;
+  const int n_tiles = (k_hi - k_lo + BKV - 1) / BKV;
+  const int32_t* pages = a.table + int64_t(owner) * a.pages_per_seq;
+  bool bad = false;
+
+  u32x4 qf[DH / 16];
+  {
+    const int m = m0 + min(wave * 32 + fr, n_cols - 1);  // lanes past the last column repeat it
+    const uint16_t* qp = static_cast<const uint16_t*>(a.q) + int64_t(lo + m / G) * a.ldq + (head * G + m % G) * DH;
+#pragma unroll
+    for (int kb = 0; kb < DH / 16; ++kb) {
+      qf[kb] = *reinterpret_cast<const u32x4*>(qp + kb * 16 + fh * 8);
+      if constexpr (__is_same(T, uint16_t)) qf[kb] = bf8_to_h8(qf[kb]);
+    }
+  }
+
+  uint32_t koff[LOADS], voff[LOADS];
+#pragma unroll
+  for (int j = 0; j < LOADS; ++j) {
+    const int idx = tid + j * kThreads, d = idx >> 3, c = idx & 7;
+    koff[j] = uint32_t(idx * 16);
+    voff[j] = uint32_t(((c >> 2) * kv_tile_keys * DH + d * kv_tile_keys + (c & 3) * 8) * 2);
+  }
+  u32x4 rk[LOADS], rv[LOADS];
+  auto slot_of = [&](int t) { return first_lane(pages[(k_lo + min(t, n_tiles - 1) * BKV) / a.page]); };
+  auto gload = [&](int t, int slot) {
+    const bool ok = slot >= 0 && slot < a.n_slots;
+    bad |= !ok;
+    const int64_t at = ok ? slot * slot_elems + head * head_elems + int64_t((k_lo + t * BKV) % a.page) * DH : int64_t(0);
+    const uint32_t bytes = ok ? uint32_t(WideSmem<DH>::kTile) : 0u;
+    auto res = [&](const uint16_t* store) {
+      const uint64_t p = reinterpret_cast<uint64_t>(store + at);
+      const uint64_t u = (uint64_t(uint32_t(first_lane(int(p >> 32)))) << 32) | uint32_t(first_lane(int(p)));
+      return make_rsrc(reinterpret_cast<const void*>(u), bytes);
+    };
+    const __amdgpu_buffer_rsrc_t kres = res(a.k), vres = res(a.v);
+#pragma unroll
+    for (int j = 0; j < LOADS; ++j) rk[j] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(kres, koff[j], 0, 0));
+#pragma unroll
+    for (int j = 0; j < LOADS; ++j) rv[j] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(vres, voff[j], 0, 0));
+  };
+  // Values past the range may be anything; 0 * NaN must not reach the sum.
+  auto vmask = [&](int t) {
+    if (k_lo + (t + 1) * BKV <= k_hi) return;
+#pragma unroll
+    for (int j = 0; j < LOADS; ++j) {
+      const int left = k_hi - (k_lo + t * BKV + ((tid + j * kThreads) & 7) * 8);
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        rv[j][e] &= (2 * e < left ? 0x0000ffffu : 0u) | (2 * e + 1 < left ? 0xffff0000u : 0u);
+    }
+  };
+  auto lstore = [&](int stage) {
+    uint8_t* ks = sm.tile[stage][0];
+    uint8_t* vs = sm.tile[stage][1];
+#pragma unroll
+    for (int j = 0; j < LOADS; ++j) {
+      const int idx = tid + j * kThreads, row = idx / KCH, c = idx % KCH;
+      *reinterpret_cast<u32x4*>(ks + row * KROW + kphys<DH>(row, c) * 16) = rk[j];
+    }
+#pragma unroll
+    for (int j = 0; j < LOADS; ++j) {
+      const int idx = tid + j * kThreads, d = idx >> 3, c = idx & 7;
+      *reinterpret_cast<u32x4*>(vs + d * 128 + vphys(d, c) * 16) = rv[j];
+    }
+  };
+
+  f32x16 o[NDS];
+#pragma unroll
+  for (int i = 0; i < NDS; ++i)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[i][r] = 0.0f;
+  float m_run = -kInf, l_run = 0.0f;
+
+  gload(0, slot_of(0));
+  vmask(0);
+  lstore(0);
+  int slot = slot_of(1);
+  __syncthreads();
+  const bool busy = wave * 32 < n_cols;
+  for (int t = 0; t < n_tiles; ++t) {
+    if (t + 1 < n_tiles) gload(t + 1, slot);
+    slot = slot_of(t + 2);
+    if (busy) {
+      const uint8_t* ks = sm.tile[t & 1][0];
+      const uint8_t* vs = sm.tile[t & 1][1];
+      f32x16 sc[2];
+#pragma unroll
+      for (int st = 0; st < 2; ++st)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sc[st][r] = 0.0f;
+      // Fragments are read a step ahead of the products that use them.
+      auto kfrag = [&](int kb, int st) {
+        const int row = 32 * st + perm32(fr);
+        return *reinterpret_cast<const u32x4*>(ks + row * KROW + kphys<DH>(row, 2 * kb + fh) * 16);
+      };
+      u32x4 kf[2][2];
+      kf[0][0] = kfrag(0, 0);
+      kf[0][1] = kfrag(0, 1);
+      __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+#pragma unroll
+      for (int kb = 0; kb < DH / 16; ++kb) {
+        if (kb + 1 < DH / 16) {
+          kf[(kb + 1) & 1][0] = kfrag(kb + 1, 0);
+          kf[(kb + 1) & 1][1] = kfrag(kb + 1, 1);
+        }
+        sc[0] = mfma32(kf[kb & 1][0], qf[kb], sc[0]);
+        sc[1] = mfma32(kf[kb & 1][1], qf[kb], sc[1]);
+        if (kb + 1 < DH / 16) {
+          __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+          __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      u32x4 pf[4];
+      const int last = k_hi - 1 - (k_lo + t * BKV);  // the tile's last key
+      softmax_tile<NDS>(sc, o, pf, m_run, l_run, a.scale_log2, last < BKV - 1, last - 8 * fh);
+      auto vfrag = [&](int kb2, int i) {
+        const int d = 32 * i + fr;
+        return *reinterpret_cast<const u32x4*>(vs + d * 128 + vphys(d, 2 * kb2 + fh) * 16);
+      };
+      u32x4 vf[2][NDS];
+#pragma unroll
+      for (int i = 0; i < NDS; ++i) vf[0][i] = vfrag(0, i);
+      __builtin_amdgcn_sched_group_barrier(0x100, NDS, 0);
+#pragma unroll
+      for (int kb2 = 0; kb2 < 4; ++kb2) {
+        if (kb2 + 1 < 4) {
+#pragma unroll
+          for (int i = 0; i < NDS; ++i) vf[(kb2 + 1) & 1][i] = vfrag(kb2 + 1, i);
+        }
+#pragma unroll
+        for (int i = 0; i < NDS; ++i) o[i] = mfma32(vf[kb2 & 1][i], pf[kb2], o[i]);
+        if (kb2 + 1 < 4) {
+          __builtin_amdgcn_sched_group_barrier(0x100, NDS, 0);
+          __builtin_amdgcn_sched_group_barrier(0x008, NDS, 0);
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    if (t + 1 < n_tiles) {
+      vmask(t + 1);
+      lstore((t + 1) & 1);
+    }
+    __syncthreads();
+  }
+  if (!busy) return;
+
+  // A wavefront's states leave through its part of LDS as rows.
+  const float l_tot = l_run + xor_lane<32>(l_run);
+  float* stats = part_stats(a, splits);
+  if (fh == 0 && wave * 32 + fr < n_cols) {
+    const int m = m0 + wave * 32 + fr;
+    const int64_t p = part_index(a, split, lo + m / G, head * G + m % G);
+    stats[2 * p] = m_run;
+    stats[2 * p + 1] = bad ? __builtin_nanf("") : l_tot;
+  }
+  float(*mine)[WideSmem<DH>::kRow] = sm.out[wave];
+#pragma unroll
+  for (int pass = 0; pass < DH / 64; ++pass) {
+    asm volatile("" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const f32x16& v = o[2 * pass + i];
+        *reinterpret_cast<f32x4*>(&mine[fr][32 * i + 8 * g + 4 * fh]) =
+            f32x4{v[4 * g], v[4 * g + 1], v[4 * g + 2], v[4 * g + 3]};
+      }
+    asm volatile("" ::: "memory");
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int col = 4 * j + (lane >> 4), d = (lane & 15) * 4;
+      if (wave * 32 + col >= n_cols) continue;
+      const int m = m0 + wave * 32 + col;
+      const int64_t p = part_index(a, split, lo + m / G, head * G + m % G);
+      *reinterpret_cast<f32x4*>(static_cast<float*>(a.part) + p * DH + 64 * pass + d) =
+          *reinterpret_cast<const f32x4*>(&mine[col][d]);
+    }
+  }
+}
+
 // Blocks of the prefixes (key/value head, row tile, split), then those of what rows
 // have to themselves (key/value head, row, split).
-template <int DH, int NQ, typename T>
+// WIDE: the prefixes' tiles are wide ones.
+template <int DH, int NQ, bool WIDE, typename T>
 __global__ __launch_bounds__(kThreads, 2) void prefix_kernel(PrefixArgs a, PrefixShape s) {
-  __shared__ __attribute__((aligned(16))) Smem<DH, NQ> sm;
+  union Lds {
+    Smem<DH, NQ> narrow;
+    typename Choose<WIDE, WideSmem<DH>, Smem<DH, NQ>>::type wide;
+  };
+  __shared__ __attribute__((aligned(16))) Lds sm;
+  constexpr int kCols = WIDE ? 128 : 16 * NQ;
   const int G = a.hq / a.hkv, splits = s.prefix_splits + s.rest_splits;
   const int64_t reach = int64_t(a.pages_per_seq) * a.page;  // positions that the table covers
   uint32_t id = blockIdx.x;
@@ -370,12 +592,15 @@ __global__ __launch_bounds__(kThreads, 2) void prefix_kernel(PrefixArgs a, Prefi
   if (id < prefix_blocks) {
     id /= a.hkv;
     const int split = id % s.prefix_splits, tile = id / s.prefix_splits;
-    const Group g = group_of_tile(a, tile, 16 * NQ, G);
-    const int m0 = g.tile * 16 * NQ, n_cols = min((g.hi - g.lo) * G - m0, 16 * NQ);
+    const Group g = group_of_tile(a, tile, kCols, G);
+    const int m0 = g.tile * kCols, n_cols = min((g.hi - g.lo) * G - m0, kCols);
     const int prefix = int(min(int64_t(clamped(g.prefix, 0, a.max_prefix)), reach));
     const int k_lo = split * s.prefix_keys, k_hi = min(prefix, k_lo + s.prefix_keys);
     if (n_cols < 1 || k_hi <= k_lo) return;
-    unit<DH, NQ, T>(a, g.lo, m0, n_cols, head, g.lo, k_lo, k_hi, split, splits, sm);
+    if constexpr (WIDE)
+      wide_unit<DH, T>(a, g.lo, m0, n_cols, head, g.lo, k_lo, k_hi, split, splits, sm.wide);
+    else
+      unit<DH, NQ, T>(a, g.lo, m0, n_cols, head, g.lo, k_lo, k_hi, split, splits, sm.narrow);
   } else {
     id = (id - prefix_blocks) / a.hkv;
     const int split = id % s.rest_splits, row = id / s.rest_splits;
@@ -387,57 +612,86 @@ __global__ __launch_bounds__(kThreads, 2) void prefix_kernel(PrefixArgs a, Prefi
     for (int m0 = 0; m0 < G; m0 += 16 * NQ) {
       if (m0 > 0) __syncthreads();  // the last unit's states have been read
       unit<DH, NQ, T>(a, row, m0, min(G - m0, 16 * NQ), head, row, int(k_lo), int(k_hi), s.prefix_splits + split,
-                      splits, sm);
+                      splits, sm.narrow);
     }
   }
 }
 
-// One wavefront a (row, query head).
-template <int DH, typename T>
+// W wavefronts a (row, query head): each adds up every W-th of its partial states, all
+// of a batch's loads in flight, and the first what they have.
+constexpr int kJoinBatch = 8;
+
+template <int DH, int W, typename T>
 __global__ __launch_bounds__(kThreads) void prefix_join_kernel(PrefixArgs a, PrefixShape s) {
-  const int lane = threadIdx.x & 63;
-  const int64_t index = int64_t(blockIdx.x) * 4 + first_lane(threadIdx.x >> 6);
-  if (index >= int64_t(a.n_seqs) * a.hq) return;
-  const int row = int(index / a.hq), head = int(index % a.hq);
-  const int prefix = prefix_of_row(a, row), len = a.lens[row];
+  constexpr int V = DH / 64;
+  typedef float Vec __attribute__((ext_vector_type(V)));
+  __shared__ float sums[4][DH + 2];
+  const int lane = threadIdx.x & 63, wave = first_lane(threadIdx.x >> 6), member = wave % W;
+  const int64_t index = int64_t(blockIdx.x) * (4 / W) + wave / W;
+  const bool mine = index < int64_t(a.n_seqs) * a.hq;
+  const int row = mine ? int(index / a.hq) : 0, head = int(index % a.hq);
+  const int len = a.lens[row], prefix = prefix_of_row(a, row);
   const int64_t reach = int64_t(a.pages_per_seq) * a.page;
   const bool wrong = prefix < 0 || prefix > a.max_prefix || len < prefix || len - prefix > a.max_rest || len > reach;
   const int splits = s.prefix_splits + s.rest_splits;
   const float* stats = part_stats(a, splits);
   const float* part = static_cast<const float*>(a.part);
-  const int n_prefix = wrong ? 0 : (prefix + s.prefix_keys - 1) / s.prefix_keys;
-  const int n_rest = wrong ? 0 : (len - prefix + s.rest_keys - 1) / s.rest_keys;
-  constexpr int V = DH / 64;
-  float M = -kInf, L = 0.0f, acc[V] = {};
-  for (int i0 = 0; i0 < n_prefix + n_rest; i0 += 64) {
-    // The row's partial state number i0 + lane.
-    const int i = i0 + lane, n = min(n_prefix + n_rest - i0, 64);
-    const int split = i < n_prefix ? i : s.prefix_splits + i - n_prefix;
-    float m = -kInf, l = 0.0f;
-    if (lane < n) {
-      const int64_t p = part_index(a, split, row, head);
-      m = stats[2 * p];
-      l = stats[2 * p + 1];
+  const int n_prefix = wrong || !mine ? 0 : (prefix + s.prefix_keys - 1) / s.prefix_keys;
+  const int n = wrong || !mine ? 0 : n_prefix + (len - prefix + s.rest_keys - 1) / s.rest_keys;
+  float M = -kInf, L = 0.0f;
+  Vec acc = 0.0f;
+  for (int i0 = member; i0 < n; i0 += W * kJoinBatch) {
+    float m[kJoinBatch], l[kJoinBatch];
+    Vec v[kJoinBatch];
+#pragma unroll
+    for (int j = 0; j < kJoinBatch; ++j) {
+      const int i = min(i0 + j * W, n - 1);
+      const int64_t p = part_index(a, i < n_prefix ? i : s.prefix_splits + i - n_prefix, row, head);
+      m[j] = stats[2 * p];
+      l[j] = stats[2 * p + 1];
+      v[j] = *reinterpret_cast<const Vec*>(part + p * DH + lane * V);
     }
-    const float top = fmaxf(M, reduce_wave(m, [](float x, float y) { return fmaxf(x, y); }));
-    const float w = lane < n ? exp2_raw(m - top) : 0.0f, old = exp2_raw(M - top);
-    L = L * old + reduce_wave(w * l, [](float x, float y) { return x + y; });
+    float top = M;
 #pragma unroll
-    for (int e = 0; e < V; ++e) acc[e] *= old;
-    for (int k = 0; k < n; ++k) {
-      const int sk = i0 + k < n_prefix ? i0 + k : s.prefix_splits + i0 + k - n_prefix;
-      const float wk = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), k));
-      const float* src = part + part_index(a, sk, row, head) * DH;
+    for (int j = 0; j < kJoinBatch; ++j) top = fmaxf(top, i0 + j * W < n ? m[j] : -kInf);
+    const float old = exp2_raw(M - top);
+    L *= old;
+    acc *= old;
 #pragma unroll
-      for (int e = 0; e < V; ++e) acc[e] = fmaf(wk, src[e * 64 + lane], acc[e]);
+    for (int j = 0; j < kJoinBatch; ++j) {
+      const float w = i0 + j * W < n ? exp2_raw(m[j] - top) : 0.0f;
+      if (i0 + j * W < n) {
+        L = fmaf(w, l[j], L);
+        acc += w * v[j];
+      }
     }
     M = top;
   }
-  const bool none = n_prefix + n_rest == 0;
+  if constexpr (W > 1) {
+#pragma unroll
+    for (int e = 0; e < V; ++e) sums[wave][lane * V + e] = acc[e];
+    if (lane == 0) {
+      sums[wave][DH] = M;
+      sums[wave][DH + 1] = L;
+    }
+    __syncthreads();
+    if (member != 0) return;
+    float top = -kInf;
+    for (int w = 0; w < min(W, n); ++w) top = fmaxf(top, sums[wave + w][DH]);
+    acc = 0.0f;
+    L = 0.0f;
+    for (int w = 0; w < min(W, n); ++w) {
+      const float f = exp2_raw(sums[wave + w][DH] - top);
+      L = fmaf(f, sums[wave + w][DH + 1], L);
+#pragma unroll
+      for (int e = 0; e < V; ++e) acc[e] = fmaf(f, sums[wave + w][lane * V + e], acc[e]);
+    }
+  }
+  if (!mine) return;
 #pragma unroll
   for (int e = 0; e < V; ++e) {
-    const float y = wrong ? __builtin_nanf("") : none ? 0.0f : acc[e] / L;
-    const int d = head * DH + e * 64 + lane;
+    const float y = wrong ? __builtin_nanf("") : n == 0 ? 0.0f : acc[e] / L;
+    const int d = head * DH + lane * V + e;
     if (a.out_k8_rows) {
       static_cast<uint16_t*>(a.out)[act_index(row, d, 0, a.out_k8_rows)] = f2h(y);
     } else if constexpr (__is_same(T, uint16_t)) {
@@ -457,12 +711,17 @@ hipError_t launch(const PrefixArgs& a, int cus, hipStream_t st) {
   const int64_t blocks = prefix_blocks(s, a.n_seqs, a.hkv);
   if (blocks > 0) {
     if (s.prefix_rows == 16)
-      hipLaunchKernelGGL((prefix_kernel<DH, 1, T>), dim3(uint32_t(blocks)), dim3(kThreads), 0, st, a, s);
+      hipLaunchKernelGGL((prefix_kernel<DH, 1, false, T>), dim3(uint32_t(blocks)), dim3(kThreads), 0, st, a, s);
+    else if (s.prefix_rows == 128)
+      hipLaunchKernelGGL((prefix_kernel<DH, 1, true, T>), dim3(uint32_t(blocks)), dim3(kThreads), 0, st, a, s);
     else
-      hipLaunchKernelGGL((prefix_kernel<DH, 2, T>), dim3(uint32_t(blocks)), dim3(kThreads), 0, st, a, s);
+      hipLaunchKernelGGL((prefix_kernel<DH, 2, false, T>), dim3(uint32_t(blocks)), dim3(kThreads), 0, st, a, s);
   }
   const int64_t rows = int64_t(a.n_seqs) * a.hq;
-  hipLaunchKernelGGL((prefix_join_kernel<DH, T>), dim3(uint32_t((rows + 3) / 4)), dim3(kThreads), 0, st, a, s);
+  if (s.prefix_splits + s.rest_splits > 4 && rows <= 16 * int64_t(cus))
+    hipLaunchKernelGGL((prefix_join_kernel<DH, 4, T>), dim3(uint32_t(rows)), dim3(kThreads), 0, st, a, s);
+  else
+    hipLaunchKernelGGL((prefix_join_kernel<DH, 1, T>), dim3(uint32_t((rows + 3) / 4)), dim3(kThreads), 0, st, a, s);
   return hipGetLastError();
 }
 
