@@ -178,6 +178,9 @@ hs_status hs_prefix_attention_workspace_size(int32_t n_q_heads, int32_t n_kv_hea
   HS_TRY(check_heads(n_kv_heads, head_dim));
   if (n_q_heads < 1 || n_q_heads % n_kv_heads != 0)
     return fail(HS_ERR_INVALID_ARG, "%d query heads on %d key/value heads", n_q_heads, n_kv_heads);
+  if (n_q_heads / n_kv_heads > kPrefixMaxPerHead)
+    return fail(HS_ERR_UNSUPPORTED, "%d query heads per key/value head: at most %d", n_q_heads / n_kv_heads,
+                kPrefixMaxPerHead);
   if (n_seqs < 0 || max_prefix < 0 || max_rest < 0)
     return fail(HS_ERR_INVALID_ARG, "%d rows, prefixes up to %d and %d keys more", n_seqs, max_prefix, max_rest);
   if (int64_t(max_prefix) + max_rest > (int64_t(1) << 30) || n_q_heads > (1 << 16) ||
@@ -253,6 +256,7 @@ hs_status hs_prefix_attention(hs_context* ctx, const void* q, int32_t type, int6
   a.hq = n_q_heads;
   a.hkv = n_kv_heads;
   a.dh = head_dim;
+  a.per_head_inv = prefix_inverse(n_q_heads / n_kv_heads);
   a.scale_log2 = 1.4426950408889634f / sqrtf(float(head_dim));
   a.part = workspace;
   return run(ctx, cu_budget, stream, n_seqs == 0, HS_KERNEL_PREFIX_ATTN,

@@ -63,6 +63,7 @@ struct PrefixArgs {
   int n_groups;
   int max_prefix, max_rest; // bounds of the prefixes and of what the rows have to themselves
   int hq, hkv, dh;
+  uint32_t per_head_inv;    // prefix_inverse(hq / hkv)
   float scale_log2;         // log2(e) / sqrt(dh)
   void* part;               // prefix_workspace() bytes
 };

@@ -33,6 +33,11 @@ constexpr uint32_t copy_segments(int tiles, int dh) {
   return uint32_t((int64_t(tiles) * 64 * dh + kCopySegment - 1) / kCopySegment);
 }
 
+// m / per_head = 2 m prefix_inverse(per_head) >> 32 for m < 2^31 / per_head: a launch
+// has at most 2^25 columns, and at most this many query heads share a key/value head.
+constexpr int kPrefixMaxPerHead = 64;
+constexpr uint32_t prefix_inverse(int per_head) { return ((uint32_t(1) << 31) + per_head - 1) / per_head; }
+
 // hs_prefix_attention: which rows go through one block together, and how the keys
 // are split over blocks.
 struct PrefixShape {

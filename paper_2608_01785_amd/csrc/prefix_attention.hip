@@ -33,63 +33,53 @@ constexpr int kThreads = 256;
 constexpr int kTileKeys = kv_tile_keys;
 constexpr float kInf = __builtin_inff();
 
+__device__ __forceinline__ int clamped(int v, int lo, int hi) { return min(max(v, lo), hi); }
+__device__ __forceinline__ int first_lane(int v) { return __builtin_amdgcn_readfirstlane(v); }
+
+// m / per_head, by the product with its rounded-up inverse.
+__device__ __forceinline__ int row_of(const PrefixArgs& a, int m) {
+  return int(__umulhi(2u * uint32_t(m), a.per_head_inv));
+}
+
 struct Group {
   int lo, hi;   // its rows
   int prefix;   // its shared positions
   int tile;     // of the group's row tiles
 };
 
-__device__ __forceinline__ int clamped(int v, int lo, int hi) { return min(max(v, lo), hi); }
-
-// Rows [lo, hi) and prefix of group g, inside what the arguments allow.
-__device__ __forceinline__ Group group_at(const PrefixArgs& a, int g) {
-  Group r;
-  r.lo = clamped(a.offsets[g], 0, a.n_seqs);
-  r.hi = clamped(a.offsets[g + 1], r.lo, a.n_seqs);
-  r.prefix = a.prefix[g];
-  r.tile = 0;
-  return r;
-}
-
-__device__ __forceinline__ int first_lane(int v) { return __builtin_amdgcn_readfirstlane(v); }
-
-// The group that holds row tile `t` (tiles of `rows` columns, `per_head` of them a
-// row); lo == hi where there is none.  A wavefront looks at 64 groups at a time.
-__device__ __forceinline__ Group group_of_tile(const PrefixArgs& a, int t, int rows, int per_head) {
-  const int lane = threadIdx.x & 63;
+// The group that holds row tile `t` (of COLS columns, per_head of them a row); lo == hi
+// where there is none.  The tiles of group g have the numbers from
+// offsets[g] per_head / COLS + g on, which leaves each group enough of them and needs
+// no sum over the groups before.  A wavefront looks at 64 groups at a time.
+template <int COLS>
+__device__ __forceinline__ Group group_of_tile(const PrefixArgs& a, int t) {
+  const int lane = threadIdx.x & 63, per_head = a.hq / a.hkv;
+  Group f{0, 0, 0, 0};
   for (int g0 = 0; g0 < a.n_groups; g0 += 64) {
-    Group r{0, 0, 0, 0};
-    if (g0 + lane < a.n_groups) r = group_at(a, g0 + lane);
-    const int tiles = int((int64_t(r.hi - r.lo) * per_head + rows - 1) / rows);
-    int end = tiles;  // tiles up to and with this lane's group
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int below = __shfl_up(end, o, 64);
-      if (lane >= o) end += below;
-    }
-    const uint64_t mask = __ballot(t < end);
-    if (mask != 0) {
-      const int w = __builtin_ctzll(mask);
-      Group f;
-      f.lo = __shfl(r.lo, w, 64);
-      f.hi = __shfl(r.hi, w, 64);
-      f.prefix = __shfl(r.prefix, w, 64);
-      f.tile = t - __shfl(end - tiles, w, 64);
-      return f;
-    }
-    t -= __shfl(end, 63, 64);
+    const int g = min(g0 + lane, a.n_groups - 1);
+    const int lo = clamped(a.offsets[g], 0, a.n_seqs), hi = clamped(a.offsets[g + 1], lo, a.n_seqs);
+    const int prefix = a.prefix[g];
+    const int start = int(uint32_t(lo) * uint32_t(per_head) / COLS) + g;
+    const uint64_t mask = __ballot(g0 + lane < a.n_groups && start <= t);
+    if (mask == 0) break;
+    const int w = 63 - __builtin_clzll(mask);
+    f.lo = __builtin_amdgcn_readlane(lo, w);
+    f.hi = __builtin_amdgcn_readlane(hi, w);
+    f.prefix = __builtin_amdgcn_readlane(prefix, w);
+    f.tile = t - __builtin_amdgcn_readlane(start, w);
+    if (w < 63) break;
   }
-  return Group{0, 0, 0, 0};
+  return f;
 }
 
 // The prefix of a row's group (0 where no group holds the row).
 __device__ __forceinline__ int prefix_of_row(const PrefixArgs& a, int row) {
   const int lane = threadIdx.x & 63;
   for (int g0 = 0; g0 < a.n_groups; g0 += 64) {
-    const int g = g0 + lane;
-    const bool mine = g < a.n_groups && a.offsets[g] <= row && row < a.offsets[g + 1];
-    const uint64_t mask = __ballot(mine);
-    if (mask != 0) return a.prefix[first_lane(g0 + __builtin_ctzll(mask))];
+    const int g = min(g0 + lane, a.n_groups - 1);
+    const int lo = a.offsets[g], hi = a.offsets[g + 1], prefix = a.prefix[g];
+    const uint64_t mask = __ballot(g0 + lane < a.n_groups && lo <= row && row < hi);
+    if (mask != 0) return __builtin_amdgcn_readlane(prefix, __builtin_ctzll(mask));
   }
   return 0;
 }
@@ -106,7 +96,7 @@ template <int DH, int NQ>
 struct Smem {
   static constexpr int kTile = kTileKeys * DH * 2;  // bytes of a tile's keys, and of its values
   static constexpr int kCols = 16 * NQ;
-  static constexpr int kPass = 64;                  // dimensions of a pass of the join of wavefronts
+  static constexpr int kPass = NQ == 1 ? DH : 64;   // dimensions of a pass of the join of wavefronts
   union {
     uint8_t tile[4][kTile];
     float red_o[4][kPass][kCols + 1];
@@ -142,20 +132,28 @@ __device__ __forceinline__ void unit(const PrefixArgs& a, int lo, int m0, int n_
   const int my_tiles = n_tiles > wave ? (n_tiles - wave + 3) / 4 : 0;
   const int32_t* pages = a.table + int64_t(owner) * a.pages_per_seq;
 
-  // The page of the wavefront's tile i (clamped to its last one) and the tile's
-  // place in it.
+  // The wavefront's tiles lie 4 TK positions apart: the page of the next one to load, and
+  // its place in it.
   bool bad = false;
-  auto slot_of = [&](int i) {
-    const int key = (t0 + wave + 4 * min(i, my_tiles - 1)) * TK;
-    return first_lane(pages[key / a.page]);
+  int page_no = 0, page_at = 0;
+  if (my_tiles > 0) {
+    const int key = (t0 + wave) * TK;
+    page_no = first_lane(key / a.page);
+    page_at = key - page_no * a.page;
+  }
+  auto advance = [&](int& no, int& at) {
+    at += 4 * TK;
+    while (at >= a.page) {
+      at -= a.page;
+      ++no;
+    }
   };
   struct {
     u32x4 k[NL], v[NL];
   } tl;
-  auto base_of = [&](int i, int slot, uint32_t& bytes) {
-    const int key = (t0 + wave + 4 * i) * TK;
-    bytes = i < my_tiles && slot >= 0 && slot < a.n_slots ? uint32_t(kTile) : 0u;
-    return bytes ? slot * slot_elems + head * head_elems + int64_t(key % a.page) * DH : int64_t(0);
+  auto base_of = [&](int slot, int at, uint32_t& bytes) {
+    bytes = slot >= 0 && slot < a.n_slots ? uint32_t(kTile) : 0u;
+    return bytes ? slot * slot_elems + head * head_elems + int64_t(at) * DH : int64_t(0);
   };
   auto load = [&](u32x4 (&d)[NL], const uint16_t* store, int64_t at, uint32_t bytes) {
     const uint64_t p = reinterpret_cast<uint64_t>(store + at);
@@ -171,7 +169,8 @@ __device__ __forceinline__ void unit(const PrefixArgs& a, int lo, int m0, int n_
 #pragma unroll
   for (int j = 0; j < NQ; ++j) {
     const int m = m0 + min(16 * j + fr, n_cols - 1);  // lanes past the last column repeat it
-    const uint16_t* qp = static_cast<const uint16_t*>(a.q) + int64_t(lo + m / G) * a.ldq + (head * G + m % G) * DH;
+    const int i = row_of(a, m);
+    const uint16_t* qp = static_cast<const uint16_t*>(a.q) + int64_t(lo + i) * a.ldq + (head * G + m - i * G) * DH;
 #pragma unroll
     for (int kb = 0; kb < NKB; ++kb) {
       // bf16 values convert exactly but for magnitudes below 2^-14 or beyond fp16.
@@ -217,17 +216,23 @@ __device__ __forceinline__ void unit(const PrefixArgs& a, int lo, int m0, int n_
   }
 
   if (my_tiles > 0) {
-    int slot = slot_of(0), slot_next = slot_of(1);
     uint32_t bytes;
-    int64_t at = base_of(0, slot, bytes);
+    int64_t at = base_of(pages[page_no], page_at, bytes);
     bad |= bytes == 0;
+    // Tiles past the last one are read through an empty resource: zeros, no traffic.
+    // Their entries of the table may not exist.
+    int slot = -1;
+    advance(page_no, page_at);
+    if (my_tiles > 1) slot = pages[page_no];
     load(tl.k, a.k, at, bytes);
     load(tl.v, a.v, at, bytes);
     for (int i = 0; i < my_tiles; ++i) {
       const int kv0 = (t0 + wave + 4 * i) * TK;
-      at = base_of(i + 1, slot_next, bytes);
+      at = base_of(slot, page_at, bytes);
       bad |= i + 1 < my_tiles && bytes == 0;
-      slot_next = slot_of(i + 2);
+      slot = -1;
+      advance(page_no, page_at);
+      if (i + 2 < my_tiles) slot = pages[page_no];
       asm volatile("" ::: "memory");
 #pragma unroll
       for (int l = 0; l < NL; ++l) *reinterpret_cast<u32x4*>(ks + kw[l / kPer] + (l % kPer) * 1024) = tl.k[l];
@@ -315,7 +320,8 @@ __device__ __forceinline__ void unit(const PrefixArgs& a, int lo, int m0, int n_
     }
   }
 
-  // The wavefronts' states become one.
+  // The wavefronts' states become one: wavefront w adds up columns w, w + 4, ..., a lane
+  // a dimension.
 #pragma unroll
   for (int j = 0; j < NQ; ++j) {
     const float l_tot = quarter_sum(l_run[j]);
@@ -326,7 +332,6 @@ __device__ __forceinline__ void unit(const PrefixArgs& a, int lo, int m0, int n_
   }
   float* stats = part_stats(a, splits);
   constexpr int kPass = Smem<DH, NQ>::kPass;
-  static_assert(kPass == 64, "the index arithmetic below");
 #pragma unroll
   for (int pass = 0; pass < DH / kPass; ++pass) {
     __syncthreads();  // the states take the tiles' place, and the last pass's
@@ -338,25 +343,26 @@ __device__ __forceinline__ void unit(const PrefixArgs& a, int lo, int m0, int n_
         for (int r = 0; r < 4; ++r)
           sm.red_o[wave][16 * d + 4 * fh + r][16 * j + fr] = o[j][pass * (kPass / 16) + d][r];
     __syncthreads();
-    for (int idx = tid; idx < n_cols * kPass; idx += kThreads) {
-      const int q = idx / kPass, d = idx % kPass;
-      const int m = m0 + q;
-      float M = -kInf;
-#pragma unroll
-      for (int w = 0; w < 4; ++w) M = fmaxf(M, sm.red_m[w][q]);
-      float num = 0.0f, den = 0.0f;
+    for (int q = wave; q < n_cols; q += 4) {
+      float m[4], M = -kInf;
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
-        const float sc = exp2_raw(sm.red_m[w][q] - M);
-        num += sc * sm.red_o[w][d][q];
-        den += sc * sm.red_l[w][q];
+        m[w] = sm.red_m[w][q];
+        M = fmaxf(M, m[w]);
       }
-      const int64_t p = part_index(a, split, lo + m / G, head * G + m % G);
-      static_cast<float*>(a.part)[p * DH + pass * kPass + d] = num;
-      if (pass == 0 && d == 0) {
-        stats[2 * p] = M;
-        stats[2 * p + 1] = den;
+      float num[kPass / 64] = {}, den = 0.0f;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const float f = exp2_raw(m[w] - M);
+        den = fmaf(f, sm.red_l[w][q], den);
+#pragma unroll
+        for (int e = 0; e < kPass / 64; ++e) num[e] = fmaf(f, sm.red_o[w][64 * e + lane][q], num[e]);
       }
+      const int i = row_of(a, m0 + q);
+      const int64_t p = part_index(a, split, lo + i, head * G + m0 + q - i * G);
+#pragma unroll
+      for (int e = 0; e < kPass / 64; ++e) static_cast<float*>(a.part)[p * DH + pass * kPass + 64 * e + lane] = num[e];
+      if (pass == 0 && lane == 0) *reinterpret_cast<float2*>(stats + 2 * p) = make_float2(M, den);
     }
   }
 }
@@ -399,7 +405,8 @@ __device__ __forceinline__ void wide_unit(const PrefixArgs& a, int lo, int m0, i
   u32x4 qf[DH / 16];
   {
     const int m = m0 + min(wave * 32 + fr, n_cols - 1);  // lanes past the last column repeat it
-    const uint16_t* qp = static_cast<const uint16_t*>(a.q) + int64_t(lo + m / G) * a.ldq + (head * G + m % G) * DH;
+    const int i = row_of(a, m);
+    const uint16_t* qp = static_cast<const uint16_t*>(a.q) + int64_t(lo + i) * a.ldq + (head * G + m - i * G) * DH;
 #pragma unroll
     for (int kb = 0; kb < DH / 16; ++kb) {
       qf[kb] = *reinterpret_cast<const u32x4*>(qp + kb * 16 + fh * 8);
@@ -415,11 +422,12 @@ __device__ __forceinline__ void wide_unit(const PrefixArgs& a, int lo, int m0, i
     voff[j] = uint32_t(((c >> 2) * kv_tile_keys * DH + d * kv_tile_keys + (c & 3) * 8) * 2);
   }
   u32x4 rk[LOADS], rv[LOADS];
-  auto slot_of = [&](int t) { return first_lane(pages[(k_lo + min(t, n_tiles - 1) * BKV) / a.page]); };
-  auto gload = [&](int t, int slot) {
+  // The page of the next tile to load, and the tile's place in it.
+  int page_no = first_lane(k_lo / a.page), page_at = k_lo - page_no * a.page;
+  auto gload = [&](int slot) {
     const bool ok = slot >= 0 && slot < a.n_slots;
     bad |= !ok;
-    const int64_t at = ok ? slot * slot_elems + head * head_elems + int64_t((k_lo + t * BKV) % a.page) * DH : int64_t(0);
+    const int64_t at = ok ? slot * slot_elems + head * head_elems + int64_t(page_at) * DH : int64_t(0);
     const uint32_t bytes = ok ? uint32_t(WideSmem<DH>::kTile) : 0u;
     auto res = [&](const uint16_t* store) {
       const uint64_t p = reinterpret_cast<uint64_t>(store + at);
@@ -431,6 +439,11 @@ __device__ __forceinline__ void wide_unit(const PrefixArgs& a, int lo, int m0, i
     for (int j = 0; j < LOADS; ++j) rk[j] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(kres, koff[j], 0, 0));
 #pragma unroll
     for (int j = 0; j < LOADS; ++j) rv[j] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(vres, voff[j], 0, 0));
+    page_at += BKV;  // pages are whole tiles
+    if (page_at == a.page) {
+      page_at = 0;
+      ++page_no;
+    }
   };
   // Values past the range may be anything; 0 * NaN must not reach the sum.
   auto vmask = [&](int t) {
@@ -465,15 +478,15 @@ __device__ __forceinline__ void wide_unit(const PrefixArgs& a, int lo, int m0, i
     for (int r = 0; r < 16; ++r) o[i][r] = 0.0f;
   float m_run = -kInf, l_run = 0.0f;
 
-  gload(0, slot_of(0));
+  gload(pages[page_no]);
+  int slot = n_tiles > 1 ? pages[page_no] : 0;  // a tile ahead; past the last one there may be no entry
   vmask(0);
   lstore(0);
-  int slot = slot_of(1);
   __syncthreads();
   const bool busy = wave * 32 < n_cols;
   for (int t = 0; t < n_tiles; ++t) {
-    if (t + 1 < n_tiles) gload(t + 1, slot);
-    slot = slot_of(t + 2);
+    if (t + 1 < n_tiles) gload(slot);
+    if (t + 2 < n_tiles) slot = pages[page_no];
     if (busy) {
       const uint8_t* ks = sm.tile[t & 1][0];
       const uint8_t* vs = sm.tile[t & 1][1];
@@ -543,10 +556,9 @@ __device__ __forceinline__ void wide_unit(const PrefixArgs& a, int lo, int m0, i
   const float l_tot = l_run + xor_lane<32>(l_run);
   float* stats = part_stats(a, splits);
   if (fh == 0 && wave * 32 + fr < n_cols) {
-    const int m = m0 + wave * 32 + fr;
-    const int64_t p = part_index(a, split, lo + m / G, head * G + m % G);
-    stats[2 * p] = m_run;
-    stats[2 * p + 1] = bad ? __builtin_nanf("") : l_tot;
+    const int m = m0 + wave * 32 + fr, i = row_of(a, m);
+    const int64_t p = part_index(a, split, lo + i, head * G + m - i * G);
+    *reinterpret_cast<float2*>(stats + 2 * p) = make_float2(m_run, bad ? __builtin_nanf("") : l_tot);
   }
   float(*mine)[WideSmem<DH>::kRow] = sm.out[wave];
 #pragma unroll
@@ -565,8 +577,8 @@ __device__ __forceinline__ void wide_unit(const PrefixArgs& a, int lo, int m0, i
     for (int j = 0; j < 8; ++j) {
       const int col = 4 * j + (lane >> 4), d = (lane & 15) * 4;
       if (wave * 32 + col >= n_cols) continue;
-      const int m = m0 + wave * 32 + col;
-      const int64_t p = part_index(a, split, lo + m / G, head * G + m % G);
+      const int m = m0 + wave * 32 + col, i = row_of(a, m);
+      const int64_t p = part_index(a, split, lo + i, head * G + m - i * G);
       *reinterpret_cast<f32x4*>(static_cast<float*>(a.part) + p * DH + 64 * pass + d) =
           *reinterpret_cast<const f32x4*>(&mine[col][d]);
     }
@@ -592,7 +604,7 @@ __global__ __launch_bounds__(kThreads, 2) void prefix_kernel(PrefixArgs a, Prefi
   if (id < prefix_blocks) {
     id /= a.hkv;
     const int split = id % s.prefix_splits, tile = id / s.prefix_splits;
-    const Group g = group_of_tile(a, tile, kCols, G);
+    const Group g = group_of_tile<kCols>(a, tile);
     const int m0 = g.tile * kCols, n_cols = min((g.hi - g.lo) * G - m0, kCols);
     const int prefix = int(min(int64_t(clamped(g.prefix, 0, a.max_prefix)), reach));
     const int k_lo = split * s.prefix_keys, k_hi = min(prefix, k_lo + s.prefix_keys);
@@ -647,8 +659,9 @@ __global__ __launch_bounds__(kThreads) void prefix_join_kernel(PrefixArgs a, Pre
     for (int j = 0; j < kJoinBatch; ++j) {
       const int i = min(i0 + j * W, n - 1);
       const int64_t p = part_index(a, i < n_prefix ? i : s.prefix_splits + i - n_prefix, row, head);
-      m[j] = stats[2 * p];
-      l[j] = stats[2 * p + 1];
+      const float2 ml = *reinterpret_cast<const float2*>(stats + 2 * p);
+      m[j] = ml.x;
+      l[j] = ml.y;
       v[j] = *reinterpret_cast<const Vec*>(part + p * DH + lane * V);
     }
     float top = M;
@@ -718,7 +731,7 @@ hipError_t launch(const PrefixArgs& a, int cus, hipStream_t st) {
       hipLaunchKernelGGL((prefix_kernel<DH, 2, false, T>), dim3(uint32_t(blocks)), dim3(kThreads), 0, st, a, s);
   }
   const int64_t rows = int64_t(a.n_seqs) * a.hq;
-  if (s.prefix_splits + s.rest_splits > 4 && rows <= 16 * int64_t(cus))
+  if (s.prefix_splits + s.rest_splits > 4 && rows <= 4 * int64_t(cus))
     hipLaunchKernelGGL((prefix_join_kernel<DH, 4, T>), dim3(uint32_t(rows)), dim3(kThreads), 0, st, a, s);
   else
     hipLaunchKernelGGL((prefix_join_kernel<DH, 1, T>), dim3(uint32_t((rows + 3) / 4)), dim3(kThreads), 0, st, a, s);

@@ -112,6 +112,7 @@ REFUSED = [
     (prefix, dict(hkv=0), INVALID, "heads"),
     (prefix, dict(hq=3), INVALID, "query heads"),
     (prefix, dict(hq=0), INVALID, "query heads"),
+    (prefix, dict(hq=130, ldq=8320, ldo=8320), UNSUPPORTED, "at most 64"),
     (prefix, dict(n=-1), INVALID, "rows"),
     (prefix, dict(mp=-1), INVALID, "prefixes"),
     (prefix, dict(mr=-1), INVALID, "prefixes"),
