@@ -99,7 +99,7 @@ struct Smem {
   static constexpr int kPass = NQ == 1 ? DH : 64;   // dimensions of a pass of the join of wavefronts
   union {
     uint8_t tile[4][kTile];
-    float red_o[4][kPass][kCols + 1];
+    float red_o[4][kCols][kPass + 4];  // 16 columns apart in banks
   };
   float red_m[4][kCols], red_l[4][kCols];
 };
@@ -320,8 +320,7 @@ __device__ __forceinline__ void unit(const PrefixArgs& a, int lo, int m0, int n_
     }
   }
 
-  // The wavefronts' states become one: wavefront w adds up columns w, w + 4, ..., a lane
-  // a dimension.
+  // The wavefronts' states become one; a lane adds up four dimensions of a column.
 #pragma unroll
   for (int j = 0; j < NQ; ++j) {
     const float l_tot = quarter_sum(l_run[j]);
@@ -332,6 +331,7 @@ __device__ __forceinline__ void unit(const PrefixArgs& a, int lo, int m0, int n_
   }
   float* stats = part_stats(a, splits);
   constexpr int kPass = Smem<DH, NQ>::kPass;
+  constexpr int kLanes = kPass / 4, kStep = 256 / kLanes;  // of a column; columns at a time
 #pragma unroll
   for (int pass = 0; pass < DH / kPass; ++pass) {
     __syncthreads();  // the states take the tiles' place, and the last pass's
@@ -339,30 +339,32 @@ __device__ __forceinline__ void unit(const PrefixArgs& a, int lo, int m0, int n_
     for (int j = 0; j < NQ; ++j)
 #pragma unroll
       for (int d = 0; d < kPass / 16; ++d)
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-          sm.red_o[wave][16 * d + 4 * fh + r][16 * j + fr] = o[j][pass * (kPass / 16) + d][r];
+        *reinterpret_cast<f32x4*>(&sm.red_o[wave][16 * j + fr][16 * d + 4 * fh]) = o[j][pass * (kPass / 16) + d];
     __syncthreads();
-    for (int q = wave; q < n_cols; q += 4) {
+#pragma unroll
+    for (int q0 = 0; q0 < 16 * NQ; q0 += kStep) {
+      const int q = q0 + tid / kLanes, d = tid % kLanes * 4;
+      if (q >= n_cols) break;
       float m[4], M = -kInf;
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
         m[w] = sm.red_m[w][q];
         M = fmaxf(M, m[w]);
       }
-      float num[kPass / 64] = {}, den = 0.0f;
+      f32x4 num = {0.0f, 0.0f, 0.0f, 0.0f};
+      float den = 0.0f;
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
         const float f = exp2_raw(m[w] - M);
+        const f32x4 v = *reinterpret_cast<const f32x4*>(&sm.red_o[w][q][d]);
         den = fmaf(f, sm.red_l[w][q], den);
 #pragma unroll
-        for (int e = 0; e < kPass / 64; ++e) num[e] = fmaf(f, sm.red_o[w][64 * e + lane][q], num[e]);
+        for (int e = 0; e < 4; ++e) num[e] = fmaf(f, v[e], num[e]);
       }
       const int i = row_of(a, m0 + q);
       const int64_t p = part_index(a, split, lo + i, head * G + m0 + q - i * G);
-#pragma unroll
-      for (int e = 0; e < kPass / 64; ++e) static_cast<float*>(a.part)[p * DH + pass * kPass + 64 * e + lane] = num[e];
-      if (pass == 0 && lane == 0) *reinterpret_cast<float2*>(stats + 2 * p) = make_float2(M, den);
+      *reinterpret_cast<f32x4*>(static_cast<float*>(a.part) + p * DH + pass * kPass + d) = num;
+      if (pass == 0 && d == 0) *reinterpret_cast<float2*>(stats + 2 * p) = make_float2(M, den);
     }
   }
 }
