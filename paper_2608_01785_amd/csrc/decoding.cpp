@@ -190,6 +190,13 @@ hs_status hs_prefix_attention_workspace_size(int32_t n_q_heads, int32_t n_kv_hea
   return HS_OK;
 }
 
+// Bytes of the partial states of one call on `cus` CUs (see prefix_shape).  Internal to
+// the library and its tests (not declared in horizon.h).
+uint64_t hs_prefix_attention_states(int32_t n_seqs, int32_t n_groups, int32_t max_prefix, int32_t max_rest, int32_t hq,
+                                    int32_t hkv, int32_t dh, int32_t cus) {
+  return prefix_states_bytes(prefix_shape(n_seqs, n_groups, max_prefix, max_rest, hq, hkv, cus), n_seqs, hq, dh);
+}
+
 hs_status hs_prefix_attention(hs_context* ctx, const void* q, int32_t type, int64_t ldq, void* out, int64_t ldo,
                               int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, const void* k, const void* v,
                               int32_t n_slots, int32_t page_positions, const int32_t* block_table,
@@ -231,8 +238,10 @@ hs_status hs_prefix_attention(hs_context* ctx, const void* q, int32_t type, int6
   HS_TRY(check_disjoint(so, sws));
   if (n_seqs) HS_TRY(check_workspace(workspace, ws_bytes, need));
   const int32_t shared = n_groups ? max_prefix : 0;
-  if (prefix_blocks(prefix_shape(n_seqs, n_groups, shared, max_rest, n_q_heads, n_kv_heads, 256), n_seqs, n_kv_heads) >
-      kMaxBlocks)
+  const PrefixShape shape = prefix_shape(n_seqs, n_groups, shared, max_rest, n_q_heads, n_kv_heads, cu_budget);
+  if (prefix_states_bytes(shape, n_seqs, n_q_heads, head_dim) > need)
+    return fail(HS_ERR_INTERNAL, "the launch's partial states exceed the workspace");
+  if (prefix_blocks(shape, n_seqs, n_kv_heads) > kMaxBlocks)
     return fail(HS_ERR_UNSUPPORTED, "%d rows in %d groups need more blocks than a launch has", n_seqs, n_groups);
   PrefixArgs a{};
   a.q = q;

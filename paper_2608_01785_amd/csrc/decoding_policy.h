@@ -58,20 +58,24 @@ inline int prefix_split_keys(int64_t keys, int64_t blocks, int cus, int per_cu) 
   if (keys < 1) return kPrefixKeys;
   int64_t splits = prefix_up(per_cu * int64_t(cus), blocks < 1 ? 1 : blocks);
   if (splits > kPrefixMaxSplits) splits = kPrefixMaxSplits;
-  int64_t each = prefix_up(prefix_up(keys, splits), kPrefixKeys) * kPrefixKeys;
-  const int64_t least = 2 * kPrefixKeys;
-  if (each < least) each = least;
-  return int(each);
+  return int(prefix_up(prefix_up(keys, splits), kPrefixKeys) * kPrefixKeys);
 }
 
+// Narrow tiles: one block a CU.  More leave more states than the shorter ranges save:
+// 8 rows of 28 heads behind 8192 positions take 15.5 us with one, 21 with two; behind
+// 30000, 23.7 and 29.8.  What rows have to themselves: two blocks a CU beside the prefixes'
+// (20 rows in 5 groups behind 1501 positions 17.9 us against 20.6 with four), eight
+// alone (45 rows of up to 2000 keys 38.9 us against 43.2 with two).
 inline PrefixShape prefix_shape(int n_seqs, int n_groups, int max_prefix, int max_rest, int hq, int hkv, int cus) {
   const int64_t per_head = hq / hkv, rows = int64_t(n_seqs) * per_head;
   PrefixShape s{};
-  s.prefix_rows = rows <= 16 * int64_t(n_groups) ? 16 : rows <= 64 * int64_t(n_groups) ? 32 : 128;
+  s.prefix_rows = max_prefix < 1 || rows <= 16 * int64_t(n_groups) ? 16 : rows <= 64 * int64_t(n_groups) ? 32 : 128;
   s.prefix_tiles = max_prefix > 0 ? int(rows / s.prefix_rows + n_groups) : 0;
-  s.prefix_keys = prefix_split_keys(max_prefix, prefix_up(rows, s.prefix_rows) * hkv, cus, s.prefix_rows == 128 ? 2 : 4);
+  s.prefix_keys = prefix_split_keys(max_prefix, prefix_up(rows, s.prefix_rows) * hkv, cus,
+                                    s.prefix_rows == 128 ? 2 : 1);
   s.prefix_splits = int(prefix_up(max_prefix, s.prefix_keys));
-  s.rest_keys = prefix_split_keys(max_rest, int64_t(n_seqs) * hkv, cus, 4);
+  const bool beside = int64_t(s.prefix_tiles) * s.prefix_splits * hkv >= cus / 2;
+  s.rest_keys = prefix_split_keys(max_rest, int64_t(n_seqs) * hkv, cus, beside ? 2 : 8);
   s.rest_splits = int(prefix_up(max_rest, s.rest_keys));
   return s;
 }
@@ -84,6 +88,11 @@ inline int64_t prefix_blocks(const PrefixShape& s, int n_seqs, int hkv) {
 // A partial state: dh unnormalised outputs, and the maximum and sum behind them.
 inline size_t prefix_part_bytes(int dh) { return size_t(4 * dh + 8); }
 
+// What a launch of this shape writes.
+inline size_t prefix_states_bytes(const PrefixShape& s, int n_seqs, int hq, int dh) {
+  return size_t(n_seqs) * hq * size_t(s.prefix_splits + s.rest_splits) * prefix_part_bytes(dh);
+}
+
 // Workspace bytes for at most n_seqs rows, on any budget.  Fewer rows or groups, a
 // smaller bound and fewer CUs never take more partial states than this: `blocks`
 // blocks take at most 4 cus / blocks + 1 splits, and each block holds prefix_rows
@@ -91,12 +100,12 @@ inline size_t prefix_part_bytes(int dh) { return size_t(4 * dh + 8); }
 inline size_t prefix_workspace(int n_seqs, int max_prefix, int max_rest, int hq, int hkv, int dh) {
   const int64_t rows = int64_t(n_seqs) * hq;
   auto states = [&](int64_t keys, int64_t of_block) {
-    int64_t splits = prefix_up(keys, 2 * kPrefixKeys);
+    int64_t splits = prefix_up(keys, kPrefixKeys);
     if (splits > kPrefixMaxSplits) splits = kPrefixMaxSplits;
     const int64_t shared = 256 * of_block + rows, each = rows * splits;
     return splits < 1 ? 0 : each < shared ? each : shared;
   };
-  return size_t(states(max_prefix, 2 * 128) + states(max_rest, 4 * (hq / hkv))) * prefix_part_bytes(dh);
+  return size_t(states(max_prefix, 2 * 128) + states(max_rest, 8 * (hq / hkv))) * prefix_part_bytes(dh);
 }
 
 }  // namespace hs

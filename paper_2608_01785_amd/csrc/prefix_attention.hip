@@ -593,8 +593,8 @@ __device__ __forceinline__ void wide_unit(const PrefixArgs& a, int lo, int m0, i
 template <int DH, int NQ, bool WIDE, typename T>
 __global__ __launch_bounds__(kThreads, 2) void prefix_kernel(PrefixArgs a, PrefixShape s) {
   union Lds {
-    Smem<DH, NQ> narrow;
-    typename Choose<WIDE, WideSmem<DH>, Smem<DH, NQ>>::type wide;
+    Smem<DH, 1> rest;
+    typename Choose<WIDE, WideSmem<DH>, Smem<DH, NQ>>::type prefix;
   };
   __shared__ __attribute__((aligned(16))) Lds sm;
   constexpr int kCols = WIDE ? 128 : 16 * NQ;
@@ -612,9 +612,9 @@ __global__ __launch_bounds__(kThreads, 2) void prefix_kernel(PrefixArgs a, Prefi
     const int k_lo = split * s.prefix_keys, k_hi = min(prefix, k_lo + s.prefix_keys);
     if (n_cols < 1 || k_hi <= k_lo) return;
     if constexpr (WIDE)
-      wide_unit<DH, T>(a, g.lo, m0, n_cols, head, g.lo, k_lo, k_hi, split, splits, sm.wide);
+      wide_unit<DH, T>(a, g.lo, m0, n_cols, head, g.lo, k_lo, k_hi, split, splits, sm.prefix);
     else
-      unit<DH, NQ, T>(a, g.lo, m0, n_cols, head, g.lo, k_lo, k_hi, split, splits, sm.narrow);
+      unit<DH, NQ, T>(a, g.lo, m0, n_cols, head, g.lo, k_lo, k_hi, split, splits, sm.prefix);
   } else {
     id = (id - prefix_blocks) / a.hkv;
     const int split = id % s.rest_splits, row = id / s.rest_splits;
@@ -623,10 +623,10 @@ __global__ __launch_bounds__(kThreads, 2) void prefix_kernel(PrefixArgs a, Prefi
     const int64_t k_lo = int64_t(prefix) + int64_t(split) * s.rest_keys;
     const int64_t k_hi = min(end, k_lo + s.rest_keys);
     if (k_hi <= k_lo) return;
-    for (int m0 = 0; m0 < G; m0 += 16 * NQ) {
+    for (int m0 = 0; m0 < G; m0 += 16) {
       if (m0 > 0) __syncthreads();  // the last unit's states have been read
-      unit<DH, NQ, T>(a, row, m0, min(G - m0, 16 * NQ), head, row, int(k_lo), int(k_hi), s.prefix_splits + split,
-                      splits, sm.narrow);
+      unit<DH, 1, T>(a, row, m0, min(G - m0, 16), head, row, int(k_lo), int(k_hi), s.prefix_splits + split, splits,
+                     sm.rest);
     }
   }
 }

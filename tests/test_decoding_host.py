@@ -167,6 +167,23 @@ def test_workspaces_cover_smaller_calls(b):
     assert b.hs_prefix_attention_workspace_size(28, 4, 128, 0, 4096, 100) == 0
 
 
+def test_partial_states_fit_the_workspace(b):
+    """Every grouping and budget of a call, and of smaller ones, writes no more than its workspace holds."""
+    states = b.lib().hs_prefix_attention_states
+    states.restype = ctypes.c_uint64
+    rng = np.random.default_rng(1)
+    for heads in ((28, 4, 128), (16, 16, 64), (64, 1, 128), (4, 2, 64), (1, 1, 64)):
+        for _ in range(4000):
+            n = int(np.exp(rng.uniform(0, np.log(600))))
+            p, r = (int(np.exp(rng.uniform(0, np.log(200000)))) - 1 for _ in range(2))
+            size = b.hs_prefix_attention_workspace_size(*heads, n, p, r)
+            for cus in (1, 64, 160, 256):
+                m, g = int(rng.integers(1, n + 1)), int(rng.integers(0, n + 2))
+                less = int(rng.integers(0, p + 1)), int(rng.integers(0, r + 1))
+                assert states(n, g, p if g else 0, r, *heads, cus) <= size, (heads, n, g, p, r, cus)
+                assert states(m, g, less[0] if g else 0, less[1], *heads, cus) <= size, (heads, n, m, g, p, r, less, cus)
+
+
 # ---------------------------------------------------------------------------- pages
 
 class Model:
