@@ -11,9 +11,9 @@
 // each other.  The scan's read of the logits bounds the call; ended and empty beams
 // are not read.
 //
-// Values are held in 64 bits from the scan's fp32 sums on: continuations of two
-// beams that lie closer than the 2^-20 that fp32 resolves at -10 are common among
-// the many near a selection's border, and their order decides whole sequences.
+// Values are held in 64 bits from the sums of a row on: continuations of two beams
+// that lie closer than the 2^-20 that fp32 resolves at -10 are common among the many
+// near a selection's border, and their order decides whole sequences.
 #include "decoding_kernels.h"
 #include "logits_scan.h"
 
@@ -24,15 +24,9 @@ using namespace scan;
 
 constexpr int kJoinWaves = 16;
 
-__device__ __forceinline__ double first_lane(double v) {
-  const uint64_t u = __builtin_bit_cast(uint64_t, v);
-  const uint32_t lo = __builtin_amdgcn_readfirstlane(uint32_t(u)), hi = __builtin_amdgcn_readfirstlane(uint32_t(u >> 32));
-  return __builtin_bit_cast(double, (uint64_t(hi) << 32) | lo);
-}
-
 // Block: one group.  `team` wavefronts share a beam.
 __global__ __launch_bounds__(64 * kJoinWaves) void beam_join_kernel(BeamArgs a, LogprobsArgs scanned, int splits,
-                                                                    int team) {
+                                                                    int team, int span) {
   __shared__ uint64_t lists[kJoinWaves][64];
   __shared__ int counts[kBeamMaxBeams];
   extern __shared__ double values[];                                   // [beams][select]
@@ -44,22 +38,24 @@ __global__ __launch_bounds__(64 * kJoinWaves) void beam_join_kernel(BeamArgs a, 
   for (int b0 = 0; b0 < a.beams; b0 += teams) {
     const int b = b0 + wave / team;
     const bool mine = b < a.beams;
-    const int64_t row = row0 + b;
-    const bool ended = mine && a.finished && a.finished[row] != 0;
-    const float score = mine ? a.scores[row] : -kInf;
-    const bool live = mine && !ended && score > -kInf;
-    uint64_t list = 0;
-    if (live) {
-      const uint64_t* src = partial_keys(scanned, int64_t(scanned.rows) * splits) + row * splits * k;
-      // The best key of a split is a list's first, or its last where it is merged into another.
-      auto key = [&](int split, int i) { return split < splits && i < k ? src[int64_t(split) * k + i] : 0; };
-      list = key(member, lane);
-      uint64_t next = key(member + team, 63 - lane);
-      for (int s = member + team; s < splits; s += team) {
-        const uint64_t other = next;
-        next = key(s + team, 63 - lane);
-        list = merge_stages<32>(list > other ? list : other, true);
-      }
+    const int64_t row = row0 + min(b, a.beams - 1);
+    // Everything the beam needs is asked for at once; a beam that was not scanned has
+    // left nothing, and nothing of it is used.
+    const float score = a.scores[row];
+    const bool ended = a.finished && a.finished[row] != 0;
+    const uint64_t* src = partial_keys(scanned, int64_t(scanned.rows) * splits) + row * splits * k;
+    // The best key of a split is a list's first, or its last where it is merged into another.
+    auto key = [&](int split, int i) { return split < splits && i < k ? src[int64_t(split) * k + i] : 0; };
+    uint64_t list = key(member, lane), next = key(member + team, 63 - lane);
+    Sums sums{kLowest, 0.0f, 0.0f, 0.0f};
+    if (lane < splits) {
+      const f32x4 v = static_cast<const f32x4*>(a.part)[row * splits + lane];
+      sums = Sums{v[0], v[1], v[2], v[3]};
+    }
+    for (int s = member + team; s < splits; s += team) {
+      const uint64_t other = next;
+      next = key(s + team, 63 - lane);
+      list = merge_stages<32>(list > other ? list : other, true);
     }
     if (team > 1) {
       lists[wave][lane] = list;
@@ -67,28 +63,21 @@ __global__ __launch_bounds__(64 * kJoinWaves) void beam_join_kernel(BeamArgs a, 
     }
     if (mine && member == 0) {
       int n = 0;
-      if (live) {
+      if (!ended && score > -kInf) {
         for (int w = 1; w < min(team, splits); ++w) {
           const uint64_t other = lists[wave + w][63 - lane];
           list = merge_stages<32>(list > other ? list : other, true);
         }
-        Sums sums{kLowest, 0.0f, 0.0f, 0.0f};
-        if (lane < splits) {
-          const f32x4 v = static_cast<const f32x4*>(a.part)[row * splits + lane];
-          sums = Sums{v[0], v[1], v[2], v[3]};
-        }
         // The splits' sums against the row's maximum; F without the elements at it.
         const float m = max_wave(sums.m);
-        const double f = exp(fmax(double(sums.m) - double(m), -700.0));
-        double s = double(sums.s) * f, rest = sums.m < m ? s : double(sums.f);
+        const float f = exp_of(fmaxf(sums.m - m, kFar));
+        double s = double(sums.s * f), rest = sums.m < m ? s : double(sums.f);
+        // (No product is left for the sums to contract with: every lane adds the same.)
         s = reduce_wave(s, [](double x, double y) { return x + y; });
         rest = reduce_wave(rest, [](double x, double y) { return x + y; });
-        // One lane's for all: a product contracted into the first sum rounds differently
-        // on either side of a lane pair.
-        const double log_sum = first_lane(double(m) + (s < 1.5 ? log1p(rest) : log(s)));
+        const double log_sum = double(m) + (s < 1.5 ? log1p(rest) : log(s));
         // A row without a distribution (NaN, +inf, all masked) has no continuation.
-        const uint64_t some = s > 0.0 ? __ballot(lane < k && list != 0) : 0;
-        n = __popcll(some);
+        n = s > 0.0 ? __popcll(__ballot(lane < k && list != 0)) : 0;
         if (lane < n) {
           values[b * k + lane] = double(score) + (double(value_of(list)) - log_sum);
           tokens[b * k + lane] = token_of(list);
@@ -106,36 +95,45 @@ __global__ __launch_bounds__(64 * kJoinWaves) void beam_join_kernel(BeamArgs a, 
   }
   // The lists are sorted: a candidate's rank is its place in its own and, by
   // bisection, the number of larger values in each other (of equal ones, those of
-  // lower beams).
-  int total = 0;
-  for (int b = 0; b < a.beams; ++b) total += counts[b];
+  // lower beams).  A lane takes one of the other lists; `span` lanes, a power of two,
+  // a candidate.
   const int64_t out0 = int64_t(blockIdx.x) * k;
-  for (int c = threadIdx.x; c < a.beams * k; c += blockDim.x) {
+  const int o = threadIdx.x & (span - 1);
+  for (int c0 = 0; c0 < a.beams * k; c0 += blockDim.x / span) {
+    const int c = c0 + threadIdx.x / span;
     const int b = c / k, i = c - b * k;
-    if (i >= counts[b]) continue;
-    const double v = values[c];
-    int rank = i;
-    for (int o = 0; o < a.beams && rank < k; ++o) {
-      if (o == b) continue;
-      int lo = 0, hi = counts[o];
-      while (lo < hi) {
-        const int mid = (lo + hi) >> 1;
-        const double w = values[o * k + mid];
-        if (w > v || (w == v && o < b))
-          lo = mid + 1;
-        else
-          hi = mid;
+    const bool there = b < a.beams && i < counts[min(b, a.beams - 1)];
+    const double v = there ? values[c] : 0.0;
+    int rank = 0;
+    if (there && o < a.beams) {
+      int hi = counts[o];
+      if (o == b) {
+        rank = i;
+      } else {
+        while (rank < hi) {
+          const int mid = (rank + hi) >> 1;
+          const double w = values[o * k + mid];
+          if (w > v || (w == v && o < b))
+            rank = mid + 1;
+          else
+            hi = mid;
+        }
       }
-      rank += lo;
     }
-    if (rank >= k) continue;
+    for (int d = 1; d < span; d <<= 1) rank += __shfl_xor(rank, d, 64);
+    if (!there || o != 0 || rank >= k) continue;
+    const int token = tokens[c];
     a.out_scores[out0 + rank] = float(v);
     a.out_parents[out0 + rank] = b;
-    a.out_tokens[out0 + rank] = tokens[c];
+    a.out_tokens[out0 + rank] = token;
     if (a.out_finished)
-      a.out_finished[out0 + rank] = (a.finished && a.finished[row0 + b] != 0) || (a.end_token >= 0 && tokens[c] == a.end_token);
+      a.out_finished[out0 + rank] =
+          (a.finished && a.finished[row0 + b] != 0) || (a.end_token >= 0 && token == a.end_token);
   }
-  for (int r = total + int(threadIdx.x); r < k; r += blockDim.x) {
+  if (wave != 0) return;
+  int total = lane < a.beams ? counts[lane] : 0;
+  for (int d = 1; d < 64; d <<= 1) total += __shfl_xor(total, d, 64);
+  for (int r = total + lane; r < k; r += 64) {
     a.out_scores[out0 + r] = -kInf;
     a.out_parents[out0 + r] = -1;
     a.out_tokens[out0 + r] = -1;
@@ -162,11 +160,13 @@ hipError_t launch(const BeamArgs& a, int cus, hipStream_t s) {
   else
     hipLaunchKernelGGL((logprobs_kernel<T, 4, true, true, BeamScanArgs>), dim3(p.rows * shape.splits), dim3(256), 0, s, p,
                        shape.splits);
+  int span = 1;
+  while (span < a.beams) span *= 2;
   int team = a.beams < kJoinWaves ? kJoinWaves / a.beams : 1;
   if (team > shape.splits) team = shape.splits;
   const int waves = a.beams * team < kJoinWaves ? a.beams * team : kJoinWaves / team * team;
   hipLaunchKernelGGL(beam_join_kernel, dim3(a.groups), dim3(64 * waves), size_t(a.beams) * a.select * 12, s, a, p,
-                     shape.splits, team);
+                     shape.splits, team, span);
   return hipGetLastError();
 }
 
