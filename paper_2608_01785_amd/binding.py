@@ -8,6 +8,7 @@ has not been built.
 """
 from __future__ import annotations
 
+import array
 import ctypes
 import os
 from typing import Dict, List, Optional, Sequence, Tuple
@@ -193,7 +194,7 @@ def lib() -> ctypes.CDLL:
             "hs_beam_select_workspace_size": [i32, i32, i32, i32, ctypes.POINTER(ctypes.c_size_t)],
             "hs_beam_select": [vp, vp, i32, i64, i32, i32, i32, vp, vp, i32, i32, vp, vp, vp, vp, i32, vp, vp,
                                ctypes.c_size_t],
-            "hs_cache_copy": [vp, ctypes.POINTER(KvCache), i32, i32, i32, i32p, i32p, i32p, i32, i32, vp],
+            "hs_cache_copy": [vp, ctypes.POINTER(KvCache), i32, i32, i32, vp, vp, vp, i32, i32, vp],
             "hs_prefix_attention_workspace_size": [i32, i32, i32, i32, i32, i32, ctypes.POINTER(ctypes.c_size_t)],
             "hs_prefix_attention": [vp, vp, i32, i64, vp, i64, i32, i32, i32, vp, vp, i32, i32, vp, i32, vp, i32, vp,
                                     vp, i32, i32, i32, i32, vp, vp, ctypes.c_size_t],
@@ -791,10 +792,31 @@ def _cache_layers(ctx: Context, k, v, n_slots: int, max_ctx: int) -> Tuple[int, 
     if k[0].dim() != 4:
         _refuse(ctx, k[0], "k", _Kinds.f16, 4)
     hkv, dh = k[0].shape[1], k[0].shape[3]
-    for kl, vl in zip(k, v):
-        _dense(ctx, kl, "k", _Kinds.f16, n_slots, hkv, max_ctx, dh)
-        _dense(ctx, vl, "v", _Kinds.f16, n_slots, hkv, max_ctx // 32, dh, 32)
+    for layers, name, shape in ((k, "k", (n_slots, hkv, max_ctx, dh)), (v, "v", (n_slots, hkv, max_ctx // 32, dh, 32))):
+        for t in layers:
+            if (t.shape != shape or t.dtype not in _Kinds.f16 or t.get_device() != ctx.device
+                    or not t.is_contiguous()):
+                _dense(ctx, t, name, _Kinds.f16, *shape)   # the message of what does not fit
     return hkv, dh
+
+
+def _host_ints(values, name: str):
+    """(keeper, address) of host integers as 32-bit words."""
+    if values is None:
+        return None, None
+    if isinstance(values, np.ndarray):
+        if values.ndim != 1 or (values.size and (values.min() < -2 ** 31 or values.max() > _INT32_MAX)):
+            raise ValueError(f"{name} holds no list of 32-bit numbers")
+        a = np.ascontiguousarray(values, dtype=np.int32)
+        return a, a.ctypes.data
+    try:
+        a = array.array("i", values)
+    except (OverflowError, TypeError) as e:
+        raise ValueError(f"{name} holds no list of 32-bit numbers: {e}") from None
+    return a, a.buffer_info()[0]
+
+
+_PointerArray = ctypes.POINTER(ctypes.c_void_p)
 
 
 def hs_cache_copy(ctx: Context, kv, src, dst, positions=None, cu_budget: int = 256, stream=None) -> None:
@@ -808,8 +830,12 @@ def hs_cache_copy(ctx: Context, kv, src, dst, positions=None, cu_budget: int = 2
     if len(dst) != n or (positions is not None and len(positions) != n):
         raise ValueError(f"{n} sources, {len(dst)} destinations"
                          + ("" if positions is None else f", {len(positions)} numbers of positions"))
-    _check(lib().hs_cache_copy(ctx.handle, ctypes.byref(_kv_struct((k, v, n_slots, max_ctx))), len(k), hkv, dh,
-                               _i32_array(src), _i32_array(dst), _i32_array(positions), n, cu_budget, _ptr(stream)))
+    ks, vs = ((ctypes.c_void_p * len(t))(*[x.data_ptr() for x in t]) for t in (k, v))
+    arg = KvCache(ctypes.cast(ks, _PointerArray), ctypes.cast(vs, _PointerArray), n_slots, max_ctx, None, 0)
+    (s, ps), (d, pd), (p, pp) = _host_ints(src, "src"), _host_ints(dst, "dst"), _host_ints(positions, "positions")
+    status = lib().hs_cache_copy(ctx.handle, ctypes.byref(arg), len(k), hkv, dh, ps, pd, pp, n, cu_budget, _ptr(stream))
+    if status:
+        _check(status)
 
 
 def hs_prefix_attention_workspace_size(n_q_heads: int, n_kv_heads: int, head_dim: int, n_seqs: int, max_prefix: int,

@@ -153,7 +153,7 @@ hipError_t launch(const BeamArgs& a, int cus, hipStream_t s) {
   p.part = a.part;
   p.scores = a.scores;
   p.finished = a.finished;
-  const LogprobsShape shape = logprobs_shape(p.rows, p.vocab, sizeof(T), cus);
+  const LogprobsShape shape = beam_shape(p.rows, p.vocab, sizeof(T), cus);
   if (shape.waves == 1)
     hipLaunchKernelGGL((logprobs_kernel<T, 1, true, true, BeamScanArgs>), dim3(p.rows * shape.splits), dim3(64), 0, s, p,
                        shape.splits);

@@ -4,7 +4,8 @@
 // The first n positions of a head, n rounded up to whole value tiles, are one
 // contiguous run in the keys and one in the values, 2 n dh bytes each: a copy is
 // 2 heads layers runs between two slots.  A block moves a segment of a run, every
-// thread a few 16-byte words, all loaded before the first is stored.  Memory bounds
+// thread two 16-byte words, both loaded before the first is stored.  The runs'
+// segments are numbered without gaps, however long each copy is.  Memory bounds
 // it, at two bytes moved for each copied.
 #include "decoding_kernels.h"
 #include "hs_device.h"
@@ -16,12 +17,17 @@ constexpr int kCopyThreads = 256;
 constexpr int kCopyWords = kCopySegment / (kCopyThreads * 16);  // of a thread
 
 __global__ __launch_bounds__(kCopyThreads) void cache_copy_kernel(CacheCopyArgs a) {
-  // x: (segment, head); y: (layer, keys or values); z: copy.
-  const CacheCopyArgs::Copy c = a.copies[blockIdx.z];
-  const uint32_t segments = copy_segments(a.max_tiles, a.dh);
-  const int segment = blockIdx.x % segments, head = blockIdx.x / segments;
-  const int64_t first = int64_t(segment) * kCopySegment, bytes = int64_t(c.tiles) * 64 * a.dh;
-  if (first >= bytes) return;
+  // x: (head, segment); y: (layer, keys or values).
+  const int head = blockIdx.x / uint32_t(a.segments), at_segment = blockIdx.x % uint32_t(a.segments);
+  // The last copy that starts at or before the segment.
+  int which = -1;
+#pragma unroll
+  for (int i0 = 0; i0 < kCopyList; i0 += 64) {
+    const int i = i0 + int(threadIdx.x & 63);
+    if (i0 < a.n_copies) which += __popcll(__ballot(i < a.n_copies && a.copies[min(i, a.n_copies - 1)].first <= at_segment));
+  }
+  const CacheCopyArgs::Copy c = a.copies[__builtin_amdgcn_readfirstlane(which)];
+  const int64_t first = int64_t(at_segment - c.first) * kCopySegment, bytes = int64_t(c.tiles) * 64 * a.dh;
   uint16_t* base = (blockIdx.y & 1) ? a.v[blockIdx.y >> 1] : a.k[blockIdx.y >> 1];
   uint8_t* p = reinterpret_cast<uint8_t*>(base) + head * a.head_bytes + first;
   const int64_t slot = a.head_bytes * a.heads;
@@ -45,7 +51,7 @@ __global__ __launch_bounds__(kCopyThreads) void cache_copy_kernel(CacheCopyArgs 
 
 hipError_t launch_cache_copy(const CacheCopyArgs& a, int, hipStream_t s) {
   if (a.n_copies < 1) return hipSuccess;
-  hipLaunchKernelGGL(cache_copy_kernel, dim3(copy_segments(a.max_tiles, a.dh) * a.heads, 2 * a.layers, a.n_copies), dim3(kCopyThreads), 0, s, a);
+  hipLaunchKernelGGL(cache_copy_kernel, dim3(uint32_t(a.segments) * a.heads, 2 * a.layers), dim3(kCopyThreads), 0, s, a);
   return hipGetLastError();
 }
 

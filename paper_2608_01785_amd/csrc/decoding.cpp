@@ -65,8 +65,13 @@ hs_status hs_beam_select_workspace_size(int32_t max_groups, int32_t beams, int32
                 kBeamMaxSelect);
   const int64_t rows = int64_t(max_groups) * beams;
   if (rows > kBeamMaxRows) return fail(HS_ERR_UNSUPPORTED, "%lld rows: at most %d", (long long)rows, kBeamMaxRows);
-  *bytes = beam_workspace(rows, vocab, n_select);
+  *bytes = beam_workspace(rows, n_select);
   return HS_OK;
+}
+
+// Bytes of the partial results of one call on `cus` CUs, as internal.
+uint64_t hs_beam_select_states(int32_t rows, int32_t vocab, int32_t elem_bytes, int32_t n_select, int32_t cus) {
+  return uint64_t(rows) * beam_shape(rows, vocab, elem_bytes, cus).splits * logprobs_partial_bytes(n_select);
 }
 
 hs_status hs_beam_select(hs_context* ctx, const void* logits, int32_t type, int64_t ld, int32_t groups, int32_t beams,
@@ -98,6 +103,9 @@ hs_status hs_beam_select(hs_context* ctx, const void* logits, int32_t type, int6
     for (const Span& other : outs)
       if (&other > &out) HS_TRY(check_disjoint(out, other));
   if (groups) HS_TRY(check_workspace(workspace, ws_bytes, need));
+  if (cu_budget < 1) return fail(HS_ERR_BUDGET, "CU budget %d", cu_budget);  // sizes the launch below
+  if (groups && hs_beam_select_states(rows, vocab, int32_t(type_size(type)), n_select, cu_budget) > need)
+    return fail(HS_ERR_INTERNAL, "the launch's partial results exceed the workspace");
   BeamArgs a{logits,   type,       ld,          groups,     beams,        vocab,    scores,
              finished, end_token,  n_select,    out_scores, out_parents,  out_tokens, out_finished,
              workspace};
@@ -129,13 +137,13 @@ hs_status hs_cache_copy(hs_context* ctx, const hs_kv_cache* kv, int32_t n_layers
   }
   try {
     // Copies run at the same time: what one writes no other may touch.
-    std::vector<int32_t> written(dst, dst + n_copies);
-    std::sort(written.begin(), written.end());
-    const auto twice = std::adjacent_find(written.begin(), written.end());
-    if (twice != written.end()) return fail(HS_ERR_INVALID_ARG, "slot %d is the destination of two copies", *twice);
+    std::vector<uint8_t> written(size_t(kv->n_slots), 0);
+    for (int32_t i = 0; i < n_copies; ++i) {
+      if (written[dst[i]]) return fail(HS_ERR_INVALID_ARG, "slot %d is the destination of two copies", dst[i]);
+      written[dst[i]] = 1;
+    }
     for (int32_t i = 0; i < n_copies; ++i)
-      if (std::binary_search(written.begin(), written.end(), src[i]))
-        return fail(HS_ERR_INVALID_ARG, "slot %d is a source and a destination", src[i]);
+      if (written[src[i]]) return fail(HS_ERR_INVALID_ARG, "slot %d is a source and a destination", src[i]);
   } catch (const std::bad_alloc&) {
     return fail(HS_ERR_INTERNAL, "out of host memory");
   }
@@ -147,15 +155,19 @@ hs_status hs_cache_copy(hs_context* ctx, const hs_kv_cache* kv, int32_t n_layers
     a.head_bytes = kv->max_ctx * position_bytes;
     for (int32_t i = 0; i < n_copies;) {
       a.n_copies = 0;
-      a.max_tiles = 0;
+      a.segments = 0;
       for (; i < n_copies && a.n_copies < kCopyList; ++i) {
         const int64_t n = positions ? (int64_t(positions[i]) + 31) / 32 * 32 : kv->max_ctx;
         if (n == 0) continue;
-        CacheCopyArgs::Copy& c = a.copies[a.n_copies++];
+        CacheCopyArgs::Copy& c = a.copies[a.n_copies];
         c.src = src[i];
         c.dst = dst[i];
         c.tiles = int32_t(n / 32);
-        a.max_tiles = std::max(a.max_tiles, c.tiles);
+        c.first = a.segments;
+        const int32_t more = copy_segments(c.tiles, head_dim);
+        if (a.n_copies > 0 && (int64_t(a.segments) + more) * n_kv_heads > kMaxBlocks) break;  // of the next launch
+        a.segments += more;
+        ++a.n_copies;
       }
       for (int32_t l = 0; l < n_layers; l += kCopyLayers) {
         a.layers = std::min(n_layers - l, kCopyLayers);
@@ -237,6 +249,7 @@ hs_status hs_prefix_attention(hs_context* ctx, const void* q, int32_t type, int6
     for (const Span& in : {sq, sk, sv, st, sl, sg, sp}) HS_TRY(check_disjoint(written, in));
   HS_TRY(check_disjoint(so, sws));
   if (n_seqs) HS_TRY(check_workspace(workspace, ws_bytes, need));
+  if (cu_budget < 1) return fail(HS_ERR_BUDGET, "CU budget %d", cu_budget);  // sizes the launch below
   const int32_t shared = n_groups ? max_prefix : 0;
   const PrefixShape shape = prefix_shape(n_seqs, n_groups, shared, max_rest, n_q_heads, n_kv_heads, cu_budget);
   if (prefix_states_bytes(shape, n_seqs, n_q_heads, head_dim) > need)

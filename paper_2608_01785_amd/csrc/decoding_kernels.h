@@ -32,15 +32,16 @@ hipError_t launch_beam_select(const BeamArgs& a, int cus, hipStream_t s);
 struct CacheCopyArgs {
   struct Copy {
     int32_t src, dst, tiles;  // slots, value tiles (32 positions) to copy
+    int32_t first;            // segments of a head's runs before this copy's
   };
   uint16_t* k[kCopyLayers];
   uint16_t* v[kCopyLayers];
   Copy copies[kCopyList];
-  int32_t layers, n_copies, heads;
-  int32_t max_tiles;          // most of a copy
-  int32_t dh;
+  int32_t layers, n_copies, heads, dh;
+  int32_t segments;           // of a head's runs, all copies together
   int64_t head_bytes;         // bytes of one head of a slot
 };
+static_assert(sizeof(CacheCopyArgs) <= 4096, "kernel arguments");
 hipError_t launch_cache_copy(const CacheCopyArgs& a, int cus, hipStream_t s);
 
 // Attention of one row a sequence (see prefix_attention.hip).

@@ -15,22 +15,37 @@ namespace hs {
 constexpr int kBeamMaxBeams = 64;
 constexpr int kBeamMaxSelect = kLogprobsMaxTop;
 
-// Workspace bytes of a call of at most max_rows rows on any budget and type: a
-// partial result for every block of a row, of which there is one, or where rows
-// are split as many as hs_logprobs takes.
-inline size_t beam_workspace(int64_t max_rows, int64_t vocab, int select) {
-  const size_t whole = size_t(max_rows) * logprobs_partial_bytes(select);
-  const size_t split = logprobs_workspace(max_rows, vocab, select);
-  return whole > split ? whole : split;
+// The scan's blocks: as hs_logprobs (see logprobs_shape), but the join is there in any
+// case, so rows are split wherever CUs would idle: 85 rows of 50001 fp16 take 14.3 us in
+// 3 blocks each and 18.0 whole.  Two or four blocks a CU cost the join what they save
+// (32 rows of 65536: 13.7 us with one, 14.0 with two, 14.5 with four).
+constexpr int kBeamPerCu = 1;
+inline LogprobsShape beam_shape(int rows, int vocab, int elem_bytes, int cus) {
+  const int chunk = 4096 / elem_bytes;
+  const int chunks = int((int64_t(vocab) + 16 / elem_bytes - 1 + chunk - 1) / chunk);  // any row start
+  if (int64_t(rows) >= 8 * int64_t(cus) || chunks < 2) return LogprobsShape{1, 1};
+  int splits = rows < kBeamPerCu * cus ? kBeamPerCu * cus / rows : 1;
+  if (splits > (chunks + 3) / 4) splits = (chunks + 3) / 4;
+  if (splits > kLogprobsMaxSplits) splits = kLogprobsMaxSplits;
+  return LogprobsShape{4, splits};
 }
 
-// hs_cache_copy: layers and copies of one launch (kernel arguments hold 4 KB).
+// Workspace bytes of a call of at most max_rows rows on any budget and type: a
+// partial result for every block.
+inline size_t beam_workspace(int64_t max_rows, int select) {
+  const int64_t blocks = max_rows > kBeamPerCu * 256 ? max_rows : max_rows * kLogprobsMaxSplits < kBeamPerCu * 256
+                                                                      ? max_rows * kLogprobsMaxSplits
+                                                                      : kBeamPerCu * 256;
+  return size_t(blocks) * logprobs_partial_bytes(select);
+}
+
+// hs_cache_copy: layers and copies of one launch (kernel arguments hold 4 KB), bytes of
+// a block.  A head's run of so many value tiles (2^33 bytes at most) has copy_segments.
 constexpr int kCopyLayers = 32;
-constexpr int kCopyList = 240;
-constexpr int kCopySegment = 16384;  // bytes of a block
-// Segments of a head's run of so many value tiles (2^33 bytes at most: 2^19).
-constexpr uint32_t copy_segments(int tiles, int dh) {
-  return uint32_t((int64_t(tiles) * 64 * dh + kCopySegment - 1) / kCopySegment);
+constexpr int kCopyList = 200;
+constexpr int kCopySegment = 8192;
+constexpr int32_t copy_segments(int tiles, int dh) {
+  return int32_t((int64_t(tiles) * 64 * dh + kCopySegment - 1) / kCopySegment);
 }
 
 // m / per_head = 2 m prefix_inverse(per_head) >> 32 for m < 2^31 / per_head: a launch

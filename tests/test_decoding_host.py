@@ -5,7 +5,7 @@ import numpy as np
 import pytest
 
 P = 0x10000000   # fake device addresses, far apart and never dereferenced
-INVALID, UNSUPPORTED, WORKSPACE = 1, 2, 4
+INVALID, UNSUPPORTED, BUDGET, WORKSPACE = 1, 2, 3, 4
 
 
 @pytest.fixture(scope="module")
@@ -17,10 +17,10 @@ def b():
 
 def beam(b, **kw):
     a = dict(z=P, t=0, ld=64, groups=2, beams=4, vocab=64, scores=2 * P, fin=3 * P, end=1, k=8, os=4 * P, op=5 * P,
-             ot=6 * P, of=7 * P, ws=8 * P, wsb=1 << 30)
+             ot=6 * P, of=7 * P, ws=8 * P, wsb=1 << 30, cus=256)
     a.update(kw)
     st = b.lib().hs_beam_select(None, a["z"], a["t"], a["ld"], a["groups"], a["beams"], a["vocab"], a["scores"],
-                                a["fin"], a["end"], a["k"], a["os"], a["op"], a["ot"], a["of"], 256, None, a["ws"],
+                                a["fin"], a["end"], a["k"], a["os"], a["op"], a["ot"], a["of"], a["cus"], None, a["ws"],
                                 a["wsb"])
     return st, b.hs_last_error()
 
@@ -43,11 +43,11 @@ def copy(b, **kw):
 
 def prefix(b, **kw):
     a = dict(q=P, t=2, ldq=256, o=2 * P, ldo=256, hq=4, hkv=2, dh=64, k=3 * P, v=4 * P, slots=8, page=64, tab=5 * P,
-             pps=4, lens=6 * P, n=3, off=7 * P, pre=8 * P, g=2, mp=128, mr=100, ws=9 * P, wsb=1 << 28)
+             pps=4, lens=6 * P, n=3, off=7 * P, pre=8 * P, g=2, mp=128, mr=100, ws=9 * P, wsb=1 << 28, cus=256)
     a.update(kw)
     st = b.lib().hs_prefix_attention(None, a["q"], a["t"], a["ldq"], a["o"], a["ldo"], a["hq"], a["hkv"], a["dh"],
                                      a["k"], a["v"], a["slots"], a["page"], a["tab"], a["pps"], a["lens"], a["n"],
-                                     a["off"], a["pre"], a["g"], a["mp"], a["mr"], 256, None, a["ws"], a["wsb"])
+                                     a["off"], a["pre"], a["g"], a["mp"], a["mr"], a["cus"], None, a["ws"], a["wsb"])
     return st, b.hs_last_error()
 
 
@@ -81,6 +81,8 @@ REFUSED = [
     (beam, dict(ws=8 * P + 8), INVALID, "aligned"),
     (beam, dict(wsb=16), WORKSPACE, "needed"),
     (beam, dict(), INVALID, "context is null"),
+    (beam, dict(cus=0), BUDGET, "budget"),
+    (prefix, dict(cus=-5), BUDGET, "budget"),
     (beam, dict(fin=None, end=-1, of=None), INVALID, "context is null"),
     (beam, dict(groups=0, z=None, scores=None, fin=None, os=None, op=None, ot=None, of=None, ws=None), INVALID,
      "context is null"),
@@ -165,6 +167,20 @@ def test_workspaces_cover_smaller_calls(b):
                 for r in (0, 1, 257, 3000):
                     assert b.hs_prefix_attention_workspace_size(*heads, n, p, r) <= most, (n, p, r)
     assert b.hs_prefix_attention_workspace_size(28, 4, 128, 0, 4096, 100) == 0
+
+
+def test_partial_results_of_beams_fit_the_workspace(b):
+    states = b.lib().hs_beam_select_states
+    states.restype = ctypes.c_uint64
+    rng = np.random.default_rng(2)
+    for _ in range(20000):
+        groups, beams = int(np.exp(rng.uniform(0, np.log(1000)))), int(rng.integers(1, 65))
+        vocab, select = int(np.exp(rng.uniform(0, np.log(300000)))), int(rng.integers(1, 65))
+        size = b.hs_beam_select_workspace_size(groups, beams, vocab, select)
+        for cus in (1, 64, 160, 256):
+            less = int(rng.integers(1, groups + 1))
+            for g, elem in ((groups, 2), (groups, 4), (less, 2), (less, 4)):
+                assert states(g * beams, vocab, elem, select, cus) <= size, (groups, g, beams, vocab, select, cus)
 
 
 def test_partial_states_fit_the_workspace(b):
