@@ -598,6 +598,29 @@ hs_status hs_prefix_attention(hs_context* ctx, const void* q, int32_t type, int6
                               int32_t max_prefix, int32_t max_rest, int32_t cu_budget, void* stream, void* workspace,
                               size_t ws_bytes);
 
+/* Workspace bytes of hs_downstream_decode_step_prefix for at most batch rows whose
+ * positions stay below max_pos, on pages of page_positions, with prefixes up to max_prefix
+ * and at most max_rest keys of a row behind its prefix (the new one included). */
+hs_status hs_workspace_size_prefix(const hs_layer_cfg* cfg, int32_t batch, int32_t max_pos, int32_t page_positions,
+                                   int32_t max_prefix, int32_t max_rest, size_t* bytes);
+
+/* hs_downstream_decode_step on a paged cache whose rows share prefixes: the attention of
+ * every layer is hs_prefix_attention's.
+ *   group_offsets  host [n_groups + 1], non-decreasing from 0 to batch: group g has
+ *                  rows group_offsets[g] .. group_offsets[g + 1] - 1 (1 <= n_groups <= batch);
+ *   prefix_lens    host [n_groups]: the first positions that group g's rows share, at
+ *                  most kv_lens of each of them (0: none).
+ * The rows of a group list the same slots for the whole pages of their prefix
+ * (HS_ERR_INVALID_ARG otherwise); a page that the prefix ends in may be a copy of its
+ * own in each, and is read from the group's first row.
+ * Everything else as hs_downstream_decode_step; the attention differs from that call's
+ * by its roundings. */
+hs_status hs_downstream_decode_step_prefix(hs_context* ctx, const hs_layer_cfg* cfg, const hs_layer_weights* w,
+                                           int32_t n_layers, const void* x_in, void* x_out, const hs_kv_cache* kv,
+                                           const int32_t* kv_lens, int32_t batch, const int32_t* group_offsets,
+                                           const int32_t* prefix_lens, int32_t n_groups, int32_t cu_budget,
+                                           void* stream, void* workspace, size_t ws_bytes);
+
 /* Which page holds what: the block tables of the sequences that share a cache's
  * pages.  Host only; it moves no data but names the copies that hs_cache_copy has
  * to make, on the stream of the step and before the step.

@@ -75,6 +75,16 @@ class AnswerHead:
             out.top_logprobs, out.top_tokens = new(rows, self.top_k), new(rows, self.top_k, dtype=torch.int32)
         return out
 
+    def product(self, y, cu_budget: int = 256, stream=None):
+        """The logits of at most max_rows residual rows: a view of this head's buffer, overwritten by its next pass."""
+        n = y.shape[0]
+        if n > self.max_rows:
+            raise ValueError(f"{n} rows, the head takes {self.max_rows} at a time")
+        q, q_scale, z = self.q[:n], self.q_scale[:n], self.logits[:n]
+        binding.hs_quantize_rows(self.ctx, y, q, q_scale, self.gain, self.eps, cu_budget, stream)
+        binding.hs_linear_i8(self.ctx, q, q_scale, self.w, self.w_scale, z, self.bias, cu_budget, stream)
+        return z
+
     def __call__(self, y, out: Answers, tokens=None, cu_budget: int = 256, stream=None) -> None:
         """y: fp32 (bf16, fp16) [rows, hidden] residual rows -> out; tokens: int32 [rows, n_tokens] or None."""
         if y.dim() != 2 or y.shape[1] != self.hidden:
@@ -85,10 +95,7 @@ class AnswerHead:
                 raise ValueError(f"{name} has {t.shape[0] if t.shape else 'no'} rows, y {rows}")
         for first in range(0, rows, self.max_rows):
             part = slice(first, min(first + self.max_rows, rows))
-            n = part.stop - first
-            q, q_scale, z = self.q[:n], self.q_scale[:n], self.logits[:n]
-            binding.hs_quantize_rows(self.ctx, y[part], q, q_scale, self.gain, self.eps, cu_budget, stream)
-            binding.hs_linear_i8(self.ctx, q, q_scale, self.w, self.w_scale, z, self.bias, cu_budget, stream)
+            z = self.product(y[part], cu_budget, stream)
             given = {k: t[part] for k, t in vars(out).items() if t is not None}
             binding.hs_logprobs(self.ctx, z, None if tokens is None else tokens[part], cu_budget=cu_budget,
                                 stream=stream, workspace=self.ws, **given)

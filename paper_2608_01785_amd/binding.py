@@ -32,7 +32,7 @@ SYMBOLS = (
     "hs_temporal_create", "hs_temporal_step", "hs_temporal_destroy",
     "hs_quantize_rows", "hs_linear_i8", "hs_logprobs_workspace_size", "hs_logprobs",
     "hs_beam_select_workspace_size", "hs_beam_select", "hs_cache_copy", "hs_prefix_attention_workspace_size",
-    "hs_prefix_attention", "hs_pages_create", "hs_pages_destroy", "hs_pages_reserve", "hs_pages_fork",
+    "hs_prefix_attention", "hs_workspace_size_prefix", "hs_downstream_decode_step_prefix", "hs_pages_create", "hs_pages_destroy", "hs_pages_reserve", "hs_pages_fork",
     "hs_pages_compact", "hs_pages_table", "hs_pages_shared", "hs_pages_free_count",
 )
 HS_WEIGHTS_BF16, HS_WEIGHTS_F16 = 0, 1
@@ -198,6 +198,11 @@ def lib() -> ctypes.CDLL:
             "hs_prefix_attention_workspace_size": [i32, i32, i32, i32, i32, i32, ctypes.POINTER(ctypes.c_size_t)],
             "hs_prefix_attention": [vp, vp, i32, i64, vp, i64, i32, i32, i32, vp, vp, i32, i32, vp, i32, vp, i32, vp,
                                     vp, i32, i32, i32, i32, vp, vp, ctypes.c_size_t],
+            "hs_workspace_size_prefix": [ctypes.POINTER(LayerCfg), i32, i32, i32, i32, i32,
+                                         ctypes.POINTER(ctypes.c_size_t)],
+            "hs_downstream_decode_step_prefix": [vp, ctypes.POINTER(LayerCfg), ctypes.POINTER(LayerWeights), i32, vp,
+                                                 vp, ctypes.POINTER(KvCache), i32p, i32, i32p, i32p, i32, i32, vp, vp,
+                                                 ctypes.c_size_t],
             "hs_pages_create": [i32, i32, i32, i32, ctypes.POINTER(vp)],
             "hs_pages_destroy": [vp],
             "hs_pages_reserve": [vp, i32p, i32p, i32, i32p, i32p, i32p, i32p],
@@ -517,6 +522,33 @@ def hs_downstream_decode_step_noalloc(ctx: Context, cfg, weights, x_in, x_out, k
     _check(lib().hs_downstream_decode_step_noalloc(
         ctx.handle, ctypes.byref(LayerCfg.of(cfg)), warr, len(weights), _ptr(x_in), _ptr(x_out),
         ctypes.byref(kvs) if kvs is not None else None, lens, len(lens), cu_budget, _ptr(stream)))
+
+
+def hs_workspace_size_prefix(cfg, batch: int, max_pos: int, page_positions: int, max_prefix: int,
+                             max_rest: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib().hs_workspace_size_prefix(ctypes.byref(LayerCfg.of(cfg)), batch, max_pos, page_positions, max_prefix,
+                                          max_rest, ctypes.byref(n)))
+    return int(n.value)
+
+
+def hs_downstream_decode_step_prefix(ctx: Context, cfg, weights, x_in, x_out, kv, kv_lens, group_offsets, prefix_lens,
+                                     cu_budget: int, stream=None, workspace=None,
+                                     ws_bytes: Optional[int] = None) -> None:
+    """The decode step on a paged cache whose rows share prefixes; group_offsets, prefix_lens: host lists."""
+    warr = _weights_array(weights)
+    kvs = _kv_struct(kv)
+    lens = _i32_array(kv_lens)
+    if len(group_offsets) != len(prefix_lens) + 1:
+        raise ValueError(f"{len(group_offsets)} offsets, {len(prefix_lens)} prefixes")
+    if len(kv) > 4 and kv[4] is not None and len(kv[4]) != len(lens):
+        raise ValueError(f"the block table has {len(kv[4])} rows, the batch {len(lens)}")
+    if ws_bytes is None:
+        ws_bytes = workspace.numel() * workspace.element_size()
+    _check(lib().hs_downstream_decode_step_prefix(
+        ctx.handle, ctypes.byref(LayerCfg.of(cfg)), warr, len(weights), _ptr(x_in), _ptr(x_out),
+        ctypes.byref(kvs), lens, len(lens), _i32_array(group_offsets), _i32_array(prefix_lens), len(prefix_lens),
+        cu_budget, _ptr(stream), _ptr(workspace), ws_bytes))
 
 
 class DecodeGraph:

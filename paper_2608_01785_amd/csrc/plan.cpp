@@ -2,6 +2,7 @@
 // batch metadata, attention work lists and the workspace layout.
 #include "plan.h"
 #include "decode_policy.h"
+#include "decoding_policy.h"
 #include "skinny_policy.h"
 
 #include <stdarg.h>
@@ -417,6 +418,71 @@ hs_status build_plan(const hs_layer_cfg& c, const int32_t* off, const int32_t* c
     }
   }
   return HS_OK;
+}
+
+hs_status check_prefix_groups(const hs_kv_cache& kv, const int32_t* kv_lens, int32_t batch, const PrefixGroups& groups,
+                              int32_t* max_prefix, int32_t* max_rest) {
+  const int32_t* off = groups.offsets;
+  *max_prefix = 0;
+  *max_rest = 1;
+  if (off[0] != 0 || off[groups.n] != batch)
+    return fail(HS_ERR_INVALID_ARG, "group_offsets run from %d to %d, expected 0 to %d", off[0], off[groups.n], batch);
+  for (int32_t g = 0; g < groups.n; ++g) {
+    if (off[g + 1] < off[g] || off[g + 1] > batch)
+      return fail(HS_ERR_INVALID_ARG, "group_offsets decrease at %d (%d -> %d)", g, off[g], off[g + 1]);
+    const int32_t p = groups.prefix[g];
+    if (p < 0) return fail(HS_ERR_INVALID_ARG, "prefix_lens[%d] = %d", g, p);
+    if (off[g] == off[g + 1]) continue;
+    *max_prefix = std::max(*max_prefix, p);
+    const int32_t* first = kv.block_table + int64_t(off[g]) * kv.pages_per_seq;
+    for (int32_t b = off[g]; b < off[g + 1]; ++b) {
+      if (p > kv_lens[b])
+        return fail(HS_ERR_INVALID_ARG, "prefix_lens[%d] = %d, but row %d has %d cached rows", g, p, b, kv_lens[b]);
+      const int32_t* row = kv.block_table + int64_t(b) * kv.pages_per_seq;
+      for (int32_t j = 0; j < p / kv.max_ctx; ++j)
+        if (row[j] != first[j])
+          return fail(HS_ERR_INVALID_ARG, "rows %d and %d of group %d do not share page %d of their prefix", off[g], b, g,
+                      j);
+      *max_rest = std::max(*max_rest, kv_lens[b] + 1 - p);
+    }
+  }
+  return HS_OK;
+}
+
+hs_status prefix_layout(const hs_layer_cfg& c, int32_t batch, int32_t max_pos, int32_t page_keys, int32_t max_prefix,
+                        int32_t max_rest, WsLayout* lay, PrefixPlan* out) {
+  if (int64_t(max_prefix) + max_rest > (int64_t(1) << 30) || int64_t(batch) * c.n_q_heads > (int64_t(1) << 25))
+    return fail(HS_ERR_UNSUPPORTED, "%d rows of %d heads over %d + %d keys", batch, c.n_q_heads, max_prefix, max_rest);
+  PrefixPlan& p = *out;
+  p.pages_per_seq = int32_t(ceil_div(max_pos, page_keys));
+  p.max_prefix = max_prefix;
+  p.max_rest = max_rest;
+  p.table = align_up(lay->meta_bytes, kAlign);
+  p.lens = p.table + size_t(batch) * p.pages_per_seq * 4;
+  p.prefix = p.lens + size_t(batch) * 4;
+  p.offsets = p.prefix + size_t(batch) * 4;  // batch groups at most
+  lay->meta = align_up(lay->total, kAlign);
+  lay->meta_bytes = p.offsets + size_t(batch + 1) * 4;
+  p.part = align_up(lay->meta + lay->meta_bytes, kAlign);
+  lay->total = align_up(p.part + prefix_workspace(batch, max_prefix, max_rest, c.n_q_heads, c.n_kv_heads, c.head_dim),
+                        kAlign);
+  return HS_OK;
+}
+
+void append_prefix(const hs_kv_cache& kv, const int32_t* kv_lens, const PrefixGroups& groups, Plan* plan,
+                   PrefixPlan* prefix) {
+  PrefixPlan& p = *prefix;
+  p.n_groups = groups.n;
+  plan->image.resize(p.offsets + size_t(plan->B + 1) * 4, 0);
+  auto* table = reinterpret_cast<int32_t*>(plan->image.data() + p.table);
+  auto* lens = reinterpret_cast<int32_t*>(plan->image.data() + p.lens);
+  for (int32_t b = 0; b < plan->B; ++b) {
+    lens[b] = kv_lens[b] + 1;
+    const int64_t pages = ceil_div(lens[b], kv.max_ctx);
+    memcpy(table + int64_t(b) * p.pages_per_seq, kv.block_table + int64_t(b) * kv.pages_per_seq, size_t(pages) * 4);
+  }
+  memcpy(plan->image.data() + p.offsets, groups.offsets, size_t(groups.n + 1) * 4);
+  memcpy(plan->image.data() + p.prefix, groups.prefix, size_t(groups.n) * 4);
 }
 
 }  // namespace hs

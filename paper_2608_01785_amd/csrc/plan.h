@@ -126,4 +126,33 @@ hs_status build_plan(const hs_layer_cfg& c, const int32_t* seq_offsets, const in
                      int32_t n_seqs, const KvPlacement& kv, Plan* out, const int32_t* positions3 = nullptr,
                      const PlanCapacity* cap = nullptr, bool bidirectional = false);
 
+// A decode step whose rows share prefixes: groups of consecutive rows (host arrays).
+struct PrefixGroups {
+  const int32_t* offsets;  // [n + 1]
+  const int32_t* prefix;   // [n]
+  int32_t n;
+};
+
+// Where the step's arrays lie, in the metadata image and (part) in the workspace.
+struct PrefixPlan {
+  size_t table = 0, lens = 0, offsets = 0, prefix = 0;
+  size_t part = 0;         // partial states
+  int32_t pages_per_seq = 0, n_groups = 0;
+  int32_t max_prefix = 0, max_rest = 0;
+};
+
+// Checks the groups of a step against its batch and its block table (which has been
+// checked itself); the longest prefix, and the most keys of a row behind its own.
+hs_status check_prefix_groups(const hs_kv_cache& kv, const int32_t* kv_lens, int32_t batch, const PrefixGroups& groups,
+                              int32_t* max_prefix, int32_t* max_rest);
+
+// Extends the layout of a plain call of `batch` rows on a paged cache: the metadata
+// moves behind it, with room for the groups' arrays, and the partial states follow.
+hs_status prefix_layout(const hs_layer_cfg& c, int32_t batch, int32_t max_pos, int32_t page_keys, int32_t max_prefix,
+                        int32_t max_rest, WsLayout* lay, PrefixPlan* out);
+
+// Appends the groups' arrays to the plan's image.
+void append_prefix(const hs_kv_cache& kv, const int32_t* kv_lens, const PrefixGroups& groups, Plan* plan,
+                   PrefixPlan* prefix);
+
 }  // namespace hs

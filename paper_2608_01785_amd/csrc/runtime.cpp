@@ -5,9 +5,11 @@
 #include <string.h>
 
 #include <algorithm>
+#include <new>
 #include <vector>
 
 #include "context_call.h"
+#include "decoding_kernels.h"
 #include "hs_kernels.h"
 #include "plan.h"
 
@@ -297,6 +299,7 @@ struct LaunchSet {
   int32_t budget;
   bool pos3;
   bool fixed;
+  const hs::PrefixPlan* prefix = nullptr;  // single-row attention behind shared prefixes
 };
 
 hs_status launch_layers(hs_context* ctx, const LaunchSet& L, hipStream_t s) {
@@ -423,7 +426,37 @@ hs_status launch_layers(hs_context* ctx, const LaunchSet& L, hipStream_t s) {
     da.hkv = hkv;
     da.dh = dh;
     da.scale_log2 = scale_log2;
-    if (plan.n_dec_rows > 0 || L.fixed) TIMED(HS_KERNEL_DECODE_ATTN, hs::launch_decode_attention(da, s));
+    if (L.prefix) {
+      const hs::PrefixPlan& pp = *L.prefix;
+      hs::PrefixArgs pa{};
+      pa.q = q_buf;
+      pa.type = HS_TYPE_F16;
+      pa.ldq = pa.ldo = int64_t(hq) * dh;
+      pa.out = o_buf;
+      pa.out_k8_rows = k8;
+      pa.k = kstore;
+      pa.v = vstore;
+      pa.n_slots = kv->n_slots;
+      pa.page = kv->max_ctx;
+      pa.table = reinterpret_cast<const int32_t*>(meta + pp.table);
+      pa.pages_per_seq = pp.pages_per_seq;
+      pa.lens = reinterpret_cast<const int32_t*>(meta + pp.lens);
+      pa.n_seqs = T;
+      pa.offsets = reinterpret_cast<const int32_t*>(meta + pp.offsets);
+      pa.prefix = reinterpret_cast<const int32_t*>(meta + pp.prefix);
+      pa.n_groups = pp.n_groups;
+      pa.max_prefix = pp.max_prefix;
+      pa.max_rest = pp.max_rest;
+      pa.hq = hq;
+      pa.hkv = hkv;
+      pa.dh = dh;
+      pa.per_head_inv = hs::prefix_inverse(hq / hkv);
+      pa.scale_log2 = scale_log2;
+      pa.part = at<void>(ws, pp.part);
+      TIMED(HS_KERNEL_PREFIX_ATTN, hs::launch_prefix_attention(pa, budget, s));
+    } else if (plan.n_dec_rows > 0 || L.fixed) {
+      TIMED(HS_KERNEL_DECODE_ATTN, hs::launch_decode_attention(da, s));
+    }
 
     hs::GemmArgs go{};
     go.part = sk_part;
@@ -498,10 +531,14 @@ hs_status launch_layers(hs_context* ctx, const LaunchSet& L, hipStream_t s) {
 // noalloc: the workspace is the context's static scratch (ws and ws_bytes are
 // ignored), laid out without the packed key/value slot (a cache is required),
 // and the metadata goes through the fixed staging ring.
+// groups: the rows (one a sequence, on a paged cache) share prefixes; the metadata,
+// with the groups' arrays behind the plan's, and the partial states of the attention
+// lie behind the layout of the plain call.
 hs_status run_stack(hs_context* ctx, const hs_layer_cfg* cfg, const hs_layer_weights* w, int32_t n_layers,
                     const void* x_in, void* x_out, const int32_t* seq_offsets, const int32_t* ctx_lens,
                     int32_t n_seqs, const hs_kv_cache* kv, int32_t budget, int role, void* stream,
-                    void* ws, size_t ws_bytes, const int32_t* pos3 = nullptr, bool noalloc = false) {
+                    void* ws, size_t ws_bytes, const int32_t* pos3 = nullptr, bool noalloc = false,
+                    const hs::PrefixGroups* groups = nullptr) {
   hs::clear_error();
   hs_status st = hs::validate_cfg(cfg);
   if (st != HS_OK) return st;
@@ -520,6 +557,7 @@ hs_status run_stack(hs_context* ctx, const hs_layer_cfg* cfg, const hs_layer_wei
   st = hs::check_32bit_extents(*cfg, T, kv ? kv->max_ctx : 0);
   if (st != HS_OK) return st;
   hs::KvPlacement place;
+  int32_t max_prefix = 0, max_rest = 0;  // of the groups
   if (kv) {
     if (!ctx_lens) return hs::fail(HS_ERR_INVALID_ARG, "a key/value cache needs ctx_lens");
     if (!kv->k || !kv->v) return hs::fail(HS_ERR_INVALID_ARG, "cache pointer arrays are null");
@@ -533,6 +571,10 @@ hs_status run_stack(hs_context* ctx, const hs_layer_cfg* cfg, const hs_layer_wei
       if (st != HS_OK) return st;
       place.table = kv->block_table;
       place.pages_per_seq = kv->pages_per_seq;
+      if (groups) {
+        st = hs::check_prefix_groups(*kv, ctx_lens, n_seqs, *groups, &max_prefix, &max_rest);
+        if (st != HS_OK) return st;
+      }
     } else {
       if (n_seqs > kv->n_slots)
         return hs::fail(HS_ERR_INVALID_ARG, "%d sequences but only %d cache slots", n_seqs, kv->n_slots);
@@ -566,7 +608,12 @@ hs_status run_stack(hs_context* ctx, const hs_layer_cfg* cfg, const hs_layer_wei
     ws_bytes = hs::noalloc_scratch_bytes();
   }
   if (!ws) return hs::fail(HS_ERR_WORKSPACE, "workspace is null");
-  const hs::WsLayout lay = hs::ws_layout(*cfg, T, n_seqs, max_pos, place.table ? place.max_ctx : 0, !noalloc);
+  hs::WsLayout lay = hs::ws_layout(*cfg, T, n_seqs, max_pos, place.table ? place.max_ctx : 0, !noalloc);
+  hs::PrefixPlan prefix;
+  if (groups) {
+    st = hs::prefix_layout(*cfg, n_seqs, max_pos, place.max_ctx, max_prefix, max_rest, &lay, &prefix);
+    if (st != HS_OK) return st;
+  }
   if (ws_bytes < lay.total) {
     if (noalloc)
       return hs::fail(HS_ERR_WORKSPACE, "the call needs %zu bytes of scratch; the static scratch holds %zu",
@@ -577,6 +624,7 @@ hs_status run_stack(hs_context* ctx, const hs_layer_cfg* cfg, const hs_layer_wei
   hs::Plan plan;
   st = hs::build_plan(*cfg, seq_offsets, ctx_lens, n_seqs, place, &plan, pos3);
   if (st != HS_OK) return st;
+  if (groups) hs::append_prefix(*kv, ctx_lens, *groups, &plan, &prefix);
   if (plan.image.size() > lay.meta_bytes) return hs::fail(HS_ERR_INTERNAL, "metadata image exceeds its region");
   if (noalloc && plan.image.size() > kFixedSlotBytes)
     return hs::fail(HS_ERR_WORKSPACE, "metadata of %zu bytes exceeds the %zu-byte staging slot of the "
@@ -592,6 +640,7 @@ hs_status run_stack(hs_context* ctx, const hs_layer_cfg* cfg, const hs_layer_wei
   TIMED(HS_KERNEL_ROPE_TABLE,
         hs::launch_rope_table(at<float2>(ws, lay.rope), max_pos, cfg->head_dim, cfg->rope_base, s));
   LaunchSet L{cfg, w, n_layers, x_in, x_out, kv, place.cache, ws, lay, &plan, budget, pos3 != nullptr, false};
+  L.prefix = groups ? &prefix : nullptr;
   return launch_layers(ctx, L, s);
 }
 
@@ -796,6 +845,48 @@ hs_status hs_downstream_decode_step(hs_context* ctx, const hs_layer_cfg* cfg, co
   for (int32_t b = 0; b <= batch; ++b) off[b] = b;
   return run_stack(ctx, cfg, w, n_layers, x_in, x_out, off.data(), kv_lens, batch, kv, cu_budget,
                    HS_ROLE_DOWN, stream, workspace, ws_bytes);
+}
+
+hs_status hs_workspace_size_prefix(const hs_layer_cfg* cfg, int32_t batch, int32_t max_pos, int32_t page_positions,
+                                   int32_t max_prefix, int32_t max_rest, size_t* bytes) {
+  hs::clear_error();
+  hs_status st = hs::validate_cfg(cfg);
+  if (st != HS_OK) return st;
+  if (!bytes) return hs::fail(HS_ERR_INVALID_ARG, "bytes output is null");
+  if (batch < 1 || max_pos < 1 || max_prefix < 0 || max_rest < 0)
+    return hs::fail(HS_ERR_INVALID_ARG, "batch %d, positions %d, prefixes up to %d and %d keys more", batch, max_pos,
+                    max_prefix, max_rest);
+  if (page_positions < 64 || page_positions % 64 != 0)
+    return hs::fail(HS_ERR_INVALID_ARG, "page size %d must be a positive multiple of 64", page_positions);
+  hs::WsLayout lay = hs::ws_layout(*cfg, batch, batch, max_pos, page_positions);
+  hs::PrefixPlan plan;
+  st = hs::prefix_layout(*cfg, batch, max_pos, page_positions, max_prefix, max_rest, &lay, &plan);
+  if (st != HS_OK) return st;
+  *bytes = lay.total;
+  return HS_OK;
+}
+
+hs_status hs_downstream_decode_step_prefix(hs_context* ctx, const hs_layer_cfg* cfg, const hs_layer_weights* w,
+                                           int32_t n_layers, const void* x_in, void* x_out, const hs_kv_cache* kv,
+                                           const int32_t* kv_lens, int32_t batch, const int32_t* group_offsets,
+                                           const int32_t* prefix_lens, int32_t n_groups, int32_t cu_budget,
+                                           void* stream, void* workspace, size_t ws_bytes) {
+  hs::clear_error();
+  if (!kv) return hs::fail(HS_ERR_INVALID_ARG, "decode needs a key/value cache");
+  if (!kv->block_table) return hs::fail(HS_ERR_INVALID_ARG, "shared prefixes need a block table");
+  if (!kv_lens) return hs::fail(HS_ERR_INVALID_ARG, "kv_lens is null");
+  if (batch < 1) return hs::fail(HS_ERR_INVALID_ARG, "batch %d < 1", batch);
+  if (!group_offsets || !prefix_lens) return hs::fail(HS_ERR_INVALID_ARG, "the groups are null");
+  if (n_groups < 1 || n_groups > batch) return hs::fail(HS_ERR_INVALID_ARG, "%d groups of %d rows", n_groups, batch);
+  try {
+    std::vector<int32_t> off(size_t(batch) + 1);
+    for (int32_t b = 0; b <= batch; ++b) off[b] = b;
+    const hs::PrefixGroups groups{group_offsets, prefix_lens, n_groups};
+    return run_stack(ctx, cfg, w, n_layers, x_in, x_out, off.data(), kv_lens, batch, kv, cu_budget, HS_ROLE_DOWN, stream,
+                     workspace, ws_bytes, nullptr, false, &groups);
+  } catch (const std::bad_alloc&) {
+    return hs::fail(HS_ERR_INTERNAL, "out of host memory");
+  }
 }
 
 hs_status hs_downstream_decode_step_noalloc(hs_context* ctx, const hs_layer_cfg* cfg, const hs_layer_weights* w,
