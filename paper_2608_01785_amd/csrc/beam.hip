@@ -24,6 +24,115 @@ using namespace scan;
 
 constexpr int kJoinWaves = 16;
 
+// log sum e^z of a row from its splits' partial results, the same bits in every lane;
+// NaN or -inf where the row has no distribution (NaN, +inf, all masked).
+__device__ __forceinline__ double log_sum_of(Sums sums) {
+  // The splits' sums against the row's maximum; F without the elements at it.
+  const float m = max_wave(sums.m);
+  const float f = exp_of(fmaxf(sums.m - m, kFar));
+  // (No product is left for the sums to contract with: every lane adds the same.)
+  double s = double(sums.s * f), rest = sums.m < m ? s : double(sums.f);
+  s = reduce_wave(s, [](double x, double y) { return x + y; });
+  rest = reduce_wave(rest, [](double x, double y) { return x + y; });
+  if (!(s > 0.0)) return -double(kInf);
+  return double(m) + (s < 1.5 ? log1p(rest) : log(s));
+}
+
+__device__ __forceinline__ void write_selected(const BeamArgs& a, int64_t group, int rank, double value, int beam,
+                                               int token) {
+  const int64_t o = group * a.select + rank;
+  a.out_scores[o] = float(value);
+  a.out_parents[o] = beam;
+  a.out_tokens[o] = token;
+  if (a.out_finished)
+    a.out_finished[o] =
+        beam >= 0 && ((a.finished && a.finished[group * a.beams + beam] != 0) || (a.end_token >= 0 && token == a.end_token));
+}
+
+// Few candidates: the splits' keys of all beams, as they were left, are ranked against
+// each other.  Block: one group, a thread or more for each of its n candidates;
+// wavefronts take the beams' sums in turn.
+constexpr int kFewCandidates = 256;
+
+__global__ __launch_bounds__(64 * kJoinWaves) void beam_few_kernel(BeamArgs a, LogprobsArgs scanned, int splits) {
+  __shared__ double values[kFewCandidates];
+  __shared__ int32_t tokens[kFewCandidates];
+  __shared__ double log_sums[kBeamMaxBeams];
+  __shared__ int total;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+  const int per_beam = splits * a.select, n = a.beams * per_beam;
+  const int64_t row0 = int64_t(blockIdx.x) * a.beams;
+  const int c = threadIdx.x;
+  uint64_t key = 0;
+  float score = -kInf;
+  bool ended = false;
+  const int beam = c / per_beam;
+  if (c < n) {
+    key = partial_keys(scanned, int64_t(scanned.rows) * splits)[row0 * per_beam + c];
+    score = a.scores[row0 + beam];
+    ended = a.finished && a.finished[row0 + beam] != 0;
+  }
+  for (int b = wave; b < a.beams; b += waves) {
+    Sums sums{kLowest, 0.0f, 0.0f, 0.0f};
+    if (lane < splits) {
+      const f32x4 v = static_cast<const f32x4*>(a.part)[(row0 + b) * splits + lane];
+      sums = Sums{v[0], v[1], v[2], v[3]};
+    }
+    const double l = log_sum_of(sums);  // (of an unscanned row: anything, not used)
+    if (lane == 0) log_sums[b] = l;
+  }
+  if (threadIdx.x == 0) total = 0;
+  __syncthreads();
+  double value = -double(kInf);
+  int token = -1;
+  if (c < n && score > -kInf) {
+    if (ended) {
+      if (c == beam * per_beam) {
+        value = double(score);
+        token = a.end_token;
+      }
+    } else if (key != 0 && log_sums[beam] > -double(kInf)) {
+      value = double(score) + (double(value_of(key)) - log_sums[beam]);
+      token = token_of(key);
+    }
+  }
+  if (c < kFewCandidates) {
+    values[c] = value;
+    tokens[c] = token;
+  }
+  const int here = __popcll(__ballot(value > -double(kInf)));
+  if (lane == 0 && here) atomicAdd(&total, here);
+  __syncthreads();
+  // Eight lanes count what goes before a candidate.
+  const int o = threadIdx.x & 7;
+  for (int c0 = 0; c0 < n; c0 += blockDim.x / 8) {
+    const int me = c0 + int(threadIdx.x >> 3);
+    const double v = me < n ? values[me] : -double(kInf);
+    uint32_t rank = 0;
+    if (v > -double(kInf)) {
+      int same = 0;  // as large, the candidate itself among them
+#pragma unroll 8
+      for (int j = o; j < n; j += 8) {
+        const double w = values[j];
+        rank += w > v;
+        same += w == v;
+      }
+      if (same > int(((me ^ o) & 7) == 0)) {
+        const int t = tokens[me], first = me / per_beam * per_beam;
+        for (int j = o; j < n; j += 8)
+          if (values[j] == v) rank += j < first || (j < first + per_beam && tokens[j] < t);
+      }
+    }
+    rank += xor_lane<1>(rank);
+    rank += xor_lane<2>(rank);
+    rank += xor_lane<4>(rank);
+    if (o == 0 && v > -double(kInf) && rank < uint32_t(a.select))
+      write_selected(a, blockIdx.x, rank, v, me / per_beam, tokens[me]);
+  }
+  for (int r = total + int(threadIdx.x); r < a.select; r += blockDim.x)
+    write_selected(a, blockIdx.x, r, -double(kInf), -1, -1);
+}
+
 // Block: one group.  `team` wavefronts share a beam.
 __global__ __launch_bounds__(64 * kJoinWaves) void beam_join_kernel(BeamArgs a, LogprobsArgs scanned, int splits,
                                                                     int team, int span) {
@@ -68,16 +177,8 @@ __global__ __launch_bounds__(64 * kJoinWaves) void beam_join_kernel(BeamArgs a, 
           const uint64_t other = lists[wave + w][63 - lane];
           list = merge_stages<32>(list > other ? list : other, true);
         }
-        // The splits' sums against the row's maximum; F without the elements at it.
-        const float m = max_wave(sums.m);
-        const float f = exp_of(fmaxf(sums.m - m, kFar));
-        double s = double(sums.s * f), rest = sums.m < m ? s : double(sums.f);
-        // (No product is left for the sums to contract with: every lane adds the same.)
-        s = reduce_wave(s, [](double x, double y) { return x + y; });
-        rest = reduce_wave(rest, [](double x, double y) { return x + y; });
-        const double log_sum = double(m) + (s < 1.5 ? log1p(rest) : log(s));
-        // A row without a distribution (NaN, +inf, all masked) has no continuation.
-        n = s > 0.0 ? __popcll(__ballot(lane < k && list != 0)) : 0;
+        const double log_sum = log_sum_of(sums);
+        n = log_sum > -double(kInf) ? __popcll(__ballot(lane < k && list != 0)) : 0;
         if (lane < n) {
           values[b * k + lane] = double(score) + (double(value_of(list)) - log_sum);
           tokens[b * k + lane] = token_of(list);
@@ -97,7 +198,6 @@ __global__ __launch_bounds__(64 * kJoinWaves) void beam_join_kernel(BeamArgs a, 
   // bisection, the number of larger values in each other (of equal ones, those of
   // lower beams).  A lane takes one of the other lists; `span` lanes, a power of two,
   // a candidate.
-  const int64_t out0 = int64_t(blockIdx.x) * k;
   const int o = threadIdx.x & (span - 1);
   for (int c0 = 0; c0 < a.beams * k; c0 += blockDim.x / span) {
     const int c = c0 + threadIdx.x / span;
@@ -122,23 +222,12 @@ __global__ __launch_bounds__(64 * kJoinWaves) void beam_join_kernel(BeamArgs a, 
     }
     for (int d = 1; d < span; d <<= 1) rank += __shfl_xor(rank, d, 64);
     if (!there || o != 0 || rank >= k) continue;
-    const int token = tokens[c];
-    a.out_scores[out0 + rank] = float(v);
-    a.out_parents[out0 + rank] = b;
-    a.out_tokens[out0 + rank] = token;
-    if (a.out_finished)
-      a.out_finished[out0 + rank] =
-          (a.finished && a.finished[row0 + b] != 0) || (a.end_token >= 0 && token == a.end_token);
+    write_selected(a, blockIdx.x, rank, v, b, tokens[c]);
   }
   if (wave != 0) return;
   int total = lane < a.beams ? counts[lane] : 0;
   for (int d = 1; d < 64; d <<= 1) total += __shfl_xor(total, d, 64);
-  for (int r = total + lane; r < k; r += 64) {
-    a.out_scores[out0 + r] = -kInf;
-    a.out_parents[out0 + r] = -1;
-    a.out_tokens[out0 + r] = -1;
-    if (a.out_finished) a.out_finished[out0 + r] = 0;
-  }
+  for (int r = total + lane; r < k; r += 64) write_selected(a, blockIdx.x, r, -double(kInf), -1, -1);
 }
 
 template <typename T>
@@ -160,6 +249,12 @@ hipError_t launch(const BeamArgs& a, int cus, hipStream_t s) {
   else
     hipLaunchKernelGGL((logprobs_kernel<T, 4, true, true, BeamScanArgs>), dim3(p.rows * shape.splits), dim3(256), 0, s, p,
                        shape.splits);
+  const int candidates = a.beams * shape.splits * a.select;
+  if (candidates <= kFewCandidates) {
+    const int threads = 8 * candidates <= 256 ? 256 : 8 * candidates <= 512 ? 512 : 1024;
+    hipLaunchKernelGGL(beam_few_kernel, dim3(a.groups), dim3(threads), 0, s, a, p, shape.splits);
+    return hipGetLastError();
+  }
   int span = 1;
   while (span < a.beams) span *= 2;
   int team = a.beams < kJoinWaves ? kJoinWaves / a.beams : 1;
