@@ -553,7 +553,8 @@ hs_status hs_beam_select(hs_context* ctx, const void* logits, int32_t type, int6
  * to 32 (what the source holds there is copied too); 0 copies nothing.
  * A slot may be the source of several copies; a destination is no other copy's
  * destination and no copy's source (HS_ERR_INVALID_ARG).  A slot of a layer is
- * at most 2^33 bytes, n_kv_heads at most 1024. */
+ * at most 2^33 bytes, n_kv_heads at most 1024, n_slots at most 2^28 (else
+ * HS_ERR_UNSUPPORTED; so too below). */
 hs_status hs_cache_copy(hs_context* ctx, const hs_kv_cache* kv, int32_t n_layers, int32_t n_kv_heads, int32_t head_dim,
                         const int32_t* src, const int32_t* dst, const int32_t* positions, int32_t n_copies,
                         int32_t cu_budget, void* stream);
@@ -626,7 +627,8 @@ hs_status hs_downstream_decode_step_prefix(hs_context* ctx, const hs_layer_cfg* 
  * to make, on the stream of the step and before the step.
  * A sequence 0 .. max_seqs - 1 has a length and the pages that hold it, at most
  * pages_per_seq; a page belongs to as many sequences as list it, and is free
- * without any.  Every call leaves the state as it was when it fails. */
+ * without any.  Every call leaves the state as it was when it fails.  One thread at
+ * a time. */
 typedef struct hs_pages hs_pages;
 
 /* n_pages pages of page_positions positions (a positive multiple of 64), all

@@ -56,7 +56,7 @@ constexpr int kFewCandidates = 256;
 
 __global__ __launch_bounds__(64 * kJoinWaves) void beam_few_kernel(BeamArgs a, LogprobsArgs scanned, int splits) {
   __shared__ double values[kFewCandidates];
-  __shared__ int32_t tokens[kFewCandidates];
+  __shared__ uint64_t keys[kFewCandidates];
   __shared__ double log_sums[kBeamMaxBeams];
   __shared__ int total;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
@@ -84,21 +84,19 @@ __global__ __launch_bounds__(64 * kJoinWaves) void beam_few_kernel(BeamArgs a, L
   if (threadIdx.x == 0) total = 0;
   __syncthreads();
   double value = -double(kInf);
-  int token = -1;
   if (c < n && score > -kInf) {
     if (ended) {
       if (c == beam * per_beam) {
         value = double(score);
-        token = a.end_token;
+        key = key_of(0.0f, uint32_t(a.end_token));
       }
     } else if (key != 0 && log_sums[beam] > -double(kInf)) {
       value = double(score) + (double(value_of(key)) - log_sums[beam]);
-      token = token_of(key);
     }
   }
   if (c < kFewCandidates) {
     values[c] = value;
-    tokens[c] = token;
+    keys[c] = key;
   }
   const int here = __popcll(__ballot(value > -double(kInf)));
   if (lane == 0 && here) atomicAdd(&total, here);
@@ -118,16 +116,17 @@ __global__ __launch_bounds__(64 * kJoinWaves) void beam_few_kernel(BeamArgs a, L
         same += w == v;
       }
       if (same > int(((me ^ o) & 7) == 0)) {
-        const int t = tokens[me], first = me / per_beam * per_beam;
+        const uint64_t mine = keys[me];
+        const int first = me / per_beam * per_beam;
         for (int j = o; j < n; j += 8)
-          if (values[j] == v) rank += j < first || (j < first + per_beam && tokens[j] < t);
+          if (values[j] == v) rank += j < first || (j < first + per_beam && keys[j] > mine);
       }
     }
     rank += xor_lane<1>(rank);
     rank += xor_lane<2>(rank);
     rank += xor_lane<4>(rank);
     if (o == 0 && v > -double(kInf) && rank < uint32_t(a.select))
-      write_selected(a, blockIdx.x, rank, v, me / per_beam, tokens[me]);
+      write_selected(a, blockIdx.x, rank, v, me / per_beam, token_of(keys[me]));
   }
   for (int r = total + int(threadIdx.x); r < a.select; r += blockDim.x)
     write_selected(a, blockIdx.x, r, -double(kInf), -1, -1);

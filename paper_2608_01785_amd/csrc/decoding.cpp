@@ -16,7 +16,9 @@ namespace {
 
 constexpr int32_t kBeamMaxRows = 1 << 22;      // a block of 256 threads each, 64 splits or one: fewer than 2^32 threads
 constexpr int64_t kMaxSlotBytes = int64_t(1) << 33;
+constexpr int32_t kMaxSlots = 1 << 28;  // a cache's bytes stay below 2^62
 constexpr int32_t kMaxKvHeads = 1024;
+constexpr int32_t kMaxCus = 256;        // of a device: no launch is sized for more
 constexpr int64_t kMaxBlocks = (int64_t(1) << 24) - 1;  // of 256 threads: fewer than 2^32 in a grid
 
 hs_status check_workspace(const void* workspace, size_t ws_bytes, size_t need) {
@@ -46,6 +48,7 @@ hs_status check_pages(int32_t n_slots, int32_t page, int32_t hkv, int32_t dh) {
     return fail(HS_ERR_INVALID_ARG, "%d positions a slot: must be a positive multiple of 64", page);
   if (int64_t(page) * hkv * dh * 2 > kMaxSlotBytes)
     return fail(HS_ERR_UNSUPPORTED, "a slot of %d positions exceeds %lld bytes", page, (long long)kMaxSlotBytes);
+  if (n_slots > kMaxSlots) return fail(HS_ERR_UNSUPPORTED, "%d slots: at most %d", n_slots, kMaxSlots);
   return HS_OK;
 }
 
@@ -104,7 +107,7 @@ hs_status hs_beam_select(hs_context* ctx, const void* logits, int32_t type, int6
       if (&other > &out) HS_TRY(check_disjoint(out, other));
   if (groups) HS_TRY(check_workspace(workspace, ws_bytes, need));
   if (cu_budget < 1) return fail(HS_ERR_BUDGET, "CU budget %d", cu_budget);  // sizes the launch below
-  if (groups && hs_beam_select_states(rows, vocab, int32_t(type_size(type)), n_select, cu_budget) > need)
+  if (groups && hs_beam_select_states(rows, vocab, int32_t(type_size(type)), n_select, std::min(cu_budget, kMaxCus)) > need)
     return fail(HS_ERR_INTERNAL, "the launch's partial results exceed the workspace");
   BeamArgs a{logits,   type,       ld,          groups,     beams,        vocab,    scores,
              finished, end_token,  n_select,    out_scores, out_parents,  out_tokens, out_finished,
@@ -251,7 +254,8 @@ hs_status hs_prefix_attention(hs_context* ctx, const void* q, int32_t type, int6
   if (n_seqs) HS_TRY(check_workspace(workspace, ws_bytes, need));
   if (cu_budget < 1) return fail(HS_ERR_BUDGET, "CU budget %d", cu_budget);  // sizes the launch below
   const int32_t shared = n_groups ? max_prefix : 0;
-  const PrefixShape shape = prefix_shape(n_seqs, n_groups, shared, max_rest, n_q_heads, n_kv_heads, cu_budget);
+  const PrefixShape shape =
+      prefix_shape(n_seqs, n_groups, shared, max_rest, n_q_heads, n_kv_heads, std::min(cu_budget, kMaxCus));
   if (prefix_states_bytes(shape, n_seqs, n_q_heads, head_dim) > need)
     return fail(HS_ERR_INTERNAL, "the launch's partial states exceed the workspace");
   if (prefix_blocks(shape, n_seqs, n_kv_heads) > kMaxBlocks)

@@ -83,6 +83,8 @@ REFUSED = [
     (beam, dict(), INVALID, "context is null"),
     (beam, dict(cus=0), BUDGET, "budget"),
     (prefix, dict(cus=-5), BUDGET, "budget"),
+    (beam, dict(cus=100000), INVALID, "context is null"),
+    (prefix, dict(cus=100000), INVALID, "context is null"),
     (beam, dict(fin=None, end=-1, of=None), INVALID, "context is null"),
     (beam, dict(groups=0, z=None, scores=None, fin=None, os=None, op=None, ot=None, of=None, ws=None), INVALID,
      "context is null"),
@@ -96,6 +98,7 @@ REFUSED = [
     (copy, dict(slots=0), INVALID, "slots"),
     (copy, dict(page=96), INVALID, "multiple of 64"),
     (copy, dict(page=2 ** 31 - 64, hkv=1024, dh=128), UNSUPPORTED, "exceeds"),
+    (copy, dict(slots=(1 << 28) + 1), UNSUPPORTED, "slots"),
     (copy, dict(n=-1), INVALID, "copies"),
     (copy, dict(src=None, n=2), INVALID, "null"),
     (copy, dict(dst=None), INVALID, "null"),
@@ -121,6 +124,7 @@ REFUSED = [
     (prefix, dict(mp=2 ** 31 - 1), UNSUPPORTED, "keys"),
     (prefix, dict(n=2 ** 31 - 1), UNSUPPORTED, "rows"),
     (prefix, dict(slots=0), INVALID, "slots"),
+    (prefix, dict(slots=2 ** 31 - 1), UNSUPPORTED, "slots"),
     (prefix, dict(page=32), INVALID, "multiple of 64"),
     (prefix, dict(pps=0), INVALID, "pages_per_seq"),
     (prefix, dict(g=-1), INVALID, "n_groups"),

@@ -185,6 +185,26 @@ def test_rows_without_a_distribution(env, dtype):
         assert set(parents[0].tolist()) <= {1, 3} and torch.all(parents[1:] == -1)
 
 
+@pytest.mark.parametrize("select", [4, 60])
+def test_scores_that_swallow_the_logits(env, select):
+    """Beyond 2^60 every continuation of a beam has one value: its logits' order is left, then the lower beam's."""
+    torch = env[0]
+    s = Beams(env, 1, 3, 2000, select, "f32", seed=20)
+    s.scores.copy_(torch.tensor([[-2e30, -1e30, -1e30]]))
+    torch.cuda.synchronize()
+    s.call()
+    torch.cuda.synchronize()
+    want = torch.sort(s.z[1], descending=True, stable=True).indices[:select].tolist()
+    assert s.out["out_tokens"][0].tolist() == want and s.out["out_parents"][0].tolist() == [1] * select
+    s.scores.fill_(math.inf)
+    torch.cuda.synchronize()
+    s.call()
+    torch.cuda.synchronize()
+    want = torch.sort(s.z[0], descending=True, stable=True).indices[:select].tolist()
+    assert s.out["out_tokens"][0].tolist() == want and s.out["out_parents"][0].tolist() == [0] * select
+    assert torch.all(s.out["out_scores"] == math.inf)
+
+
 def test_far_scores_and_certain_tokens(env):
     """A token with all the probability: its distance from 0 counts; logits beyond 2^20; scores from many steps."""
     torch = env[0]
