@@ -76,7 +76,10 @@ inline int prefix_split_keys(int64_t keys, int64_t blocks, int cus, int per_cu) 
   return int(prefix_up(prefix_up(keys, splits), kPrefixKeys) * kPrefixKeys);
 }
 
-// Narrow tiles: one block a CU.  More leave more states than the shorter ranges save:
+// Wide tiles: two blocks a CU, whose products and exponentials overlap (128 rows of 32
+// heads behind 16384 positions 66 us, with one 77); one where the rows' own keys take
+// more than about a fourth as long to read, which then share the CUs from the start
+// (with up to 512 keys more 80 us against 84).  Narrow tiles: one block a CU.  More leave more states than the shorter ranges save:
 // 8 rows of 28 heads behind 8192 positions take 15.5 us with one, 21 with two; behind
 // 30000, 23.7 and 29.8.  What rows have to themselves: two blocks a CU beside the prefixes'
 // (20 rows in 5 groups behind 1501 positions 17.9 us against 20.6 with four), eight
@@ -86,8 +89,8 @@ inline PrefixShape prefix_shape(int n_seqs, int n_groups, int max_prefix, int ma
   PrefixShape s{};
   s.prefix_rows = max_prefix < 1 || rows <= 16 * int64_t(n_groups) ? 16 : rows <= 64 * int64_t(n_groups) ? 32 : 128;
   s.prefix_tiles = max_prefix > 0 ? int(rows / s.prefix_rows + n_groups) : 0;
-  s.prefix_keys = prefix_split_keys(max_prefix, prefix_up(rows, s.prefix_rows) * hkv, cus,
-                                    s.prefix_rows == 128 ? 2 : 1);
+  const bool wide = s.prefix_rows == 128, long_rest = 240 * int64_t(max_rest) > per_head * max_prefix;
+  s.prefix_keys = prefix_split_keys(max_prefix, prefix_up(rows, s.prefix_rows) * hkv, cus, wide && !long_rest ? 2 : 1);
   s.prefix_splits = int(prefix_up(max_prefix, s.prefix_keys));
   const bool beside = int64_t(s.prefix_tiles) * s.prefix_splits * hkv >= cus / 2;
   s.rest_keys = prefix_split_keys(max_rest, int64_t(n_seqs) * hkv, cus, beside ? 2 : 8);
