@@ -76,18 +76,23 @@ inline int prefix_split_keys(int64_t keys, int64_t blocks, int cus, int per_cu) 
   return int(prefix_up(prefix_up(keys, splits), kPrefixKeys) * kPrefixKeys);
 }
 
+// Tiles: up to 128 columns a group on average go in narrow ones, which read the keys
+// again for every 32 (out of L2): 98 columns behind 8192 positions 17.7 us against 20.1
+// in a wide one; 168 behind 30000 53 against 37.
 // Wide tiles: two blocks a CU, whose products and exponentials overlap (128 rows of 32
 // heads behind 16384 positions 66 us, with one 77); one where the rows' own keys take
 // more than about a fourth as long to read, which then share the CUs from the start
-// (with up to 512 keys more 80 us against 84).  Narrow tiles: one block a CU.  More leave more states than the shorter ranges save:
-// 8 rows of 28 heads behind 8192 positions take 15.5 us with one, 21 with two; behind
-// 30000, 23.7 and 29.8.  What rows have to themselves: two blocks a CU beside the prefixes'
+// (with up to 512 keys more 80 us against 84).
+// Narrow tiles: one block a CU.  More leave more states than the shorter ranges save: 8
+// rows of 28 heads behind 8192 positions take 15.5 us with one, 21 with two; behind
+// 30000, 23.7 and 29.8.
+// What rows have to themselves: two blocks a CU beside the prefixes'
 // (20 rows in 5 groups behind 1501 positions 17.9 us against 20.6 with four), eight
 // alone (45 rows of up to 2000 keys 38.9 us against 43.2 with two).
 inline PrefixShape prefix_shape(int n_seqs, int n_groups, int max_prefix, int max_rest, int hq, int hkv, int cus) {
   const int64_t per_head = hq / hkv, rows = int64_t(n_seqs) * per_head;
   PrefixShape s{};
-  s.prefix_rows = max_prefix < 1 || rows <= 16 * int64_t(n_groups) ? 16 : rows <= 64 * int64_t(n_groups) ? 32 : 128;
+  s.prefix_rows = max_prefix < 1 || rows <= 16 * int64_t(n_groups) ? 16 : rows <= 128 * int64_t(n_groups) ? 32 : 128;
   s.prefix_tiles = max_prefix > 0 ? int(rows / s.prefix_rows + n_groups) : 0;
   const bool wide = s.prefix_rows == 128, long_rest = 240 * int64_t(max_rest) > per_head * max_prefix;
   s.prefix_keys = prefix_split_keys(max_prefix, prefix_up(rows, s.prefix_rows) * hkv, cus, wide && !long_rest ? 2 : 1);
