@@ -194,7 +194,7 @@ def lib() -> ctypes.CDLL:
             "hs_beam_select_workspace_size": [i32, i32, i32, i32, ctypes.POINTER(ctypes.c_size_t)],
             "hs_beam_select": [vp, vp, i32, i64, i32, i32, i32, vp, vp, i32, i32, vp, vp, vp, vp, i32, vp, vp,
                                ctypes.c_size_t],
-            "hs_cache_copy": [vp, ctypes.POINTER(KvCache), i32, i32, i32, vp, vp, vp, i32, i32, vp],
+            "hs_cache_copy": [vp, vp, i32, i32, i32, vp, vp, vp, i32, i32, vp],
             "hs_prefix_attention_workspace_size": [i32, i32, i32, i32, i32, i32, ctypes.POINTER(ctypes.c_size_t)],
             "hs_prefix_attention": [vp, vp, i32, i64, vp, i64, i32, i32, i32, vp, vp, i32, i32, vp, i32, vp, i32, vp,
                                     vp, i32, i32, i32, i32, vp, vp, ctypes.c_size_t],
@@ -823,12 +823,12 @@ def _cache_layers(ctx: Context, k, v, n_slots: int, max_ctx: int) -> Tuple[int, 
         raise ValueError(f"{len(k)} layers of keys, {len(v)} of values")
     if k[0].dim() != 4:
         _refuse(ctx, k[0], "k", _Kinds.f16, 4)
-    hkv, dh = k[0].shape[1], k[0].shape[3]
+    _, hkv, _, dh = k[0].shape
+    f16, device = _Kinds.f16, ctx.device
     for layers, name, shape in ((k, "k", (n_slots, hkv, max_ctx, dh)), (v, "v", (n_slots, hkv, max_ctx // 32, dh, 32))):
         for t in layers:
-            if (t.shape != shape or t.dtype not in _Kinds.f16 or t.get_device() != ctx.device
-                    or not t.is_contiguous()):
-                _dense(ctx, t, name, _Kinds.f16, *shape)   # the message of what does not fit
+            if t.shape != shape or t.dtype not in f16 or t.get_device() != device or not t.is_contiguous():
+                _dense(ctx, t, name, f16, *shape)   # the message of what does not fit
     return hkv, dh
 
 
@@ -848,7 +848,10 @@ def _host_ints(values, name: str):
     return a, a.buffer_info()[0]
 
 
-_PointerArray = ctypes.POINTER(ctypes.c_void_p)
+class _KvAddresses(ctypes.Structure):
+    """KvCache with plain addresses, which cost less to fill in."""
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("n_slots", ctypes.c_int32), ("max_ctx", ctypes.c_int32),
+                ("block_table", ctypes.c_void_p), ("pages_per_seq", ctypes.c_int32)]
 
 
 def hs_cache_copy(ctx: Context, kv, src, dst, positions=None, cu_budget: int = 256, stream=None) -> None:
@@ -862,8 +865,8 @@ def hs_cache_copy(ctx: Context, kv, src, dst, positions=None, cu_budget: int = 2
     if len(dst) != n or (positions is not None and len(positions) != n):
         raise ValueError(f"{n} sources, {len(dst)} destinations"
                          + ("" if positions is None else f", {len(positions)} numbers of positions"))
-    ks, vs = ((ctypes.c_void_p * len(t))(*[x.data_ptr() for x in t]) for t in (k, v))
-    arg = KvCache(ctypes.cast(ks, _PointerArray), ctypes.cast(vs, _PointerArray), n_slots, max_ctx, None, 0)
+    ks, vs = array.array("Q", [t.data_ptr() for t in k]), array.array("Q", [t.data_ptr() for t in v])
+    arg = _KvAddresses(ks.buffer_info()[0], vs.buffer_info()[0], n_slots, max_ctx, None, 0)
     (s, ps), (d, pd), (p, pp) = _host_ints(src, "src"), _host_ints(dst, "dst"), _host_ints(positions, "positions")
     status = lib().hs_cache_copy(ctx.handle, ctypes.byref(arg), len(k), hkv, dh, ps, pd, pp, n, cu_budget, _ptr(stream))
     if status:
@@ -886,31 +889,33 @@ def hs_prefix_attention(ctx: Context, q, out, k, v, block_table, lens, group_off
     all on the device (group_offsets and prefix_lens None: no prefixes)."""
     if not _Kinds.rows:
         _Kinds.fill()
-    pq, ldq, n, cols = _matrix(ctx, q, "q", _Kinds.halves)
-    po, ldo, *o_shape = _matrix(ctx, out, "out", {q.dtype: 0})
-    if o_shape != [n, cols]:
-        raise ValueError(f"out has shape {tuple(o_shape)}, q ({n}, {cols})")
-    if k.dim() != 4:
+    halves = _Kinds.halves
+    pq, ldq, n, cols = _matrix(ctx, q, "q", halves)
+    po, ldo, o_rows, o_cols = _matrix(ctx, out, "out", halves)
+    if out.dtype is not q.dtype or o_rows != n or o_cols != cols:
+        raise ValueError(f"out has type {out.dtype} and shape {tuple(out.shape)}, q {q.dtype} and {tuple(q.shape)}")
+    if len(k.shape) != 4:
         _refuse(ctx, k, "k", _Kinds.f16, 4)
     n_slots, hkv, page, dh = k.shape
-    _cache_layers(ctx, (k,), (v,), n_slots, page)
+    pk = _dense(ctx, k, "k", _Kinds.f16, n_slots, hkv, page, dh)
+    pv = _dense(ctx, v, "v", _Kinds.f16, n_slots, hkv, page // 32, dh, 32)
     if dh < 1 or cols % dh:
         raise ValueError(f"q has {cols} columns, the cache heads of {dh}")
-    if block_table.dim() != 2:
+    if len(block_table.shape) != 2:
         _refuse(ctx, block_table, "block_table", _Kinds.i32, 2)
     per_seq = block_table.shape[1]
-    if (group_offsets is None) != (prefix_lens is None):
-        raise ValueError("group_offsets and prefix_lens go together")
     groups = 0
-    if prefix_lens is not None:
-        if prefix_lens.dim() != 1:
+    if prefix_lens is not None and group_offsets is not None:
+        if len(prefix_lens.shape) != 1:
             _refuse(ctx, prefix_lens, "prefix_lens", _Kinds.i32, 1)
         groups = prefix_lens.shape[0]
+    elif prefix_lens is not group_offsets:
+        raise ValueError("group_offsets and prefix_lens go together")
     i32 = _Kinds.i32
     ws, ws_bytes = _workspace(ctx, workspace, ws_bytes)
     status = lib().hs_prefix_attention(
-        ctx.handle, pq, _Kinds.halves[q.dtype], ldq, po, ldo, cols // dh, hkv, dh, k.data_ptr(), v.data_ptr(), n_slots,
-        page, _dense(ctx, block_table, "block_table", i32, n, per_seq), per_seq, _dense(ctx, lens, "lens", i32, n), n,
+        ctx.handle, pq, halves[q.dtype], ldq, po, ldo, cols // dh, hkv, dh, pk, pv, n_slots, page,
+        _dense(ctx, block_table, "block_table", i32, n, per_seq), per_seq, _dense(ctx, lens, "lens", i32, n), n,
         _dense(ctx, group_offsets, "group_offsets", i32, groups + 1),
         _dense(ctx, prefix_lens, "prefix_lens", i32, groups), groups, min(max_prefix, _INT32_MAX),
         min(max_rest, _INT32_MAX), cu_budget, stream and _ptr(stream), ws, ws_bytes)
