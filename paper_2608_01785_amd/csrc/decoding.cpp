@@ -258,7 +258,8 @@ hs_status hs_prefix_attention(hs_context* ctx, const void* q, int32_t type, int6
       prefix_shape(n_seqs, n_groups, shared, max_rest, n_q_heads, n_kv_heads, std::min(cu_budget, kMaxCus));
   if (prefix_states_bytes(shape, n_seqs, n_q_heads, head_dim) > need)
     return fail(HS_ERR_INTERNAL, "the launch's partial states exceed the workspace");
-  if (prefix_blocks(shape, n_seqs, n_kv_heads) > kMaxBlocks)
+  if (prefix_blocks(shape, n_seqs, n_kv_heads) > kMaxBlocks ||
+      prefix_short_blocks(n_seqs, n_groups, n_q_heads, n_kv_heads) > kMaxBlocks)
     return fail(HS_ERR_UNSUPPORTED, "%d rows in %d groups need more blocks than a launch has", n_seqs, n_groups);
   PrefixArgs a{};
   a.q = q;

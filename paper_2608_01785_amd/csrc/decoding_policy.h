@@ -103,6 +103,18 @@ inline PrefixShape prefix_shape(int n_seqs, int n_groups, int max_prefix, int ma
   return s;
 }
 
+// Whether one block takes 16 columns over all that they look at: so many tiles of 32 keys
+// at most, for four wavefronts.
+constexpr int kPrefixShortTiles = 16;
+inline bool prefix_short(int n_seqs, int max_prefix, int max_rest, int hq, int hkv) {
+  const int64_t touched = prefix_up(16, hq / hkv) + 1, rows = touched < n_seqs ? touched : n_seqs;
+  return prefix_up(max_prefix, 32) + rows * (max_rest ? prefix_up(max_rest, 32) + 1 : 0) <= kPrefixShortTiles;
+}
+
+inline int64_t prefix_short_blocks(int n_seqs, int n_groups, int hq, int hkv) {
+  return (int64_t(n_seqs) * (hq / hkv) / 16 + (n_groups > 0 ? n_groups : 1)) * hkv;
+}
+
 // Blocks of a launch: of the prefixes, then of what rows have to themselves.
 inline int64_t prefix_blocks(const PrefixShape& s, int n_seqs, int hkv) {
   return (int64_t(s.prefix_tiles) * s.prefix_splits + int64_t(n_seqs) * s.rest_splits) * hkv;

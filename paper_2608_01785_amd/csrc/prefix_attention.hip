@@ -114,13 +114,107 @@ __device__ __forceinline__ float quarter_sum(float v) {
   return v + xor_lane<32>(v);
 }
 
+// A 32-key tile for one wavefront.
+struct Tile {
+  int slot, at;       // where its keys lie: slot (any value), position in it
+  int first, last;    // keys [first, last) of the tile count
+  int c_lo, c_hi;     // for these columns of the unit
+  bool there;
+};
+
+// The wavefront's tiles of the keys [k_lo, k_hi) of one sequence: every fourth one.  Entries
+// of the table are read a tile ahead, and none that no key needs.
+struct Range {
+  static constexpr bool kSomeColumns = false;
+  const int32_t* pages;
+  int page, kv0, k_lo, k_hi, left, no, at, slot;
+
+  __device__ __forceinline__ Range(const PrefixArgs& a, int owner, int lo, int hi, int wave) {
+    pages = a.table + int64_t(owner) * a.pages_per_seq;
+    page = a.page;
+    k_lo = lo;
+    k_hi = hi;
+    const int t0 = lo / kTileKeys, n = (hi + kTileKeys - 1) / kTileKeys - t0;
+    left = n > wave ? (n - wave + 3) / 4 : 0;
+    kv0 = (t0 + wave) * kTileKeys;
+    no = left > 0 ? first_lane(kv0 / page) : 0;
+    at = kv0 - no * page;
+    slot = left > 0 ? pages[no] : -1;
+  }
+  __device__ __forceinline__ Tile next() {
+    const Tile t{slot, at, k_lo - kv0, k_hi - kv0, 0, 0, left > 0};
+    --left;
+    kv0 += 4 * kTileKeys;
+    at += 4 * kTileKeys;
+    while (at >= page) {
+      at -= page;
+      ++no;
+    }
+    slot = left > 0 ? pages[no] : -1;
+    return t;
+  }
+};
+
+// The wavefront's tiles of everything that a unit's columns look at: the prefix of
+// their group, for all of them, and what each of their rows (at most 16) has to
+// itself, for the row's columns.
+struct Everything {
+  static constexpr bool kSomeColumns = true;
+  const PrefixArgs& a;
+  int lo, m0, n_cols, prefix, rows, row0;  // row0: the columns' first row, behind lo
+  int owner, pos, segment, tiles;          // segment 0: the prefix, then the rows
+  int end;                                 // lane r: where row r's keys end
+  int start, stop;                         // keys of the segment
+  Tile ahead;
+
+  __device__ __forceinline__ Everything(const PrefixArgs& args, int lo_, int m0_, int n, int prefix_, int reach, int wave)
+      : a(args), lo(lo_), m0(m0_), n_cols(n), prefix(min(prefix_, reach)) {
+    row0 = row_of(a, m0);
+    rows = row_of(a, m0 + n_cols - 1) - row0 + 1;
+    const int lane = threadIdx.x & 63;
+    const int len = a.lens[lo + row0 + min(lane, rows - 1)];
+    end = int(min(int64_t(len), min(int64_t(prefix_) + a.max_rest, int64_t(reach))));
+    segment = 0;
+    start = 0;
+    stop = prefix;
+    tiles = (stop + kTileKeys - 1) / kTileKeys;
+    pos = wave;
+    look();
+  }
+  // Finds the tile at `pos` and asks for its entry of the table.
+  __device__ __forceinline__ void look() {
+    while (pos >= tiles && segment <= rows) {
+      pos -= tiles;
+      if (++segment > rows) break;
+      start = prefix;
+      stop = __builtin_amdgcn_readlane(end, segment - 1);
+      tiles = stop > start ? (stop + kTileKeys - 1) / kTileKeys - start / kTileKeys : 0;
+    }
+    ahead = Tile{-1, 0, 0, 0, 0, 0, segment <= rows};
+    if (!ahead.there) return;
+    const int per_head = a.hq / a.hkv, row = lo + (segment ? row0 + segment - 1 : 0);
+    const int kv0 = (start / kTileKeys + pos) * kTileKeys, no = first_lane(kv0 / a.page);
+    ahead.at = kv0 - no * a.page;
+    ahead.slot = a.table[int64_t(row) * a.pages_per_seq + no];
+    ahead.first = start - kv0;
+    ahead.last = stop - kv0;
+    ahead.c_lo = segment ? (row0 + segment - 1) * per_head - m0 : 0;
+    ahead.c_hi = segment ? ahead.c_lo + per_head : n_cols;
+  }
+  __device__ __forceinline__ Tile next() {
+    const Tile t = ahead;
+    pos += 4;
+    look();
+    return t;
+  }
+};
+
 // Columns m0 .. m0 + n_cols - 1 of rows lo .. (column m: row lo + m / G, query head
-// head * G + m % G) over keys [k_lo, k_hi) of sequence `owner`'s pages, as partial
-// state `split`.
-template <int DH, int NQ, typename T>
-__device__ __forceinline__ void unit(const PrefixArgs& a, int lo, int m0, int n_cols, int head, int owner, int k_lo,
-                                     int k_hi, int split, int splits, Smem<DH, NQ>& sm) {
-  constexpr int TK = kTileKeys;
+// head * G + m % G) over the tiles of `steps`.  emit(q, d, sums, maximum, sum): column m0 + q's
+// unnormalised outputs d .. d + 3.
+template <int DH, int NQ, typename T, typename Steps, typename Emit>
+__device__ __forceinline__ void unit(const PrefixArgs& a, int lo, int m0, int n_cols, int head, Steps steps,
+                                     Smem<DH, NQ>& sm, Emit emit) {
   constexpr int NKB = DH / 32, NDS = DH / 16;
   constexpr int kTile = Smem<DH, NQ>::kTile, NL = kTile / 1024;
   const int tid = threadIdx.x, lane = tid & 63;
@@ -128,32 +222,16 @@ __device__ __forceinline__ void unit(const PrefixArgs& a, int lo, int m0, int n_
   const int fr = lane & 15, fh = lane >> 4;
   const int G = a.hq / a.hkv;
   const int64_t head_elems = int64_t(a.page) * DH, slot_elems = head_elems * a.hkv;
-  const int t0 = k_lo / TK, n_tiles = (k_hi + TK - 1) / TK - t0;
-  const int my_tiles = n_tiles > wave ? (n_tiles - wave + 3) / 4 : 0;
-  const int32_t* pages = a.table + int64_t(owner) * a.pages_per_seq;
-
-  // The wavefront's tiles lie 4 TK positions apart: the page of the next one to load, and
-  // its place in it.
-  bool bad = false;
-  int page_no = 0, page_at = 0;
-  if (my_tiles > 0) {
-    const int key = (t0 + wave) * TK;
-    page_no = first_lane(key / a.page);
-    page_at = key - page_no * a.page;
-  }
-  auto advance = [&](int& no, int& at) {
-    at += 4 * TK;
-    while (at >= a.page) {
-      at -= a.page;
-      ++no;
-    }
-  };
+  bool bad = false;  // of the lane's columns
   struct {
     u32x4 k[NL], v[NL];
   } tl;
-  auto base_of = [&](int slot, int at, uint32_t& bytes) {
-    bytes = slot >= 0 && slot < a.n_slots ? uint32_t(kTile) : 0u;
-    return bytes ? slot * slot_elems + head * head_elems + int64_t(at) * DH : int64_t(0);
+  // Tiles past the last one, and slots outside the cache, are read through an empty
+  // resource: zeros, no traffic.
+  auto base_of = [&](const Tile& t, uint32_t& bytes) {
+    const int slot = first_lane(t.slot);
+    bytes = t.there && slot >= 0 && slot < a.n_slots ? uint32_t(kTile) : 0u;
+    return bytes ? slot * slot_elems + head * head_elems + int64_t(t.at) * DH : int64_t(0);
   };
   auto load = [&](u32x4 (&d)[NL], const uint16_t* store, int64_t at, uint32_t bytes) {
     const uint64_t p = reinterpret_cast<uint64_t>(store + at);
@@ -215,24 +293,19 @@ __device__ __forceinline__ void unit(const PrefixArgs& a, int lo, int m0, int n_
     for (int i = 0; i < NDS; ++i) o[j][i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   }
 
-  if (my_tiles > 0) {
+  Tile tile = steps.next();
+  if (tile.there) {
     uint32_t bytes;
-    int64_t at = base_of(pages[page_no], page_at, bytes);
-    bad |= bytes == 0;
-    // Tiles past the last one are read through an empty resource: zeros, no traffic.
-    // Their entries of the table may not exist.
-    int slot = -1;
-    advance(page_no, page_at);
-    if (my_tiles > 1) slot = pages[page_no];
+    int64_t at = base_of(tile, bytes);
+    bool lost = bytes == 0;
     load(tl.k, a.k, at, bytes);
     load(tl.v, a.v, at, bytes);
-    for (int i = 0; i < my_tiles; ++i) {
-      const int kv0 = (t0 + wave + 4 * i) * TK;
-      at = base_of(slot, page_at, bytes);
-      bad |= i + 1 < my_tiles && bytes == 0;
-      slot = -1;
-      advance(page_no, page_at);
-      if (i + 2 < my_tiles) slot = pages[page_no];
+    while (tile.there) {
+      const Tile next = steps.next();
+      at = base_of(next, bytes);
+      const bool mine = !Steps::kSomeColumns || (fr >= tile.c_lo && fr < tile.c_hi);
+      bad |= lost && mine;
+      lost = bytes == 0;
       asm volatile("" ::: "memory");
 #pragma unroll
       for (int l = 0; l < NL; ++l) *reinterpret_cast<u32x4*>(ks + kw[l / kPer] + (l % kPer) * 1024) = tl.k[l];
@@ -253,8 +326,8 @@ __device__ __forceinline__ void unit(const PrefixArgs& a, int lo, int m0, int n_
         }
       // Score row i of subtile st is key 8 (i / 4) + 4 st + i % 4: the lane holds keys
       // 8 fh .. 8 fh + 7.
-      const bool edge = kv0 < k_lo || kv0 + TK > k_hi;
-      const int first = k_lo - kv0 - 8 * fh, last = k_hi - kv0 - 8 * fh;
+      const bool edge = tile.first > 0 || tile.last < kTileKeys;
+      const int first = tile.first - 8 * fh, last = tile.last - 8 * fh;
       u32x4 pf[NQ];
 #pragma unroll
       for (int j = 0; j < NQ; ++j) {
@@ -265,18 +338,26 @@ __device__ __forceinline__ void unit(const PrefixArgs& a, int lo, int m0, int n_
             for (int r = 0; r < 4; ++r)
               if (4 * st + r < first || 4 * st + r >= last) sc[j][st][r] = -kInf;
         }
-        // Every tile holds a key of the range, so the new maximum is finite.
+        if constexpr (Steps::kSomeColumns) {
+#pragma unroll
+          for (int st = 0; st < 2; ++st)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) sc[j][st][r] = mine ? sc[j][st][r] : -kInf;
+        }
+        // Every tile holds a key of the range: the new maximum is finite, where the tile
+        // is the column's.
         float mx = fmaxf(sc[j][0][0], sc[j][1][0]);
 #pragma unroll
         for (int r = 1; r < 4; ++r) mx = fmaxf(mx, fmaxf(sc[j][0][r], sc[j][1][r]));
         const float m_new = fmaxf(m_run[j], quarter_max(mx) * a.scale_log2);
-        const float alpha = exp2_raw(m_run[j] - m_new);
+        const float use = Steps::kSomeColumns && m_new == -kInf ? 0.0f : m_new;
+        const float alpha = exp2_raw(m_run[j] - use);
         float psum = 0.0f;
 #pragma unroll
         for (int st = 0; st < 2; ++st)
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
-            const float p = exp2_raw(fmaf(sc[j][st][r], a.scale_log2, -m_new));
+            const float p = exp2_raw(fmaf(sc[j][st][r], a.scale_log2, -use));
             sc[j][st][r] = p;
             psum += p;
           }
@@ -296,7 +377,7 @@ __device__ __forceinline__ void unit(const PrefixArgs& a, int lo, int m0, int n_
       asm volatile("" ::: "memory");
       if (edge) {
         // Values outside the range may be anything; 0 * NaN must not reach the sum.
-        const int vfirst = k_lo - kv0 - 8 * (lane & 3), vlast = k_hi - kv0 - 8 * (lane & 3);
+        const int vfirst = tile.first - 8 * (lane & 3), vlast = tile.last - 8 * (lane & 3);
         u32x4 keep;
 #pragma unroll
         for (int e = 0; e < 4; ++e)
@@ -314,9 +395,15 @@ __device__ __forceinline__ void unit(const PrefixArgs& a, int lo, int m0, int n_
       for (int d = 0; d < NDS; ++d) {
         const u32x4 vf = *reinterpret_cast<const u32x4*>(ks + vr + d * 1024);
 #pragma unroll
-        for (int j = 0; j < NQ; ++j) o[j][d] = mfma16(vf, pf[j], o[j][d]);
+        for (int j = 0; j < NQ; ++j) {
+          const f32x4 y = mfma16(vf, pf[j], o[j][d]);
+          // Another row's values may be NaN, which 0 does not take out.
+#pragma unroll
+          for (int r = 0; r < 4; ++r) o[j][d][r] = mine ? y[r] : o[j][d][r];
+        }
       }
       __builtin_amdgcn_sched_barrier(0);
+      tile = next;
     }
   }
 
@@ -329,7 +416,6 @@ __device__ __forceinline__ void unit(const PrefixArgs& a, int lo, int m0, int n_
       sm.red_l[wave][16 * j + fr] = bad ? __builtin_nanf("") : l_tot;
     }
   }
-  float* stats = part_stats(a, splits);
   constexpr int kPass = Smem<DH, NQ>::kPass;
   constexpr int kLanes = kPass / 4, kStep = 256 / kLanes;  // of a column; columns at a time
 #pragma unroll
@@ -361,12 +447,24 @@ __device__ __forceinline__ void unit(const PrefixArgs& a, int lo, int m0, int n_
 #pragma unroll
         for (int e = 0; e < 4; ++e) num[e] = fmaf(f, v[e], num[e]);
       }
-      const int i = row_of(a, m0 + q);
-      const int64_t p = part_index(a, split, lo + i, head * G + m0 + q - i * G);
-      *reinterpret_cast<f32x4*>(static_cast<float*>(a.part) + p * DH + pass * kPass + d) = num;
-      if (pass == 0 && d == 0) *reinterpret_cast<float2*>(stats + 2 * p) = make_float2(M, den);
+      emit(q, pass * kPass + d, num, M, den);
     }
   }
+}
+
+// The unit over a range of one sequence's keys, as partial state `split`.
+template <int DH, int NQ, typename T>
+__device__ __forceinline__ void range_unit(const PrefixArgs& a, int lo, int m0, int n_cols, int head, int owner, int k_lo,
+                                           int k_hi, int split, int splits, Smem<DH, NQ>& sm) {
+  float* stats = part_stats(a, splits);
+  const int G = a.hq / a.hkv;
+  unit<DH, NQ, T>(a, lo, m0, n_cols, head, Range(a, owner, k_lo, k_hi, first_lane(threadIdx.x >> 6)), sm,
+                  [&](int q, int d, const f32x4& num, float m, float sum) {
+                    const int i = row_of(a, m0 + q);
+                    const int64_t p = part_index(a, split, lo + i, head * G + m0 + q - i * G);
+                    *reinterpret_cast<f32x4*>(static_cast<float*>(a.part) + p * DH + d) = num;
+                    if (d == 0) *reinterpret_cast<float2*>(stats + 2 * p) = make_float2(m, sum);
+                  });
 }
 
 template <bool C, typename A, typename B>
@@ -614,7 +712,7 @@ __global__ __launch_bounds__(kThreads, 2) void prefix_kernel(PrefixArgs a, Prefi
     if constexpr (WIDE)
       wide_unit<DH, T>(a, g.lo, m0, n_cols, head, g.lo, k_lo, k_hi, split, splits, sm.prefix);
     else
-      unit<DH, NQ, T>(a, g.lo, m0, n_cols, head, g.lo, k_lo, k_hi, split, splits, sm.prefix);
+      range_unit<DH, NQ, T>(a, g.lo, m0, n_cols, head, g.lo, k_lo, k_hi, split, splits, sm.prefix);
   } else {
     id = (id - prefix_blocks) / a.hkv;
     const int split = id % s.rest_splits, row = id / s.rest_splits;
@@ -625,10 +723,52 @@ __global__ __launch_bounds__(kThreads, 2) void prefix_kernel(PrefixArgs a, Prefi
     if (k_hi <= k_lo) return;
     for (int m0 = 0; m0 < G; m0 += 16) {
       if (m0 > 0) __syncthreads();  // the last unit's states have been read
-      unit<DH, 1, T>(a, row, m0, min(G - m0, 16), head, row, int(k_lo), int(k_hi), s.prefix_splits + split, splits,
-                     sm.rest);
+      range_unit<DH, 1, T>(a, row, m0, min(G - m0, 16), head, row, int(k_lo), int(k_hi), s.prefix_splits + split,
+                           splits, sm.rest);
     }
   }
+}
+
+// Output d of (row, query head): fp16 as the products take it, or the type of q.
+template <int DH, typename T>
+__device__ __forceinline__ void write_out(const PrefixArgs& a, int row, int head, int e, float y) {
+  const int d = head * DH + e;
+  if (a.out_k8_rows) {
+    static_cast<uint16_t*>(a.out)[act_index(row, d, 0, a.out_k8_rows)] = f2h(y);
+  } else if constexpr (__is_same(T, uint16_t)) {
+    // bf16, to nearest even; NaN stays NaN.
+    const uint32_t b = __float_as_uint(y);
+    static_cast<uint16_t*>(a.out)[row * a.ldo + d] =
+        y != y ? uint16_t(0x7fc0) : uint16_t((b + 0x7fffu + ((b >> 16) & 1)) >> 16);
+  } else {
+    static_cast<_Float16*>(a.out)[row * a.ldo + d] = _Float16(y);
+  }
+}
+
+__device__ __forceinline__ bool wrong_lengths(const PrefixArgs& a, int prefix, int len) {
+  return prefix < 0 || prefix > a.max_prefix || len < prefix || len - prefix > a.max_rest ||
+         len > int64_t(a.pages_per_seq) * a.page;
+}
+
+// Short ranges in one launch: a block takes 16 columns of a group over everything that
+// they look at and writes their outputs.
+template <int DH, typename T>
+__global__ __launch_bounds__(kThreads, 2) void prefix_short_kernel(PrefixArgs a) {
+  __shared__ __attribute__((aligned(16))) Smem<DH, 1> sm;
+  const int G = a.hq / a.hkv, head = blockIdx.x % uint32_t(a.hkv), tile = blockIdx.x / uint32_t(a.hkv);
+  const Group g = a.n_groups ? group_of_tile<16>(a, tile) : Group{0, a.n_seqs, 0, tile};
+  const int m0 = g.tile * 16, n_cols = min((g.hi - g.lo) * G - m0, 16);
+  if (n_cols < 1) return;
+  const int prefix = clamped(g.prefix, 0, a.max_prefix);
+  const int reach = int(min(int64_t(a.pages_per_seq) * a.page, int64_t(1) << 30));
+  unit<DH, 1, T>(a, g.lo, m0, n_cols, head, Everything(a, g.lo, m0, n_cols, prefix, reach, first_lane(threadIdx.x >> 6)),
+                 sm, [&](int q, int d, const f32x4& num, float, float sum) {
+                   const int i = row_of(a, m0 + q), row = g.lo + i, len = a.lens[row];
+#pragma unroll
+                   for (int e = 0; e < 4; ++e)
+                     write_out<DH, T>(a, row, head * G + m0 + q - i * G, d + e,
+                                      wrong_lengths(a, g.prefix, len) ? __builtin_nanf("") : len == 0 ? 0.0f : num[e] / sum);
+                 });
 }
 
 // W wavefronts a (row, query head): each adds up every W-th of its partial states, all
@@ -645,8 +785,7 @@ __global__ __launch_bounds__(kThreads) void prefix_join_kernel(PrefixArgs a, Pre
   const bool mine = index < int64_t(a.n_seqs) * a.hq;
   const int row = mine ? int(index / a.hq) : 0, head = int(index % a.hq);
   const int len = a.lens[row], prefix = prefix_of_row(a, row);
-  const int64_t reach = int64_t(a.pages_per_seq) * a.page;
-  const bool wrong = prefix < 0 || prefix > a.max_prefix || len < prefix || len - prefix > a.max_rest || len > reach;
+  const bool wrong = wrong_lengths(a, prefix, len);
   const int splits = s.prefix_splits + s.rest_splits;
   const float* stats = part_stats(a, splits);
   const float* part = static_cast<const float*>(a.part);
@@ -704,24 +843,17 @@ __global__ __launch_bounds__(kThreads) void prefix_join_kernel(PrefixArgs a, Pre
   }
   if (!mine) return;
 #pragma unroll
-  for (int e = 0; e < V; ++e) {
-    const float y = wrong ? __builtin_nanf("") : n == 0 ? 0.0f : acc[e] / L;
-    const int d = head * DH + lane * V + e;
-    if (a.out_k8_rows) {
-      static_cast<uint16_t*>(a.out)[act_index(row, d, 0, a.out_k8_rows)] = f2h(y);
-    } else if constexpr (__is_same(T, uint16_t)) {
-      // bf16, to nearest even; NaN stays NaN.
-      const uint32_t b = __float_as_uint(y);
-      static_cast<uint16_t*>(a.out)[row * a.ldo + d] =
-          y != y ? uint16_t(0x7fc0) : uint16_t((b + 0x7fffu + ((b >> 16) & 1)) >> 16);
-    } else {
-      static_cast<_Float16*>(a.out)[row * a.ldo + d] = _Float16(y);
-    }
-  }
+  for (int e = 0; e < V; ++e)
+    write_out<DH, T>(a, row, head, lane * V + e, wrong ? __builtin_nanf("") : n == 0 ? 0.0f : acc[e] / L);
 }
 
 template <int DH, typename T>
 hipError_t launch(const PrefixArgs& a, int cus, hipStream_t st) {
+  if (prefix_short(a.n_seqs, a.max_prefix, a.max_rest, a.hq, a.hkv)) {
+    hipLaunchKernelGGL((prefix_short_kernel<DH, T>), dim3(uint32_t(prefix_short_blocks(a.n_seqs, a.n_groups, a.hq, a.hkv))),
+                       dim3(kThreads), 0, st, a);
+    return hipGetLastError();
+  }
   const PrefixShape s = prefix_shape(a.n_seqs, a.n_groups, a.max_prefix, a.max_rest, a.hq, a.hkv, cus);
   const int64_t blocks = prefix_blocks(s, a.n_seqs, a.hkv);
   if (blocks > 0) {

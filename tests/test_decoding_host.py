@@ -128,6 +128,8 @@ REFUSED = [
     (prefix, dict(page=32), INVALID, "multiple of 64"),
     (prefix, dict(pps=0), INVALID, "pages_per_seq"),
     (prefix, dict(g=-1), INVALID, "n_groups"),
+    (prefix, dict(g=1 << 25, mp=0, mr=3), UNSUPPORTED, "blocks"),
+    (prefix, dict(g=1 << 24), UNSUPPORTED, "blocks"),
     (prefix, dict(ldq=255), INVALID, "stride"),
     (prefix, dict(ldq=260), INVALID, "multiple of 8"),
     (prefix, dict(q=P + 8), INVALID, "aligned"),

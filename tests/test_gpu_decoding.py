@@ -429,9 +429,11 @@ def test_many_groups(env):
     s.call().check()
 
 
-def test_without_groups(env):
-    s = Prefix(env, [1] * 6, [0] * 6, [1, 0, 500, 64, 65, 3], HEADS["thinker"], 128, "f16", seed=5, grouped=False)
-    s.call().check()
+@pytest.mark.parametrize("heads", ["thinker", "talker", "many"])
+def test_without_groups(env, heads):
+    for rest in ([1, 0, 500, 64, 65, 3], [1, 0, 31, 20, 32, 3]):
+        s = Prefix(env, [1] * 6, [0] * 6, rest, HEADS[heads], 128, "f16", seed=5, grouped=False)
+        s.call().check()
 
 
 def test_sharp_scores(env):
@@ -440,15 +442,21 @@ def test_sharp_scores(env):
         Prefix(env, [4], [900], [3, 100, 0, 64], HEADS["thinker"], 64, "f16", seed=6, scale=scale).call().check()
 
 
-def test_wrong_lengths_and_slots_make_their_rows_nan(env):
+# Groups whose ranges go through one block each, and longer ones that are split and joined.
+SHORT = dict(rows=[3, 4], prefix=[40, 65], rest=[5, 30, 1, 9, 20, 3, 24], heads=HEADS["thinker"])
+LONG = dict(rows=[3, 4], prefix=[100, 200], rest=[5, 70, 1, 9, 80, 3, 64], heads=HEADS["tiny"])
+
+
+@pytest.mark.parametrize("case", [SHORT, LONG], ids=["short", "long"])
+def test_wrong_lengths_and_slots_make_their_rows_nan(env, case):
     torch = env[0]
-    s = Prefix(env, [3, 4], [100, 200], [5, 70, 1, 9, 80, 3, 64], HEADS["tiny"], 64, "f16", seed=7, poison=False)
+    s = Prefix(env, page=64, dtype="f16", seed=7, poison=False, **case)
     clean = s.call().check()
-    table, lens = s.table.copy(), list(s.lens)
-    s.table[1, 1] = s.k.shape[0]                # beyond the cache: row 1's own keys from 100 on
-    s.table[4, 3] = -5
-    s.lens[2] = 99                              # shorter than its prefix
-    s.lens[5] = 200 + s.max_rest + 1            # beyond the bound
+    table, lens, prefix = s.table.copy(), list(s.lens), list(s.prefix)
+    s.table[1, (prefix[0] + case["rest"][1] - 1) // 64] = s.k.shape[0]   # beyond the cache: keys of row 1 alone
+    s.table[4, (lens[4] - 1) // 64] = -5
+    s.lens[2] = prefix[0] - 1                   # shorter than its prefix
+    s.lens[5] = prefix[1] + s.max_rest + 1      # beyond the bound
     s.lens[6] = 64 * s.table.shape[1] + 1       # beyond the table (and the bound)
     s.upload()
     s.call()
@@ -460,23 +468,54 @@ def test_wrong_lengths_and_slots_make_their_rows_nan(env):
         else:
             assert (got[i] == clean[i].reshape(-1)).all(), i
     s.table, s.lens = table, lens
-    s.prefix = [101, -1]                        # beyond its bound, negative
-    s.max_prefix = 100
+    s.table[0, 0] = 10 ** 6                     # under a prefix: the whole group
+    s.upload()
+    s.call()
+    torch.cuda.synchronize()
+    got = s.out.double().cpu().numpy()
+    assert np.isnan(got[:3]).all() and (got[3:] == clean[3:].reshape(4, -1)).all()
+    s.table = table
+    s.prefix = [max(prefix) + 1, -1]            # beyond its bound, negative
+    s.max_prefix = max(prefix)
     s.upload()
     s.call()
     torch.cuda.synchronize()
     assert torch.all(torch.isnan(s.out))
 
 
+@pytest.mark.parametrize("case", [SHORT, LONG], ids=["short", "long"])
+def test_nan_and_infinity_stay_with_their_rows(env, case):
+    """In the keys or values of one row, in its query: the rows beside it in the same products keep their bits."""
+    torch = env[0]
+    s = Prefix(env, page=64, dtype="f16", seed=13, poison=False, **case)
+    clean = s.call().check()
+    page, at = s.table[4, (s.lens[4] - 1) // 64], (s.lens[4] - 1) % 64
+    s.v[page, :, at // 32, :, at % 32] = float("nan")
+    page, at = s.table[1, (s.lens[1] - 1) // 64], (s.lens[1] - 1) % 64
+    s.k[page, :, at, 3] = math.inf
+    s.v[page, :, at // 32, :, at % 32] = math.inf
+    s.q[5] = float("nan")
+    torch.cuda.synchronize()
+    s.call()
+    torch.cuda.synchronize()
+    got = s.out.double().cpu().numpy()
+    for i in range(7):
+        if i in (4, 5):
+            assert np.isnan(got[i]).all()
+        elif i != 1:
+            assert (got[i] == clean[i].reshape(-1)).all(), i
+
+
 def test_offsets_that_make_no_sense_touch_nothing(env):
     torch = env[0]
-    s = Prefix(env, [3, 4], [100, 200], [5, 70, 1, 9, 80, 3, 64], HEADS["tiny"], 64, "f16", seed=8, poison=False)
-    for offsets in ([5, 2, 900], [-7, 100, 3], [0, 0, 0], [2 ** 31 - 1, -2 ** 31, 5]):
-        s.offsets = offsets
-        s.upload()
-        s.call()
-        torch.cuda.synchronize()
-        assert torch.all(s.store[:, 256:] == 7.0)
+    for case in (SHORT, LONG):
+        s = Prefix(env, page=64, dtype="f16", seed=8, poison=False, **case)
+        for offsets in ([5, 2, 900], [-7, 100, 3], [0, 0, 0], [2 ** 31 - 1, -2 ** 31, 5]):
+            s.offsets = offsets
+            s.upload()
+            s.call()
+            torch.cuda.synchronize()
+            assert torch.all(s.store[:, s.out.shape[1]:] == 7.0)
 
 
 def test_offsets_beyond_32_bits(env):
