@@ -6,10 +6,14 @@
 // Two launches.  The scan of hs_logprobs (logits_scan.h) reads every row once and
 // leaves, for each block of it, the sums behind the logarithm and the keys of its
 // `select` best logits: no continuation outside a row's `select` best can be among
-// the group's.  The join, a block per group, takes the logarithm of each beam's sum,
-// merges the beam's sorted lists to one, and ranks the beams' candidates against
-// each other.  The scan's read of the logits bounds the call; ended and empty beams
+// the group's.  The join, a block per group, takes the logarithm of each beam's sum and
+// ranks the beams' candidates against each other: up to 256 as the splits left them,
+// more after each beam's sorted lists have been merged to one.  Ended and empty beams
 // are not read.
+//
+// The read of the logits bounds a large call (512 rows of 131072 bf16: 27.5 us for the scan,
+// 4.9 TB/s, and 5.2 for the join), the chain of each kernel a small one (4 rows of 32000
+// fp32: 4.9 and 3.6; with merged lists the join took 6.2).
 //
 // Values are held in 64 bits from the sums of a row on: continuations of two beams
 // that lie closer than the 2^-20 that fp32 resolves at -10 are common among the many
