@@ -632,7 +632,8 @@ hs_status hs_downstream_decode_step_prefix(hs_context* ctx, const hs_layer_cfg* 
 typedef struct hs_pages hs_pages;
 
 /* n_pages pages of page_positions positions (a positive multiple of 64), all
- * free; every sequence is empty. */
+ * free; every sequence is empty.  At most 2^28 pages, 2^24 sequences and 2^30
+ * positions of a sequence. */
 hs_status hs_pages_create(int32_t n_pages, int32_t page_positions, int32_t max_seqs, int32_t pages_per_seq,
                           hs_pages** out);
 hs_status hs_pages_destroy(hs_pages* pages);

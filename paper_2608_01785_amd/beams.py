@@ -85,14 +85,15 @@ class BeamSearch:
         return list(range(g * self.beams, (g + 1) * self.beams))
 
     def start(self, x, offsets) -> None:
-        """x: bf16 [T, hidden] prompt rows on the device; offsets: host [groups + 1], no prompt empty.  Ends the
-        search before and selects every group's first tokens."""
+        """x: bf16 [T, hidden] prompt rows on the device, as torch's current stream leaves them; offsets: host
+        [groups + 1], no prompt empty.  Ends the search before and selects every group's first tokens."""
         groups = len(offsets) - 1
         lengths = [int(b) - int(a) for a, b in zip(offsets, offsets[1:])]
         if not 1 <= groups <= self.max_groups or min(lengths) < 1 or max(lengths) > self.max_prompt:
             raise ValueError(f"prompts of {lengths} positions: 1 to {self.max_groups} of 1 to {self.max_prompt}")
         if x.shape != (int(offsets[-1]), self.shape.hidden) or int(offsets[0]) != 0:
             raise ValueError(f"x has shape {tuple(x.shape)}, the offsets end at {int(offsets[-1])}")
+        self.torch_stream.wait_stream(torch.cuda.current_stream(x.device))
         self.pages.release(list(range(self.max_groups * self.beams)))
         self.groups, self.steps, self.at = groups, 0, 0
         firsts = [g * self.beams for g in range(groups)]

@@ -39,6 +39,8 @@ struct hs_pages {
 
 namespace {
 
+constexpr int32_t kMaxPages = 1 << 28, kMaxSequences = 1 << 24;
+
 hs_status check_seqs(const hs_pages* p, const int32_t* seqs, int32_t n, bool distinct) {
   if (!p) return fail(HS_ERR_INVALID_ARG, "pages is null");
   if (n < 0 || (n > 0 && !seqs)) return fail(HS_ERR_INVALID_ARG, "%d sequences, or their list is null", n);
@@ -80,6 +82,9 @@ hs_status hs_pages_create(int32_t n_pages, int32_t page_positions, int32_t max_s
       return fail(HS_ERR_INVALID_ARG, "%d pages, %d sequences of %d", n_pages, max_seqs, pages_per_seq);
     if (page_positions < 64 || page_positions % 64 != 0)
       return fail(HS_ERR_INVALID_ARG, "page size %d must be a positive multiple of 64", page_positions);
+    if (n_pages > kMaxPages || max_seqs > kMaxSequences)
+      return fail(HS_ERR_UNSUPPORTED, "%d pages, %d sequences: at most %d and %d", n_pages, max_seqs, kMaxPages,
+                  kMaxSequences);
     if (int64_t(pages_per_seq) * page_positions > (int64_t(1) << 30))
       return fail(HS_ERR_UNSUPPORTED, "%lld positions a sequence", (long long)pages_per_seq * page_positions);
     auto* p = new hs_pages();

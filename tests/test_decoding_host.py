@@ -319,6 +319,9 @@ def test_pages_refusals(b):
     for bad in ((0, 64, 1, 1), (4, 96, 1, 1), (4, 64, 0, 1), (4, 64, 1, 0), (4, 0, 1, 1)):
         with pytest.raises(b.HorizonError):
             b.Pages(*bad)
+    for bad in (((1 << 28) + 1, 64, 1, 1), (4, 64, (1 << 24) + 1, 1)):
+        with pytest.raises(b.HorizonError, match="at most"):
+            b.Pages(*bad)
     with pytest.raises(b.HorizonError, match="positions a sequence"):
         b.Pages(4, 1 << 20, 1, 1 << 20)
     p = b.Pages(4, 64, 2, 3)

@@ -289,6 +289,24 @@ def test_beams_that_end(env):
     assert all(beam.tokens.count(end) <= 1 for g in results for beam in g)
 
 
+def test_prompts_still_being_written(env):
+    """Rows that torch's stream has yet to write when the search starts."""
+    torch, b, ctx = env
+    s = Search(env, 3, 1, 100, 60, 3, seed=93)
+    x, offsets = s.prompts([60])
+    s.search.start(x, offsets)
+    first = s.search.results()
+    late = torch.zeros_like(x)
+    big = torch.randn((4096, 4096), device="cuda")
+    torch.cuda.synchronize()
+    for _ in range(20):
+        big = torch.matmul(big, big).clamp(-1, 1)
+    late.copy_(x + big[:1, :1].mul(0).to(x.dtype))
+    s.search.start(late, offsets)
+    again = s.search.results()
+    assert [(q.tokens, q.score) for q in first[0]] == [(q.tokens, q.score) for q in again[0]]
+
+
 def test_search_refusals(env):
     torch, b, ctx = env
     s = Search(env, 2, 2, 50, 20, 3)
