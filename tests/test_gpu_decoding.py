@@ -429,6 +429,44 @@ def test_many_groups(env):
     s.call().check()
 
 
+def test_many_short_groups(env):
+    rng = np.random.default_rng(5)
+    rows = rng.integers(0, 5, 150).tolist()
+    prefix = rng.integers(0, 65, 150).tolist()
+    s = Prefix(env, rows, prefix, rng.integers(0, 30, sum(rows)).tolist(), HEADS["thinker"], 64, "bf16", seed=6)
+    s.call().check()
+
+
+@pytest.mark.parametrize("seed", range(24))
+def test_drawn_attention(env, seed):
+    """Groups, lengths, pages, heads, types and strides drawn together."""
+    rng = np.random.default_rng(1000 + seed)
+    heads = HEADS[sorted(HEADS)[rng.integers(len(HEADS))]]
+    groups = int(rng.integers(1, 7))
+    rows = rng.integers(0, 8, groups).tolist()
+    rows[rng.integers(groups)] += 1
+    reach = int(rng.choice((20, 100, 700, 3000)))
+    prefix = rng.integers(0, reach + 1, groups).tolist()
+    rest = rng.integers(0, int(rng.choice((1, 2, 40, 300))), sum(rows)).tolist()
+    page, dtype = 64 * int(rng.integers(1, 9)), str(rng.choice(("f16", "bf16")))
+    log(f"[prefix] drawn {seed}: {heads} rows {rows} prefix {prefix} rest {rest[:6]} page {page} {dtype}")
+    Prefix(env, rows, prefix, rest, heads, page, dtype, pad=int(rng.choice((0, 8, 40))), seed=seed,
+           scale=float(rng.choice((0.3, 1.0, 4.0)))).call(int(rng.choice((64, 128, 256)))).check()
+
+
+@pytest.mark.parametrize("seed", range(24))
+def test_drawn_selection(env, seed):
+    rng = np.random.default_rng(2000 + seed)
+    beams, groups = int(rng.integers(1, 13)), int(rng.integers(1, 12))
+    vocab = int(np.exp(rng.uniform(np.log(2), np.log(60000))))
+    select, dtype = int(rng.integers(1, min(64, 3 * beams) + 1)), str(rng.choice(("f32", "f16", "bf16")))
+    end = int(rng.integers(0, vocab)) if rng.random() < 0.6 else -1
+    log(f"[beam] drawn {seed}: {groups} x {beams}, {vocab}, {select}, {dtype}, end {end}")
+    s = Beams(env, groups, beams, vocab, select, dtype, pad=int(rng.integers(0, 9)), first=int(rng.integers(0, 5)),
+              seed=seed, end=end, finished=end >= 0 and rng.random() < 0.6, masked=float(rng.choice((0.0, 0.0, 0.7, 0.999))))
+    s.call(int(rng.choice((64, 128, 256)))).check()
+
+
 @pytest.mark.parametrize("heads", ["thinker", "talker", "many"])
 def test_without_groups(env, heads):
     for rest in ([1, 0, 500, 64, 65, 3], [1, 0, 31, 20, 32, 3]):
