@@ -123,21 +123,28 @@ hs_status hs_pages_reserve(hs_pages* p, const int32_t* seqs, const int32_t* add,
     // the last of its users that write to it a page, and that one too while others
     // still list it.
     int64_t need = 0;
-    std::vector<int32_t> left(p->users);
-    for (int32_t i = 0; i < n; ++i) {
-      const hs_pages::Sequence& s = p->seqs[seqs[i]];
-      if (add[i] < 0) return fail(HS_ERR_INVALID_ARG, "add[%d] = %d", i, add[i]);
-      const int64_t len = int64_t(s.len) + add[i];
-      if (len > int64_t(p->per_seq) * p->positions)
-        return fail(HS_ERR_INVALID_ARG, "sequence %d would hold %lld positions, beyond its %d pages of %d", seqs[i],
-                    (long long)len, p->per_seq, p->positions);
-      if (add[i] == 0) continue;
-      need += pages_for(p, len) - int32_t(s.pages.size());
-      if (s.len % p->positions != 0 && left[s.pages.back()] > 1) {
-        --left[s.pages.back()];
-        ++need;
+    std::vector<int32_t> left;  // pages that a sequence of the call would leave
+    left.reserve(size_t(n));
+    st = [&] {
+      for (int32_t i = 0; i < n; ++i) {
+        const hs_pages::Sequence& s = p->seqs[seqs[i]];
+        if (add[i] < 0) return fail(HS_ERR_INVALID_ARG, "add[%d] = %d", i, add[i]);
+        const int64_t len = int64_t(s.len) + add[i];
+        if (len > int64_t(p->per_seq) * p->positions)
+          return fail(HS_ERR_INVALID_ARG, "sequence %d would hold %lld positions, beyond its %d pages of %d", seqs[i],
+                      (long long)len, p->per_seq, p->positions);
+        if (add[i] == 0) continue;
+        need += pages_for(p, len) - int32_t(s.pages.size());
+        if (s.len % p->positions != 0 && p->users[s.pages.back()] > 1) {
+          --p->users[s.pages.back()];
+          left.push_back(s.pages.back());
+          ++need;
+        }
       }
-    }
+      return HS_OK;
+    }();
+    for (int32_t page : left) ++p->users[page];  // as it was
+    if (st != HS_OK) return st;
     if (need > int64_t(p->free.size()))
       return fail(HS_ERR_WORKSPACE, "%lld pages needed, %zu are free", (long long)need, p->free.size());
     for (int32_t i = 0; i < n; ++i) p->seqs[seqs[i]].pages.reserve(size_t(p->per_seq));
