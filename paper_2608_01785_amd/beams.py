@@ -75,7 +75,7 @@ class BeamSearch:
         self.select_ws = new(max(binding.hs_beam_select_workspace_size(max_groups, beams, head.vocab, beams),
                                  binding.hs_beam_select_workspace_size(max_groups, 1, head.vocab, beams)),
                              dtype=torch.uint8)
-        self.groups = 0
+        self.groups, self.ready = 0, False  # ready: the pages hold what the history says, and no more
         torch.cuda.synchronize(device)
 
     def _kv(self, table):
@@ -94,8 +94,9 @@ class BeamSearch:
         if x.shape != (int(offsets[-1]), self.shape.hidden) or int(offsets[0]) != 0:
             raise ValueError(f"x has shape {tuple(x.shape)}, the offsets end at {int(offsets[-1])}")
         self.torch_stream.wait_stream(torch.cuda.current_stream(x.device))
+        self.groups, self.ready = 0, False
         self.pages.release(list(range(self.max_groups * self.beams)))
-        self.groups, self.steps, self.at = groups, 0, 0
+        self.steps, self.at = 0, 0
         firsts = [g * self.beams for g in range(groups)]
         self.pages.reserve(firsts, lengths)
         table, _ = self.pages.table(firsts)
@@ -111,16 +112,21 @@ class BeamSearch:
         # Every beam starts from its prompt.
         for g in range(groups):
             self.pages.fork(self._seqs(g), [g * self.beams] * self.beams)
+        self.groups, self.ready = groups, True
 
     def step(self) -> bool:
-        """One more token for every beam; False once all of them have ended, or max_new tokens are there."""
-        if self.groups == 0:
-            raise ValueError("no search has been started")
+        """One more token for every beam; False once all of them have ended, or max_new tokens are there.
+
+        A step that runs out of pages changes nothing; after any other failure the results stay and the
+        search cannot go on."""
+        if not self.ready:
+            raise ValueError("no search has been started, or its last step failed")
         if self.steps >= self.max_new or bool(self.host[2][:self.groups].all()):
             return False
         n = self.groups * self.beams
         seqs = list(range(n))
         copies = self.pages.reserve(seqs, [1] * n)
+        self.ready = False
         if copies[0]:
             binding.hs_cache_copy(self.ctx, self.cache.as_arg(), *copies, cu_budget=self.cu_budget, stream=self.stream)
         table, lens = self.pages.table(seqs)
@@ -138,11 +144,12 @@ class BeamSearch:
         for g in range(self.groups):
             first = g * self.beams
             self.pages.fork(self._seqs(g), [first + max(int(p), 0) for p in parents[g]])
+        self.ready = True
         return True
 
     def _select(self, z, scores, finished) -> np.ndarray:
         """The best continuations into the other buffers; their parents, and everything else, on the host too."""
-        g, to = self.groups, 1 - self.at
+        g, to = scores.shape[0], 1 - self.at
         binding.hs_beam_select(
             self.ctx, z, scores, self.scores[to][:g], self.parents[:g], self.tokens[:g],
             finished=finished if self.end_token >= 0 else None, out_finished=self.finished[to][:g],

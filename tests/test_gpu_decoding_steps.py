@@ -325,3 +325,53 @@ def test_search_refusals(env):
         a.update(kw)
         with pytest.raises(ValueError, match=text):
             BeamSearch(ctx, s.shape, s.w, s.head, None, **a)
+
+
+def test_search_after_a_failure(env):
+    """A step that failed after it had reserved its positions is not gone on from; a new start works as before."""
+    torch, b, ctx = env
+    s = Search(env, 3, 2, 60, 40, 4, seed=94)
+    x, offsets = s.prompts([40, 17])
+    s.search.start(x, offsets)
+    s.search.step()
+    before = s.search.results()
+    embed = s.search.embed
+
+    def failing(tokens, out):
+        raise RuntimeError("no rows")
+    s.search.embed = failing
+    with pytest.raises(RuntimeError, match="no rows"):
+        s.search.step()
+    s.search.embed = embed
+    with pytest.raises(ValueError, match="failed"):
+        s.search.step()
+    assert s.search.results() == before
+    s.search.start(x, offsets)
+    s.search.step()
+    assert s.search.results() == before
+    s.check(x, offsets)
+
+    # A start that fails leaves no search.
+    product = s.search.head.product
+    s.search.head.product = lambda *a: failing(None, None)
+    with pytest.raises(RuntimeError, match="no rows"):
+        s.search.start(x, offsets)
+    s.search.head.product = product
+    assert s.search.results() == []
+    with pytest.raises(ValueError, match="started"):
+        s.search.step()
+
+
+def test_search_without_pages(env):
+    """A step for which the cache has too few pages changes nothing."""
+    torch, b, ctx = env
+    from paper_2608_01785_amd.beams import BeamSearch
+    s = Search(env, 2, 1, 60, 64, 4, seed=95)
+    search = BeamSearch(ctx, s.shape, s.w, s.head.sharing(), s.search.embed, 2, 1, 64, 4, n_pages=2)
+    x, offsets = s.prompts([64])
+    search.start(x, offsets)      # the prompt's page; each beam's next token needs one of its own
+    before = search.results()
+    for _ in range(2):
+        with pytest.raises(b.HorizonError, match="pages"):
+            search.step()
+    assert search.results() == before and search.pages.free_count() == 1
