@@ -582,7 +582,8 @@ hs_status hs_prefix_attention_workspace_size(int32_t n_q_heads, int32_t n_kv_hea
  *   max_prefix, max_rest  bounds of prefix_lens and of lens - prefix, which size the
  *                  launches (close bounds are fast ones).
  * n_groups 0: no row has a prefix.  head_dim 64 or 128, at most 64 query heads per
- * key/value head.  A row without keys gives 0.
+ * key/value head.  A row without keys gives 0.  A key whose score is -inf has weight
+ * 0; a row that has no other keys gives NaN.
  * A row with prefix or lens - prefix negative or beyond its bound, or with keys
  * beyond the table, gives NaN, and so does one that needs a slot outside
  * [0, n_slots); entries that no key needs are not read.  Other group_offsets than

@@ -43,6 +43,10 @@ constexpr float kInf = __builtin_inff();
 __device__ __forceinline__ int clamped(int v, int lo, int hi) { return min(max(v, lo), hi); }
 __device__ __forceinline__ int first_lane(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
+// What exponents are taken against under the maximum m: 0 where only scores of -inf
+// have been seen, whose weights are 0 then.
+__device__ __forceinline__ float against(float m) { return m == -kInf ? 0.0f : m; }
+
 // m / per_head, by the product with its rounded-up inverse.
 __device__ __forceinline__ int row_of(const PrefixArgs& a, int m) {
   return int(__umulhi(2u * uint32_t(m), a.per_head_inv));
@@ -351,13 +355,11 @@ __device__ __forceinline__ void unit(const PrefixArgs& a, int lo, int m0, int n_
 #pragma unroll
             for (int r = 0; r < 4; ++r) sc[j][st][r] = mine ? sc[j][st][r] : -kInf;
         }
-        // Every tile holds a key of the range: the new maximum is finite, where the tile
-        // is the column's.
         float mx = fmaxf(sc[j][0][0], sc[j][1][0]);
 #pragma unroll
         for (int r = 1; r < 4; ++r) mx = fmaxf(mx, fmaxf(sc[j][0][r], sc[j][1][r]));
         const float m_new = fmaxf(m_run[j], quarter_max(mx) * a.scale_log2);
-        const float use = Steps::kSomeColumns && m_new == -kInf ? 0.0f : m_new;
+        const float use = against(m_new);
         const float alpha = exp2_raw(m_run[j] - use);
         float psum = 0.0f;
 #pragma unroll
@@ -444,11 +446,12 @@ __device__ __forceinline__ void unit(const PrefixArgs& a, int lo, int m0, int n_
         m[w] = sm.red_m[w][q];
         M = fmaxf(M, m[w]);
       }
+      const float use = against(M);
       f32x4 num = {0.0f, 0.0f, 0.0f, 0.0f};
       float den = 0.0f;
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
-        const float f = exp2_raw(m[w] - M);
+        const float f = exp2_raw(m[w] - use);
         const f32x4 v = *reinterpret_cast<const f32x4*>(&sm.red_o[w][q][d]);
         den = fmaf(f, sm.red_l[w][q], den);
 #pragma unroll
@@ -815,12 +818,12 @@ __global__ __launch_bounds__(kThreads) void prefix_join_kernel(PrefixArgs a, Pre
     float top = M;
 #pragma unroll
     for (int j = 0; j < kJoinBatch; ++j) top = fmaxf(top, i0 + j * W < n ? m[j] : -kInf);
-    const float old = exp2_raw(M - top);
+    const float use = against(top), old = exp2_raw(M - use);
     L *= old;
     acc *= old;
 #pragma unroll
     for (int j = 0; j < kJoinBatch; ++j) {
-      const float w = i0 + j * W < n ? exp2_raw(m[j] - top) : 0.0f;
+      const float w = i0 + j * W < n ? exp2_raw(m[j] - use) : 0.0f;
       if (i0 + j * W < n) {
         L = fmaf(w, l[j], L);
         acc += w * v[j];
@@ -839,10 +842,11 @@ __global__ __launch_bounds__(kThreads) void prefix_join_kernel(PrefixArgs a, Pre
     if (member != 0) return;
     float top = -kInf;
     for (int w = 0; w < min(W, n); ++w) top = fmaxf(top, sums[wave + w][DH]);
+    const float use = against(top);
     acc = 0.0f;
     L = 0.0f;
     for (int w = 0; w < min(W, n); ++w) {
-      const float f = exp2_raw(sums[wave + w][DH] - top);
+      const float f = exp2_raw(sums[wave + w][DH] - use);
       L = fmaf(f, sums[wave + w][DH + 1], L);
 #pragma unroll
       for (int e = 0; e < V; ++e) acc[e] = fmaf(f, sums[wave + w][lane * V + e], acc[e]);
