@@ -141,3 +141,44 @@ def test_many_splits_at_minus_infinity(env):
             put(s, 0, *hidden, -math.inf)
             run(s)
             check_without(s, list(range(rows)))
+
+
+def test_wrong_lengths_and_slots(case):
+    s = case
+    clean = run(s)
+    prefix, table, lens = list(s.prefix), s.table.copy(), list(s.lens)
+    s.table[1, (s.lens[1] - 1) // 64] = s.k.shape[0]   # beyond the cache: keys of row 1 alone
+    s.table[4, (s.lens[4] - 1) // 64] = -5
+    s.lens[2] = prefix[0] - 1                   # shorter than its prefix
+    s.lens[5] = prefix[1] + s.max_rest + 1      # beyond the bound
+    s.lens[6] = 64 * s.table.shape[1] + 1       # beyond the table (and the bound)
+    s.upload()
+    got = run(s)
+    for i in range(7):
+        assert np.isnan(got[i]).all() if i in (1, 2, 4, 5, 6) else (got[i] == clean[i]).all(), i
+    # A page inside a prefix, and the one that it ends in: all rows of the group.
+    for group, page in ((0, prefix[0] // 128), (1, (prefix[1] - 1) // 64)):
+        s.table, s.lens = table.copy(), list(lens)
+        s.table[s.offsets[group], page] = 10 ** 6
+        s.upload()
+        got = run(s)
+        mine = np.arange(s.offsets[group], s.offsets[group + 1])
+        rest = np.setdiff1d(np.arange(7), mine)
+        assert np.isnan(got[mine]).all() and (got[rest] == clean[rest]).all(), group
+    s.table = table
+    s.prefix = [max(prefix) + 1, -1]            # beyond its bound, negative
+    s.upload()
+    assert np.isnan(run(s)).all()
+
+
+def test_nan_stays_with_its_rows(case):
+    """In one row's own keys, values and query, the rows beside it in the same products keep their bits."""
+    s = case
+    clean = run(s)
+    slots, at = keys_of(s, 4, s.lens[4] - 1, s.lens[4])
+    s.v[slots, :, at // 32, :, at % 32] = math.nan
+    put(s, 1, s.lens[1] - 1, s.lens[1], math.nan)
+    s.q[5] = math.nan
+    got = run(s)
+    for i in range(7):
+        assert np.isnan(got[i]).all() if i in (1, 4, 5) else (got[i] == clean[i]).all(), i
