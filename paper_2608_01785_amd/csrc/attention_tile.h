@@ -69,7 +69,7 @@ __device__ __forceinline__ void softmax_tile(f32x16 (&s)[2], f32x16 (&o)[NDS], u
   // against 0, which gives weight 0.
   const bool move = mx > m_run + kLazyMax;
   const float m_new = move ? mx : m_run;
-  const float m_use = m_new == -INFINITY ? 0.0f : m_new;
+  const float m_use = against(m_new);
   const float alpha = exp2_raw(m_run - m_use);
   m_run = m_new;
   float psum = 0.0f;

@@ -221,19 +221,19 @@ __device__ __forceinline__ void decode_attn_unit(const DecodeAttnArgs& a, int it
           if (4 * st + r >= left) sc[st][r] = -INFINITY;
     }
     // The maximum is taken on the raw scores (the scale is positive) and the
-    // scale folded into the exponent's FMA.  Every tile holds at least one
-    // valid key, so m_new is finite.
+    // scale folded into the exponent's FMA.
     float mx = fmaxf(sc[0][0], sc[1][0]);
 #pragma unroll
     for (int r = 1; r < 4; ++r) mx = fmaxf(mx, fmaxf(sc[0][r], sc[1][r]));
     const float m_new = fmaxf(m_run, quarter_max(mx) * a.scale_log2);
-    const float alpha = exp2_raw(m_run - m_new);  // 0 on the first tile
+    const float use = against(m_new);
+    const float alpha = exp2_raw(m_run - use);  // 0 on the first tile
     float psum = 0.0f;
 #pragma unroll
     for (int st = 0; st < 2; ++st)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        const float p = exp2_raw(fmaf(sc[st][r], a.scale_log2, -m_new));
+        const float p = exp2_raw(fmaf(sc[st][r], a.scale_log2, -use));
         sc[st][r] = p;
         psum += p;
       }
@@ -280,10 +280,11 @@ __device__ __forceinline__ void decode_attn_unit(const DecodeAttnArgs& a, int it
     float M = -INFINITY;
 #pragma unroll
     for (int w = 0; w < 4; ++w) M = fmaxf(M, red_m[w][q]);
+    const float use = against(M);
     float num = 0.0f, den = 0.0f;
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
-      const float sc = exp2f(red_m[w][q] - M);
+      const float sc = exp2f(red_m[w][q] - use);
       num += sc * red_o[w][d][q];
       den += sc * red_l[w][q];
     }
@@ -331,13 +332,14 @@ __device__ __forceinline__ void decode_attn_unit(const DecodeAttnArgs& a, int it
 #pragma unroll
       for (int k = 0; k < 8; ++k)
         if (sp0 + k < n_split) bm = fmaxf(bm, mv[k]);
-      const float rescale = exp2f(M - bm);  // M = -inf on the first batch: 0
+      const float use = against(bm);
+      const float rescale = exp2f(M - use);  // M = -inf on the first batch: 0
       num *= rescale;
       den *= rescale;
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
         if (sp0 + k < n_split) {
-          const float sc = exp2f(mv[k] - bm);
+          const float sc = exp2f(mv[k] - use);
           num += sc * ov[k];
           den += sc * lv[k];
         }

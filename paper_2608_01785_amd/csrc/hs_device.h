@@ -58,6 +58,10 @@ __device__ __forceinline__ uint32_t pack2h(float lo, float hi) {
 // normal range flush to zero, which softmax weights can afford).
 __device__ __forceinline__ float exp2_raw(float x) { return __builtin_amdgcn_exp2f(x); }
 
+// What a softmax's exponents are taken against under the maximum m: 0 where only
+// scores of -inf have been seen, whose weights are 0 then.
+__device__ __forceinline__ float against(float m) { return m == -INFINITY ? 0.0f : m; }
+
 // Two bf16 values (one 32-bit word) -> two fp16 values.  Exact for
 // magnitudes in [2^-14, 65504]; smaller values become fp16 subnormals
 // (absolute error below 2^-24).  Round-toward-zero conversion is used because

@@ -43,10 +43,6 @@ constexpr float kInf = __builtin_inff();
 __device__ __forceinline__ int clamped(int v, int lo, int hi) { return min(max(v, lo), hi); }
 __device__ __forceinline__ int first_lane(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
-// What exponents are taken against under the maximum m: 0 where only scores of -inf
-// have been seen, whose weights are 0 then.
-__device__ __forceinline__ float against(float m) { return m == -kInf ? 0.0f : m; }
-
 // m / per_head, by the product with its rounded-up inverse.
 __device__ __forceinline__ int row_of(const PrefixArgs& a, int m) {
   return int(__umulhi(2u * uint32_t(m), a.per_head_inv));
