@@ -8,8 +8,8 @@ then each beam takes the pages of its parent.  The selection and the decoding ru
 the device, the pages' bookkeeping on the host, which reads the selection back
 once a step.
 
-A beam that has ended, or stands for no continuation, stays in the batch; it proposes
-its own score, or nothing.
+A beam that has ended, or stands for no continuation, stays in the batch while any other
+goes on; it proposes its own score, or nothing, and takes a position a step like the others.
 """
 from __future__ import annotations
 
@@ -115,13 +115,14 @@ class BeamSearch:
         self.groups, self.ready = groups, True
 
     def step(self) -> bool:
-        """One more token for every beam; False once all of them have ended, or max_new tokens are there.
+        """One more token for every beam; False once each of them has ended or stands for no continuation, or
+        max_new tokens are there.
 
         A step that runs out of pages changes nothing; after any other failure the results stay and the
         search cannot go on."""
         if not self.ready:
             raise ValueError("no search has been started, or its last step failed")
-        if self.steps >= self.max_new or bool(self.host[2][:self.groups].all()):
+        if self.steps >= self.max_new or not self._goes_on():
             return False
         n = self.groups * self.beams
         seqs = list(range(n))
@@ -146,6 +147,11 @@ class BeamSearch:
             self.pages.fork(self._seqs(g), [first + max(int(p), 0) for p in parents[g]])
         self.ready = True
         return True
+
+    def _goes_on(self) -> bool:
+        """Whether any beam of the last selection proposes something new."""
+        parents, _, finished = (h[:self.groups] for h in self.host)
+        return bool(((parents >= 0) & (finished == 0)).any())
 
     def _select(self, z, scores, finished) -> np.ndarray:
         """The best continuations into the other buffers; their parents, and everything else, on the host too."""

@@ -1,0 +1,88 @@
+"""Beam searches with groups that have fewer continuations than beams, or none."""
+import math
+
+import pytest
+
+from tests.gpu_common import log, require_gpu
+from tests.test_gpu_decoding_steps import Search
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def env():
+    torch = require_gpu()
+    from paper_2608_01785_amd import binding
+    ctx = binding.Context(0, budgets=(128, 256))
+    yield torch, binding, ctx
+    torch.cuda.synchronize()
+    ctx.close()
+
+
+def with_tokens(s, tokens, end, beams, groups, max_new):
+    """A search as `s`, whose head gives every other token no probability."""
+    from paper_2608_01785_amd.answer import AnswerHead
+    from paper_2608_01785_amd.beams import BeamSearch
+    torch, head = s.torch, s.head
+    bias = torch.full((head.vocab,), -math.inf, dtype=torch.bfloat16, device="cuda")
+    bias[tokens] = 0
+    only = AnswerHead(s.ctx, head.gain, (head.w, head.w_scale), bias, max_rows=head.max_rows)
+    return BeamSearch(s.ctx, s.shape, s.w, only, s.search.embed, beams, groups, 50, max_new, end)
+
+
+def steps_of(search):
+    steps = 1
+    while search.step():
+        steps += 1
+    return steps
+
+
+def test_search_ends_where_nothing_goes_on(env):
+    """One group whose only token ends it, one of rows that have no distribution."""
+    torch, b, ctx = env
+    log("[beam search] an ended group and one of NaN")
+    s = Search(env, 3, 2, 40, 50, 6, seed=96)
+    x, offsets = s.prompts([30, 20])
+    search = with_tokens(s, [7], 7, 3, 2, 6)
+    search.start(x, offsets)
+    assert steps_of(search) == 1
+    bad = x.clone()
+    bad[offsets[1]:] = math.nan
+    torch.cuda.synchronize()
+    search.start(bad, offsets)
+    assert steps_of(search) == 1
+    first, second = search.results()
+    assert first[0].tokens == [7] and first[0].finished and first[0].score == 0
+    for beam in first[1:] + second:
+        assert beam.tokens == [] and beam.score == -math.inf and not beam.finished
+
+
+def test_search_goes_on_beside_a_group_without_continuations(env):
+    """The other group's beams are those that it finds alone."""
+    torch, b, ctx = env
+    log("[beam search] a group of NaN beside another")
+    s = Search(env, 3, 2, 40, 50, 6, seed=97)
+    x, offsets = s.prompts([30, 20])
+    bad = x.clone()
+    bad[offsets[1]:] = math.nan
+    torch.cuda.synchronize()
+    s.search.start(bad, offsets)
+    assert steps_of(s.search) == 6
+    results = s.search.results()
+    assert all(beam.tokens == [] and beam.score == -math.inf for beam in results[1])
+    s.search.start(x, offsets)
+    assert steps_of(s.search) == 6
+    assert s.search.results()[0] == results[0]
+
+
+def test_search_of_fewer_continuations_than_beams(env):
+    """Two tokens, one of which ends: after t steps there are t ended sequences and one that goes on."""
+    torch, b, ctx = env
+    log("[beam search] two tokens, five beams")
+    s = Search(env, 5, 1, 40, 50, 4, seed=98)
+    x, offsets = s.prompts([25])
+    search = with_tokens(s, [3, 9], 9, 5, 1, 4)
+    search.start(x, offsets)
+    assert steps_of(search) == 4
+    got = sorted(tuple(beam.tokens) for beam in search.results()[0])
+    assert got == sorted([(9,), (3, 9), (3, 3, 9), (3, 3, 3, 9), (3, 3, 3, 3)])
