@@ -65,9 +65,14 @@ class BeamSearch:
         self.y = new(max(rows, max_groups * max_prompt), shape.hidden)
         self.last = new(max_groups, shape.hidden)
         self.scores = [new(max_groups, beams) for _ in range(2)]
-        self.finished = [new(max_groups, beams, dtype=torch.uint8) for _ in range(2)]
-        self.parents, self.tokens = (new(max_groups, beams, dtype=torch.int32) for _ in range(2))
-        self.host = [new(max_groups, beams, dtype=t, pinned=True) for t in (torch.int32, torch.int32, torch.uint8)]
+        # What a selection leaves, and where the host reads it: parents, tokens, and finished flags of two steps.
+        self.left, self.left_host = (new(10 * rows, dtype=torch.uint8, pinned=p) for p in (False, True))
+
+        def parts(left):
+            ints = left[:8 * rows].view(torch.int32).view(2, max_groups, beams)
+            return ints[0], ints[1], list(left[8 * rows:].view(2, max_groups, beams))
+        self.parents, self.tokens, self.finished = parts(self.left)
+        self.host = parts(self.left_host)
         self.zero = torch.zeros((max_groups, 1), device=device)
         self.ws = new(max(binding.hs_workspace_size_paged(shape, max_groups * max_prompt, max_groups, self.max_pos, page),
                           binding.hs_workspace_size_prefix(shape, rows, self.max_pos, page, self.max_pos, self.max_pos)),
@@ -150,8 +155,8 @@ class BeamSearch:
 
     def _goes_on(self) -> bool:
         """Whether any beam of the last selection proposes something new."""
-        parents, _, finished = (h[:self.groups] for h in self.host)
-        return bool(((parents >= 0) & (finished == 0)).any())
+        parents, _, finished = self.host
+        return bool(((parents[:self.groups] >= 0) & (finished[self.at][:self.groups] == 0)).any())
 
     def _select(self, z, scores, finished) -> np.ndarray:
         """The best continuations into the other buffers; their parents, and everything else, on the host too."""
@@ -160,11 +165,11 @@ class BeamSearch:
             self.ctx, z, scores, self.scores[to][:g], self.parents[:g], self.tokens[:g],
             finished=finished if self.end_token >= 0 else None, out_finished=self.finished[to][:g],
             end_token=self.end_token, cu_budget=self.cu_budget, stream=self.stream, workspace=self.select_ws)
+        # A copy that is waited for: torch remembers the stream of any other until the pinned memory is given back,
+        # and by then the context may have closed it.
         with torch.cuda.stream(self.torch_stream):
-            for host, device in zip(self.host, (self.parents, self.tokens, self.finished[to])):
-                host[:g].copy_(device[:g], non_blocking=True)
-        self.torch_stream.synchronize()
-        parents, tokens, _ = (h[:g].numpy() for h in self.host)
+            self.left_host.copy_(self.left)
+        parents, tokens = (h[:g].numpy() for h in self.host[:2])
         self.history = [[self._continued(i, int(parents[i, j]), int(tokens[i, j])) for j in range(self.beams)]
                         for i in range(g)]
         self.at, self.steps = to, self.steps + 1
@@ -181,6 +186,6 @@ class BeamSearch:
         """Every group's beams, best first."""
         self.torch_stream.synchronize()
         scores = self.scores[self.at][:self.groups].cpu().numpy()
-        finished = self.host[2][:self.groups].numpy()
+        finished = self.host[2][self.at][:self.groups].numpy()
         return [[Beam(self.history[g][j], float(scores[g, j]), bool(finished[g, j])) for j in range(self.beams)]
                 for g in range(self.groups)]

@@ -18,8 +18,10 @@ def search(parents, finished, max_new=9, steps=1):
     s = object.__new__(BeamSearch)
     s.beams, s.max_new, s.steps, s.ready, s.groups = len(parents[0]), max_new, steps, True, len(parents)
     # One group more than there are: what an earlier search left.
-    s.host = [torch.tensor(x + [[0] * s.beams], dtype=t) for x, t in (
-        (parents, torch.int32), (parents, torch.int32), (finished, torch.uint8))]
+    s.at = 0
+    parents, finished = (torch.tensor(x + [[0] * s.beams], dtype=t) for x, t in (
+        (parents, torch.int32), (finished, torch.uint8)))
+    s.host = parents, parents, [finished, 1 - finished]
     s.pages = Untouched()
     return s
 

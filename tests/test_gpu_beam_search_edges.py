@@ -86,3 +86,31 @@ def test_search_of_fewer_continuations_than_beams(env):
     assert steps_of(search) == 4
     got = sorted(tuple(beam.tokens) for beam in search.results()[0])
     assert got == sorted([(9,), (3, 9), (3, 3, 9), (3, 3, 3, 9), (3, 3, 3, 3)])
+
+
+@pytest.mark.parametrize("closed", [True, False])
+def test_a_search_given_back_after_its_context(env, closed):
+    """Its buffers, pinned ones among them, outlive the context's streams: closed before, or held by nothing else."""
+    import gc
+    torch, b, _ = env
+    ctx = b.Context(0, budgets=(128,))
+    log(f"[beam search] given back after its context, closed {closed}")
+    s = Search((torch, b, ctx), 3, 1, 40, 50, 3, seed=99)
+    x, offsets = s.prompts([25])
+    s.search.start(x, offsets)
+    assert steps_of(s.search) == 3
+    want = s.search.results()
+    torch.cuda.synchronize()
+    if closed:
+        ctx.close()
+    del ctx, s, x
+    gc.collect()
+    for _ in range(3):
+        pinned = torch.full((64,), 5.0).pin_memory()
+        assert float(pinned.cuda().sum()) == 320.0
+    torch.cuda.synchronize()
+    again = Search(env, 3, 1, 40, 50, 3, seed=99)
+    x, offsets = again.prompts([25])
+    again.search.start(x, offsets)
+    assert steps_of(again.search) == 3
+    assert again.search.results() == want
