@@ -98,6 +98,9 @@ class BeamSearch:
             raise ValueError(f"prompts of {lengths} positions: 1 to {self.max_groups} of 1 to {self.max_prompt}")
         if x.shape != (int(offsets[-1]), self.shape.hidden) or int(offsets[0]) != 0:
             raise ValueError(f"x has shape {tuple(x.shape)}, the offsets end at {int(offsets[-1])}")
+        if x.dtype != torch.bfloat16 or x.device != self.x.device or not x.is_contiguous():
+            raise ValueError(f"x is {x.dtype} on {x.device} with strides {x.stride()}: contiguous bfloat16 rows on "
+                             f"{self.x.device} expected")
         self.torch_stream.wait_stream(torch.cuda.current_stream(x.device))
         self.groups, self.ready = 0, False
         self.pages.release(list(range(self.max_groups * self.beams)))

@@ -1,4 +1,6 @@
 """Beam search without a GPU: when a step has nothing to do, and what a start refuses before it touches anything."""
+from types import SimpleNamespace
+
 import pytest
 
 torch = pytest.importorskip("torch")
@@ -43,3 +45,19 @@ def test_a_step_with_something_to_continue(parents, finished):
     with pytest.raises(AssertionError, match="reserve was reached"):
         search(parents, finished).step()
     assert search(parents, finished, max_new=1).step() is False   # but no token left
+
+
+@pytest.mark.parametrize("x,text", [
+    (torch.zeros((5, 8)), "float32"), (torch.zeros((5, 8), dtype=torch.float16), "float16"),
+    (torch.zeros((5, 8), dtype=torch.int8), "int8"), (torch.zeros((5, 8), dtype=torch.bfloat16, device="meta"), "meta"),
+    (torch.zeros((8, 5), dtype=torch.bfloat16).t(), "contiguous"),
+    (torch.zeros((10, 8), dtype=torch.bfloat16)[::2], "contiguous"),
+])
+def test_a_start_refuses_rows_of_another_kind(x, text):
+    s = search([[0]], [[0]])
+    s.max_groups, s.max_prompt, s.shape = 2, 5, SimpleNamespace(hidden=8)
+    s.x, s.torch_stream = torch.zeros((2, 8), dtype=torch.bfloat16), Untouched()
+    for offsets in ([0, 5], [0, 2, 5]):
+        with pytest.raises(ValueError, match=text):
+            s.start(x, offsets)
+    assert s.ready and s.groups == 1   # the search before goes on
