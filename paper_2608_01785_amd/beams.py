@@ -81,6 +81,7 @@ class BeamSearch:
                                  binding.hs_beam_select_workspace_size(max_groups, 1, head.vocab, beams)),
                              dtype=torch.uint8)
         self.groups, self.ready = 0, False  # ready: the pages hold what the history says, and no more
+        self.steps, self.at, self.history = 0, 0, []
         torch.cuda.synchronize(device)
 
     def _kv(self, table):
@@ -186,7 +187,7 @@ class BeamSearch:
         return before if ended else before + [token]
 
     def results(self) -> List[List[Beam]]:
-        """Every group's beams, best first."""
+        """Every group's beams, best first; no groups before a start and after one that failed."""
         self.torch_stream.synchronize()
         scores = self.scores[self.at][:self.groups].cpu().numpy()
         finished = self.host[2][self.at][:self.groups].numpy()

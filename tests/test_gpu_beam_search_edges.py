@@ -114,3 +114,11 @@ def test_a_search_given_back_after_its_context(env, closed):
     again.search.start(x, offsets)
     assert steps_of(again.search) == 3
     assert again.search.results() == want
+
+
+def test_results_before_a_start(env):
+    s = Search(env, 2, 2, 50, 20, 3)
+    assert s.search.results() == []
+    x, offsets = s.prompts([20, 5])
+    s.search.start(x, offsets)
+    assert [len(g) for g in s.search.results()] == [2, 2]
