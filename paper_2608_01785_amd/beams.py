@@ -191,5 +191,5 @@ class BeamSearch:
         self.torch_stream.synchronize()
         scores = self.scores[self.at][:self.groups].cpu().numpy()
         finished = self.host[2][self.at][:self.groups].numpy()
-        return [[Beam(self.history[g][j], float(scores[g, j]), bool(finished[g, j])) for j in range(self.beams)]
+        return [[Beam(list(self.history[g][j]), float(scores[g, j]), bool(finished[g, j])) for j in range(self.beams)]
                 for g in range(self.groups)]

@@ -122,3 +122,18 @@ def test_results_before_a_start(env):
     x, offsets = s.prompts([20, 5])
     s.search.start(x, offsets)
     assert [len(g) for g in s.search.results()] == [2, 2]
+
+
+def test_results_are_the_callers(env):
+    """What is done to them leaves the search as it is."""
+    s = Search(env, 3, 1, 40, 50, 5, seed=100)
+    x, offsets = s.prompts([25])
+    s.search.start(x, offsets)
+    assert steps_of(s.search) == 5
+    want = s.search.results()
+    s.search.start(x, offsets)
+    for _ in range(4):
+        for beam in s.search.results()[0]:
+            beam.tokens.append(-5)
+        assert s.search.step()
+    assert s.search.results() == want
