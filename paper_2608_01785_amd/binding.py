@@ -236,10 +236,20 @@ def hs_last_error() -> str:
     return lib().hs_last_error().decode()
 
 
+def _as_i32(values, name: str = "a list") -> np.ndarray:
+    """Host integers as a contiguous array of 32-bit words; others are refused, not cut to their lower bits."""
+    if isinstance(values, (list, tuple)):
+        return np.asarray(values, dtype=np.int32)   # (numpy refuses what does not fit)
+    a = np.asarray(values)
+    if a.dtype != np.int32 and a.size and (a.dtype.kind not in "iub" or a.min() < -2 ** 31 or a.max() > _INT32_MAX):
+        raise ValueError(f"{name} holds no 32-bit numbers")
+    return np.ascontiguousarray(a, dtype=np.int32)
+
+
 def _i32_array(values) -> Optional[ctypes.Array]:
     if values is None:
         return None
-    a = np.ascontiguousarray(np.asarray(values, dtype=np.int32))
+    a = _as_i32(values)
     return (ctypes.c_int32 * len(a))(*a.tolist())
 
 
@@ -442,7 +452,7 @@ def _kv_struct(kv) -> Optional[KvCache]:
     vp = (ctypes.c_void_p * len(v_list))(*[_ptr(t) for t in v_list])
     tp, pps = None, 0
     if table is not None:
-        table = np.ascontiguousarray(table, dtype=np.int32)
+        table = np.ascontiguousarray(_as_i32(table, "the block table"))
         assert table.ndim == 2
         pps = table.shape[1]
         tp = table.ctypes.data_as(ctypes.POINTER(ctypes.c_int32))
@@ -527,8 +537,8 @@ def hs_downstream_decode_step_noalloc(ctx: Context, cfg, weights, x_in, x_out, k
 def hs_workspace_size_prefix(cfg, batch: int, max_pos: int, page_positions: int, max_prefix: int,
                              max_rest: int) -> int:
     n = ctypes.c_size_t(0)
-    _check(lib().hs_workspace_size_prefix(ctypes.byref(LayerCfg.of(cfg)), batch, max_pos, page_positions, max_prefix,
-                                          max_rest, ctypes.byref(n)))
+    args = (min(v, _INT32_MAX) for v in (batch, max_pos, page_positions, max_prefix, max_rest))
+    _check(lib().hs_workspace_size_prefix(ctypes.byref(LayerCfg.of(cfg)), *args, ctypes.byref(n)))
     return int(n.value)
 
 
@@ -808,7 +818,7 @@ def hs_beam_select(ctx: Context, logits, scores, out_scores, out_parents, out_to
     status = lib().hs_beam_select(
         ctx.handle, pz, _Kinds.rows[logits.dtype], ld, groups, beams, vocab,
         _dense(ctx, scores, "scores", f32, groups, beams), _dense(ctx, finished, "finished", u8, groups, beams),
-        end_token, select, _dense(ctx, out_scores, "out_scores", f32, groups, select),
+        max(-2, min(end_token, _INT32_MAX)), select, _dense(ctx, out_scores, "out_scores", f32, groups, select),
         _dense(ctx, out_parents, "out_parents", i32, groups, select),
         _dense(ctx, out_tokens, "out_tokens", i32, groups, select),
         _dense(ctx, out_finished, "out_finished", u8, groups, select), cu_budget, stream and _ptr(stream), ws, ws_bytes)
@@ -837,9 +847,9 @@ def _host_ints(values, name: str):
     if values is None:
         return None, None
     if isinstance(values, np.ndarray):
-        if values.ndim != 1 or (values.size and (values.min() < -2 ** 31 or values.max() > _INT32_MAX)):
+        if values.ndim != 1:
             raise ValueError(f"{name} holds no list of 32-bit numbers")
-        a = np.ascontiguousarray(values, dtype=np.int32)
+        a = _as_i32(values, name)
         return a, a.ctypes.data
     try:
         a = array.array("i", values)
@@ -931,9 +941,10 @@ class Pages:
     def __init__(self, n_pages: int, page_positions: int, max_seqs: int, pages_per_seq: int):
         self.handle = None
         h = ctypes.c_void_p()
-        _check(lib().hs_pages_create(n_pages, page_positions, max_seqs, pages_per_seq, ctypes.byref(h)))
+        args = (min(v, _INT32_MAX) for v in (n_pages, page_positions, max_seqs, pages_per_seq))
+        _check(lib().hs_pages_create(*args, ctypes.byref(h)))
         self.handle = h
-        self.pages_per_seq = pages_per_seq
+        self.n_pages, self.pages_per_seq = n_pages, pages_per_seq
 
     def _copies(self, room: int, call) -> Tuple[List[int], List[int], List[int]]:
         lists = [(ctypes.c_int32 * max(room, 1))() for _ in range(3)]
@@ -956,6 +967,7 @@ class Pages:
         self.fork(seqs, [-1] * len(seqs))
 
     def compact(self, room: int):
+        room = min(room, self.n_pages)   # no more can move
         return self._copies(room, lambda *out: lib().hs_pages_compact(self.handle, room, *out))
 
     def table(self, seqs) -> Tuple[np.ndarray, np.ndarray]:

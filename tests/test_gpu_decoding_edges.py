@@ -182,3 +182,13 @@ def test_nan_stays_with_its_rows(case):
     got = run(s)
     for i in range(7):
         assert np.isnan(got[i]).all() if i in (1, 4, 5) else (got[i] == clean[i]).all(), i
+
+
+def test_an_end_token_beyond_32_bits_is_refused(env):
+    from tests.test_gpu_decoding import Beams
+    torch, b, ctx = env
+    for end in (2 ** 32 + 5, 5 - 2 ** 32):
+        s = Beams(env, 2, 3, 100, 4, end=5)
+        s.end = end
+        with pytest.raises(b.HorizonError, match="end_token"):
+            s.call()
