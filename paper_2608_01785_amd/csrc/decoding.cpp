@@ -18,8 +18,6 @@ constexpr int32_t kBeamMaxRows = 1 << 22;      // a block of 256 threads each, 6
 constexpr int64_t kMaxSlotBytes = int64_t(1) << 33;
 constexpr int32_t kMaxSlots = 1 << 28;  // a cache's bytes stay below 2^62
 constexpr int32_t kMaxKvHeads = 1024;
-constexpr int32_t kMaxCus = 256;        // of a device: no launch is sized for more
-constexpr int64_t kMaxBlocks = (int64_t(1) << 24) - 1;  // of 256 threads: fewer than 2^32 in a grid
 
 hs_status check_workspace(const void* workspace, size_t ws_bytes, size_t need) {
   if (!need) return HS_OK;
@@ -254,13 +252,7 @@ hs_status hs_prefix_attention(hs_context* ctx, const void* q, int32_t type, int6
   if (n_seqs) HS_TRY(check_workspace(workspace, ws_bytes, need));
   if (cu_budget < 1) return fail(HS_ERR_BUDGET, "CU budget %d", cu_budget);  // sizes the launch below
   const int32_t shared = n_groups ? max_prefix : 0;
-  const PrefixShape shape =
-      prefix_shape(n_seqs, n_groups, shared, max_rest, n_q_heads, n_kv_heads, std::min(cu_budget, kMaxCus));
-  if (prefix_states_bytes(shape, n_seqs, n_q_heads, head_dim) > need)
-    return fail(HS_ERR_INTERNAL, "the launch's partial states exceed the workspace");
-  if (prefix_blocks(shape, n_seqs, n_kv_heads) > kMaxBlocks ||
-      prefix_short_blocks(n_seqs, n_groups, n_q_heads, n_kv_heads) > kMaxBlocks)
-    return fail(HS_ERR_UNSUPPORTED, "%d rows in %d groups need more blocks than a launch has", n_seqs, n_groups);
+  HS_TRY(check_prefix_launch(n_seqs, n_groups, shared, max_rest, n_q_heads, n_kv_heads, head_dim, cu_budget, need));
   PrefixArgs a{};
   a.q = q;
   a.type = type;

@@ -9,6 +9,9 @@
 
 namespace hs {
 
+constexpr int kMaxCus = 256;  // of a device: no launch is sized for more
+constexpr int64_t kMaxBlocks = (int64_t(1) << 24) - 1;  // of 256 threads: fewer than 2^32 in a grid
+
 // hs_beam_select: beams of a group and selected continuations at most; the join
 // holds beams * select candidates in LDS (48 KB at most) and its lists of keys
 // cover a wavefront.

@@ -449,6 +449,19 @@ hs_status check_prefix_groups(const hs_kv_cache& kv, const int32_t* kv_lens, int
   return HS_OK;
 }
 
+hs_status check_prefix_launch(int32_t n_seqs, int32_t n_groups, int32_t max_prefix, int32_t max_rest, int32_t hq,
+                              int32_t hkv, int32_t dh, int32_t cus, size_t room) {
+  const PrefixShape s = prefix_shape(n_seqs, n_groups, max_prefix, max_rest, hq, hkv, std::clamp(cus, 1, kMaxCus));
+  if (prefix_states_bytes(s, n_seqs, hq, dh) > room)
+    return fail(HS_ERR_INTERNAL, "the launch's partial states exceed the workspace");
+  const int64_t blocks = prefix_short(n_seqs, max_prefix, max_rest, hq, hkv)
+                             ? prefix_short_blocks(n_seqs, n_groups, hq, hkv)
+                             : prefix_blocks(s, n_seqs, hkv);
+  if (blocks > kMaxBlocks)
+    return fail(HS_ERR_UNSUPPORTED, "%d rows in %d groups need more blocks than a launch has", n_seqs, n_groups);
+  return HS_OK;
+}
+
 hs_status prefix_layout(const hs_layer_cfg& c, int32_t batch, int32_t max_pos, int32_t page_keys, int32_t max_prefix,
                         int32_t max_rest, WsLayout* lay, PrefixPlan* out) {
   if (int64_t(max_prefix) + max_rest > (int64_t(1) << 30) || int64_t(batch) * c.n_q_heads > (int64_t(1) << 25))

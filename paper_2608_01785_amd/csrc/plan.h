@@ -146,6 +146,11 @@ struct PrefixPlan {
 hs_status check_prefix_groups(const hs_kv_cache& kv, const int32_t* kv_lens, int32_t batch, const PrefixGroups& groups,
                               int32_t* max_prefix, int32_t* max_rest);
 
+// That the attention's launch has no more blocks than a grid, and no more partial states
+// than `room` bytes hold.
+hs_status check_prefix_launch(int32_t n_seqs, int32_t n_groups, int32_t max_prefix, int32_t max_rest, int32_t hq,
+                              int32_t hkv, int32_t dh, int32_t cus, size_t room);
+
 // Extends the layout of a plain call of `batch` rows on a paged cache: the metadata
 // moves behind it, with room for the groups' arrays, and the partial states follow.
 hs_status prefix_layout(const hs_layer_cfg& c, int32_t batch, int32_t max_pos, int32_t page_keys, int32_t max_prefix,

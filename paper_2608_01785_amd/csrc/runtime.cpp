@@ -574,6 +574,12 @@ hs_status run_stack(hs_context* ctx, const hs_layer_cfg* cfg, const hs_layer_wei
       if (groups) {
         st = hs::check_prefix_groups(*kv, ctx_lens, n_seqs, *groups, &max_prefix, &max_rest);
         if (st != HS_OK) return st;
+        // (The layout below reserves as much.)
+        st = hs::check_prefix_launch(n_seqs, groups->n, max_prefix, max_rest, cfg->n_q_heads, cfg->n_kv_heads,
+                                     cfg->head_dim, budget,
+                                     hs::prefix_workspace(n_seqs, max_prefix, max_rest, cfg->n_q_heads,
+                                                          cfg->n_kv_heads, cfg->head_dim));
+        if (st != HS_OK) return st;
       }
     } else {
       if (n_seqs > kv->n_slots)
