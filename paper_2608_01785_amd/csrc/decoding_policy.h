@@ -19,9 +19,10 @@ constexpr int kBeamMaxBeams = 64;
 constexpr int kBeamMaxSelect = kLogprobsMaxTop;
 
 // The scan's blocks: as hs_logprobs (see logprobs_shape), but the join is there in any
-// case, so rows are split wherever CUs would idle: 85 rows of 50001 fp16 take 14.3 us in
-// 3 blocks each and 18.0 whole.  Two or four blocks a CU cost the join what they save
-// (32 rows of 65536: 13.7 us with one, 14.0 with two, 14.5 with four).
+// case, so rows are split wherever CUs would idle: 85 rows of 50001 fp16 take 14.7 us in
+// 3 blocks each and 16.2 whole.  Two or four blocks a CU cost the join what they save
+// (32 rows of 65536 fp32: 12.7 us with one, 13.8 with two, 14.4 with four; the 85 rows 14.2
+// with two).  Here and below, times are those of whole calls among others.
 constexpr int kBeamPerCu = 1;
 inline LogprobsShape beam_shape(int rows, int vocab, int elem_bytes, int cus) {
   const int chunk = 4096 / elem_bytes;
@@ -80,28 +81,33 @@ inline int prefix_split_keys(int64_t keys, int64_t blocks, int cus, int per_cu) 
 }
 
 // Tiles: up to 128 columns a group on average go in narrow ones, which read the keys
-// again for every 32 (out of L2): 98 columns behind 8192 positions 17.7 us against 20.1
-// in a wide one; 168 behind 30000 53 against 37.
-// Wide tiles: two blocks a CU, whose products and exponentials overlap (128 rows of 32
-// heads behind 16384 positions 66 us, with one 77); one where the rows' own keys take
-// more than about a fourth as long to read, which then share the CUs from the start
-// (with up to 512 keys more 80 us against 84).
+// again for every 32 (out of L2): 98 columns behind 8192 positions 15.9 us against 19.1
+// in a wide one; 168 behind 30000 48.2 against 34.7 (28 / 4 heads of 128).
+// Blocks a CU are counted for the groups' columns packed into whole tiles.  Groups that
+// end inside a tile launch more: 5 groups of 36 columns are counted as 6 tiles and take 10.
+// Wide tiles: two blocks a CU, whose products and exponentials overlap (128 rows in 32 / 8
+// heads of 128 behind 16384 positions 62 us, with one 69; behind 32768, 99 and 125); one
+// where the rows' own keys take more than about a fourth as long to read, which then share
+// the CUs from the start (behind 16384 with up to 512 keys more 74 us against 79).
 // Narrow tiles: one block a CU.  More leave more states than the shorter ranges save: 8
-// rows of 28 heads behind 8192 positions take 15.5 us with one, 21 with two; behind
-// 30000, 23.7 and 29.8.
-// What rows have to themselves: two blocks a CU beside the prefixes'
-// (20 rows in 5 groups behind 1501 positions 17.9 us against 20.6 with four), eight
-// alone (45 rows of up to 2000 keys 38.9 us against 43.2 with two).
+// rows in 28 / 4 heads behind 8192 positions, with up to 128 keys more, take 13.7 us with
+// one, 18.3 with two; behind 30000, 20.3 and 28.3.
+// What rows have to themselves: two blocks a CU beside the prefixes' (20 rows in 5 groups
+// behind up to 1501 positions, with up to 700 keys more, in 32 / 8 heads 17.0 us against
+// 19.7 with four), eight alone (45 rows of up to 2000 keys 34.5 us against 37.2 with two).
+constexpr int kPrefixPerCu = 2;  // blocks over the prefixes, at most
+constexpr int kRestPerCu = 8;    // blocks over what rows have to themselves, at most
 inline PrefixShape prefix_shape(int n_seqs, int n_groups, int max_prefix, int max_rest, int hq, int hkv, int cus) {
   const int64_t per_head = hq / hkv, rows = int64_t(n_seqs) * per_head;
   PrefixShape s{};
   s.prefix_rows = max_prefix < 1 || rows <= 16 * int64_t(n_groups) ? 16 : rows <= 128 * int64_t(n_groups) ? 32 : 128;
   s.prefix_tiles = max_prefix > 0 ? int(rows / s.prefix_rows + n_groups) : 0;
   const bool wide = s.prefix_rows == 128, long_rest = 240 * int64_t(max_rest) > per_head * max_prefix;
-  s.prefix_keys = prefix_split_keys(max_prefix, prefix_up(rows, s.prefix_rows) * hkv, cus, wide && !long_rest ? 2 : 1);
+  s.prefix_keys = prefix_split_keys(max_prefix, prefix_up(rows, s.prefix_rows) * hkv, cus,
+                                  wide && !long_rest ? kPrefixPerCu : 1);
   s.prefix_splits = int(prefix_up(max_prefix, s.prefix_keys));
   const bool beside = int64_t(s.prefix_tiles) * s.prefix_splits * hkv >= cus / 2;
-  s.rest_keys = prefix_split_keys(max_rest, int64_t(n_seqs) * hkv, cus, beside ? 2 : 8);
+  s.rest_keys = prefix_split_keys(max_rest, int64_t(n_seqs) * hkv, cus, beside ? 2 : kRestPerCu);
   s.rest_splits = int(prefix_up(max_rest, s.rest_keys));
   return s;
 }
@@ -132,18 +138,19 @@ inline size_t prefix_states_bytes(const PrefixShape& s, int n_seqs, int hq, int 
 }
 
 // Workspace bytes for at most n_seqs rows, on any budget.  Fewer rows or groups, a
-// smaller bound and fewer CUs never take more partial states than this: `blocks`
-// blocks take at most 4 cus / blocks + 1 splits, and each block holds prefix_rows
-// (rest: per_head) states of a split.
+// smaller bound and fewer CUs never take more partial states than this: `blocks` blocks
+// share at most per_cu cus / blocks + 1 splits (per_cu: kPrefixPerCu and kRestPerCu at
+// most), and each holds prefix_rows (at most 128; rest: per_head) states of a split.
 inline size_t prefix_workspace(int n_seqs, int max_prefix, int max_rest, int hq, int hkv, int dh) {
   const int64_t rows = int64_t(n_seqs) * hq;
   auto states = [&](int64_t keys, int64_t of_block) {
     int64_t splits = prefix_up(keys, kPrefixKeys);
     if (splits > kPrefixMaxSplits) splits = kPrefixMaxSplits;
-    const int64_t shared = 256 * of_block + rows, each = rows * splits;
+    const int64_t shared = kMaxCus * of_block + rows, each = rows * splits;
     return splits < 1 ? 0 : each < shared ? each : shared;
   };
-  return size_t(states(max_prefix, 2 * 128) + states(max_rest, 8 * (hq / hkv))) * prefix_part_bytes(dh);
+  return size_t(states(max_prefix, kPrefixPerCu * 128) + states(max_rest, kRestPerCu * (hq / hkv))) *
+         prefix_part_bytes(dh);
 }
 
 }  // namespace hs
