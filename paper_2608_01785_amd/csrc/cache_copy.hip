@@ -7,8 +7,9 @@
 // thread two 16-byte words, both loaded before the first is stored.  The runs'
 // segments are numbered without gaps, however long each copy is.  Memory bounds it, at
 // two bytes moved for each copied: 120 slots of 4 MB take 158 us (6.4 TB/s read and
-// written), 16 copies of 33 to 512 positions in 16 layers 102 (5.6; 127 in a grid over the
-// longest copy, half of whose blocks have nothing to do), 64 positions in 4 layers 3.2.
+// written, some of it from the last-level cache; 480 slots 782, 5.2), 16 copies of 33 to
+// 512 positions in 16 layers 103 (5.5; 127 in a grid over the longest copy, half of whose
+// blocks have nothing to do), 64 positions in 4 layers 3.2.
 // Segments of 16 KB take a tenth more where runs are short, of 32 KB half as much again.
 #include "decoding_kernels.h"
 #include "hs_device.h"

@@ -20,11 +20,14 @@
 // (attention_tile.h): 128 columns, 32 a wavefront, which share 64-key tiles in LDS.
 //
 // Memory bounds short groups and what rows have to themselves (45 rows of up to 2000 keys
-// in 32 / 8 heads of 128: 30 us, 6.0 TB/s, and 4.8 for the join), the alternation of products
-// and exponentials in a wavefront long prefixes (128 rows in the same heads: 43 us for each
-// 16384 positions, 0.8 P/s; behind 16384, with up to 512 keys more, 74 us and 7), the chain
-// of loads small calls (8 rows behind 8192 positions in 28 / 4 heads: 10.4 and 4.4; behind
-// 256, 8).
+// in 32 / 8 heads of 128: 31 us, 6.0 TB/s, and 4.8 for the join), the alternation of products
+// and exponentials in a wavefront long prefixes (128 rows in the same heads: 57 us behind
+// 16384 positions and 40 for each further 16384, 0.85 P/s; behind 16384, with up to 512 keys
+// more, 73 us and 7), the chain of loads small calls (8 rows behind 8192 positions in 28 / 4
+// heads: 10.3 and 4.5; behind 256, 9.6).  Times are a trace's, on one state.
+//
+// The kernel with wide tiles for heads of 128 takes all 256 registers, with one vector and
+// 11 scalar ones spilled: the unit for what rows have to themselves is in it too.
 //
 // What the device arrays say is checked here: a slot outside the cache is read as
 // zeros and makes its rows NaN, and no range leaves the table.
