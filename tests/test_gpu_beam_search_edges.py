@@ -137,3 +137,29 @@ def test_results_are_the_callers(env):
             beam.tokens.append(-5)
         assert s.search.step()
     assert s.search.results() == want
+
+
+def test_pages_of_a_search(env):
+    """Free are those that no beam lists: during a search, after it, and after another start."""
+    torch, b, ctx = env
+    beams, page = 4, 64
+    s = Search(env, beams, 3, 500, 130, 9, seed=101)
+    rows, per_seq = 3 * beams, -(-(130 + 9) // page)
+
+    def check():
+        table, lens = s.search.pages.table(list(range(rows)))
+        used = {int(table[i, j]) for i in range(rows) for j in range(-(-int(lens[i]) // page))}
+        assert s.search.pages.free_count() == rows * per_seq - len(used)
+        return len(used)
+    assert check() == 0
+    x, offsets = s.prompts([70, 5, 130])
+    s.search.start(x, offsets)
+    assert check() == 2 + 1 + 3      # the prompts' pages, each listed by its beams
+    while s.search.step():
+        # A group's whole pages are shared; each beam's last one is its own, or its siblings' after the fork.
+        assert 6 <= check() <= (1 + beams) + beams + (2 + beams)
+    x, offsets = s.prompts([64])
+    s.search.start(x, offsets)
+    assert check() == 1
+    s.search.step()
+    assert 2 <= check() <= 1 + beams
