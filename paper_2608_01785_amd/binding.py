@@ -239,7 +239,10 @@ def hs_last_error() -> str:
 def _as_i32(values, name: str = "a list") -> np.ndarray:
     """Host integers as a contiguous array of 32-bit words; others are refused, not cut to their lower bits."""
     if isinstance(values, (list, tuple)):
-        return np.asarray(values, dtype=np.int32)   # (numpy refuses what does not fit)
+        try:
+            return np.array(array.array("i", values), dtype=np.int32)
+        except (OverflowError, TypeError):
+            pass   # refused below, or a list of lists
     a = np.asarray(values)
     if a.dtype != np.int32 and a.size and (a.dtype.kind not in "iub" or a.min() < -2 ** 31 or a.max() > _INT32_MAX):
         raise ValueError(f"{name} holds no 32-bit numbers")

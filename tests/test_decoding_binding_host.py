@@ -39,7 +39,7 @@ def test_lists_of_pages(b, make):
 
 def test_fractions_are_no_pages(b):
     p = b.Pages(4, 64, 2, 3)
-    for values in (np.array([0.5]), np.array([np.nan])):
+    for values in (np.array([0.5]), np.array([np.nan]), [0.5], (0.5,), [np.float32(1)], [[0.5]]):
         with pytest.raises(ValueError):
             p.reserve([0], values)
     assert p.free_count() == 4
@@ -73,5 +73,9 @@ def test_block_tables(b):
     for table in (np.array([[0, BIG + 1]]), np.array([[0.0, 1.5]])):
         with pytest.raises(ValueError, match="32-bit"):
             b._kv_struct(([1], [2], 4, 64, table))
-    s = b._kv_struct(([1], [2], 4, 64, np.array([[0, 3], [1, -1]])))
-    assert [s.block_table[i] for i in range(4)] == [0, 3, 1, -1] and s.pages_per_seq == 2
+    for table in ([[0, BIG + 1]], [[0.0, 1.5]]):
+        with pytest.raises(ValueError, match="32-bit"):
+            b._kv_struct(([1], [2], 4, 64, table))
+    for table in (np.array([[0, 3], [1, -1]]), np.array([[0, 3], [1, -1]], np.int32), [[0, 3], [1, -1]]):
+        s = b._kv_struct(([1], [2], 4, 64, table))
+        assert [s.block_table[i] for i in range(4)] == [0, 3, 1, -1] and s.pages_per_seq == 2
