@@ -36,7 +36,7 @@ def test_decode_step_with_keys_at_minus_infinity(env, shape, call):
     torch, b, ctx = env
     from paper_2608_01785_amd.device_data import DeviceCache, PagedCache, to_device, upload_weights
     log(f"[infinite keys] head size {shape.head_dim}, {call}")
-    n, top, page, dh = len(KV_LENS), 3072, 256, shape.head_dim
+    n, top, page, dh = len(KV_LENS), 3328, 256, shape.head_dim
     kv_lens, d = np.array(KV_LENS, np.int32), dh // 2 - 1
     layers = W.make_weights(shape, 1, 51)
     bias = np.zeros((shape.n_q_heads + 2 * shape.n_kv_heads, dh), np.float32)
